@@ -343,6 +343,80 @@ int cats_tp_lm_head_shard(const cats_model_cfg *cfg, const void *d_final_norm, c
 int cats_tp_argmax_merge(const float *d_max, const int32_t *d_idx, int32_t n_shards, int32_t T, int32_t *d_argmax,
                          void *stream);
 
+/* ---- 8-bit integer path ------------------------------------------------------
+ * (The paper stores its weights in 16 bits; this path is this library's.  The
+ * forward is bound by reading the weights, Section 1, and 8-bit weights are half
+ * the bytes.)  Projections multiply int8 activations, one scale per token, with
+ * int8 weights, one scale per output channel.
+ *
+ * A row y of `cols` values is held as
+ *     a = max(max_c |y[c]|, 2^-100),  q[c] = rint(127 y[c] / a) (ties to even),
+ *     scale = a / 127,                so that y[c] ~ q[c] * scale;
+ * y, a and the quotient are fp32.  A row with an infinity or a NaN gets a NaN
+ * scale and zeros, and so makes NaN of whatever is computed from it.
+ *
+ * Matrices are row-major with a row stride (ld*) in ELEMENTS, at least cols;
+ * columns behind cols are neither read nor written.  Rows may start anywhere
+ * their element type may; 16-byte starts (8 for int8) and column counts that are
+ * multiples of 8 are the fast case.  Types are CATS_F32 or CATS_BF16.  rows == 0
+ * launches nothing.  Except where a parameter says so, outputs must not overlap
+ * inputs.  Calls need no workspace and may run on any streams at once. */
+enum { CATS_F32 = 0, CATS_BF16 = 1 };
+
+/* q, scale from x [rows][cols]: attention outputs in front of the O projection,
+ * or a weight matrix [outs][cols] (one scale per output channel), which
+ * cats_pack_weights_i8 then lays out. */
+int cats_quantize_i8(const void *d_x, int32_t x_type, int64_t ldx, int32_t rows, int32_t cols, int8_t *d_q, int64_t ldq,
+                     float *d_scale, void *stream);
+/* out[r][c] = q[r][c] * scale[r], rounded to out_type. */
+int cats_dequantize_i8(const int8_t *d_q, int64_t ldq, const float *d_scale, int32_t rows, int32_t cols, void *d_out,
+                       int32_t out_type, int64_t ldo, void *stream);
+/* y = r / sqrt(mean_c r^2 + eps) * gain with r = resid + delta (delta may be
+ * NULL); resid_out (may be NULL, may be resid itself) receives r in resid's type.
+ * The mean is taken of the unrounded fp32 sums; a row whose squares add up past
+ * the fp32 range is outside what the norm can take (scale 2^-100 / 127 or NaN).
+ * gain: bf16 [cols].  eps >= 0. */
+int cats_rmsnorm_i8(const void *d_resid, int32_t resid_type, int64_t ldr, const void *d_delta, int32_t delta_type, int64_t ldd,
+                    const void *d_gain, float eps, int32_t rows, int32_t cols, void *d_resid_out, int64_t ldo, int8_t *d_q,
+                    int64_t ldq, float *d_scale, void *stream);
+/* y = silu(gate) * up; a row of d_gate_up holds cols gate values, then cols up
+ * values (ld >= 2 * cols). */
+int cats_swiglu_i8(const void *d_gate_up, int32_t type, int64_t ld, int32_t rows, int32_t cols, int8_t *d_q, int64_t ldq,
+                   float *d_scale, void *stream);
+
+/* The layout cats_linear_i8 reads weights in: per block of 128 columns, groups of
+ * 8 rows x 128 bytes as the tensor cores read them, zeros beyond the matrix.
+ * d_dst: cats_packed_weight_i8_bytes bytes (0 for sizes that are not supported),
+ * 1024-byte aligned.  Done once, at load time.  rows = output channels. */
+size_t cats_packed_weight_i8_bytes(int32_t rows, int32_t cols);
+int cats_pack_weights_i8(const int8_t *d_src, int64_t ld, int32_t rows, int32_t cols, void *d_dst, void *stream);
+
+/* out[t][n] = (sum_c x[t][c] w[n][c]) * x_scale[t] * w_scale[n], t < rows, n < outs:
+ * the sums are exact 32-bit integers, both scales are applied in fp32 in this
+ * order, the product is rounded once to out_type.  x must start on 16 bytes and
+ * ldx be a multiple of 16.  d_w: cats_pack_weights_i8 of w [outs][cols];
+ * cols <= 131071 (more could overflow the sums): CATS_ERR_UNSUPPORTED. */
+int cats_linear_i8(const int8_t *d_x, int64_t ldx, const float *d_x_scale, const void *d_w, const float *d_w_scale, int32_t rows,
+                   int32_t cols, int32_t outs, void *d_out, int32_t out_type, int64_t ldo, int32_t *d_status, void *stream);
+
+/* One layer's weights of the 8-bit path.  attn_norm, mlp_norm: bf16 [hidden].
+ * Packed int8 (cats_pack_weights_i8) and fp32 scales, one per row: wqkv of the
+ * stacked rows of Wq, Wk, Wv; wo; w_gate_up of the stacked rows of W_gate, W_up;
+ * w_down. */
+typedef struct {
+    const void *attn_norm, *wqkv, *wo, *mlp_norm, *w_gate_up, *w_down;
+    const float *s_qkv, *s_o, *s_gate_up, *s_down;
+} cats_layer_weights_i8;
+
+/* cats_verify_layer with 8-bit projections: norm, QKV, rotation and KV append,
+ * tree attention (bf16, as in cats_verify_layer), O, norm, gate/up, SwiGLU, down.
+ * Residual stream and projection outputs are fp32; projection inputs are int8.
+ * Workspace: cats_workspace_i8_bytes, 1024-byte aligned, one per stream. */
+size_t cats_workspace_i8_bytes(const cats_model_cfg *cfg, int32_t T);
+int cats_verify_layer_i8(const cats_model_cfg *cfg, const cats_layer_weights_i8 *w, float *d_resid, void *d_kcache,
+                         void *d_vcache, const uint64_t *d_mask, const int32_t *d_pos, int32_t T, int32_t prefix_len, void *d_ws,
+                         size_t ws_bytes, int32_t *d_status, void *stream);
+
 /* Number of kernel launches the last call of this thread issued (for reports). */
 int cats_last_launch_count(void);
 

@@ -350,6 +350,156 @@ def cats_tp_argmax_merge(max_all, idx_all, n_shards, T, argmax):
     _check(lib.cats_tp_argmax_merge(_ptr(max_all), _ptr(idx_all), n_shards, T, _ptr(argmax), _stream()), "cats_tp_argmax_merge")
 
 
+F32, BF16 = 0, 1
+
+
+class LayerWeightsI8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in LAYER_FIELDS + ("s_qkv", "s_o", "s_gate_up", "s_down")]
+
+
+lib.cats_quantize_i8.argtypes = [_vp, _i32, _i64, _i32, _i32, _vp, _i64, _vp, _vp]
+lib.cats_dequantize_i8.argtypes = [_vp, _i64, _vp, _i32, _i32, _vp, _i32, _i64, _vp]
+lib.cats_rmsnorm_i8.argtypes = [_vp, _i32, _i64, _vp, _i32, _i64, _vp, C.c_float, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp]
+lib.cats_swiglu_i8.argtypes = [_vp, _i32, _i64, _i32, _i32, _vp, _i64, _vp, _vp]
+lib.cats_packed_weight_i8_bytes.restype = C.c_size_t
+lib.cats_packed_weight_i8_bytes.argtypes = [_i32, _i32]
+lib.cats_pack_weights_i8.argtypes = [_vp, _i64, _i32, _i32, _vp, _vp]
+lib.cats_linear_i8.argtypes = [_vp, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _i64, _vp, _vp]
+lib.cats_workspace_i8_bytes.restype = C.c_size_t
+lib.cats_workspace_i8_bytes.argtypes = [C.POINTER(ModelCfg), _i32]
+lib.cats_verify_layer_i8.argtypes = [C.POINTER(ModelCfg), C.POINTER(LayerWeightsI8), _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp,
+                                     C.c_size_t, _vp, _vp]
+
+_FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _check_i8(what, rows, cols, device, *mats):
+    """Shapes, element types and devices of the 8-bit calls: the C entry points see pointers only.  mats: (tensor, shape, types)."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError("%s: tensors are on %s, the current device is cuda:%d" % (what, device, torch.cuda.current_device()))
+    for t, shape, types in mats:
+        if t.dtype not in types or tuple(t.shape) != shape or t.device != device:
+            raise ValueError("%s: expected %s of %s on %s, got %s of %s on %s" % (what, shape, types, device, tuple(t.shape), t.dtype, t.device))
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError("%s: the last dimension must be contiguous" % what)
+
+
+def _ld(t):
+    """Row stride in elements (a single row's stride means nothing to torch)."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+
+
+def new_i8(rows: int, cols: int, device="cuda"):
+    """(q, scale) for `rows` rows held in 8 bits: int8 [rows][cols] whose rows start on 16 bytes, fp32 [rows]."""
+    return (torch.empty(rows, -(-cols // 16) * 16, dtype=torch.int8, device=device)[:, :cols],
+            torch.empty(rows, dtype=torch.float32, device=device))
+
+
+def cats_quantize_i8(x, q, scale):
+    rows, cols = x.shape
+    _check_i8("cats_quantize_i8", rows, cols, x.device, (x, (rows, cols), _FLOATS), (q, (rows, cols), (torch.int8,)),
+              (scale, (rows,), (torch.float32,)))
+    _check(lib.cats_quantize_i8(x.data_ptr(), _FLOATS[x.dtype], _ld(x), rows, cols, q.data_ptr(), _ld(q), scale.data_ptr(), _stream()),
+           "cats_quantize_i8")
+
+
+def cats_dequantize_i8(q, scale, out):
+    rows, cols = q.shape
+    _check_i8("cats_dequantize_i8", rows, cols, q.device, (q, (rows, cols), (torch.int8,)), (scale, (rows,), (torch.float32,)),
+              (out, (rows, cols), _FLOATS))
+    _check(lib.cats_dequantize_i8(q.data_ptr(), _ld(q), scale.data_ptr(), rows, cols, out.data_ptr(), _FLOATS[out.dtype], _ld(out),
+                                  _stream()), "cats_dequantize_i8")
+
+
+def cats_rmsnorm_i8(resid, delta, gain, eps, resid_out, q, scale):
+    """delta and resid_out may be None; resid_out may be resid itself."""
+    rows, cols = resid.shape
+    mats = [(resid, (rows, cols), _FLOATS), (gain, (cols,), (torch.bfloat16,)), (q, (rows, cols), (torch.int8,)),
+            (scale, (rows,), (torch.float32,))]
+    if delta is not None:
+        mats.append((delta, (rows, cols), _FLOATS))
+    if resid_out is not None:
+        mats.append((resid_out, (rows, cols), (resid.dtype,)))
+    _check_i8("cats_rmsnorm_i8", rows, cols, resid.device, *mats)
+    _check(lib.cats_rmsnorm_i8(resid.data_ptr(), _FLOATS[resid.dtype], _ld(resid),
+                               None if delta is None else delta.data_ptr(), F32 if delta is None else _FLOATS[delta.dtype],
+                               0 if delta is None else _ld(delta), gain.data_ptr(), eps, rows, cols,
+                               None if resid_out is None else resid_out.data_ptr(), 0 if resid_out is None else _ld(resid_out),
+                               q.data_ptr(), _ld(q), scale.data_ptr(), _stream()), "cats_rmsnorm_i8")
+
+
+def cats_swiglu_i8(gate_up, q, scale):
+    rows, cols = q.shape
+    _check_i8("cats_swiglu_i8", rows, cols, q.device, (gate_up, (rows, 2 * cols), _FLOATS), (q, (rows, cols), (torch.int8,)),
+              (scale, (rows,), (torch.float32,)))
+    _check(lib.cats_swiglu_i8(gate_up.data_ptr(), _FLOATS[gate_up.dtype], _ld(gate_up), rows, cols, q.data_ptr(), _ld(q),
+                              scale.data_ptr(), _stream()), "cats_swiglu_i8")
+
+
+def pack_weights_i8(w: torch.Tensor) -> torch.Tensor:
+    """cats_pack_weights_i8: int8 [outs][cols] -> packed buffer (uint8 CUDA tensor, 1024-byte aligned)."""
+    rows, cols = w.shape
+    _check_i8("pack_weights_i8", rows, cols, w.device, (w, (rows, cols), (torch.int8,)))
+    n = int(lib.cats_packed_weight_i8_bytes(rows, cols))
+    if n == 0:
+        raise CatsError(-3, "cats_packed_weight_i8_bytes")
+    buf = torch.empty(n + 1024, dtype=torch.uint8, device=w.device)
+    off = (-buf.data_ptr()) % 1024
+    out = buf[off:off + n]
+    _check(lib.cats_pack_weights_i8(w.data_ptr(), _ld(w), rows, cols, out.data_ptr(), _stream()), "cats_pack_weights_i8")
+    return out
+
+
+def cats_linear_i8(x, x_scale, w_packed, w_scale, out, status):
+    """x int8 [rows][cols], rows starting on 16 bytes (see new_i8); w_packed: pack_weights_i8 of [outs][cols]; out [rows][outs]."""
+    (rows, cols), outs = x.shape, w_scale.shape[0]
+    _check_i8("cats_linear_i8", rows, cols, x.device, (x, (rows, cols), (torch.int8,)), (x_scale, (rows,), (torch.float32,)),
+              (w_packed, (-(-cols // 128) * -(-outs // 8) * 1024,), (torch.uint8,)), (w_scale, (outs,), (torch.float32,)),
+              (out, (rows, outs), _FLOATS), (status, (1,), (torch.int32,)))
+    _check(lib.cats_linear_i8(x.data_ptr(), _ld(x), x_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(), rows, cols, outs,
+                              out.data_ptr(), _FLOATS[out.dtype], _ld(out), status.data_ptr(), _stream()), "cats_linear_i8")
+
+
+def quantize_weights_i8(w: torch.Tensor):
+    """(packed, scale) of a bf16 or fp32 matrix [outs][cols]: one scale per output channel."""
+    q, scale = new_i8(*w.shape, device=w.device)
+    cats_quantize_i8(w, q, scale)
+    return pack_weights_i8(q), scale
+
+
+def pack_layer_i8(w: dict) -> dict:
+    """nn.Linear-layout bf16 layer weights (as for pack_layer) -> packed 8-bit layer."""
+    out = {"attn_norm": w["attn_norm"].contiguous(), "mlp_norm": w["mlp_norm"].contiguous()}
+    for name, scale, mats in (("wqkv", "s_qkv", ("wq", "wk", "wv")), ("wo", "s_o", ("wo",)), ("w_gate_up", "s_gate_up", ("w_gate", "w_up")),
+                              ("w_down", "s_down", ("w_down",))):
+        out[name], out[scale] = quantize_weights_i8(torch.cat([w[m] for m in mats]))
+    return out
+
+
+def layer_weights_i8(w: dict) -> LayerWeightsI8:
+    """``w``: a packed 8-bit layer (see pack_layer_i8)."""
+    s = LayerWeightsI8()
+    for n, _ in LayerWeightsI8._fields_:
+        t = w[n]
+        assert t.is_cuda and t.is_contiguous(), n
+        setattr(s, n, t.data_ptr())
+    return s
+
+
+def new_workspace_i8(cfg: ModelCfg, T: int, device="cuda") -> torch.Tensor:
+    n = int(lib.cats_workspace_i8_bytes(C.byref(cfg), T))
+    if n == 0:
+        raise CatsError(-3, "cats_workspace_i8_bytes")
+    buf = torch.empty(n + 1024, dtype=torch.uint8, device=device)
+    off = (-buf.data_ptr()) % 1024
+    return buf[off:off + n]
+
+
+def cats_verify_layer_i8(cfg, w: LayerWeightsI8, resid, kcache, vcache, mask, pos, T, prefix_len, ws, status):
+    _check(lib.cats_verify_layer_i8(C.byref(cfg), C.byref(w), _ptr(resid), _ptr(kcache), _ptr(vcache), _ptr(mask), _ptr(pos), T,
+                                    prefix_len, _ptr(ws), ws.numel(), _ptr(status), _stream()), "cats_verify_layer_i8")
+
+
 class VerifyForward:
     """Holds the argument block of ``cats_verify_forward`` for one model / tree size: device buffers for
     every output plus the workspace, all allocated once here (the library itself allocates nothing)."""

@@ -270,7 +270,8 @@ int cats_debug_timeline(int kernel, void* host, size_t bytes) {
 void cats_debug_inject_fault(int which) { g_debug_fault = (which == 1 || which == 2) ? which : 0; }
 int cats_debug_wait_limit_ns(unsigned long long ns) {
     if (ns == 0) ns = kWaitLimitNs;
-    if (set_wait_limit_gemm(ns) != cudaSuccess || set_wait_limit_attn(ns) != cudaSuccess || set_wait_limit_small(ns) != cudaSuccess)
+    if (set_wait_limit_gemm(ns) != cudaSuccess || set_wait_limit_attn(ns) != cudaSuccess || set_wait_limit_small(ns) != cudaSuccess ||
+        set_wait_limit_i8(ns) != cudaSuccess)
         return CATS_ERR_CUDA;
     return CATS_OK;
 }
@@ -586,6 +587,196 @@ int cats_tp_argmax_merge(const float* d_max, const int32_t* d_idx, int32_t n_sha
     g_call_boundary = true;
     if (!d_max || !d_idx || !d_argmax || n_shards < 1 || T < 1 || T > CATS_MAX_TREE) return CATS_ERR_INVALID_ARG;
     CATS_CUDA(launch_argmax_reduce(d_max, d_idx, n_shards, T, T, d_argmax, nullptr, 0, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+/* ---- 8-bit integer path (see cats.h) ---- */
+static inline int type_size(int32_t type) { return type == CATS_F32 ? 4 : 2; }
+static inline bool bad_type(int32_t type) { return type != CATS_F32 && type != CATS_BF16; }
+
+size_t cats_packed_weight_i8_bytes(int32_t rows, int32_t cols) {
+    if (rows < 1 || cols < 1 || cols > kMaxI8Cols) return 0;
+    return packed_weight_i8_bytes(rows, cols);
+}
+
+int cats_pack_weights_i8(const int8_t* d_src, int64_t ld, int32_t rows, int32_t cols, void* d_dst, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_pack_weights_i8");
+    g_call_boundary = true;
+    if (!d_src || !d_dst || cats_packed_weight_i8_bytes(rows, cols) == 0 || ld < cols) return CATS_ERR_INVALID_ARG;
+    if (misaligned(d_dst, 1024)) return CATS_ERR_INVALID_ARG;
+    CATS_CUDA(launch_pack_weights_i8(d_src, ld, rows, cols, d_dst, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+int cats_quantize_i8(const void* d_x, int32_t x_type, int64_t ldx, int32_t rows, int32_t cols, int8_t* d_q, int64_t ldq,
+                     float* d_scale, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_quantize_i8");
+    g_call_boundary = true;
+    if (rows < 0 || cols < 1 || bad_type(x_type) || ldx < cols || ldq < cols) return CATS_ERR_INVALID_ARG;
+    if (rows == 0) return CATS_OK;
+    if (!d_x || !d_q || !d_scale || misaligned(d_x, type_size(x_type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
+    I8RowsDev p = {};
+    p.x = d_x; p.x_f32 = x_type == CATS_F32; p.ldx = ldx; p.rows = rows; p.cols = cols; p.q = d_q; p.ldq = ldq; p.scale = d_scale;
+    CATS_CUDA(launch_i8_rows(I8_QUANTIZE, p, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+int cats_dequantize_i8(const int8_t* d_q, int64_t ldq, const float* d_scale, int32_t rows, int32_t cols, void* d_out, int32_t out_type,
+                       int64_t ldo, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_dequantize_i8");
+    g_call_boundary = true;
+    if (rows < 0 || cols < 1 || bad_type(out_type) || ldq < cols || ldo < cols) return CATS_ERR_INVALID_ARG;
+    if (rows == 0) return CATS_OK;
+    if (!d_q || !d_scale || !d_out || misaligned(d_out, type_size(out_type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
+    CATS_CUDA(launch_i8_dequantize(d_q, ldq, d_scale, rows, cols, d_out, out_type == CATS_F32, ldo, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+int cats_rmsnorm_i8(const void* d_resid, int32_t resid_type, int64_t ldr, const void* d_delta, int32_t delta_type, int64_t ldd,
+                    const void* d_gain, float eps, int32_t rows, int32_t cols, void* d_resid_out, int64_t ldo, int8_t* d_q, int64_t ldq,
+                    float* d_scale, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_rmsnorm_i8");
+    g_call_boundary = true;
+    if (rows < 0 || cols < 1 || bad_type(resid_type) || ldr < cols || ldq < cols || !(eps >= 0.f)) return CATS_ERR_INVALID_ARG;
+    if (d_delta && (bad_type(delta_type) || ldd < cols || misaligned(d_delta, type_size(delta_type)))) return CATS_ERR_INVALID_ARG;
+    if (d_resid_out && (ldo < cols || misaligned(d_resid_out, type_size(resid_type)))) return CATS_ERR_INVALID_ARG;
+    if (d_resid_out == d_resid && d_resid_out && ldo != ldr) return CATS_ERR_INVALID_ARG;     // in place means the same rows
+    if (rows == 0) return CATS_OK;
+    if (!d_resid || !d_gain || !d_q || !d_scale) return CATS_ERR_INVALID_ARG;
+    if (misaligned(d_resid, type_size(resid_type)) || misaligned(d_gain, 2) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
+    I8RowsDev p = {};
+    p.x = d_resid; p.x_f32 = resid_type == CATS_F32; p.ldx = ldr; p.delta = d_delta; p.d_f32 = delta_type == CATS_F32; p.ldd = ldd;
+    p.gain = d_gain; p.eps = eps; p.resid_out = d_resid_out; p.ldo = ldo; p.rows = rows; p.cols = cols; p.q = d_q; p.ldq = ldq;
+    p.scale = d_scale;
+    CATS_CUDA(launch_i8_rows(I8_NORM, p, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+int cats_swiglu_i8(const void* d_gate_up, int32_t type, int64_t ld, int32_t rows, int32_t cols, int8_t* d_q, int64_t ldq, float* d_scale,
+                   void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_swiglu_i8");
+    g_call_boundary = true;
+    if (rows < 0 || cols < 1 || bad_type(type) || ld < 2 * (int64_t)cols || ldq < cols) return CATS_ERR_INVALID_ARG;
+    if (rows == 0) return CATS_OK;
+    if (!d_gate_up || !d_q || !d_scale || misaligned(d_gate_up, type_size(type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
+    I8RowsDev p = {};
+    p.x = d_gate_up; p.x_f32 = type == CATS_F32; p.ldx = ld; p.rows = rows; p.cols = cols; p.q = d_q; p.ldq = ldq; p.scale = d_scale;
+    CATS_CUDA(launch_i8_rows(I8_SWIGLU, p, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+int cats_linear_i8(const int8_t* d_x, int64_t ldx, const float* d_x_scale, const void* d_w, const float* d_w_scale, int32_t rows,
+                   int32_t cols, int32_t outs, void* d_out, int32_t out_type, int64_t ldo, int32_t* d_status, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_linear_i8");
+    g_call_boundary = true;
+    if (rows < 0 || cols < 1 || outs < 1 || bad_type(out_type) || ldx < cols || ldx % 16 || ldo < outs) return CATS_ERR_INVALID_ARG;
+    if (cols > kMaxI8Cols) return CATS_ERR_UNSUPPORTED;
+    if (rows == 0) return CATS_OK;
+    if (!d_x || !d_x_scale || !d_w || !d_w_scale || !d_out || !d_status) return CATS_ERR_INVALID_ARG;
+    if (misaligned(d_x, 16) || misaligned(d_w, 1024) || misaligned(d_out, type_size(out_type)) || misaligned(d_x_scale, 4) ||
+        misaligned(d_w_scale, 4))
+        return CATS_ERR_INVALID_ARG;
+    I8Linear p = {d_x, ldx, d_x_scale, d_w, d_w_scale, rows, cols, outs, d_out, out_type == CATS_F32, ldo, d_status};
+    CATS_CUDA(launch_linear_i8(p, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+namespace {
+struct WorkspaceI8 {
+    int8_t* x;              // [T][ldx]: the int8 input of the projection at hand
+    long long ldx;
+    float* scale;           // [T]
+    float* wide;            // [T][max(3 D, 2 ffn)] fp32: QKV, then gate and up
+    float* delta;           // [T][hidden] fp32: O, then down projection
+    uint16_t *q, *o;        // [T][D] bf16
+    float *attn_o, *attn_ml;
+    size_t bytes;
+};
+WorkspaceI8 carve_i8(const cats_model_cfg* c, int T, void* base) {
+    WorkspaceI8 w;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 1024); return (uint8_t*)base + o; };
+    const size_t D = (size_t)c->n_heads * c->head_dim, H = (size_t)c->hidden, F = (size_t)c->ffn;
+    const size_t tpad = (size_t)(T + 15) / 16 * 16;
+    w.ldx = (long long)align_up(H > D ? (H > F ? H : F) : (D > F ? D : F), 16);
+    w.x = (int8_t*)take((size_t)T * w.ldx);
+    w.scale = (float*)take((size_t)T * 4);
+    w.wide = (float*)take((size_t)T * (3 * D > 2 * F ? 3 * D : 2 * F) * 4);
+    w.delta = (float*)take((size_t)T * H * 4);
+    w.q = (uint16_t*)take((size_t)T * D * 2);
+    w.o = (uint16_t*)take((size_t)T * D * 2);
+    const size_t ns = (size_t)attn_split_bound(c->n_heads);
+    w.attn_o = (float*)take((size_t)c->n_heads * ns * tpad * c->head_dim * 4);
+    w.attn_ml = (float*)take((size_t)c->n_heads * ns * tpad * 2 * 4);
+    w.bytes = off;
+    return w;
+}
+}  // namespace
+
+size_t cats_workspace_i8_bytes(const cats_model_cfg* cfg, int32_t T) {
+    if (check_cfg(cfg) != CATS_OK || T < 1 || T > CATS_MAX_TREE) return 0;
+    return carve_i8(cfg, T, nullptr).bytes;
+}
+
+int cats_verify_layer_i8(const cats_model_cfg* cfg, const cats_layer_weights_i8* w, float* d_resid, void* d_kcache, void* d_vcache,
+                         const uint64_t* d_mask, const int32_t* d_pos, int32_t T, int32_t prefix_len, void* d_ws, size_t ws_bytes,
+                         int32_t* d_status, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_verify_layer_i8");
+    g_call_boundary = true;
+    int rc = check_cfg(cfg);
+    if (rc) return rc;
+    if (!w || !d_resid || !d_kcache || !d_vcache || !d_mask || !d_pos || !d_ws || !d_status) return CATS_ERR_INVALID_ARG;
+    const float* scales[] = {w->s_qkv, w->s_o, w->s_gate_up, w->s_down};
+    const void* mats[] = {w->wqkv, w->wo, w->w_gate_up, w->w_down};
+    for (const float* s : scales) if (!s || misaligned(s, 4)) return CATS_ERR_INVALID_ARG;
+    for (const void* m : mats) if (!m || misaligned(m, 1024)) return CATS_ERR_INVALID_ARG;
+    if (!w->attn_norm || !w->mlp_norm || misaligned(w->attn_norm, 16) || misaligned(w->mlp_norm, 16)) return CATS_ERR_INVALID_ARG;
+    rc = check_tree_args(T, prefix_len);
+    if (rc) return rc;
+    if (T > cfg->max_seq || prefix_len > cfg->max_seq - T) return CATS_ERR_INVALID_ARG;
+    if (misaligned(d_ws, 1024)) return CATS_ERR_WORKSPACE;
+    if (misaligned(d_resid, 16) || misaligned(d_kcache, 16) || misaligned(d_vcache, 16)) return CATS_ERR_INVALID_ARG;
+    const WorkspaceI8 ws = carve_i8(cfg, T, d_ws);
+    if (ws.bytes > ws_bytes) return CATS_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)stream;
+    const int H = cfg->hidden, D = cfg->n_heads * cfg->head_dim, F = cfg->ffn;
+
+    I8RowsDev n = {};                                       // norm of the residual stream
+    n.x = d_resid; n.x_f32 = 1; n.ldx = H; n.rows = T; n.cols = H; n.gain = w->attn_norm; n.eps = cfg->rms_eps;
+    n.q = ws.x; n.ldq = ws.ldx; n.scale = ws.scale;
+    CATS_CUDA(launch_i8_rows(I8_NORM, n, st));
+    auto linear = [&](const void* m, const float* s, int cols, int outs, float* out) {
+        const I8Linear l = {ws.x, ws.ldx, ws.scale, m, s, T, cols, outs, out, 1, outs, d_status};
+        return launch_linear_i8(l, st);
+    };
+    CATS_CUDA(linear(w->wqkv, w->s_qkv, H, 3 * D, ws.wide));
+    CATS_CUDA(launch_i8_qkv(ws.wide, d_pos, T, cfg->n_heads, cfg->head_dim, cfg->rope_base, prefix_len, ws.q, d_kcache, d_vcache, st));
+    AttnProblem a = {};
+    a.q = ws.q; a.k = d_kcache; a.v = d_vcache; a.mask = d_mask; a.T = T; a.prefix_len = prefix_len; a.nh = cfg->n_heads;
+    a.hd = cfg->head_dim; a.kv_stride = D; a.scale = 1.0f / sqrtf((float)cfg->head_dim); a.out = ws.o;
+    a.part_o = ws.attn_o; a.part_ml = ws.attn_ml; a.d_status = d_status;
+    attn_plan(a);
+    CATS_CUDA(launch_tree_attention(a, st));
+    I8RowsDev r = {};                                       // attention output
+    r.x = ws.o; r.ldx = D; r.rows = T; r.cols = D; r.q = ws.x; r.ldq = ws.ldx; r.scale = ws.scale;
+    CATS_CUDA(launch_i8_rows(I8_QUANTIZE, r, st));
+    CATS_CUDA(linear(w->wo, w->s_o, D, H, ws.delta));
+    n.gain = w->mlp_norm; n.delta = ws.delta; n.d_f32 = 1; n.ldd = H; n.resid_out = d_resid; n.ldo = H;
+    CATS_CUDA(launch_i8_rows(I8_NORM, n, st));
+    CATS_CUDA(linear(w->w_gate_up, w->s_gate_up, H, 2 * F, ws.wide));
+    I8RowsDev g = {};
+    g.x = ws.wide; g.x_f32 = 1; g.ldx = 2 * (long long)F; g.rows = T; g.cols = F; g.q = ws.x; g.ldq = ws.ldx; g.scale = ws.scale;
+    CATS_CUDA(launch_i8_rows(I8_SWIGLU, g, st));
+    CATS_CUDA(linear(w->w_down, w->s_down, F, H, ws.delta));
+    CATS_CUDA(launch_rmsnorm(d_resid, nullptr, ws.delta, 1, (size_t)T * H, nullptr, T, H, cfg->rms_eps, nullptr, nullptr, nullptr, nullptr,
+                             cfg->head_dim, cfg->rope_base, nullptr, 0, st, d_status));
     return CATS_OK;
 }
 

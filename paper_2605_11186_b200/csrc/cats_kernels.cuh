@@ -168,4 +168,46 @@ struct AttnProblem {
 size_t attn_plan(AttnProblem& p);
 cudaError_t launch_tree_attention(const AttnProblem& p, cudaStream_t st);
 
+// ---- 8-bit integer path ----------------------------------------------------------------------------
+enum I8RowsOp : int { I8_NORM = 0, I8_SWIGLU = 1, I8_QUANTIZE = 2 };
+// Rows to int8 with one scale each.  Strides in elements; types: fp32 or (x_f32 == 0, d_f32 == 0) bf16.
+struct I8RowsDev {
+    const void* x;          // NORM: residual stream; SWIGLU: [rows][2 * cols], gate then up; QUANTIZE: the rows
+    const void* delta;      // NORM: added to the residual stream first, or null
+    const void* gain;       // NORM: bf16 [cols]
+    void* resid_out;        // NORM: the sum in x's type, or null; may be x itself
+    int8_t* q;
+    float* scale;           // [rows]
+    long long ldx, ldd, ldo, ldq;
+    int rows, cols;
+    int x_f32, d_f32;
+    float eps;
+};
+cudaError_t launch_i8_rows(int op, const I8RowsDev& p, cudaStream_t st);
+cudaError_t launch_i8_dequantize(const int8_t* q, long long ldq, const float* scale, int rows, int cols, void* out, int out_f32,
+                                 long long ldo, cudaStream_t st);
+
+// fp32 [T][3 * nh * hd] of the QKV projection: rotates q and k, leaves q as bf16 [T][nh * hd], appends k and v to the caches.
+cudaError_t launch_i8_qkv(const float* qkv, const int32_t* pos, int T, int nh, int hd, float rope_base, int prefix_len, void* q, void* kc,
+                          void* vc, cudaStream_t st);
+
+// out[t][n] = (sum_k x[t][k] w[n][k]) * sx[t] * sw[n], int8 operands, w packed by launch_pack_weights_i8.
+constexpr int kMaxI8Cols = 131071;     // K * 128 * 128 fits the int32 sums
+struct I8Linear {
+    const int8_t* x;        // rows of ldx bytes (a multiple of 16)
+    long long ldx;
+    const float* sx;        // [rows]
+    const void* w;
+    const float* sw;        // [outs]
+    int rows, cols, outs;
+    void* out;
+    int out_f32;
+    long long ldo;
+    int32_t* d_status;
+};
+cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st);
+size_t packed_weight_i8_bytes(int rows, int cols);
+cudaError_t launch_pack_weights_i8(const int8_t* src, long long ld, int rows, int cols, void* dst, cudaStream_t st);
+cudaError_t set_wait_limit_i8(unsigned long long ns);
+
 }  // namespace cats
