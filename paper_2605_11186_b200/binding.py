@@ -370,23 +370,12 @@ lib.cats_workspace_i8_bytes.argtypes = [C.POINTER(ModelCfg), _i32]
 lib.cats_verify_layer_i8.argtypes = [C.POINTER(ModelCfg), C.POINTER(LayerWeightsI8), _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp,
                                      C.c_size_t, _vp, _vp]
 
-_FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
+# Checks and marshals the operands of the calls below (csrc/cats_py.cpp).
+if not os.path.exists(_build.PY_EXT):
+    _build.build_python()
+from . import _cats_py  # noqa: E402
 
-
-def _check_i8(what, rows, cols, device, *mats):
-    """Shapes, element types and devices of the 8-bit calls: the C entry points see pointers only.  mats: (tensor, shape, types)."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError("%s: tensors are on %s, the current device is cuda:%d" % (what, device, torch.cuda.current_device()))
-    for t, shape, types in mats:
-        if t.dtype not in types or tuple(t.shape) != shape or t.device != device:
-            raise ValueError("%s: expected %s of %s on %s, got %s of %s on %s" % (what, shape, types, device, tuple(t.shape), t.dtype, t.device))
-        if t.stride(-1) != 1 and t.shape[-1] > 1:
-            raise ValueError("%s: the last dimension must be contiguous" % what)
-
-
-def _ld(t):
-    """Row stride in elements (a single row's stride means nothing to torch)."""
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+_cats_py.bind(*[C.cast(getattr(lib, "cats_%s_i8" % n), _vp).value for n in ("quantize", "dequantize", "rmsnorm", "swiglu", "linear")])
 
 
 def new_i8(rows: int, cols: int, device="cuda"):
@@ -396,68 +385,53 @@ def new_i8(rows: int, cols: int, device="cuda"):
 
 
 def cats_quantize_i8(x, q, scale):
-    rows, cols = x.shape
-    _check_i8("cats_quantize_i8", rows, cols, x.device, (x, (rows, cols), _FLOATS), (q, (rows, cols), (torch.int8,)),
-              (scale, (rows,), (torch.float32,)))
-    _check(lib.cats_quantize_i8(x.data_ptr(), _FLOATS[x.dtype], _ld(x), rows, cols, q.data_ptr(), _ld(q), scale.data_ptr(), _stream()),
-           "cats_quantize_i8")
+    """x fp32 or bf16 [rows][cols] -> q int8 [rows][cols], scale fp32 [rows].  Like every call below: tensors on the current
+    device, rows contiguous and any row stride; ValueError for operands that do not fit each other."""
+    rc = _cats_py.quantize_i8(x, q, scale)
+    if rc:
+        raise CatsError(rc, "cats_quantize_i8")
 
 
 def cats_dequantize_i8(q, scale, out):
-    rows, cols = q.shape
-    _check_i8("cats_dequantize_i8", rows, cols, q.device, (q, (rows, cols), (torch.int8,)), (scale, (rows,), (torch.float32,)),
-              (out, (rows, cols), _FLOATS))
-    _check(lib.cats_dequantize_i8(q.data_ptr(), _ld(q), scale.data_ptr(), rows, cols, out.data_ptr(), _FLOATS[out.dtype], _ld(out),
-                                  _stream()), "cats_dequantize_i8")
+    """out fp32 or bf16 [rows][cols]."""
+    rc = _cats_py.dequantize_i8(q, scale, out)
+    if rc:
+        raise CatsError(rc, "cats_dequantize_i8")
 
 
 def cats_rmsnorm_i8(resid, delta, gain, eps, resid_out, q, scale):
     """delta and resid_out may be None; resid_out may be resid itself."""
-    rows, cols = resid.shape
-    mats = [(resid, (rows, cols), _FLOATS), (gain, (cols,), (torch.bfloat16,)), (q, (rows, cols), (torch.int8,)),
-            (scale, (rows,), (torch.float32,))]
-    if delta is not None:
-        mats.append((delta, (rows, cols), _FLOATS))
-    if resid_out is not None:
-        mats.append((resid_out, (rows, cols), (resid.dtype,)))
-    _check_i8("cats_rmsnorm_i8", rows, cols, resid.device, *mats)
-    _check(lib.cats_rmsnorm_i8(resid.data_ptr(), _FLOATS[resid.dtype], _ld(resid),
-                               None if delta is None else delta.data_ptr(), F32 if delta is None else _FLOATS[delta.dtype],
-                               0 if delta is None else _ld(delta), gain.data_ptr(), eps, rows, cols,
-                               None if resid_out is None else resid_out.data_ptr(), 0 if resid_out is None else _ld(resid_out),
-                               q.data_ptr(), _ld(q), scale.data_ptr(), _stream()), "cats_rmsnorm_i8")
+    rc = _cats_py.rmsnorm_i8(resid, delta, gain, eps, resid_out, q, scale)
+    if rc:
+        raise CatsError(rc, "cats_rmsnorm_i8")
 
 
 def cats_swiglu_i8(gate_up, q, scale):
-    rows, cols = q.shape
-    _check_i8("cats_swiglu_i8", rows, cols, q.device, (gate_up, (rows, 2 * cols), _FLOATS), (q, (rows, cols), (torch.int8,)),
-              (scale, (rows,), (torch.float32,)))
-    _check(lib.cats_swiglu_i8(gate_up.data_ptr(), _FLOATS[gate_up.dtype], _ld(gate_up), rows, cols, q.data_ptr(), _ld(q),
-                              scale.data_ptr(), _stream()), "cats_swiglu_i8")
+    """gate_up fp32 or bf16 [rows][2 * cols]."""
+    rc = _cats_py.swiglu_i8(gate_up, q, scale)
+    if rc:
+        raise CatsError(rc, "cats_swiglu_i8")
 
 
 def pack_weights_i8(w: torch.Tensor) -> torch.Tensor:
     """cats_pack_weights_i8: int8 [outs][cols] -> packed buffer (uint8 CUDA tensor, 1024-byte aligned)."""
     rows, cols = w.shape
-    _check_i8("pack_weights_i8", rows, cols, w.device, (w, (rows, cols), (torch.int8,)))
+    assert w.is_cuda and w.dtype == torch.int8 and w.stride(1) == 1
     n = int(lib.cats_packed_weight_i8_bytes(rows, cols))
     if n == 0:
         raise CatsError(-3, "cats_packed_weight_i8_bytes")
     buf = torch.empty(n + 1024, dtype=torch.uint8, device=w.device)
     off = (-buf.data_ptr()) % 1024
     out = buf[off:off + n]
-    _check(lib.cats_pack_weights_i8(w.data_ptr(), _ld(w), rows, cols, out.data_ptr(), _stream()), "cats_pack_weights_i8")
+    _check(lib.cats_pack_weights_i8(w.data_ptr(), w.stride(0) if rows > 1 else cols, rows, cols, out.data_ptr(), _stream()), "cats_pack_weights_i8")
     return out
 
 
 def cats_linear_i8(x, x_scale, w_packed, w_scale, out, status):
     """x int8 [rows][cols], rows starting on 16 bytes (see new_i8); w_packed: pack_weights_i8 of [outs][cols]; out [rows][outs]."""
-    (rows, cols), outs = x.shape, w_scale.shape[0]
-    _check_i8("cats_linear_i8", rows, cols, x.device, (x, (rows, cols), (torch.int8,)), (x_scale, (rows,), (torch.float32,)),
-              (w_packed, (-(-cols // 128) * -(-outs // 8) * 1024,), (torch.uint8,)), (w_scale, (outs,), (torch.float32,)),
-              (out, (rows, outs), _FLOATS), (status, (1,), (torch.int32,)))
-    _check(lib.cats_linear_i8(x.data_ptr(), _ld(x), x_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(), rows, cols, outs,
-                              out.data_ptr(), _FLOATS[out.dtype], _ld(out), status.data_ptr(), _stream()), "cats_linear_i8")
+    rc = _cats_py.linear_i8(x, x_scale, w_packed, w_scale, out, status)
+    if rc:
+        raise CatsError(rc, "cats_linear_i8")
 
 
 def quantize_weights_i8(w: torch.Tensor):

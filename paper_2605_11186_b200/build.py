@@ -5,6 +5,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcats.so")
+PY_EXT = os.path.join(HERE, "_cats_py.so")
 SOURCES = ["cats_api.cu", "cats_small_kernels.cu", "cats_gemm.cu", "cats_attn.cu", "cats_i8_rows.cu", "cats_i8_linear.cu"]
 HEADERS = ["cats_common.cuh", "cats_kernels.cuh", os.path.join("..", "..", "include", "cats.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -16,6 +17,26 @@ def _stale(lib=LIB) -> bool:
         return True
     t = os.path.getmtime(lib)
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
+
+
+def build_python(force: bool = False) -> str:
+    """The CPython extension that marshals the 8-bit calls' tensors (csrc/cats_py.cpp), for the torch that is installed."""
+    import sysconfig
+
+    import torch
+    src = os.path.join(CSRC, "cats_py.cpp")
+    deps = [src, os.path.join(HERE, "..", "include", "cats.h"), torch.__file__]
+    if not force and os.path.exists(PY_EXT) and all(os.path.getmtime(f) <= os.path.getmtime(PY_EXT) for f in deps):
+        return PY_EXT
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    tmp = PY_EXT + ".tmp.%d" % os.getpid()
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                           "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(root, "include"),
+                           "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
+                           src, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", tmp])
+    os.replace(tmp, PY_EXT)
+    return PY_EXT
 
 
 TIMELINE_LIB = os.path.join(HERE, "libcats_timeline.so")
@@ -38,3 +59,4 @@ def build(force: bool = False, verbose: bool = False, timeline: bool = False) ->
 if __name__ == "__main__":
     import sys
     print(build(force=True, verbose="-v" in sys.argv))
+    print(build_python(force=True))
