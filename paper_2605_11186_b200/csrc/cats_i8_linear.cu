@@ -6,15 +6,21 @@
 // of 16 up to 256).  For the few tokens of a tree the product is bound by reading w once from HBM:
 //   * w is packed (cats_pack_weights_i8) K block by K block: [K / 128][outs / 8] groups of 8 rows x 128 bytes, each group
 //     in the 128-byte-swizzle layout tcgen05.mma reads.  Any R rows of one K block, R a multiple of 8, are one
-//     contiguous run, so R is free and is chosen so that the tiles fill the SMs evenly (linear_plan).
+//     contiguous run, so R is free and is chosen so that the tiles fill the SMs evenly (linear_tiling).
 //   * x is row-major as the row kernels leave it; TMA boxes of 128 bytes x ceil8(tokens) rows bring it in, zeros beyond the
 //     last row and column.
 // Warp 0 (one thread) copies w, warp 1 (one thread) copies x into a ring of shared-memory stages with mbarrier completion;
 // warp 2 issues tcgen05.mma into one of two TMEM accumulators; warps 4-7 drain the other one: int32 -> fp32 * sx * sw ->
 // bf16 or fp32 rows.  Rows of a stage that no copy writes (tokens beyond the last, channels beyond the last) hold
 // leftovers; they only reach accumulator rows and columns that are not stored.
+// With few tiles the K blocks are cut into `split` shares, one CTA of a cluster each.  The partial sums meet in distributed
+// shared memory: the accumulator's 16-channel groups are dealt out to the CTAs, every CTA stores its int32 partial of a group
+// into the memory of the group's owner (each sender has its own place there), one cluster barrier publishes them, and the
+// owners add and store.  Whole numbers: the order of the sums does not matter, and nothing is left in global memory.
 // Every wait is bounded; on expiry the CTA reports CATS_ERR_TIMEOUT, lets its copies land, frees its TMEM and returns.
 #include <cuda.h>
+
+#include <mutex>
 
 #include "cats_kernels.cuh"
 
@@ -31,6 +37,7 @@ constexpr int kSms = 148;
 struct LinearDev {
     int rows, outs, n_kb;
     int R;                  // output channels per tile
+    int split, kb_share;    // CTAs per tile (one cluster), K blocks of each
     int m_blocks;           // blocks of 128 tokens
     int n_tiles;            // m_blocks * ceil(outs / R), token blocks fastest
     int x_rows;             // rows of an x box
@@ -40,6 +47,7 @@ struct LinearDev {
     uint32_t x_chunk;
     uint32_t stage_bytes;
     uint32_t tail;          // bytes behind the last stage that its last x chunk is read over as 128 rows
+    uint32_t recv_bytes;    // partial sums from the other CTAs of the cluster: [own groups][split - 1 senders]
     uint32_t tmem_cols;
     const uint8_t* w;
     const float *sx, *sw;
@@ -68,6 +76,22 @@ __device__ __forceinline__ void umma_i8(uint32_t tmem_d, uint64_t desc_a, uint64
         ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"((uint32_t)accumulate)
         : "memory");
 }
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t local_smem, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local_smem), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, const float* v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Partial sums of one 16-channel group from one sender: [x_rows tokens][16] int32.  The four 16-byte pieces of a token are
+// permuted by its index, so that eight neighbouring lanes touch all 32 banks.
+__device__ __forceinline__ uint32_t part_bytes(int x_rows) { return (uint32_t)x_rows * 64u; }
+__device__ __forceinline__ uint32_t part_piece(int t, int i) { return (uint32_t)t * 64u + (uint32_t)((i ^ ((t >> 1) & 3)) << 4); }
+
 __device__ __forceinline__ void bulk_copy(void* smem_dst, const void* gsrc, uint32_t bytes, uint64_t* bar, uint64_t policy) {
     asm volatile(
         "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
@@ -96,15 +120,17 @@ __device__ __forceinline__ void store16(const LinearDev& p, long long t, int n0,
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        if (n0 + i >= p.outs) break;
-        if (p.out_f32) ((float*)p.out)[t * p.ldo + n0 + i] = v[i];
-        else ((uint16_t*)p.out)[t * p.ldo + n0 + i] = float_to_bf16_bits(v[i]);
+        if (n0 + i < p.outs) {
+            if (p.out_f32) ((float*)p.out)[t * p.ldo + n0 + i] = v[i];
+            else ((uint16_t*)p.out)[t * p.ldo + n0 + i] = float_to_bf16_bits(v[i]);
+        }
     }
 }
 
 __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const __grid_constant__ CUtensorMap tm_x) {
-    extern __shared__ __align__(1024) uint8_t smem[];      // [stages][stage_bytes], the tail, channel scales, control block
-    float* const sw_s = reinterpret_cast<float*>(smem + (size_t)p.stages * p.stage_bytes + p.tail);
+    extern __shared__ __align__(1024) uint8_t smem[];      // [stages][stage_bytes], the tail, received partials, channel scales, control block
+    uint8_t* const recv = smem + (size_t)p.stages * p.stage_bytes + p.tail;
+    float* const sw_s = reinterpret_cast<float*>(recv + p.recv_bytes);
     Ctrl* const ctrl = reinterpret_cast<Ctrl*>(sw_s + 4 * 256);
     volatile int* const abort_flag = &ctrl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -133,9 +159,14 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = ctrl->tmem_base;
+    const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
+    if (p.split > 1) cluster_arrive();        // waited for before the first store into a peer: every CTA of the cluster has started
     pdl_launch_dependents();
-    const int S = p.stages, G = (int)gridDim.x;
-    const int n_units = (p.n_kb + p.unit - 1) / p.unit;
+    const int S = p.stages;
+    // split == 1: tiles blockIdx.x, + gridDim.x, ...; else exactly one tile, K blocks [kb0, kb0 + n_kb)
+    const int G = p.split > 1 ? p.n_tiles : (int)gridDim.x, first = (int)blockIdx.x / p.split;
+    const int kb0 = rank * p.kb_share, n_kb = min(p.n_kb - kb0, p.kb_share);
+    const int n_units = (n_kb + p.unit - 1) / p.unit;
     const size_t kb_stride = (size_t)((p.outs + 7) / 8) * 1024;       // packed bytes of one K block
     // stage layout: unit chunks of w, then unit chunks of x
     if (warp <= 1) {
@@ -147,22 +178,22 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             int s = 0, issued = 0;
             uint32_t par = 1;
             bool ok = true;
-            for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += G) {
+            for (int tile = first; tile < p.n_tiles && ok; tile += G) {
                 const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
                 const int n0 = nt * p.R;
                 const uint32_t w_bytes = (uint32_t)min(p.R, (p.outs - n0 + 7) / 8 * 8) * kKb;
-                const uint8_t* src = p.w + (size_t)(n0 >> 3) * 1024;
+                const uint8_t* src = p.w + (size_t)kb0 * kb_stride + (size_t)(n0 >> 3) * 1024;
                 for (int u = 0, kb = 0; u < n_units; ++u) {
                     if (issued >= S && !mbar_wait(&ctrl->empty[s], par, abort_flag)) { ok = false; break; }
                     uint8_t* stage = smem + (size_t)s * p.stage_bytes;
-                    const int nk = min(p.unit, p.n_kb - kb);
+                    const int nk = min(p.unit, n_kb - kb);
                     if (is_w) {
                         mbar_expect_tx(&ctrl->full[s], w_bytes * nk);
                         for (int j = 0; j < nk; ++j, ++kb, src += kb_stride) bulk_copy(stage + j * p.w_chunk, src, w_bytes, &ctrl->full[s], pol);
                     } else {
                         mbar_expect_tx(&ctrl->full[s], p.x_chunk * nk);
                         for (int j = 0; j < nk; ++j, ++kb)
-                            tma_load_2d(stage + p.unit * p.w_chunk + j * p.x_chunk, &tm_x, kb * kKb, mb * 128, &ctrl->full[s], pol);
+                            tma_load_2d(stage + p.unit * p.w_chunk + j * p.x_chunk, &tm_x, (kb0 + kb) * kKb, mb * 128, &ctrl->full[s], pol);
                     }
                     ++issued;
                     if (++s == S) { s = 0; par ^= 1u; }
@@ -179,7 +210,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             int s = 0, seg = 0;
             uint32_t par = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += G, ++seg) {
+            for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
                 const int b = seg & 1;
                 if (seg >= 2) ok = mbar_wait(&ctrl->acc_empty[b], ((seg >> 1) - 1) & 1, abort_flag);
                 tc_fence_after_sync();
@@ -188,7 +219,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
                     ok = mbar_wait(&ctrl->full[s], par, abort_flag);
                     if (!ok) break;
                     tc_fence_after_sync();
-                    const int nk = min(p.unit, p.n_kb - kb);
+                    const int nk = min(p.unit, n_kb - kb);
                     const uint32_t w_addr = smem_u32(smem + (size_t)s * p.stage_bytes);
                     const uint32_t x_addr = w_addr + p.unit * p.w_chunk;
                     for (int j = 0; j < nk; ++j, ++kb) {
@@ -208,27 +239,69 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
         float* const sw = sw_s + q4 * 256;       // one copy of the tile's channel scales per warp: no barrier needed
         int seg = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += G, ++seg) {
+        for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
             const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
             const int n0 = nt * p.R, b = seg & 1;
-            const long long t = (long long)mb * 128 + q4 * 32 + lane;
+            const int tl = q4 * 32 + lane;
+            const long long t = (long long)mb * 128 + tl;
             __syncwarp();
             for (int i = lane; i < p.R; i += 32) sw[i] = n0 + i < p.outs ? __ldg(p.sw + n0 + i) : 0.f;
             __syncwarp();
             const float sx = t < p.rows ? __ldg(p.sx + t) : 0.f;
             ok = mbar_wait(&ctrl->acc_full[b], (seg >> 1) & 1, abort_flag) && !*abort_flag;
             tc_fence_after_sync();
-            if (ok && mb * 128 + q4 * 32 < p.rows) {
-                const uint32_t taddr = tmem + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * p.R);
-                for (int c = 0; c < p.R && n0 + c < p.outs; c += 16) {
+            const bool busy = mb * 128 + q4 * 32 < p.rows;         // this warp holds tokens
+            const uint32_t taddr = tmem + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * p.R);
+            const int n_groups = p.R / 16;
+            if (p.split > 1) {
+                cluster_wait();
+                if (busy)
+                    for (int g = 0; g < n_groups; ++g) {
+                        const int owner = g % p.split;
+                        if (owner == rank) continue;
+                        float acc[16];
+                        tmem_ld16(taddr + g * 16, acc);
+                        if (tl < p.x_rows) {
+                            const int from = rank < owner ? rank : rank - 1;
+                            const uint32_t dst = cluster_addr(smem_u32(recv), owner) + (uint32_t)((g / p.split) * (p.split - 1) + from) * part_bytes(p.x_rows);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) st_cluster_v4(dst + part_piece(tl, i), acc + 4 * i);
+                        }
+                    }
+                __syncwarp();
+                cluster_arrive();
+                cluster_wait();
+            }
+            if (ok && busy) {
+                for (int g = rank; g < n_groups && n0 + g * 16 < p.outs; g += p.split) {
                     float acc[16];
-                    tmem_ld16(taddr + c, acc);
-                    if (t < p.rows) store16(p, t, n0 + c, acc, sx, sw + c);
+                    tmem_ld16(taddr + g * 16, acc);
+                    if (t < p.rows) {
+                        for (int from = 0; from < p.split - 1; ++from) {
+                            const uint8_t* src = recv + ((size_t)(g / p.split) * (p.split - 1) + from) * part_bytes(p.x_rows);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int4 v = *reinterpret_cast<const int4*>(src + part_piece(tl, i));
+                                acc[4 * i] = __int_as_float(__float_as_int(acc[4 * i]) + v.x);
+                                acc[4 * i + 1] = __int_as_float(__float_as_int(acc[4 * i + 1]) + v.y);
+                                acc[4 * i + 2] = __int_as_float(__float_as_int(acc[4 * i + 2]) + v.z);
+                                acc[4 * i + 3] = __int_as_float(__float_as_int(acc[4 * i + 3]) + v.w);
+                            }
+                        }
+                        store16(p, t, n0 + g * 16, acc, sx, sw + g * 16);
+                    }
+                    __syncwarp();
                 }
             }
             tc_fence_before_sync();
             mbar_arrive(&ctrl->acc_empty[b]);
         }
+    }
+    if (p.split > 1 && warp < 4) {            // the other warps' part in the two phases of the cluster barrier
+        __syncwarp();
+        cluster_wait();
+        cluster_arrive();
+        cluster_wait();
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -283,29 +356,82 @@ bool x_tensor_map(const I8Linear& p, int box_rows, CUtensorMap* out) {
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Opts a kernel into large shared memory, once per device.
-template <typename K> cudaError_t allow_smem(K kernel, bool (&done)[64]) {
+inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+struct Tiling {
+    int R, split;
+};
+
+// Channels per tile and CTAs per tile, by what the busiest SM has to take in: an SM takes 57 bytes of w and x per ns (measured,
+// 64 tokens x 4096 columns x 22016 channels), a K block costs its issuing threads 0.1 us however small it is, and the
+// exchange of a split tile about 1.2 us.  clusters[i]: clusters of 2^i CTAs that fit the device at once.
+Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&clusters)[4]) {
+    const int n_kb = ceil_div(p.cols, kKb);
+    Tiling best = {256, 1};
+    float best_ns = 1e30f;
+    for (int i = 0; i < 4; ++i) {
+        const int c = 1 << i;
+        const int share = ceil_div(n_kb, c);
+        if ((c - 1) * share >= n_kb) break;                         // a CTA without K blocks
+        for (int R = 256; R >= 16; R -= 16) {
+            const long long tiles = (long long)m_blocks * ceil_div(p.outs, R);
+            if (c > 1 && tiles > clusters[i]) break;
+            if (ceil_div(R / 16, c) * (c - 1) * (x_rows * 64) > 64 * 1024) continue;      // received partials: 64 KB at most
+            const float waves = (float)((tiles + clusters[i] - 1) / clusters[i]);
+            const float kb_ns = fmaxf((float)(R + x_rows) * (kKb / 57.f), 100.f);
+            const float ns = waves * share * kb_ns + (c > 1 ? 1200.f : 0.f);
+            if (ns < best_ns) { best_ns = ns; best = {R, c}; }
+        }
+    }
+    return best;
+}
+
+cudaError_t launch_clusters(const LinearDev& d, const CUtensorMap& tm, int grid, size_t smem, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)d.split, 1, 1};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = g_call_boundary ? 1 : 2;
+    g_call_boundary = false;
+    ++g_launch_count;
+    return cudaLaunchKernelEx(&cfg, k_linear_i8, d, tm);
+}
+
+// Per device, once: large shared memory for the kernel, and how many clusters of 2, 4 and 8 CTAs (one CTA per SM) fit at once.
+cudaError_t linear_device(const int (**clusters)[4]) {
+    static int known[64][4];
+    static std::mutex mu;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
-    if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
-    return e;
-}
-
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
-
-// Channels per tile: the multiple of 16 that gives the busiest SM the least to read, w rows and x rows together.
-int linear_tile(const I8Linear& p, int m_blocks, int x_rows) {
-    int best = 256;
-    long long best_cost = 1ll << 62;
-    for (int R = 256; R >= 16; R -= 16) {
-        const long long tiles = (long long)m_blocks * ceil_div(p.outs, R);
-        const long long cost = (tiles + kSms - 1) / kSms * (R + x_rows);
-        if (cost < best_cost) { best_cost = cost; best = R; }
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(mu);
+    *clusters = &known[dev];
+    if (known[dev][0] != 0) return cudaSuccess;
+    e = cudaFuncSetAttribute(k_linear_i8, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
+    if (e != cudaSuccess) return e;
+    for (int i = 1; i < 4; ++i) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(kSms / (1 << i) * (1 << i));
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kSmemMax;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim = {1u << i, 1, 1};
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&known[dev][i], k_linear_i8, &cfg);
+        if (e != cudaSuccess) return e;
     }
-    return best;
+    known[dev][0] = kSms;
+    return cudaSuccess;
 }
 
 }  // namespace
@@ -320,14 +446,17 @@ cudaError_t launch_pack_weights_i8(const int8_t* src, long long ld, int rows, in
 }
 
 cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
-    static bool done[64];
-    cudaError_t e = allow_smem(k_linear_i8, done);
+    const int(*clusters)[4];
+    cudaError_t e = linear_device(&clusters);
     if (e != cudaSuccess) return e;
     LinearDev d = {};
     d.rows = p.rows; d.outs = p.outs; d.n_kb = ceil_div(p.cols, kKb);
     d.m_blocks = ceil_div(p.rows, 128);
     d.x_rows = p.rows >= 128 ? 128 : ceil_div(p.rows, 8) * 8;
-    d.R = linear_tile(p, d.m_blocks, d.x_rows);
+    const Tiling tiling = linear_tiling(p, d.m_blocks, d.x_rows, *clusters);
+    d.R = tiling.R;
+    d.split = tiling.split;
+    d.kb_share = ceil_div(d.n_kb, d.split);
     const long long tiles = (long long)d.m_blocks * ceil_div(p.outs, d.R);
     if (tiles > (1ll << 30)) return cudaErrorInvalidValue;
     d.n_tiles = (int)tiles;
@@ -337,7 +466,8 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.unit = max(1, min(8, 24 * 1024 / (int)(d.w_chunk + d.x_chunk)));
     d.stage_bytes = d.unit * (d.w_chunk + d.x_chunk);
     d.tail = 128u * kKb - d.x_chunk;
-    const int fixed = (int)d.tail + 4 * 256 * 4 + kCtrl;
+    d.recv_bytes = (uint32_t)(ceil_div(d.R / 16, d.split) * (d.split - 1) * d.x_rows * 64);
+    const int fixed = (int)(d.tail + d.recv_bytes) + 4 * 256 * 4 + kCtrl;
     d.stages = min(kMaxStages, (kSmemMax - fixed) / (int)d.stage_bytes);
     if (d.stages < 2) return cudaErrorInvalidConfiguration;
     d.tmem_cols = 32;
@@ -348,8 +478,8 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.d_status = p.d_status;
     CUtensorMap tm;
     if (!x_tensor_map(p, d.x_rows, &tm)) return cudaErrorNotSupported;
-    const int grid = d.n_tiles < kSms ? d.n_tiles : kSms;
-    return launch_pdl(k_linear_i8, dim3(grid), dim3(kThreads), (size_t)d.stages * d.stage_bytes + fixed, st, d, tm);
+    const int grid = d.split > 1 ? d.n_tiles * d.split : (d.n_tiles < kSms ? d.n_tiles : kSms);
+    return launch_clusters(d, tm, grid, (size_t)d.stages * d.stage_bytes + fixed, st);
 }
 
 cudaError_t set_wait_limit_i8(unsigned long long ns) { return cudaMemcpyToSymbol(g_wait_limit_ns, &ns, sizeof(ns)); }

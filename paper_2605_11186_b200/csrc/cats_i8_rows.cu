@@ -16,18 +16,20 @@ namespace {
 
 constexpr float kTinyMax = 7.888609052210118e-31f;    // 2^-100: the smallest maximum a scale is made from
 
-template <typename T> struct Elem;
-template <> struct Elem<float> {
-    static __device__ __forceinline__ float get(const float* p) { return __ldg(p); }
-    static __device__ __forceinline__ void get8(const float* p, float* v) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+// One vector of V elements as it lies in memory: V == 8 in 16-byte pieces, V == 1 a single element.  Loads and conversion
+// are apart so that a thread can have all its loads in flight before it uses the first.
+template <typename T, int V> struct Raw;
+template <> struct Raw<float, 8> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
+    __device__ __forceinline__ void get(float* v) const {
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
 };
-template <> struct Elem<uint16_t> {     // bf16 bits
-    static __device__ __forceinline__ float get(const uint16_t* p) { return bf16_bits_to_float(__ldg(p)); }
-    static __device__ __forceinline__ void get8(const uint16_t* p, float* v) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
+template <> struct Raw<uint16_t, 8> {     // bf16 bits
+    uint4 a;
+    __device__ __forceinline__ void load(const uint16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void get(float* v) const {
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -36,66 +38,46 @@ template <> struct Elem<uint16_t> {     // bf16 bits
         }
     }
 };
-template <typename T, int V> __device__ __forceinline__ void load_v(const T* p, float* v) {
-    if (V == 8) Elem<T>::get8(p, v);
-    else v[0] = Elem<T>::get(p);
-}
-// a residual or delta element that another thread of this launch never writes, but that may be overwritten in place by
-// the same thread afterwards: plain loads, not the read-only path
-template <int V> __device__ __forceinline__ void load_rw(const void* base, long long off, bool f32, float* v) {
-    if (f32) {
-        const float* p = (const float*)base + off;
-        if (V == 8) {
-            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            v[0] = p[0];
-        }
-    } else {
-        const uint16_t* p = (const uint16_t*)base + off;
-        if (V == 8) {
-            const uint4 a = *reinterpret_cast<const uint4*>(p);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
-        } else {
-            v[0] = bf16_bits_to_float(p[0]);
-        }
-    }
-}
-template <int V> __device__ __forceinline__ void store_rw(void* base, long long off, bool f32, const float* v) {
-    if (f32) {
-        float* p = (float*)base + off;
-        if (V == 8) {
-            reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            p[0] = v[0];
-        }
-    } else {
-        uint16_t* p = (uint16_t*)base + off;
-        if (V == 8)
-            *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-        else
-            p[0] = float_to_bf16_bits(v[0]);
-    }
-}
-// (y rs) inv and not y (rs inv): |y rs| <= a, so the result is finite and within 127 (1 + 2^-22) whatever rs and a are
-template <int V> __device__ __forceinline__ void store_q(int8_t* p, const float* y, float rs, float inv) {
+template <> struct Raw<float, 1> {
+    float a;
+    __device__ __forceinline__ void load(const float* p) { a = *p; }
+    __device__ __forceinline__ void get(float* v) const { v[0] = a; }
+};
+template <> struct Raw<uint16_t, 1> {
+    uint16_t a;
+    __device__ __forceinline__ void load(const uint16_t* p) { a = *p; }
+    __device__ __forceinline__ void get(float* v) const { v[0] = bf16_bits_to_float(a); }
+};
+template <int V> __device__ __forceinline__ void store_v(float* p, const float* v) {
     if (V == 8) {
-        uint32_t w[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            w[h] = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[h] |= ((uint32_t)__float2int_rn(y[h * 4 + i] * rs * inv) & 0xFFu) << (8 * i);
-        }
-        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
-        p[0] = (int8_t)__float2int_rn(y[0] * rs * inv);
+        p[0] = v[0];
+    }
+}
+template <int V> __device__ __forceinline__ void store_v(uint16_t* p, const float* v) {
+    if (V == 8)
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    else
+        p[0] = float_to_bf16_bits(v[0]);
+}
+// rint((y rs) inv) as bytes.  (y rs) inv and not y (rs inv): |y rs| <= a, so the result is finite and within
+// 127 (1 + 2^-23) whatever rs and a are.  The fused product and sum with 1.5 * 2^23 leaves the whole number (ties to even) in
+// the low bits of the result: the conversion instruction has a sixteenth of the FMA rate and shares its unit with ex2 and rcp.
+constexpr float kRintMagic = 12582912.f;
+template <int V> __device__ __forceinline__ void store_q(int8_t* p, const float* y, float rs, float inv) {
+    uint32_t w[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = __float_as_uint(fmaf(y[i] * rs, inv, kRintMagic));
+    if (V == 8) {
+        uint32_t o[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            o[h] = __byte_perm(__byte_perm(w[h * 4 % V], w[(h * 4 + 1) % V], 0x0040), __byte_perm(w[(h * 4 + 2) % V], w[(h * 4 + 3) % V], 0x0040), 0x5410);
+        *reinterpret_cast<uint2*>(p) = make_uint2(o[0], o[1]);
+    } else {
+        p[0] = (int8_t)(w[0] & 0xFFu);
     }
 }
 
@@ -103,64 +85,95 @@ __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v
 // silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.
 __device__ __forceinline__ float silu_mul(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
 
-// One vector of the row at column c: the values y (before the norm's row factor) of this operator.
-template <int OP, typename TX, int V>
-__device__ __forceinline__ void row_values(const I8RowsDev& p, long long row, int c, float* y, float& ss, bool write_resid) {
-    if (OP == I8_NORM) {
-        float r[V], g[V];
-        load_rw<V>(p.x, row * p.ldx + c, p.x_f32, r);
-        load_v<uint16_t, V>((const uint16_t*)p.gain + c, g);
-        if (p.delta != nullptr) {
-            float d[V];
-            load_rw<V>(p.delta, row * p.ldd + c, p.d_f32, d);
-#pragma unroll
-            for (int i = 0; i < V; ++i) r[i] += d[i];
-        }
-        if (write_resid && p.resid_out != nullptr) store_rw<V>(p.resid_out, row * p.ldo + c, p.x_f32, r);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            ss = fmaf(r[i], r[i], ss);
-            y[i] = r[i] * g[i];
-        }
-    } else if (OP == I8_SWIGLU) {
-        float g[V], u[V];
-        load_v<TX, V>((const TX*)p.x + row * p.ldx + c, g);
-        load_v<TX, V>((const TX*)p.x + row * p.ldx + p.cols + c, u);
-#pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = silu_mul(g[i], u[i]);
-    } else {
-        load_v<TX, V>((const TX*)p.x + row * p.ldx + c, y);
-    }
-}
+struct NoDelta {};        // the norm without a delta
+template <typename T, int V> struct MaybeRaw : Raw<T, V> { static constexpr bool has = true; };
+template <int V> struct MaybeRaw<NoDelta, V> {
+    static constexpr bool has = false;
+    __device__ __forceinline__ void load(const void*) {}
+    __device__ __forceinline__ void get(float*) const {}
+};
 
-// NT threads per row.  NV > 0: the row fits NV vectors of V elements per thread and stays in registers.  NV == 0: any
-// length; the row is read twice.  NT == 32: a block of 128 threads holds four rows, one per warp, and needs no barrier.
-template <int OP, typename TX, int V, int NV, int NT>
-__global__ void __launch_bounds__(NT == 32 ? 128 : NT) k_i8_rows(const I8RowsDev p) {
+// One vector of a row at column c, and from it the values y (before the norm's row factor).
+// TD: SWIGLU's up values (TX), the norm's delta, or NoDelta.
+template <int OP, typename TX, typename TD, int V> struct RowVec {
+    Raw<TX, V> x;
+    MaybeRaw<TD, V> d;
+    Raw<uint16_t, V> g;
+    __device__ __forceinline__ void load(const I8RowsDev& p, long long row, int c) {
+        x.load((const TX*)p.x + row * p.ldx + c);
+        if (OP == I8_SWIGLU) d.load((const TD*)p.x + row * p.ldx + p.cols + c);
+        if (OP == I8_NORM) {
+            d.load((const TD*)p.delta + row * p.ldd + c);
+            g.load((const uint16_t*)p.gain + c);
+        }
+    }
+    __device__ __forceinline__ void values(const I8RowsDev& p, long long row, int c, float* y, float& ss, bool write_resid) const {
+        x.get(y);
+        if (OP == I8_NORM) {
+            float t[V];
+            if (MaybeRaw<TD, V>::has) {
+                d.get(t);
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] += t[i];
+                if (write_resid && p.resid_out != nullptr) store_v<V>((TX*)p.resid_out + row * p.ldo + c, y);
+            } else if (write_resid && p.resid_out != nullptr && p.resid_out != p.x) {
+                store_v<V>((TX*)p.resid_out + row * p.ldo + c, y);
+            }
+            g.get(t);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                ss = fmaf(y[i], y[i], ss);
+                y[i] *= t[i];
+            }
+        } else if (OP == I8_SWIGLU) {
+            float u[V];
+            d.get(u);
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = silu_mul(y[i], u[i]);
+        }
+    }
+};
+
+// Largest block: two vectors of 8 of a single input fit the 64 registers of 1024 threads, the norm's three inputs do not.
+template <int OP, int V, int NV> __host__ __device__ constexpr int row_threads() { return V == 8 && NV <= 2 && OP != I8_NORM ? 1024 : 512; }
+
+// A block per row, NV vectors of V elements per thread (NV * V * blockDim.x >= cols): the row is read once and stays in
+// registers.  LONG: any length, the row is read twice.  WARP: blocks of 128 threads hold four rows, one per warp, and need
+// no barrier.
+template <int OP, typename TX, typename TD, int V, int NV, bool WARP, bool LONG>
+__global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_rows(const I8RowsDev p) {
     __shared__ float red_s[32];
     __shared__ uint32_t red_m[32];
     pdl_launch_dependents();
-    const long long row = NT == 32 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    const int tid = NT == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
+    const long long row = WARP ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    const int tid = WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
+    const int NT = WARP ? 32 : (int)blockDim.x;
     pdl_wait();
-    if (NT == 32 && row >= p.rows) return;
-    constexpr int NR = NV > 0 ? NV : 1;
-    float y[NR][V];
+    if (WARP && row >= p.rows) return;
+    float y[NV][V];
     float ss = 0.f;
     uint32_t mx = 0;
-    if (NV > 0) {
+    if (!LONG) {
+        RowVec<OP, TX, TD, V> in[NV];
 #pragma unroll
-        for (int k = 0; k < NR; ++k) {
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * NT + tid) * V;
+            if (c < p.cols) in[k].load(p, row, c);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
             const int c = (k * NT + tid) * V;
             if (c < p.cols) {
-                row_values<OP, TX, V>(p, row, c, y[k], ss, true);
+                in[k].values(p, row, c, y[k], ss, true);
 #pragma unroll
                 for (int i = 0; i < V; ++i) mx = max(mx, abs_bits(y[k][i]));
             }
         }
     } else {
         for (int c = tid * V; c < p.cols; c += NT * V) {
-            row_values<OP, TX, V>(p, row, c, y[0], ss, false);
+            RowVec<OP, TX, TD, V> in;
+            in.load(p, row, c);
+            in.values(p, row, c, y[0], ss, false);
 #pragma unroll
             for (int i = 0; i < V; ++i) mx = max(mx, abs_bits(y[0][i]));
         }
@@ -170,13 +183,13 @@ __global__ void __launch_bounds__(NT == 32 ? 128 : NT) k_i8_rows(const I8RowsDev
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     }
-    if (NT > 32) {
+    if (!WARP) {
         if ((tid & 31) == 0) {
             red_m[tid >> 5] = mx;
             red_s[tid >> 5] = ss;
         }
         __syncthreads();
-        const int nw = NT / 32, l = tid & 31;
+        const int nw = NT >> 5, l = tid & 31;
         mx = l < nw ? red_m[l] : 0u;
         mx = __reduce_max_sync(0xffffffffu, mx);
         if (OP == I8_NORM) {
@@ -194,9 +207,9 @@ __global__ void __launch_bounds__(NT == 32 ? 128 : NT) k_i8_rows(const I8RowsDev
     if (!finite) rs = 0.f;
     if (tid == 0) p.scale[row] = finite ? a / 127.f : __int_as_float(0x7FC00000);
     int8_t* const q = p.q + row * p.ldq;
-    if (NV > 0) {
+    if (!LONG) {
 #pragma unroll
-        for (int k = 0; k < NR; ++k) {
+        for (int k = 0; k < NV; ++k) {
             const int c = (k * NT + tid) * V;
             if (c < p.cols) {
                 if (!finite)
@@ -207,7 +220,9 @@ __global__ void __launch_bounds__(NT == 32 ? 128 : NT) k_i8_rows(const I8RowsDev
         }
     } else {
         for (int c = tid * V; c < p.cols; c += NT * V) {
-            row_values<OP, TX, V>(p, row, c, y[0], ss, true);
+            RowVec<OP, TX, TD, V> in;
+            in.load(p, row, c);
+            in.values(p, row, c, y[0], ss, true);
             if (!finite)
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[0][i] = 0.f;
@@ -229,13 +244,16 @@ __global__ void __launch_bounds__(256) k_i8_dequantize(const int8_t* __restrict_
     for (int c = blockIdx.y * 4096 + threadIdx.x * V; c < c_end; c += 256 * V) {
         float v[V];
         if (V == 8) {
+            // a byte b as the float 2^23 + (b + 128), then minus 2^23 + 128: exact, and no conversion instruction
             const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + row * ldq + c));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i % V] = (float)(int8_t)(((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xFFu) * s;
+            for (int i = 0; i < 8; ++i)
+                v[i % V] = (__uint_as_float(__byte_perm((i < 4 ? w.x : w.y) ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s;
         } else {
             v[0] = (float)q[row * ldq + c] * s;
         }
-        store_rw<V>(out, row * ldo + c, out_f32 != 0, v);
+        if (out_f32) store_v<V>((float*)out + row * ldo + c, v);
+        else store_v<V>((uint16_t*)out + row * ldo + c, v);
     }
 }
 
@@ -272,33 +290,40 @@ __global__ void __launch_bounds__(256) k_i8_qkv(const float* __restrict__ qkv, c
     }
 }
 
-template <int OP, typename TX, int V>
+constexpr int kMinRowsMany = 148 * 4;     // rows from which on throughput counts, not the latency of one row
+
+template <int OP, typename TX, typename TD, int V>
 cudaError_t launch_rows_v(const I8RowsDev& p, cudaStream_t st) {
-    const dim3 per_row((unsigned)p.rows);
     const int vecs = (p.cols + V - 1) / V;          // vectors of a row
-    if (vecs <= 32 * 4) return launch_pdl(k_i8_rows<OP, TX, V, 4, 32>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, st, p);
-    if (vecs <= 512) return launch_pdl(k_i8_rows<OP, TX, V, 1, 512>, per_row, dim3(512), 0, st, p);
-    if (vecs <= 1024) return launch_pdl(k_i8_rows<OP, TX, V, 2, 512>, per_row, dim3(512), 0, st, p);
-    if (vecs <= 2048) return launch_pdl(k_i8_rows<OP, TX, V, 4, 512>, per_row, dim3(512), 0, st, p);
-    return launch_pdl(k_i8_rows<OP, TX, V, 0, 512>, per_row, dim3(512), 0, st, p);
+    constexpr int N = V == 8 ? 1 : (OP == I8_NORM ? 4 : 8);     // single elements: more of them per thread, as registers allow
+    if (vecs <= 32 * 4 * N) return launch_pdl(k_i8_rows<OP, TX, TD, V, 4 * N, true, false>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, st, p);
+    const dim3 grid((unsigned)p.rows);
+    auto threads = [&](int nv) { return dim3((unsigned)((vecs + nv * 32 - 1) / (nv * 32) * 32)); };
+    const bool many = p.rows >= kMinRowsMany;
+    if (vecs <= 512 * N && !many) return launch_pdl(k_i8_rows<OP, TX, TD, V, N, false, false>, grid, threads(N), 0, st, p);
+    if (vecs <= 2 * N * row_threads<OP, V, 2 * N>() && !many) return launch_pdl(k_i8_rows<OP, TX, TD, V, 2 * N, false, false>, grid, threads(2 * N), 0, st, p);
+    if (vecs <= 2048 * N) return launch_pdl(k_i8_rows<OP, TX, TD, V, 4 * N, false, false>, grid, threads(4 * N), 0, st, p);
+    return launch_pdl(k_i8_rows<OP, TX, TD, V, N, false, true>, grid, dim3(512), 0, st, p);
+}
+
+template <int OP, typename TX, typename TD>
+cudaError_t launch_rows_t(const I8RowsDev& p, cudaStream_t st) {
+    // vectors of 8 elements where every row of every operand starts on a vector
+    auto vec = [](const void* q, long long ld, size_t size) { return q == nullptr || (((uintptr_t)q % 16) == 0 && (ld * (long long)size) % 16 == 0); };
+    const bool v8 = p.cols % 8 == 0 && vec(p.x, p.ldx, sizeof(TX)) && vec(p.delta, p.ldd, p.d_f32 ? 4 : 2) && vec(p.resid_out, p.ldo, sizeof(TX)) &&
+                    ((uintptr_t)p.gain % 16) == 0 && ((uintptr_t)p.q % 8) == 0 && p.ldq % 8 == 0;
+    return v8 ? launch_rows_v<OP, TX, TD, 8>(p, st) : launch_rows_v<OP, TX, TD, 1>(p, st);
 }
 
 }  // namespace
 
 cudaError_t launch_i8_rows(int op, const I8RowsDev& p, cudaStream_t st) {
-    // vectors of 8 elements where every row of every operand starts on a vector
-    auto vec = [&](const void* q, long long ld, int size) { return q == nullptr || (((uintptr_t)q % 16) == 0 && (ld * size) % 16 == 0); };
-    const int xs = p.x_f32 ? 4 : 2;
-    const bool v8 = p.cols % 8 == 0 && vec(p.x, p.ldx, xs) && vec(p.delta, p.ldd, p.d_f32 ? 4 : 2) && vec(p.resid_out, p.ldo, xs) &&
-                    ((uintptr_t)p.gain % 16) == 0 && ((uintptr_t)p.q % 8) == 0 && p.ldq % 8 == 0;
-#define CATS_I8_ROWS(OP) \
-    (op == OP) return p.x_f32 ? (v8 ? launch_rows_v<OP, float, 8>(p, st) : launch_rows_v<OP, float, 1>(p, st)) \
-                              : (v8 ? launch_rows_v<OP, uint16_t, 8>(p, st) : launch_rows_v<OP, uint16_t, 1>(p, st))
-    if CATS_I8_ROWS(I8_SWIGLU);
-    if CATS_I8_ROWS(I8_QUANTIZE);
-#undef CATS_I8_ROWS
-    // the norm takes its operand types at run time
-    return v8 ? launch_rows_v<I8_NORM, float, 8>(p, st) : launch_rows_v<I8_NORM, float, 1>(p, st);
+    typedef uint16_t bf16;
+    if (op == I8_SWIGLU) return p.x_f32 ? launch_rows_t<I8_SWIGLU, float, float>(p, st) : launch_rows_t<I8_SWIGLU, bf16, bf16>(p, st);
+    if (op == I8_QUANTIZE) return p.x_f32 ? launch_rows_t<I8_QUANTIZE, float, NoDelta>(p, st) : launch_rows_t<I8_QUANTIZE, bf16, NoDelta>(p, st);
+    if (p.delta == nullptr) return p.x_f32 ? launch_rows_t<I8_NORM, float, NoDelta>(p, st) : launch_rows_t<I8_NORM, bf16, NoDelta>(p, st);
+    if (p.d_f32) return p.x_f32 ? launch_rows_t<I8_NORM, float, float>(p, st) : launch_rows_t<I8_NORM, bf16, float>(p, st);
+    return p.x_f32 ? launch_rows_t<I8_NORM, float, bf16>(p, st) : launch_rows_t<I8_NORM, bf16, bf16>(p, st);
 }
 
 cudaError_t launch_i8_qkv(const float* qkv, const int32_t* pos, int T, int nh, int hd, float rope_base, int prefix_len, void* q, void* kc,
