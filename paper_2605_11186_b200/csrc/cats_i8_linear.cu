@@ -9,9 +9,8 @@
 //     contiguous run, so R is free and is chosen so that the tiles fill the SMs evenly (linear_tiling).
 //   * x is row-major as the row kernels leave it; TMA boxes of 128 bytes x ceil8(tokens) rows bring it in, zeros beyond the
 //     last row and column.
-// Warp 0 (one thread) copies w, warp 1 (one thread) copies x into a ring of shared-memory stages with mbarrier completion;
-// warp 2 issues tcgen05.mma into one of two TMEM accumulators; warps 4-7 drain the other one: int32 -> fp32 * sx * sw ->
-// bf16 or fp32 rows.  Rows of a stage that no copy writes (tokens beyond the last, channels beyond the last) hold
+// Warp 0 copies w, warp 1 copies x into a ring of shared-memory stages with mbarrier completion; warp 2 issues tcgen05.mma
+// into one of two TMEM accumulators; warps 4-11 drain the other one: int32 -> fp32 * sx * sw -> bf16 or fp32 rows.  Rows of a stage that no copy writes (tokens beyond the last, channels beyond the last) hold
 // leftovers; they only reach accumulator rows and columns that are not stored.
 // With few tiles the K blocks are cut into `split` shares, one CTA of a cluster each.  The partial sums meet in distributed
 // shared memory: the accumulator's 16-channel groups are dealt out to the CTAs, every CTA stores its int32 partial of a group
@@ -27,7 +26,8 @@
 namespace cats {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 128 + 32 * kEpiWarps;
 constexpr int kKb = 128;              // int8 columns of a K block: one swizzled row of 128 bytes
 constexpr int kMaxStages = 16;
 constexpr int kCtrl = 1024;
@@ -68,29 +68,72 @@ static_assert(sizeof(Ctrl) <= kCtrl, "control block too large");
 __device__ __forceinline__ uint32_t idesc_i8_m128(int n) {
     return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-__device__ __forceinline__ void umma_i8(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, bool accumulate) {
+// The low word of a shared-memory descriptor changes from MMA to MMA, the high word (8-row groups 1024 bytes apart,
+// descriptor version, 128-byte swizzle) never does; see umma_desc_sw128.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ void umma_i8(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %5};\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"((uint32_t)accumulate)
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], da, db, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
         : "memory");
+}
+// One lane of the warp, the same one every time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+// Bounded wait of a whole warp: the answer is the same for every lane.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+// NC accumulator columns of this thread's lane; the values may be used after tmem_loaded().
+template <int NC> __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* r) {
+#pragma unroll
+    for (int h = 0; h < NC / 16; ++h)
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+            : "=r"(r[16 * h]), "=r"(r[16 * h + 1]), "=r"(r[16 * h + 2]), "=r"(r[16 * h + 3]), "=r"(r[16 * h + 4]), "=r"(r[16 * h + 5]),
+              "=r"(r[16 * h + 6]), "=r"(r[16 * h + 7]), "=r"(r[16 * h + 8]), "=r"(r[16 * h + 9]), "=r"(r[16 * h + 10]), "=r"(r[16 * h + 11]),
+              "=r"(r[16 * h + 12]), "=r"(r[16 * h + 13]), "=r"(r[16 * h + 14]), "=r"(r[16 * h + 15])
+            : "r"(taddr + 16 * h)
+            : "memory");
+}
+template <int NC> __device__ __forceinline__ void tmem_loaded(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < NC; ++i) asm volatile("" : "+r"(r[i]));       // no use of r moves above the wait
 }
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t local_smem, int rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local_smem), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void st_cluster_v4(uint32_t addr, const float* v) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, const uint32_t* v) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_id() {
+    uint32_t r;
+    asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+    return r;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// Partial sums of one 16-channel group from one sender: [x_rows tokens][16] int32.  The four 16-byte pieces of a token are
-// permuted by its index, so that eight neighbouring lanes touch all 32 banks.
+// Partial sums of one 16-channel group from one sender: [4 channel quadruples][x_rows tokens][4] int32, so that a warp's
+// store into a peer is 512 contiguous bytes (16-byte pieces of 64-byte token rows took four times as long: 12 bytes per ns).
 __device__ __forceinline__ uint32_t part_bytes(int x_rows) { return (uint32_t)x_rows * 64u; }
-__device__ __forceinline__ uint32_t part_piece(int t, int i) { return (uint32_t)t * 64u + (uint32_t)((i ^ ((t >> 1) & 3)) << 4); }
+__device__ __forceinline__ uint32_t part_piece(int x_rows, int t, int i) { return (uint32_t)(i * x_rows + t) * 16u; }
 
 __device__ __forceinline__ void bulk_copy(void* smem_dst, const void* gsrc, uint32_t bytes, uint64_t* bar, uint64_t policy) {
     asm volatile(
@@ -99,27 +142,33 @@ __device__ __forceinline__ void bulk_copy(void* smem_dst, const void* gsrc, uint
         : "memory");
 }
 
-// 16 accumulator columns of one token to out[t][n0 .. n0 + 16).
-__device__ __forceinline__ void store16(const LinearDev& p, long long t, int n0, const float* acc, float sx, const float* sw) {
-    float v[16];
+// NC accumulator columns of one token to out[t][n0 .. n0 + NC).
+template <int NC> __device__ __forceinline__ void store_cols(const LinearDev& p, long long t, int n0, const uint32_t* acc, float sx, const float* sw) {
+    float v[NC];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = (float)__float_as_int(acc[i]) * sx * sw[i];
-    if (p.vec_out && n0 + 16 <= p.outs) {
+    for (int i = 0; i < NC / 4; ++i) {
+        const float4 w = *reinterpret_cast<const float4*>(sw + 4 * i);
+        v[4 * i] = (float)(int)acc[4 * i] * sx * w.x;
+        v[4 * i + 1] = (float)(int)acc[4 * i + 1] * sx * w.y;
+        v[4 * i + 2] = (float)(int)acc[4 * i + 2] * sx * w.z;
+        v[4 * i + 3] = (float)(int)acc[4 * i + 3] * sx * w.w;
+    }
+    if (p.vec_out && n0 + NC <= p.outs) {
         if (p.out_f32) {
             float4* o = reinterpret_cast<float4*>((float*)p.out + t * p.ldo + n0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < NC / 4; ++i) o[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         } else {
             uint4* o = reinterpret_cast<uint4*>((uint16_t*)p.out + t * p.ldo + n0);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < NC / 8; ++i)
                 o[i] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
                                   pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < NC; ++i) {
         if (n0 + i < p.outs) {
             if (p.out_f32) ((float*)p.out)[t * p.ldo + n0 + i] = v[i];
             else ((uint16_t*)p.out)[t * p.ldo + n0 + i] = float_to_bf16_bits(v[i]);
@@ -131,7 +180,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
     extern __shared__ __align__(1024) uint8_t smem[];      // [stages][stage_bytes], the tail, received partials, channel scales, control block
     uint8_t* const recv = smem + (size_t)p.stages * p.stage_bytes + p.tail;
     float* const sw_s = reinterpret_cast<float*>(recv + p.recv_bytes);
-    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(sw_s + 4 * 256);
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(sw_s + kEpiWarps * 256);
     volatile int* const abort_flag = &ctrl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((smem_u32(smem) & 1023u) != 0) {      // the swizzled tiles need this alignment
@@ -140,12 +189,12 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(&ctrl->full[s], 2);     // one arrive.expect_tx from each copying thread
+            mbar_init(&ctrl->full[s], 2);     // one arrive.expect_tx from each copying warp
             mbar_init(&ctrl->empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&ctrl->acc_full[b], 1);
-            mbar_init(&ctrl->acc_empty[b], 128);
+            mbar_init(&ctrl->acc_empty[b], 32 * kEpiWarps);
         }
         ctrl->abort_flag = 0;
         mbar_fence_init();
@@ -155,92 +204,107 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
         tmem_alloc(&ctrl->tmem_base, p.tmem_cols);
         tmem_relinquish();
     }
+    // split == 1: tiles blockIdx.x, + gridDim.x, ...; else exactly one tile, K blocks [kb0, kb0 + n_kb)
+    const int rank = p.split > 1 ? (int)cluster_rank() : 0;
+    const int first = p.split > 1 ? (int)cluster_id() : (int)blockIdx.x, G = p.split > 1 ? p.n_tiles : (int)gridDim.x;
+    const int kb0 = rank * p.kb_share, n_kb = min(p.n_kb - kb0, p.kb_share);
+    const int S = p.stages;
+    const int n_units = p.unit == 1 ? n_kb : (n_kb + p.unit - 1) / p.unit;
+    // Every CTA starts at another place of the K range: in step, all SMs would ask the same few L2 slices for the same rows of
+    // x.  Whole numbers: the order of the sums does not matter.
+    const int u_first = p.m_blocks == 1 ? (int)blockIdx.x % n_units : 0;
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = ctrl->tmem_base;
-    const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
     if (p.split > 1) cluster_arrive();        // waited for before the first store into a peer: every CTA of the cluster has started
     pdl_launch_dependents();
-    const int S = p.stages;
-    // split == 1: tiles blockIdx.x, + gridDim.x, ...; else exactly one tile, K blocks [kb0, kb0 + n_kb)
-    const int G = p.split > 1 ? p.n_tiles : (int)gridDim.x, first = (int)blockIdx.x / p.split;
-    const int kb0 = rank * p.kb_share, n_kb = min(p.n_kb - kb0, p.kb_share);
-    const int n_units = (n_kb + p.unit - 1) / p.unit;
-    const size_t kb_stride = (size_t)((p.outs + 7) / 8) * 1024;       // packed bytes of one K block
-    // stage layout: unit chunks of w, then unit chunks of x
+    // stage layout: unit chunks of w, then unit chunks of x.  All lanes of a role's warp run its loop and one of them issues:
+    // addresses and descriptors stay in uniform registers, where the copy and MMA instructions want them.
     if (warp <= 1) {
-        if (lane == 0) {
-            const bool is_w = warp == 0;
-            // many token blocks read the same rows of w soon after one another; a tree reads them once
-            const uint64_t pol = is_w && p.m_blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
-            if (!is_w) pdl_wait();            // x comes from the kernel before; w never does
-            int s = 0, issued = 0;
-            uint32_t par = 1;
-            bool ok = true;
-            for (int tile = first; tile < p.n_tiles && ok; tile += G) {
-                const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
-                const int n0 = nt * p.R;
-                const uint32_t w_bytes = (uint32_t)min(p.R, (p.outs - n0 + 7) / 8 * 8) * kKb;
-                const uint8_t* src = p.w + (size_t)kb0 * kb_stride + (size_t)(n0 >> 3) * 1024;
-                for (int u = 0, kb = 0; u < n_units; ++u) {
-                    if (issued >= S && !mbar_wait(&ctrl->empty[s], par, abort_flag)) { ok = false; break; }
-                    uint8_t* stage = smem + (size_t)s * p.stage_bytes;
-                    const int nk = min(p.unit, n_kb - kb);
+        const bool is_w = warp == 0;
+        // many token blocks read the same rows of w soon after one another; a tree reads them once
+        const uint64_t pol = is_w && p.m_blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
+        const size_t kb_stride = (size_t)((p.outs + 7) / 8) * 1024;       // packed bytes of one K block
+        if (!is_w) pdl_wait();                // x comes from the kernel before; w never does
+        int s = 0, issued = 0;
+        uint32_t par = 1;
+        bool ok = true;
+        for (int tile = first; tile < p.n_tiles && ok; tile += G) {
+            const int nt = p.m_blocks == 1 ? tile : tile / p.m_blocks, mb = tile - nt * p.m_blocks;
+            const int n0 = nt * p.R;
+            const uint32_t w_bytes = (uint32_t)min(p.R, (p.outs - n0 + 7) / 8 * 8) * kKb;
+            const uint8_t* const w_tile = p.w + (size_t)kb0 * kb_stride + (size_t)(n0 >> 3) * 1024;
+            for (int i = 0, u = u_first; i < n_units; ++i) {
+                if (issued >= S && !warp_wait(&ctrl->empty[s], par, abort_flag)) { ok = false; break; }
+                uint8_t* const stage = smem + (size_t)s * p.stage_bytes;
+                const int kb = u * p.unit, nk = min(p.unit, n_kb - kb);
+                if (elect_one()) {
                     if (is_w) {
                         mbar_expect_tx(&ctrl->full[s], w_bytes * nk);
-                        for (int j = 0; j < nk; ++j, ++kb, src += kb_stride) bulk_copy(stage + j * p.w_chunk, src, w_bytes, &ctrl->full[s], pol);
+                        for (int j = 0; j < nk; ++j) bulk_copy(stage + j * p.w_chunk, w_tile + (size_t)(kb + j) * kb_stride, w_bytes, &ctrl->full[s], pol);
                     } else {
                         mbar_expect_tx(&ctrl->full[s], p.x_chunk * nk);
-                        for (int j = 0; j < nk; ++j, ++kb)
-                            tma_load_2d(stage + p.unit * p.w_chunk + j * p.x_chunk, &tm_x, (kb0 + kb) * kKb, mb * 128, &ctrl->full[s], pol);
+                        for (int j = 0; j < nk; ++j)
+                            tma_load_2d(stage + p.unit * p.w_chunk + j * p.x_chunk, &tm_x, (kb0 + kb + j) * kKb, mb * 128, &ctrl->full[s], pol);
                     }
-                    ++issued;
-                    if (++s == S) { s = 0; par ^= 1u; }
                 }
-            }
-            if (*abort_flag) {                // let the copies in flight land before the CTA goes away
-                volatile int ignore = 0;
-                for (int j = max(0, issued - S); j < issued; ++j) mbar_wait(&ctrl->full[j % S], (j / S) & 1, &ignore);
+                __syncwarp();
+                ++issued;
+                if (++s == S) { s = 0; par ^= 1u; }
+                if (++u == n_units) u = 0;
             }
         }
+        if (*abort_flag) {                    // let the copies in flight land before the CTA goes away
+            volatile int ignore = 0;
+            for (int j = max(0, issued - S); j < issued; ++j) mbar_wait(&ctrl->full[j % S], (j / S) & 1, &ignore);
+        }
     } else if (warp == 2) {
-        if (lane == 0) {
-            const uint32_t idesc = idesc_i8_m128(p.R);
-            int s = 0, seg = 0;
-            uint32_t par = 0;
-            bool ok = true;
-            for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
-                const int b = seg & 1;
-                if (seg >= 2) ok = mbar_wait(&ctrl->acc_empty[b], ((seg >> 1) - 1) & 1, abort_flag);
+        const uint32_t idesc = idesc_i8_m128(p.R);
+        int s = 0, seg = 0;
+        uint32_t par = 0;
+        bool ok = true;
+        for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
+            const int b = seg & 1;
+            if (seg >= 2) ok = warp_wait(&ctrl->acc_empty[b], ((seg >> 1) - 1) & 1, abort_flag);
+            tc_fence_after_sync();
+            const uint32_t d = tmem + (uint32_t)(b * p.R);
+            uint32_t more = 0;                // the first MMA of a tile overwrites the accumulator
+            for (int i = 0, u = u_first; i < n_units && ok; ++i) {
+                ok = warp_wait(&ctrl->full[s], par, abort_flag);
+                if (!ok) break;
                 tc_fence_after_sync();
-                const uint32_t d = tmem + (uint32_t)(b * p.R);
-                for (int u = 0, kb = 0; u < n_units && ok; ++u) {
-                    ok = mbar_wait(&ctrl->full[s], par, abort_flag);
-                    if (!ok) break;
-                    tc_fence_after_sync();
-                    const int nk = min(p.unit, n_kb - kb);
-                    const uint32_t w_addr = smem_u32(smem + (size_t)s * p.stage_bytes);
-                    const uint32_t x_addr = w_addr + p.unit * p.w_chunk;
-                    for (int j = 0; j < nk; ++j, ++kb) {
-                        const uint64_t da = umma_desc_sw128(x_addr + j * p.x_chunk), db = umma_desc_sw128(w_addr + j * p.w_chunk);
+                const int nk = min(p.unit, n_kb - u * p.unit);
+                const uint32_t w_addr = smem_u32(smem) + (uint32_t)s * p.stage_bytes;
+                uint32_t db = desc_lo(w_addr), da = desc_lo(w_addr + p.unit * p.w_chunk);
+                if (elect_one()) {
+                    for (int j = 0; j < nk; ++j) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) umma_i8(d, da + 2 * k, db + 2 * k, idesc, kb > 0 || k > 0);
+                        for (int k = 0; k < 4; ++k) {
+                            umma_i8(d, da + 2 * k, db + 2 * k, idesc, more);
+                            more = 1;
+                        }
+                        da += p.x_chunk >> 4;
+                        db += p.w_chunk >> 4;
                     }
                     umma_commit(&ctrl->empty[s]);
-                    if (++s == S) { s = 0; par ^= 1u; }
                 }
-                umma_commit(&ctrl->acc_full[b]);      // also on abort, so that the epilogue warps wake up
+                more = 1;
+                __syncwarp();
+                if (++s == S) { s = 0; par ^= 1u; }
+                if (++u == n_units) u = 0;
             }
+            if (elect_one()) umma_commit(&ctrl->acc_full[b]);      // also on abort, so that the epilogue warps wake up
+            __syncwarp();
         }
     } else if (warp >= 4) {
         pdl_wait();
-        const int q4 = warp & 3;
-        float* const sw = sw_s + q4 * 256;       // one copy of the tile's channel scales per warp: no barrier needed
+        const int q4 = warp & 3, group = (warp - 4) >> 2;         // TMEM lane quadrant; two warps share it and take turns
+        float* const sw = sw_s + (warp - 4) * 256;                // one copy of the tile's channel scales per warp: no barrier needed
         int seg = 0;
         bool ok = true;
         for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
-            const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
+            const int nt = p.m_blocks == 1 ? tile : tile / p.m_blocks, mb = tile - nt * p.m_blocks;
             const int n0 = nt * p.R, b = seg & 1;
             const int tl = q4 * 32 + lane;
             const long long t = (long long)mb * 128 + tl;
@@ -248,49 +312,75 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             for (int i = lane; i < p.R; i += 32) sw[i] = n0 + i < p.outs ? __ldg(p.sw + n0 + i) : 0.f;
             __syncwarp();
             const float sx = t < p.rows ? __ldg(p.sx + t) : 0.f;
-            ok = mbar_wait(&ctrl->acc_full[b], (seg >> 1) & 1, abort_flag) && !*abort_flag;
+            ok = warp_wait(&ctrl->acc_full[b], (seg >> 1) & 1, abort_flag) && !__any_sync(0xffffffffu, *abort_flag);
             tc_fence_after_sync();
             const bool busy = mb * 128 + q4 * 32 < p.rows;         // this warp holds tokens
             const uint32_t taddr = tmem + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * p.R);
-            const int n_groups = p.R / 16;
             if (p.split > 1) {
+                const int n_groups = p.R / 16;
                 cluster_wait();
-                if (busy)
-                    for (int g = 0; g < n_groups; ++g) {
-                        const int owner = g % p.split;
-                        if (owner == rank) continue;
-                        float acc[16];
-                        tmem_ld16(taddr + g * 16, acc);
-                        if (tl < p.x_rows) {
-                            const int from = rank < owner ? rank : rank - 1;
-                            const uint32_t dst = cluster_addr(smem_u32(recv), owner) + (uint32_t)((g / p.split) * (p.split - 1) + from) * part_bytes(p.x_rows);
+                if (busy) {
+                    int turn = 0;
+                    for (int g = 0, owner = 0, slot = 0; g < n_groups; ++g) {
+                        if (owner != rank && (turn++ & 1) == group) {
+                            uint32_t acc[16];
+                            tmem_load<16>(taddr + g * 16, acc);
+                            tmem_loaded<16>(acc);
+                            if (tl < p.x_rows) {
+                                const int from = rank < owner ? rank : rank - 1;
+                                const uint32_t dst = cluster_addr(smem_u32(recv), owner) + (uint32_t)(slot * (p.split - 1) + from) * part_bytes(p.x_rows);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) st_cluster_v4(dst + part_piece(tl, i), acc + 4 * i);
+                                for (int i = 0; i < 4; ++i) st_cluster_v4(dst + part_piece(p.x_rows, tl, i), acc + 4 * i);
+                            }
+                            __syncwarp();
                         }
+                        if (++owner == p.split) { owner = 0; ++slot; }
                     }
+                }
                 __syncwarp();
                 cluster_arrive();
                 cluster_wait();
-            }
-            if (ok && busy) {
-                for (int g = rank; g < n_groups && n0 + g * 16 < p.outs; g += p.split) {
-                    float acc[16];
-                    tmem_ld16(taddr + g * 16, acc);
-                    if (t < p.rows) {
-                        for (int from = 0; from < p.split - 1; ++from) {
-                            const uint8_t* src = recv + ((size_t)(g / p.split) * (p.split - 1) + from) * part_bytes(p.x_rows);
+                if (ok && busy) {
+                    for (int slot = group, g = rank + group * p.split; g < n_groups && n0 + g * 16 < p.outs; slot += 2, g += 2 * p.split) {
+                        uint32_t acc[16];
+                        tmem_load<16>(taddr + g * 16, acc);
+                        tmem_loaded<16>(acc);
+                        if (t < p.rows) {
+                            for (int from = 0; from < p.split - 1; ++from) {
+                                const uint8_t* src = recv + (size_t)(slot * (p.split - 1) + from) * part_bytes(p.x_rows);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int4 v = *reinterpret_cast<const int4*>(src + part_piece(tl, i));
-                                acc[4 * i] = __int_as_float(__float_as_int(acc[4 * i]) + v.x);
-                                acc[4 * i + 1] = __int_as_float(__float_as_int(acc[4 * i + 1]) + v.y);
-                                acc[4 * i + 2] = __int_as_float(__float_as_int(acc[4 * i + 2]) + v.z);
-                                acc[4 * i + 3] = __int_as_float(__float_as_int(acc[4 * i + 3]) + v.w);
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint4 v = *reinterpret_cast<const uint4*>(src + part_piece(p.x_rows, tl, i));
+                                    acc[4 * i] += v.x;
+                                    acc[4 * i + 1] += v.y;
+                                    acc[4 * i + 2] += v.z;
+                                    acc[4 * i + 3] += v.w;
+                                }
                             }
+                            store_cols<16>(p, t, n0 + g * 16, acc, sx, sw + g * 16);
                         }
-                        store16(p, t, n0 + g * 16, acc, sx, sw + g * 16);
+                        __syncwarp();
                     }
-                    __syncwarp();
+                }
+            } else if (ok && busy) {
+                // the next columns are on their way while these are scaled and stored
+                uint32_t acc[2][32];
+                const int n_cols = min(p.R, p.outs - n0);
+                int c = group * 32;
+                if (c < n_cols) tmem_load<32>(taddr + c, acc[0]);
+                for (; c < n_cols; c += 128) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int ch = c + h * 64;
+                        if (ch >= n_cols) break;
+                        tmem_loaded<32>(acc[h]);
+                        if (ch + 64 < n_cols) tmem_load<32>(taddr + ch + 64, acc[h ^ 1]);
+                        if (t < p.rows) {                                  // R is a multiple of 16: the last columns may be 16
+                            if (p.R - ch >= 32) store_cols<32>(p, t, n0 + ch, acc[h], sx, sw + ch);
+                            else store_cols<16>(p, t, n0 + ch, acc[h], sx, sw + ch);
+                        }
+                        __syncwarp();
+                    }
                 }
             }
             tc_fence_before_sync();
@@ -462,16 +552,16 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.n_tiles = (int)tiles;
     d.w_chunk = (uint32_t)d.R * kKb;
     d.x_chunk = (uint32_t)d.x_rows * kKb;
-    // K blocks per stage: about 24 KB, so that one barrier round trip carries enough bytes
-    d.unit = max(1, min(8, 24 * 1024 / (int)(d.w_chunk + d.x_chunk)));
+    // K blocks per stage: up to 40 KB, so that one barrier round trip carries enough bytes
+    d.unit = max(1, min(8, 40 * 1024 / (int)(d.w_chunk + d.x_chunk)));
     d.stage_bytes = d.unit * (d.w_chunk + d.x_chunk);
     d.tail = 128u * kKb - d.x_chunk;
     d.recv_bytes = (uint32_t)(ceil_div(d.R / 16, d.split) * (d.split - 1) * d.x_rows * 64);
-    const int fixed = (int)(d.tail + d.recv_bytes) + 4 * 256 * 4 + kCtrl;
+    const int fixed = (int)(d.tail + d.recv_bytes) + kEpiWarps * 256 * 4 + kCtrl;
     d.stages = min(kMaxStages, (kSmemMax - fixed) / (int)d.stage_bytes);
     if (d.stages < 2) return cudaErrorInvalidConfiguration;
-    d.tmem_cols = 32;
-    while (d.tmem_cols < 2u * d.R) d.tmem_cols *= 2;
+    d.tmem_cols = 32;           // two accumulators; the second one's last columns are read 32 at a time
+    while (d.tmem_cols < (uint32_t)(d.R + (d.R + 31) / 32 * 32)) d.tmem_cols *= 2;
     d.w = (const uint8_t*)p.w; d.sx = p.sx; d.sw = p.sw;
     d.out = p.out; d.out_f32 = p.out_f32; d.ldo = p.ldo;
     d.vec_out = ((uintptr_t)p.out % 16) == 0 && (p.ldo * (p.out_f32 ? 4 : 2)) % 16 == 0;
