@@ -54,6 +54,7 @@ struct LinearDev {
     void* out;
     int out_f32, vec_out;   // vec_out: rows and columns allow 16-byte stores
     long long ldo;
+    int w_early;            // w may be read before the kernel in front has finished
     int32_t* d_status;
 };
 
@@ -142,45 +143,71 @@ __device__ __forceinline__ void bulk_copy(void* smem_dst, const void* gsrc, uint
         : "memory");
 }
 
-// NC accumulator columns of one token to out[t][n0 .. n0 + NC).
-template <int NC> __device__ __forceinline__ void store_cols(const LinearDev& p, long long t, int n0, const uint32_t* acc, float sx, const float* sw) {
-    float v[NC];
+// The way of NC accumulator columns of a warp's 32 tokens (one per lane) to out[t0 + lane][n0 .. n0 + NC), through the warp's
+// staging tile: a store instruction then covers whole runs of a few rows (from the lanes directly, every lane's 16 bytes are a
+// cache line of their own).  The sums are staged as they are and scaled on the way out, in short loops: the epilogue runs
+// once or twice per launch, and unrolled it spent its time fetching instructions.  16-byte pieces are permuted by row so that
+// neither side has bank conflicts.
+template <int NC> __device__ __forceinline__ uint32_t* staged(uint32_t* stage, int row, int piece) {
+    return stage + row * NC + ((piece ^ (NC == 32 ? row & 7 : (row >> 1) & 3)) << 2);
+}
+template <int NC> __device__ __forceinline__ void stage_cols(const uint32_t* acc, uint32_t* stage, int lane) {
 #pragma unroll
-    for (int i = 0; i < NC / 4; ++i) {
-        const float4 w = *reinterpret_cast<const float4*>(sw + 4 * i);
-        v[4 * i] = (float)(int)acc[4 * i] * sx * w.x;
-        v[4 * i + 1] = (float)(int)acc[4 * i + 1] * sx * w.y;
-        v[4 * i + 2] = (float)(int)acc[4 * i + 2] * sx * w.z;
-        v[4 * i + 3] = (float)(int)acc[4 * i + 3] * sx * w.w;
-    }
-    if (p.vec_out && n0 + NC <= p.outs) {
+    for (int i = 0; i < NC / 4; ++i)
+        *reinterpret_cast<uint4*>(staged<NC>(stage, lane, i)) = make_uint4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
+    __syncwarp();
+}
+// n_tokens: valid tokens from t0 on; n_cols <= NC: valid columns; sx: the 32 token scales; sw: scales of the columns.
+template <int NC>
+__device__ __forceinline__ void store_cols(const LinearDev& p, long long t0, int n_tokens, int n0, int n_cols, const float* sx, const float* sw,
+                                           uint32_t* stage, int lane) {
+    constexpr int NP = NC / 4;                       // pieces of 4 columns per row
+    auto scaled = [&](int row, int piece, const float4& w) {
+        const uint4 a = *reinterpret_cast<const uint4*>(staged<NC>(stage, row, piece));
+        const float s = sx[row];
+        return make_float4((float)(int)a.x * s * w.x, (float)(int)a.y * s * w.y, (float)(int)a.z * s * w.z, (float)(int)a.w * s * w.w);
+    };
+    if (p.vec_out && n_cols % 8 == 0) {
         if (p.out_f32) {
-            float4* o = reinterpret_cast<float4*>((float*)p.out + t * p.ldo + n0);
-#pragma unroll
-            for (int i = 0; i < NC / 4; ++i) o[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            const int piece = lane % NP;
+            const float4 w = *reinterpret_cast<const float4*>(sw + piece * 4);
+            float* o = (float*)p.out + (t0 + lane / NP) * p.ldo + n0 + piece * 4;
+            if (piece * 4 < n_cols)
+#pragma unroll 2
+                for (int row = lane / NP; row < n_tokens; row += 32 / NP, o += (32 / NP) * p.ldo) *reinterpret_cast<float4*>(o) = scaled(row, piece, w);
         } else {
-            uint4* o = reinterpret_cast<uint4*>((uint16_t*)p.out + t * p.ldo + n0);
-#pragma unroll
-            for (int i = 0; i < NC / 8; ++i)
-                o[i] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
-                                  pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+            const int piece = lane % (NP / 2) * 2;
+            const float4 w0 = *reinterpret_cast<const float4*>(sw + piece * 4), w1 = *reinterpret_cast<const float4*>(sw + piece * 4 + 4);
+            uint16_t* o = (uint16_t*)p.out + (t0 + lane / (NP / 2)) * p.ldo + n0 + piece * 4;
+            if (piece * 4 < n_cols)
+#pragma unroll 2
+                for (int row = lane / (NP / 2); row < n_tokens; row += 64 / NP, o += (64 / NP) * p.ldo) {
+                    const float4 a = scaled(row, piece, w0), b = scaled(row, piece + 1, w1);
+                    *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w));
+                }
         }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        if (n0 + i < p.outs) {
-            if (p.out_f32) ((float*)p.out)[t * p.ldo + n0 + i] = v[i];
-            else ((uint16_t*)p.out)[t * p.ldo + n0 + i] = float_to_bf16_bits(v[i]);
+    } else {
+        const int col = lane % NC;
+        if (col < n_cols) {
+            const float w = sw[col];
+            long long o = (t0 + lane / NC) * p.ldo + n0 + col;
+#pragma unroll 2
+            for (int row = lane / NC; row < n_tokens; row += 32 / NC, o += (32 / NC) * p.ldo) {
+                const float v = (float)(int)staged<NC>(stage, row, col >> 2)[col & 3] * sx[row] * w;
+                if (p.out_f32) ((float*)p.out)[o] = v;
+                else ((uint16_t*)p.out)[o] = float_to_bf16_bits(v);
+            }
         }
     }
+    __syncwarp();
 }
 
 __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const __grid_constant__ CUtensorMap tm_x) {
-    extern __shared__ __align__(1024) uint8_t smem[];      // [stages][stage_bytes], the tail, received partials, channel scales, control block
+    extern __shared__ __align__(1024) uint8_t smem[];      // [stages][stage_bytes], the tail, received partials, staging tiles, channel scales, control block
     uint8_t* const recv = smem + (size_t)p.stages * p.stage_bytes + p.tail;
-    float* const sw_s = reinterpret_cast<float*>(recv + p.recv_bytes);
-    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(sw_s + kEpiWarps * 256);
+    uint32_t* const stage_s = reinterpret_cast<uint32_t*>(recv + p.recv_bytes);      // one 32 x 32 tile per epilogue warp
+    float* const sw_s = reinterpret_cast<float*>(stage_s + kEpiWarps * 1024);        // 256 channel scales, 32 token scales per epilogue warp
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(sw_s + kEpiWarps * 288);
     volatile int* const abort_flag = &ctrl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((smem_u32(smem) & 1023u) != 0) {      // the swizzled tiles need this alignment
@@ -226,7 +253,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
         // many token blocks read the same rows of w soon after one another; a tree reads them once
         const uint64_t pol = is_w && p.m_blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
         const size_t kb_stride = (size_t)((p.outs + 7) / 8) * 1024;       // packed bytes of one K block
-        if (!is_w) pdl_wait();                // x comes from the kernel before; w never does
+        // x comes from the kernel before; w does not where this launch follows others of the same call
+        if (!is_w || !p.w_early) pdl_wait();
         int s = 0, issued = 0;
         uint32_t par = 1;
         bool ok = true;
@@ -300,21 +328,24 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
     } else if (warp >= 4) {
         pdl_wait();
         const int q4 = warp & 3, group = (warp - 4) >> 2;         // TMEM lane quadrant; two warps share it and take turns
-        float* const sw = sw_s + (warp - 4) * 256;                // one copy of the tile's channel scales per warp: no barrier needed
+        uint32_t* const stage = stage_s + (warp - 4) * 1024;
+        float* const sw = sw_s + (warp - 4) * 288;                // a copy of the tile's scales per warp: no barrier needed
+        float* const sx = sw + 256;
         int seg = 0;
         bool ok = true;
         for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
             const int nt = p.m_blocks == 1 ? tile : tile / p.m_blocks, mb = tile - nt * p.m_blocks;
             const int n0 = nt * p.R, b = seg & 1;
             const int tl = q4 * 32 + lane;
-            const long long t = (long long)mb * 128 + tl;
+            const long long t0 = (long long)mb * 128 + q4 * 32, t = t0 + lane;
+            const int n_tokens = (int)min(32ll, p.rows - t0);      // valid tokens of this warp (negative: none)
             __syncwarp();
             for (int i = lane; i < p.R; i += 32) sw[i] = n0 + i < p.outs ? __ldg(p.sw + n0 + i) : 0.f;
+            sx[lane] = t < p.rows ? __ldg(p.sx + t) : 0.f;
             __syncwarp();
-            const float sx = t < p.rows ? __ldg(p.sx + t) : 0.f;
             ok = warp_wait(&ctrl->acc_full[b], (seg >> 1) & 1, abort_flag) && !__any_sync(0xffffffffu, *abort_flag);
             tc_fence_after_sync();
-            const bool busy = mb * 128 + q4 * 32 < p.rows;         // this warp holds tokens
+            const bool busy = n_tokens > 0;
             const uint32_t taddr = tmem + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * p.R);
             if (p.split > 1) {
                 const int n_groups = p.R / 16;
@@ -357,30 +388,22 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
                                     acc[4 * i + 3] += v.w;
                                 }
                             }
-                            store_cols<16>(p, t, n0 + g * 16, acc, sx, sw + g * 16);
                         }
-                        __syncwarp();
+                        stage_cols<16>(acc, stage, lane);
+                        store_cols<16>(p, t0, n_tokens, n0 + g * 16, min(16, p.outs - n0 - g * 16), sx, sw + g * 16, stage, lane);
                     }
                 }
             } else if (ok && busy) {
                 // the next columns are on their way while these are scaled and stored
-                uint32_t acc[2][32];
+                uint32_t acc[32];
                 const int n_cols = min(p.R, p.outs - n0);
-                int c = group * 32;
-                if (c < n_cols) tmem_load<32>(taddr + c, acc[0]);
-                for (; c < n_cols; c += 128) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int ch = c + h * 64;
-                        if (ch >= n_cols) break;
-                        tmem_loaded<32>(acc[h]);
-                        if (ch + 64 < n_cols) tmem_load<32>(taddr + ch + 64, acc[h ^ 1]);
-                        if (t < p.rows) {                                  // R is a multiple of 16: the last columns may be 16
-                            if (p.R - ch >= 32) store_cols<32>(p, t, n0 + ch, acc[h], sx, sw + ch);
-                            else store_cols<16>(p, t, n0 + ch, acc[h], sx, sw + ch);
-                        }
-                        __syncwarp();
-                    }
+                if (group * 32 < n_cols) tmem_load<32>(taddr + group * 32, acc);
+#pragma unroll 1
+                for (int c = group * 32; c < n_cols; c += 64) {
+                    tmem_loaded<32>(acc);
+                    stage_cols<32>(acc, stage, lane);
+                    if (c + 64 < n_cols) tmem_load<32>(taddr + c + 64, acc);
+                    store_cols<32>(p, t0, n_tokens, n0 + c, min(32, n_cols - c), sx, sw + c, stage, lane);
                 }
             }
             tc_fence_before_sync();
@@ -452,11 +475,15 @@ struct Tiling {
     int R, split;
 };
 
-// Channels per tile and CTAs per tile, by what the busiest SM has to take in: an SM takes 57 bytes of w and x per ns (measured,
-// 64 tokens x 4096 columns x 22016 channels), a K block costs its issuing threads 0.1 us however small it is, and the
-// exchange of a split tile about 1.2 us.  clusters[i]: clusters of 2^i CTAs that fit the device at once.
+// Channels per tile and CTAs per tile, by the time of the busiest SM.  Measured: an SM takes in 95 bytes of w and x per ns
+// (128 x 11008 x 4096, from L2), all of them together 6500 bytes of w per ns (from HBM); the four MMAs of a K block cost
+// their issuing warp 0.12 us however small they are (1 x 4096 x 4096 as 128 whole tiles 7.8 us, as 32 tiles in four shares
+// 7.1); exchanging partial sums costs 1.5 us and 1 ns per 40 bytes sent (77 x 5120 x 15360: whole tiles 15.8, halves 17.2 us;
+// 128 x 11008 x 4096: whole tiles 18.9, halves 15.6, quarters 13.4 us).  clusters[i]: clusters of 2^i CTAs that fit the
+// device at once.
 Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&clusters)[4]) {
     const int n_kb = ceil_div(p.cols, kKb);
+    const float hbm_ns = (float)p.outs * p.cols / 6500.f;
     Tiling best = {256, 1};
     float best_ns = 1e30f;
     for (int i = 0; i < 4; ++i) {
@@ -468,8 +495,11 @@ Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&cl
             if (c > 1 && tiles > clusters[i]) break;
             if (ceil_div(R / 16, c) * (c - 1) * (x_rows * 64) > 64 * 1024) continue;      // received partials: 64 KB at most
             const float waves = (float)((tiles + clusters[i] - 1) / clusters[i]);
-            const float kb_ns = fmaxf((float)(R + x_rows) * (kKb / 57.f), 100.f);
-            const float ns = waves * share * kb_ns + (c > 1 ? 1200.f : 0.f);
+            const float kb_ns = fmaxf((float)(R + x_rows) * (kKb / 95.f), 120.f);
+            const float sent_ns = c > 1 ? 1500.f + (float)(R * (c - 1) / c) * (float)x_rows * (4.f / 40.f) : 0.f;
+            const float sm_ns = waves * (float)share * kb_ns;
+            // the two overlap, but not quite: of tilings that HBM bounds, the one that leaves the SMs the most slack is best
+            const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + sent_ns;
             if (ns < best_ns) { best_ns = ns; best = {R, c}; }
         }
     }
@@ -488,7 +518,7 @@ cudaError_t launch_clusters(const LinearDev& d, const CUtensorMap& tm, int grid,
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = g_call_boundary ? 1 : 2;
+    cfg.numAttrs = 2;         // also as the first launch of a call: nothing is touched before griddepcontrol.wait then (w_early)
     g_call_boundary = false;
     ++g_launch_count;
     return cudaLaunchKernelEx(&cfg, k_linear_i8, d, tm);
@@ -557,7 +587,7 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.stage_bytes = d.unit * (d.w_chunk + d.x_chunk);
     d.tail = 128u * kKb - d.x_chunk;
     d.recv_bytes = (uint32_t)(ceil_div(d.R / 16, d.split) * (d.split - 1) * d.x_rows * 64);
-    const int fixed = (int)(d.tail + d.recv_bytes) + kEpiWarps * 256 * 4 + kCtrl;
+    const int fixed = (int)(d.tail + d.recv_bytes) + kEpiWarps * (1024 + 288) * 4 + kCtrl;
     d.stages = min(kMaxStages, (kSmemMax - fixed) / (int)d.stage_bytes);
     if (d.stages < 2) return cudaErrorInvalidConfiguration;
     d.tmem_cols = 32;           // two accumulators; the second one's last columns are read 32 at a time
@@ -566,6 +596,7 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.out = p.out; d.out_f32 = p.out_f32; d.ldo = p.ldo;
     d.vec_out = ((uintptr_t)p.out % 16) == 0 && (p.ldo * (p.out_f32 ? 4 : 2)) % 16 == 0;
     d.d_status = p.d_status;
+    d.w_early = !g_call_boundary;
     CUtensorMap tm;
     if (!x_tensor_map(p, d.x_rows, &tm)) return cudaErrorNotSupported;
     const int grid = d.split > 1 ? d.n_tiles * d.split : (d.n_tiles < kSms ? d.n_tiles : kSms);

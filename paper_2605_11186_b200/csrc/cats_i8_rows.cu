@@ -296,14 +296,14 @@ template <int OP, typename TX, typename TD, int V>
 cudaError_t launch_rows_v(const I8RowsDev& p, cudaStream_t st) {
     const int vecs = (p.cols + V - 1) / V;          // vectors of a row
     constexpr int N = V == 8 ? 1 : (OP == I8_NORM ? 4 : 8);     // single elements: more of them per thread, as registers allow
-    if (vecs <= 32 * 4 * N) return launch_pdl(k_i8_rows<OP, TX, TD, V, 4 * N, true, false>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, st, p);
+    if (vecs <= 32 * 4 * N) return launch_i8(k_i8_rows<OP, TX, TD, V, 4 * N, true, false>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, st, p);
     const dim3 grid((unsigned)p.rows);
     auto threads = [&](int nv) { return dim3((unsigned)((vecs + nv * 32 - 1) / (nv * 32) * 32)); };
     const bool many = p.rows >= kMinRowsMany;
-    if (vecs <= 512 * N && !many) return launch_pdl(k_i8_rows<OP, TX, TD, V, N, false, false>, grid, threads(N), 0, st, p);
-    if (vecs <= 2 * N * row_threads<OP, V, 2 * N>() && !many) return launch_pdl(k_i8_rows<OP, TX, TD, V, 2 * N, false, false>, grid, threads(2 * N), 0, st, p);
-    if (vecs <= 2048 * N) return launch_pdl(k_i8_rows<OP, TX, TD, V, 4 * N, false, false>, grid, threads(4 * N), 0, st, p);
-    return launch_pdl(k_i8_rows<OP, TX, TD, V, N, false, true>, grid, dim3(512), 0, st, p);
+    if (vecs <= 512 * N && !many) return launch_i8(k_i8_rows<OP, TX, TD, V, N, false, false>, grid, threads(N), 0, st, p);
+    if (vecs <= 2 * N * row_threads<OP, V, 2 * N>() && !many) return launch_i8(k_i8_rows<OP, TX, TD, V, 2 * N, false, false>, grid, threads(2 * N), 0, st, p);
+    if (vecs <= 2048 * N) return launch_i8(k_i8_rows<OP, TX, TD, V, 4 * N, false, false>, grid, threads(4 * N), 0, st, p);
+    return launch_i8(k_i8_rows<OP, TX, TD, V, N, false, true>, grid, dim3(512), 0, st, p);
 }
 
 template <int OP, typename TX, typename TD>
@@ -328,7 +328,7 @@ cudaError_t launch_i8_rows(int op, const I8RowsDev& p, cudaStream_t st) {
 
 cudaError_t launch_i8_qkv(const float* qkv, const int32_t* pos, int T, int nh, int hd, float rope_base, int prefix_len, void* q, void* kc,
                           void* vc, cudaStream_t st) {
-    return launch_pdl(k_i8_qkv, dim3(T, 8), dim3(256), 0, st, qkv, pos, nh, hd, rope_base, prefix_len, (uint16_t*)q, (uint16_t*)kc,
+    return launch_i8(k_i8_qkv, dim3(T, 8), dim3(256), 0, st, qkv, pos, nh, hd, rope_base, prefix_len, (uint16_t*)q, (uint16_t*)kc,
                       (uint16_t*)vc);
 }
 
@@ -337,8 +337,8 @@ cudaError_t launch_i8_dequantize(const int8_t* q, long long ldq, const float* sc
     const bool v8 = cols % 8 == 0 && ((uintptr_t)q % 8) == 0 && ldq % 8 == 0 && ((uintptr_t)out % 16) == 0 &&
                     (ldo * (out_f32 ? 4 : 2)) % 16 == 0;
     const dim3 grid((unsigned)rows, (unsigned)((cols + 4095) / 4096));
-    return v8 ? launch_pdl(k_i8_dequantize<8>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo)
-              : launch_pdl(k_i8_dequantize<1>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo);
+    return v8 ? launch_i8(k_i8_dequantize<8>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo)
+              : launch_i8(k_i8_dequantize<1>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo);
 }
 
 }  // namespace cats

@@ -41,6 +41,14 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
+// The same for kernels that touch no memory at all before their griddepcontrol.wait: they may also overlap the tail of whatever
+// ran before the call.  (Every thread block waits, so a later kernel that waits for this one waits for all before it too.)
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_i8(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+    g_call_boundary = false;
+    return launch_pdl(kernel, grid, block, smem, st, args...);
+}
+
 // ---- small kernels ---------------------------------------------------------------------------
 cudaError_t launch_mask_pos(const int32_t* parent, int T, int prefix_len, uint64_t* mask, int32_t* pos, int32_t* depth,
                             int32_t* d_status, cudaStream_t st);
