@@ -426,6 +426,195 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
     if (threadIdx.x == 0 && *abort_flag) report(p.d_status, CATS_ERR_TIMEOUT);
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// The same product for many tokens, where it is bound by the tensor cores and by what an SM takes in: a pair of CTAs on two
+// SMs works on one tile of 256 tokens x R channels (tcgen05 cta_group::2).  Each CTA brings its 128 tokens and half of the
+// tile's channels, (128 + R / 2) rows per K block for 128 x R sums, where a CTA on its own takes in 128 + R; that is what lets
+// the tensor cores keep up their rate (4093 x 4096 x 22016: 219 us, 3370 TOP/s; single CTAs on 128 x 256 tiles 301 us).  Copies of both CTAs
+// count on the first CTA's barrier, whose warp 2 issues the MMAs for both; commits arrive at both.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr uint32_t kFirstOfPair = 0xFEFFFFFFu;       // a shared-memory address in the pair's first CTA
+
+__device__ __forceinline__ uint32_t idesc_i8_m256(int n) {
+    return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
+}
+__device__ __forceinline__ void umma_i8_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %5};\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+        : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {      // arrives at this barrier of both CTAs
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_u32(bar)), "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_load_pair(void* smem_dst, const void* tmap, int32_t x, int32_t y, uint64_t* bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%2, %3}], [%4], %5;"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(smem_u32(bar) & kFirstOfPair), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {     // at the first CTA's barrier
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(smem_u32(bar) & kFirstOfPair) : "memory");
+}
+
+__global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, const __grid_constant__ CUtensorMap tm_x,
+                                                             const __grid_constant__ CUtensorMap tm_w) {
+    extern __shared__ __align__(1024) uint8_t smem[];      // [stages][128 tokens, R / 2 channels], staging tiles, scales, control block
+    uint32_t* const stage_s = reinterpret_cast<uint32_t*>(smem + (size_t)p.stages * p.stage_bytes);
+    float* const sw_s = reinterpret_cast<float*>(stage_s + kEpiWarps * 1024);
+    Ctrl* const ctrl = reinterpret_cast<Ctrl*>(sw_s + kEpiWarps * 288);
+    volatile int* const abort_flag = &ctrl->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank();
+    if ((smem_u32(smem) & 1023u) != 0) {      // the swizzled tiles need this alignment (the same address in both CTAs)
+        if (threadIdx.x == 0) report(p.d_status, CATS_ERR_UNSUPPORTED);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(&ctrl->full[s], 2);     // the first CTA's: one arrive.expect_tx from each of its copying warps, for both CTAs' bytes
+            mbar_init(&ctrl->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&ctrl->acc_full[b], 1);
+            mbar_init(&ctrl->acc_empty[b], 2 * kEpiWarps);        // the first CTA's: the epilogue warps of both
+        }
+        ctrl->abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_desc(&tm_x);
+        tma_prefetch_desc(&tm_w);
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl->tmem_base)), "r"(p.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_arrive();                         // the peer's barriers are set up and its tensor memory is there
+    cluster_wait();
+    tc_fence_after_sync();
+    const uint32_t tmem = ctrl->tmem_base;
+    pdl_launch_dependents();
+    const int S = p.stages, G = (int)gridDim.x / 2, first = (int)cluster_id();
+    const int n8 = (p.outs + 7) / 8;
+    if (warp <= 1) {
+        const bool is_w = warp == 0;
+        const uint64_t pol = l2_policy_evict_last();
+        if (!is_w || !p.w_early) pdl_wait();
+        int s = 0, issued = 0;
+        uint32_t par = 1;
+        bool ok = true;
+        for (int tile = first; tile < p.n_tiles && ok; tile += G) {
+            const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
+            const int w_row = nt * p.R / 8 + rank * (p.R / 16), x_row = mb * 256 + rank * 128;
+            for (int kb = 0; kb < p.n_kb; ++kb) {
+                if (issued >= S && !warp_wait(&ctrl->empty[s], par, abort_flag)) { ok = false; break; }
+                uint8_t* const stage = smem + (size_t)s * p.stage_bytes;
+                if (elect_one()) {
+                    if (is_w) {
+                        if (rank == 0) mbar_expect_tx(&ctrl->full[s], 2 * p.w_chunk);
+                        tma_load_pair(stage + p.x_chunk, &tm_w, 0, kb * n8 + w_row, &ctrl->full[s], pol);
+                    } else {
+                        if (rank == 0) mbar_expect_tx(&ctrl->full[s], 2 * p.x_chunk);
+                        tma_load_pair(stage, &tm_x, kb * kKb, x_row, &ctrl->full[s], pol);
+                    }
+                }
+                __syncwarp();
+                ++issued;
+                if (++s == S) { s = 0; par ^= 1u; }
+            }
+        }
+        if (*abort_flag) {                    // let the copies in flight land before the CTA goes away
+            volatile int ignore = 0;
+            if (rank == 0)
+                for (int j = max(0, issued - S); j < issued; ++j) mbar_wait(&ctrl->full[j % S], (j / S) & 1, &ignore);
+            // the second CTA's copies count on barriers that it cannot wait for: a thousand times a copy's latency instead
+            for (const unsigned long long t0 = globaltimer_ns(); globaltimer_ns() - t0 < 1000000ull;) {}
+        }
+    } else if (warp == 2) {
+        if (rank == 0) {
+            const uint32_t idesc = idesc_i8_m256(p.R);
+            int s = 0, seg = 0;
+            uint32_t par = 0;
+            bool ok = true;
+            for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
+                const int b = seg & 1;
+                if (seg >= 2) ok = warp_wait(&ctrl->acc_empty[b], ((seg >> 1) - 1) & 1, abort_flag);
+                tc_fence_after_sync();
+                const uint32_t d = tmem + (uint32_t)(b * p.R);
+                for (int kb = 0; kb < p.n_kb && ok; ++kb) {
+                    ok = warp_wait(&ctrl->full[s], par, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t x_addr = smem_u32(smem) + (uint32_t)s * p.stage_bytes;
+                    const uint32_t da = desc_lo(x_addr), db = desc_lo(x_addr + p.x_chunk);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) umma_i8_pair(d, da + 2 * k, db + 2 * k, idesc, kb > 0 || k > 0);
+                        commit_pair(&ctrl->empty[s]);
+                    }
+                    __syncwarp();
+                    if (++s == S) { s = 0; par ^= 1u; }
+                }
+                if (elect_one()) commit_pair(&ctrl->acc_full[b]);      // also on abort, so that the epilogue warps wake up
+                __syncwarp();
+            }
+        }
+    } else if (warp >= 4) {
+        pdl_wait();
+        const int q4 = warp & 3, group = (warp - 4) >> 2;         // TMEM lane quadrant; two warps share it and take turns
+        uint32_t* const stage = stage_s + (warp - 4) * 1024;
+        float* const sw = sw_s + (warp - 4) * 288;
+        float* const sx = sw + 256;
+        int seg = 0;
+        bool ok = true;
+        for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
+            const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
+            const int n0 = nt * p.R, b = seg & 1;
+            const long long t0 = (long long)mb * 256 + rank * 128 + q4 * 32;
+            const int n_tokens = (int)min(32ll, p.rows - t0);      // valid tokens of this warp (negative: none)
+            __syncwarp();
+            for (int i = lane; i < p.R; i += 32) sw[i] = n0 + i < p.outs ? __ldg(p.sw + n0 + i) : 0.f;
+            sx[lane] = lane < n_tokens ? __ldg(p.sx + t0 + lane) : 0.f;
+            __syncwarp();
+            ok = warp_wait(&ctrl->acc_full[b], (seg >> 1) & 1, abort_flag) && !__any_sync(0xffffffffu, *abort_flag);
+            tc_fence_after_sync();
+            const uint32_t taddr = tmem + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * p.R);
+            if (ok && n_tokens > 0) {
+                uint32_t acc[32];
+                const int n_cols = min(p.R, p.outs - n0);
+                if (group * 32 < n_cols) tmem_load<32>(taddr + group * 32, acc);
+#pragma unroll 1
+                for (int c = group * 32; c < n_cols; c += 64) {
+                    tmem_loaded<32>(acc);
+                    stage_cols<32>(acc, stage, lane);
+                    if (c + 64 < n_cols) tmem_load<32>(taddr + c + 64, acc);
+                    store_cols<32>(p, t0, n_tokens, n0 + c, min(32, n_cols - c), sx, sw + c, stage, lane);
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) arrive_first(&ctrl->acc_empty[b]);
+        }
+    }
+    tc_fence_before_sync();
+    __syncwarp();
+    cluster_arrive();                         // nobody leaves while its peer may still reach into its memory
+    cluster_wait();
+    if (warp == 2) {
+        tc_fence_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
+    }
+    if (threadIdx.x == 0 && *abort_flag) report(p.d_status, CATS_ERR_TIMEOUT);
+}
+
 // int8 [rows][cols] -> [K block][8-row group][8 x 128 bytes], 128-byte swizzle, zeros beyond the matrix.  One thread per 16 bytes.
 __global__ void __launch_bounds__(256) k_pack_weights_i8(const int8_t* __restrict__ src, long long ld, int rows, int cols, int n8,
                                                          long long n, uint4* __restrict__ dst) {
@@ -471,20 +660,33 @@ bool x_tensor_map(const I8Linear& p, int box_rows, CUtensorMap* out) {
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// The packed weights as rows of one 8-row group (1 KB) each, K block by K block, in boxes of box_groups groups.
+bool w_tensor_map(const I8Linear& p, int box_groups, CUtensorMap* out) {
+    TensorMapEncodeFn enc = tensor_map_encoder();
+    if (enc == nullptr) return false;
+    const cuuint64_t dims[2] = {256, (cuuint64_t)ceil_div(p.cols, kKb) * (cuuint64_t)ceil_div(p.outs, 8)};
+    const cuuint64_t strides[1] = {1024};
+    const cuuint32_t box[2] = {256, (cuuint32_t)box_groups};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(out, CU_TENSOR_MAP_DATA_TYPE_INT32, 2, const_cast<void*>(p.w), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Tiling {
-    int R, split;
+    int R, split, pair;
 };
 
-// Channels per tile and CTAs per tile, by the time of the busiest SM.  Measured: an SM takes in 95 bytes of w and x per ns
-// (128 x 11008 x 4096, from L2), all of them together 6500 bytes of w per ns (from HBM); the four MMAs of a K block cost
-// their issuing warp 0.12 us however small they are (1 x 4096 x 4096 as 128 whole tiles 7.8 us, as 32 tiles in four shares
-// 7.1); exchanging partial sums costs 1.5 us and 1 ns per 40 bytes sent (77 x 5120 x 15360: whole tiles 15.8, halves 17.2 us;
-// 128 x 11008 x 4096: whole tiles 18.9, halves 15.6, quarters 13.4 us).  clusters[i]: clusters of 2^i CTAs that fit the
-// device at once.
+// Channels per tile, CTAs per tile, or CTA pairs, by the time of the busiest SM.  Measured: an SM takes in 95 bytes of w and x
+// per ns (128 x 11008 x 4096, from L2), all of them together 6500 bytes of w per ns (from HBM); the four MMAs of a K block
+// cost their issuing warp 0.15 us however small they are (1 x 4096 x 4096 as 128 whole tiles 8.4 us, as 32 tiles in four
+// shares 6.5); exchanging partial sums costs 1.2 us and 1 ns per 40 bytes sent (77 x 5120 x 15360: whole tiles 15.8, halves
+// 17.2 us; 128 x 11008 x 4096: whole tiles 18.9, halves 15.6, quarters 13.4 us); a pair takes 1 us more to set up and gains
+// from a few hundred tokens on (160 x 4096 x 4096: 10.6 against 9.5 us, 300: 12.0 against 11.5, 1000: 17.1 against 20.5;
+// 4093 x 4096 x 22016: 219 against 301).  clusters[i]: clusters of 2^i CTAs that fit the device at once.
 Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&clusters)[4]) {
     const int n_kb = ceil_div(p.cols, kKb);
     const float hbm_ns = (float)p.outs * p.cols / 6500.f;
-    Tiling best = {256, 1};
+    Tiling best = {256, 1, 0};
     float best_ns = 1e30f;
     for (int i = 0; i < 4; ++i) {
         const int c = 1 << i;
@@ -495,18 +697,29 @@ Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&cl
             if (c > 1 && tiles > clusters[i]) break;
             if (ceil_div(R / 16, c) * (c - 1) * (x_rows * 64) > 64 * 1024) continue;      // received partials: 64 KB at most
             const float waves = (float)((tiles + clusters[i] - 1) / clusters[i]);
-            const float kb_ns = fmaxf((float)(R + x_rows) * (kKb / 95.f), 120.f);
-            const float sent_ns = c > 1 ? 1500.f + (float)(R * (c - 1) / c) * (float)x_rows * (4.f / 40.f) : 0.f;
+            const float kb_ns = fmaxf((float)(R + x_rows) * (kKb / 95.f), 150.f);
+            const float sent_ns = c > 1 ? 1200.f + (float)(R * (c - 1) / c) * (float)x_rows * (4.f / 40.f) : 0.f;
             const float sm_ns = waves * (float)share * kb_ns;
             // the two overlap, but not quite: of tilings that HBM bounds, the one that leaves the SMs the most slack is best
             const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + sent_ns;
-            if (ns < best_ns) { best_ns = ns; best = {R, c}; }
+            if (ns < best_ns) { best_ns = ns; best = {R, c, 0}; }
         }
     }
+    // CTA pairs on 256 tokens: half the channels to take in, and 2 R clocks of the tensor cores
+    if (p.rows > 128)
+        for (int R = 256; R >= 64; R -= 32) {
+            const long long tiles = (long long)ceil_div(p.rows, 256) * ceil_div(p.outs, R);
+            const float waves = (float)((tiles + clusters[1] - 1) / clusters[1]);
+            const float sm_ns = waves * (float)n_kb * fmaxf(fmaxf((float)(R / 2 + 128) * (kKb / 95.f), 2.f * R / 1.7f), 150.f);
+            const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + 1000.f;
+            if (ns < best_ns) { best_ns = ns; best = {R, 1, 1}; }
+        }
     return best;
 }
 
-cudaError_t launch_clusters(const LinearDev& d, const CUtensorMap& tm, int grid, size_t smem, cudaStream_t st) {
+template <typename... Maps>
+cudaError_t launch_clusters(void (*kernel)(LinearDev, Maps...), int cluster, int grid, size_t smem, cudaStream_t st, const LinearDev& d,
+                            const Maps&... maps) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kThreads);
@@ -514,14 +727,14 @@ cudaError_t launch_clusters(const LinearDev& d, const CUtensorMap& tm, int grid,
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {(unsigned)d.split, 1, 1};
+    attr[0].val.clusterDim = {(unsigned)cluster, 1, 1};
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;         // also as the first launch of a call: nothing is touched before griddepcontrol.wait then (w_early)
     g_call_boundary = false;
     ++g_launch_count;
-    return cudaLaunchKernelEx(&cfg, k_linear_i8, d, tm);
+    return cudaLaunchKernelEx(&cfg, kernel, d, maps...);
 }
 
 // Per device, once: large shared memory for the kernel, and how many clusters of 2, 4 and 8 CTAs (one CTA per SM) fit at once.
@@ -536,6 +749,7 @@ cudaError_t linear_device(const int (**clusters)[4]) {
     *clusters = &known[dev];
     if (known[dev][0] != 0) return cudaSuccess;
     e = cudaFuncSetAttribute(k_linear_i8, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_linear_i8_pair, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
     if (e != cudaSuccess) return e;
     for (int i = 1; i < 4; ++i) {
         cudaLaunchConfig_t cfg = {};
@@ -577,13 +791,14 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.R = tiling.R;
     d.split = tiling.split;
     d.kb_share = ceil_div(d.n_kb, d.split);
+    if (tiling.pair) d.m_blocks = ceil_div(p.rows, 256);
     const long long tiles = (long long)d.m_blocks * ceil_div(p.outs, d.R);
     if (tiles > (1ll << 30)) return cudaErrorInvalidValue;
     d.n_tiles = (int)tiles;
-    d.w_chunk = (uint32_t)d.R * kKb;
+    d.w_chunk = (uint32_t)(tiling.pair ? d.R / 2 : d.R) * kKb;
     d.x_chunk = (uint32_t)d.x_rows * kKb;
     // K blocks per stage: up to 40 KB, so that one barrier round trip carries enough bytes
-    d.unit = max(1, min(8, 40 * 1024 / (int)(d.w_chunk + d.x_chunk)));
+    d.unit = tiling.pair ? 1 : max(1, min(8, 40 * 1024 / (int)(d.w_chunk + d.x_chunk)));
     d.stage_bytes = d.unit * (d.w_chunk + d.x_chunk);
     d.tail = 128u * kKb - d.x_chunk;
     d.recv_bytes = (uint32_t)(ceil_div(d.R / 16, d.split) * (d.split - 1) * d.x_rows * 64);
@@ -597,10 +812,14 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.vec_out = ((uintptr_t)p.out % 16) == 0 && (p.ldo * (p.out_f32 ? 4 : 2)) % 16 == 0;
     d.d_status = p.d_status;
     d.w_early = !g_call_boundary;
-    CUtensorMap tm;
-    if (!x_tensor_map(p, d.x_rows, &tm)) return cudaErrorNotSupported;
-    const int grid = d.split > 1 ? d.n_tiles * d.split : (d.n_tiles < kSms ? d.n_tiles : kSms);
-    return launch_clusters(d, tm, grid, (size_t)d.stages * d.stage_bytes + fixed, st);
+    const size_t smem = (size_t)d.stages * d.stage_bytes + fixed;
+    CUtensorMap tm_x, tm_w;
+    if (!x_tensor_map(p, d.x_rows, &tm_x)) return cudaErrorNotSupported;
+    if (tiling.pair) {
+        if (!w_tensor_map(p, d.R / 16, &tm_w)) return cudaErrorNotSupported;
+        return launch_clusters(k_linear_i8_pair, 2, 2 * (d.n_tiles < kSms / 2 ? d.n_tiles : kSms / 2), smem, st, d, tm_x, tm_w);
+    }
+    return launch_clusters(k_linear_i8, d.split, d.split > 1 ? d.n_tiles * d.split : (d.n_tiles < kSms ? d.n_tiles : kSms), smem, st, d, tm_x);
 }
 
 cudaError_t set_wait_limit_i8(unsigned long long ns) { return cudaMemcpyToSymbol(g_wait_limit_ns, &ns, sizeof(ns)); }
