@@ -7,8 +7,7 @@
 //
 // Bound by HBM for many rows and by latency (one trip to memory, one block-wide reduction) for the few rows of a tree.
 // A row is read once and stays in registers; the norm needs sum x^2 and max|x g|, which are independent of each other, so
-// both go through ONE reduction: y = (x g) r with r > 0 has its maximum where |x g| has.  Maxima are taken on the bit
-// patterns of |y| as unsigned integers: the order of finite values, with infinities and NaNs above them all.
+// both go through ONE reduction: y = (x g) r with r > 0 has its maximum where |x g| has.  The maxima keep NaNs.
 #include "cats_kernels.cuh"
 
 namespace cats {
@@ -66,10 +65,10 @@ template <int V> __device__ __forceinline__ void store_v(uint16_t* p, const floa
 // 127 (1 + 2^-23) whatever rs and a are.  The fused product and sum with 1.5 * 2^23 leaves the whole number (ties to even) in
 // the low bits of the result: the conversion instruction has a sixteenth of the FMA rate and shares its unit with ex2 and rcp.
 constexpr float kRintMagic = 12582912.f;
-template <int V> __device__ __forceinline__ void store_q(int8_t* p, const float* y, float rs, float inv) {
+template <int V, bool RS> __device__ __forceinline__ void store_q(int8_t* p, const float* y, float rs, float inv) {
     uint32_t w[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = __float_as_uint(fmaf(y[i] * rs, inv, kRintMagic));
+    for (int i = 0; i < V; ++i) w[i] = __float_as_uint(fmaf(RS ? y[i] * rs : y[i], inv, kRintMagic));
     if (V == 8) {
         uint32_t o[2];
 #pragma unroll
@@ -82,8 +81,25 @@ template <int V> __device__ __forceinline__ void store_q(int8_t* p, const float*
 }
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-// silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.
-__device__ __forceinline__ float silu_mul(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
+// max(m, |a|, |b|), NaN if any of them is
+__device__ __forceinline__ float max_abs(float m, float a, float b) {
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
+    return m;
+}
+template <int V> __device__ __forceinline__ float max_abs(float m, const float* y) {
+    if (V == 1) return max_abs(m, y[0], y[0]);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) m = max_abs(m, y[2 * i], y[(2 * i + 1) % V]);
+    return m;
+}
+// silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.  Flushing
+// forms of 2^x and 1/x: a quotient below 2^-126 is zero at any scale, and the others need twice the instructions.
+__device__ __forceinline__ float silu_mul(float g, float u) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return g * r * u;
+}
 
 struct NoDelta {};        // the norm without a delta
 template <typename T, int V> struct MaybeRaw : Raw<T, V> { static constexpr bool has = true; };
@@ -134,6 +150,12 @@ template <int OP, typename TX, typename TD, int V> struct RowVec {
     }
 };
 
+template <int V> __device__ __forceinline__ void zero(float* y, float& rs) {      // a row that is not finite is stored as zeros
+    rs = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = 0.f;
+}
+
 // Largest block: two vectors of 8 of a single input fit the 64 registers of 1024 threads, the norm's three inputs do not.
 template <int OP, int V, int NV> __host__ __device__ constexpr int row_threads() { return V == 8 && NV <= 2 && OP != I8_NORM ? 1024 : 512; }
 
@@ -152,7 +174,7 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
     if (WARP && row >= p.rows) return;
     float y[NV][V];
     float ss = 0.f;
-    uint32_t mx = 0;
+    float am = 0.f;                 // max |y| of this thread, NaN if any is
     if (!LONG) {
         RowVec<OP, TX, TD, V> in[NV];
 #pragma unroll
@@ -165,8 +187,7 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
             const int c = (k * NT + tid) * V;
             if (c < p.cols) {
                 in[k].values(p, row, c, y[k], ss, true);
-#pragma unroll
-                for (int i = 0; i < V; ++i) mx = max(mx, abs_bits(y[k][i]));
+                am = max_abs<V>(am, y[k]);
             }
         }
     } else {
@@ -174,11 +195,10 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
             RowVec<OP, TX, TD, V> in;
             in.load(p, row, c);
             in.values(p, row, c, y[0], ss, false);
-#pragma unroll
-            for (int i = 0; i < V; ++i) mx = max(mx, abs_bits(y[0][i]));
+            am = max_abs<V>(am, y[0]);
         }
     }
-    mx = __reduce_max_sync(0xffffffffu, mx);
+    uint32_t mx = __reduce_max_sync(0xffffffffu, abs_bits(am));      // the bits of non-negative values are in their order, NaN on top
     if (OP == I8_NORM) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
@@ -204,7 +224,6 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
     const bool finite = abs_bits(a) < 0x7F800000u;
     a = fmaxf(a, kTinyMax);
     const float inv = 127.f / a;
-    if (!finite) rs = 0.f;
     if (tid == 0) p.scale[row] = finite ? a / 127.f : __int_as_float(0x7FC00000);
     int8_t* const q = p.q + row * p.ldq;
     if (!LONG) {
@@ -212,10 +231,8 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
         for (int k = 0; k < NV; ++k) {
             const int c = (k * NT + tid) * V;
             if (c < p.cols) {
-                if (!finite)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) y[k][i] = 0.f;
-                store_q<V>(q + c, y[k], rs, inv);
+                if (!finite) zero<V>(y[k], rs);
+                store_q<V, OP == I8_NORM>(q + c, y[k], rs, inv);
             }
         }
     } else {
@@ -223,10 +240,8 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
             RowVec<OP, TX, TD, V> in;
             in.load(p, row, c);
             in.values(p, row, c, y[0], ss, true);
-            if (!finite)
-#pragma unroll
-                for (int i = 0; i < V; ++i) y[0][i] = 0.f;
-            store_q<V>(q + c, y[0], rs, inv);
+            if (!finite) zero<V>(y[0], rs);
+            store_q<V, OP == I8_NORM>(q + c, y[0], rs, inv);
         }
     }
 }
