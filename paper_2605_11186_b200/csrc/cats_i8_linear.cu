@@ -214,19 +214,18 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
         if (threadIdx.x == 0) report(p.d_status, CATS_ERR_UNSUPPORTED);
         return;
     }
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
-            mbar_init(&ctrl->full[s], 2);     // one arrive.expect_tx from each copying warp
-            mbar_init(&ctrl->empty[s], 1);
+    if (warp == 0) {                          // one stage's barriers per lane
+        if (lane < p.stages) {
+            mbar_init(&ctrl->full[lane], 2);  // one arrive.expect_tx from each copying warp
+            mbar_init(&ctrl->empty[lane], 1);
+        } else if (lane >= 30) {
+            mbar_init(&ctrl->acc_full[lane - 30], 1);
+            mbar_init(&ctrl->acc_empty[lane - 30], 32 * kEpiWarps);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(&ctrl->acc_full[b], 1);
-            mbar_init(&ctrl->acc_empty[b], 32 * kEpiWarps);
-        }
-        ctrl->abort_flag = 0;
+        if (lane == 0) ctrl->abort_flag = 0;
         mbar_fence_init();
-        tma_prefetch_desc(&tm_x);
     }
+    if (warp == 1 && lane == 0) tma_prefetch_desc(&tm_x);
     if (warp == 2) {
         tmem_alloc(&ctrl->tmem_base, p.tmem_cols);
         tmem_relinquish();
@@ -477,17 +476,18 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
         if (threadIdx.x == 0) report(p.d_status, CATS_ERR_UNSUPPORTED);
         return;
     }
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
-            mbar_init(&ctrl->full[s], 2);     // the first CTA's: one arrive.expect_tx from each of its copying warps, for both CTAs' bytes
-            mbar_init(&ctrl->empty[s], 1);
+    if (warp == 0) {                          // one stage's barriers per lane
+        if (lane < p.stages) {
+            mbar_init(&ctrl->full[lane], 2);  // the first CTA's: one arrive.expect_tx from each of its copying warps, for both CTAs' bytes
+            mbar_init(&ctrl->empty[lane], 1);
+        } else if (lane >= 30) {
+            mbar_init(&ctrl->acc_full[lane - 30], 1);
+            mbar_init(&ctrl->acc_empty[lane - 30], 2 * kEpiWarps);        // the first CTA's: the epilogue warps of both
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(&ctrl->acc_full[b], 1);
-            mbar_init(&ctrl->acc_empty[b], 2 * kEpiWarps);        // the first CTA's: the epilogue warps of both
-        }
-        ctrl->abort_flag = 0;
+        if (lane == 0) ctrl->abort_flag = 0;
         mbar_fence_init();
+    }
+    if (warp == 1 && lane == 0) {
         tma_prefetch_desc(&tm_x);
         tma_prefetch_desc(&tm_w);
     }

@@ -16,18 +16,21 @@ namespace {
 constexpr float kTinyMax = 7.888609052210118e-31f;    // 2^-100: the smallest maximum a scale is made from
 
 // One vector of V elements as it lies in memory: V == 8 in 16-byte pieces, V == 1 a single element.  Loads and conversion
-// are apart so that a thread can have all its loads in flight before it uses the first.
+// are apart so that a thread can have all its loads in flight before it uses the first.  Rows are read once and marked so:
+// left to age among them, the int8 rows were written back to HBM and fetched again by the kernel that reads them
+// (SwiGLU of 4096 x 11008 and its values: 71 -> 56 us).
 template <typename T, int V> struct Raw;
 template <> struct Raw<float, 8> {
     float4 a, b;
-    __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
+    __device__ __forceinline__ void load(const float* p) { a = __ldcs(reinterpret_cast<const float4*>(p)); b = __ldcs(reinterpret_cast<const float4*>(p) + 1); }
     __device__ __forceinline__ void get(float* v) const {
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
 };
 template <> struct Raw<uint16_t, 8> {     // bf16 bits
     uint4 a;
-    __device__ __forceinline__ void load(const uint16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load(const uint16_t* p) { a = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void load_shared(const uint16_t* p) { a = __ldg(reinterpret_cast<const uint4*>(p)); }      // by all rows
     __device__ __forceinline__ void get(float* v) const {
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -45,6 +48,7 @@ template <> struct Raw<float, 1> {
 template <> struct Raw<uint16_t, 1> {
     uint16_t a;
     __device__ __forceinline__ void load(const uint16_t* p) { a = *p; }
+    __device__ __forceinline__ void load_shared(const uint16_t* p) { a = __ldg(p); }
     __device__ __forceinline__ void get(float* v) const { v[0] = bf16_bits_to_float(a); }
 };
 template <int V> __device__ __forceinline__ void store_v(float* p, const float* v) {
@@ -87,9 +91,8 @@ __device__ __forceinline__ float max_abs(float m, float a, float b) {
     return m;
 }
 template <int V> __device__ __forceinline__ float max_abs(float m, const float* y) {
-    if (V == 1) return max_abs(m, y[0], y[0]);
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) m = max_abs(m, y[2 * i], y[(2 * i + 1) % V]);
+    for (int i = 0; i < V; i += 2) m = max_abs(m, y[i], y[(i + 1) % V]);
     return m;
 }
 // silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.  Flushing
@@ -120,7 +123,7 @@ template <int OP, typename TX, typename TD, int V> struct RowVec {
         if (OP == I8_SWIGLU) d.load((const TD*)p.x + row * p.ldx + p.cols + c);
         if (OP == I8_NORM) {
             d.load((const TD*)p.delta + row * p.ldd + c);
-            g.load((const uint16_t*)p.gain + c);
+            g.load_shared((const uint16_t*)p.gain + c);
         }
     }
     __device__ __forceinline__ void values(const I8RowsDev& p, long long row, int c, float* y, float& ss, bool write_resid) const {
