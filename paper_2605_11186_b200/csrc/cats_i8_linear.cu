@@ -615,6 +615,87 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
     if (threadIdx.x == 0 && *abort_flag) report(p.d_status, CATS_ERR_TIMEOUT);
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// The same product for very few tokens (one-token passes): there the tensor-core kernel above is a chain of latencies -- set-up,
+// copy, MMA, exchange, store -- around a copy of 2 to 3 us.  Here a block of eight warps takes one 8-row group of w; its warps
+// take the K blocks in turn, a lane one 16-byte piece of rows r and r + 4 per K block straight into registers, four-way
+// products on the ordinary cores (dp4a), T times as many as there are tokens.
+// ---------------------------------------------------------------------------------------------------------------------
+struct FewDev {
+    const int8_t* x;
+    long long ldx;
+    const float *sx, *sw;
+    const uint8_t* w;
+    int rows, cols, outs, n_kb;
+    void* out;
+    int out_f32;
+    long long ldo;
+};
+
+// 16 columns of a row; columns from cols on are not read and count as zero
+__device__ __forceinline__ int4 load_x16(const int8_t* row, int col, int cols) {
+    if (col + 16 <= cols) return *reinterpret_cast<const int4*>(row + col);
+    int v[4] = {0, 0, 0, 0};
+    for (int i = 0; col + i < cols; ++i) v[i >> 2] |= (int)((uint32_t)(uint8_t)row[col + i] << (8 * (i & 3)));
+    return make_int4(v[0], v[1], v[2], v[3]);
+}
+
+template <int T> __global__ void __launch_bounds__(256) k_linear_i8_few(const FewDev p) {
+    constexpr int U = T <= 2 ? 2 : 1;         // K blocks per step: 2 U loads of w in flight per lane
+    __shared__ int red[8][8][T];
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 7, r = lane >> 3;
+    const size_t kb_stride = (size_t)gridDim.x * 1024;
+    const uint8_t* const w0 = p.w + (size_t)blockIdx.x * 1024 + r * 128 + ((c ^ r) << 4);
+    const uint8_t* const w1 = p.w + (size_t)blockIdx.x * 1024 + (r + 4) * 128 + ((c ^ (r + 4)) << 4);
+    pdl_wait();
+    int acc[2][T] = {};
+    for (int kb = warp; kb < p.n_kb; kb += 8 * U) {
+        int4 a[U][2], b[U][T];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = kb + 8 * u;
+            const bool in = k < p.n_kb;
+            a[u][0] = in ? __ldcs(reinterpret_cast<const int4*>(w0 + k * kb_stride)) : make_int4(0, 0, 0, 0);
+            a[u][1] = in ? __ldcs(reinterpret_cast<const int4*>(w1 + k * kb_stride)) : make_int4(0, 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+                b[u][t] = in && t < p.rows ? load_x16(p.x + t * p.ldx, k * kKb + c * 16, p.cols) : make_int4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    acc[h][t] = __dp4a(a[u][h].x, b[u][t].x, acc[h][t]);
+                    acc[h][t] = __dp4a(a[u][h].y, b[u][t].y, acc[h][t]);
+                    acc[h][t] = __dp4a(a[u][h].z, b[u][t].z, acc[h][t]);
+                    acc[h][t] = __dp4a(a[u][h].w, b[u][t].w, acc[h][t]);
+                }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) acc[h][t] += __shfl_xor_sync(0xffffffffu, acc[h][t], o);
+            if (c == 0) red[warp][r + 4 * h][t] = acc[h][t];
+        }
+    __syncthreads();
+    if (threadIdx.x < 8 * T) {
+        const int row = threadIdx.x & 7, t = threadIdx.x >> 3, n = (int)blockIdx.x * 8 + row;
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += red[i][row][t];
+        if (t < p.rows && n < p.outs) {
+            const float v = (float)sum * p.sx[t] * p.sw[n];
+            if (p.out_f32) ((float*)p.out)[t * p.ldo + n] = v;
+            else ((uint16_t*)p.out)[t * p.ldo + n] = float_to_bf16_bits(v);
+        }
+    }
+}
+
 // int8 [rows][cols] -> [K block][8-row group][8 x 128 bytes], 128-byte swizzle, zeros beyond the matrix.  One thread per 16 bytes.
 __global__ void __launch_bounds__(256) k_pack_weights_i8(const int8_t* __restrict__ src, long long ld, int rows, int cols, int n8,
                                                          long long n, uint4* __restrict__ dst) {
@@ -671,6 +752,11 @@ bool w_tensor_map(const I8Linear& p, int box_groups, CUtensorMap* out) {
     return enc(out, CU_TENSOR_MAP_DATA_TYPE_INT32, 2, const_cast<void*>(p.w), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// When the kernel for few tokens is the faster one.  Measured, it against the tensor cores, us: one token 3.0 / 6.4 (4096 x
+// 4096), 7.9 / 10.7 (11008 x 4096), 15.0 / 16.1 (4096 x 22016), 15.3 / 14.2 (5120 x 15360); two tokens 4.5 / 6.5, 10.4 / 10.7,
+// 22.5 / 16.2, 21.5 / 14.2; four tokens 6.2 / 6.5, 14.5 / 10.8, 22.2 / 16.2; eight tokens of 4096 x 4096 9.8 / 6.4.
+bool linear_few(const I8Linear& p) { return p.rows == 1 || (p.rows <= 4 && (long long)p.outs * p.cols <= 1 << 24); }
 
 struct Tiling {
     int R, split, pair;
@@ -780,6 +866,13 @@ cudaError_t launch_pack_weights_i8(const int8_t* src, long long ld, int rows, in
 }
 
 cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
+    if (linear_few(p)) {
+        const FewDev f = {p.x, p.ldx, p.sx, p.sw, (const uint8_t*)p.w, p.rows, p.cols, p.outs, ceil_div(p.cols, kKb), p.out, p.out_f32, p.ldo};
+        const dim3 grid((unsigned)ceil_div(p.outs, 8));
+        if (p.rows == 1) return launch_i8(k_linear_i8_few<1>, grid, dim3(256), 0, st, f);
+        if (p.rows == 2) return launch_i8(k_linear_i8_few<2>, grid, dim3(256), 0, st, f);
+        return launch_i8(k_linear_i8_few<4>, grid, dim3(256), 0, st, f);
+    }
     const int(*clusters)[4];
     cudaError_t e = linear_device(&clusters);
     if (e != cudaSuccess) return e;
