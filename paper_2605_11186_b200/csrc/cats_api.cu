@@ -10,6 +10,7 @@ namespace cats {
 
 thread_local int g_launch_count = 0;
 thread_local bool g_call_boundary = true;
+thread_local bool g_call_overlaps = false;
 int g_debug_attn_kernel = -1;
 int g_debug_fault = 0;
 
@@ -614,6 +615,7 @@ int cats_quantize_i8(const void* d_x, int32_t x_type, int64_t ldx, int32_t rows,
     g_launch_count = 0;
     NvtxRange nvtx_range("cats_quantize_i8");
     g_call_boundary = true;
+    g_call_overlaps = true;
     if (rows < 0 || cols < 1 || bad_type(x_type) || ldx < cols || ldq < cols) return CATS_ERR_INVALID_ARG;
     if (rows == 0) return CATS_OK;
     if (!d_x || !d_q || !d_scale || misaligned(d_x, type_size(x_type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
@@ -628,6 +630,7 @@ int cats_dequantize_i8(const int8_t* d_q, int64_t ldq, const float* d_scale, int
     g_launch_count = 0;
     NvtxRange nvtx_range("cats_dequantize_i8");
     g_call_boundary = true;
+    g_call_overlaps = true;
     if (rows < 0 || cols < 1 || bad_type(out_type) || ldq < cols || ldo < cols) return CATS_ERR_INVALID_ARG;
     if (rows == 0) return CATS_OK;
     if (!d_q || !d_scale || !d_out || misaligned(d_out, type_size(out_type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
@@ -641,6 +644,7 @@ int cats_rmsnorm_i8(const void* d_resid, int32_t resid_type, int64_t ldr, const 
     g_launch_count = 0;
     NvtxRange nvtx_range("cats_rmsnorm_i8");
     g_call_boundary = true;
+    g_call_overlaps = true;
     if (rows < 0 || cols < 1 || bad_type(resid_type) || ldr < cols || ldq < cols || !(eps >= 0.f)) return CATS_ERR_INVALID_ARG;
     if (d_delta && (bad_type(delta_type) || ldd < cols || misaligned(d_delta, type_size(delta_type)))) return CATS_ERR_INVALID_ARG;
     if (d_resid_out && (ldo < cols || misaligned(d_resid_out, type_size(resid_type)))) return CATS_ERR_INVALID_ARG;
@@ -661,6 +665,7 @@ int cats_swiglu_i8(const void* d_gate_up, int32_t type, int64_t ld, int32_t rows
     g_launch_count = 0;
     NvtxRange nvtx_range("cats_swiglu_i8");
     g_call_boundary = true;
+    g_call_overlaps = true;
     if (rows < 0 || cols < 1 || bad_type(type) || ld < 2 * (int64_t)cols || ldq < cols) return CATS_ERR_INVALID_ARG;
     if (rows == 0) return CATS_OK;
     if (!d_gate_up || !d_q || !d_scale || misaligned(d_gate_up, type_size(type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
@@ -675,6 +680,7 @@ int cats_linear_i8(const int8_t* d_x, int64_t ldx, const float* d_x_scale, const
     g_launch_count = 0;
     NvtxRange nvtx_range("cats_linear_i8");
     g_call_boundary = true;
+    g_call_overlaps = true;
     if (rows < 0 || cols < 1 || outs < 1 || bad_type(out_type) || ldx < cols || ldx % 16 || ldo < outs) return CATS_ERR_INVALID_ARG;
     if (cols > kMaxI8Cols) return CATS_ERR_UNSUPPORTED;
     if (rows == 0) return CATS_OK;
@@ -730,6 +736,7 @@ int cats_verify_layer_i8(const cats_model_cfg* cfg, const cats_layer_weights_i8*
     g_launch_count = 0;
     NvtxRange nvtx_range("cats_verify_layer_i8");
     g_call_boundary = true;
+    g_call_overlaps = false;
     int rc = check_cfg(cfg);
     if (rc) return rc;
     if (!w || !d_resid || !d_kcache || !d_vcache || !d_mask || !d_pos || !d_ws || !d_status) return CATS_ERR_INVALID_ARG;

@@ -817,7 +817,7 @@ cudaError_t launch_clusters(void (*kernel)(LinearDev, Maps...), int cluster, int
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;         // also as the first launch of a call: nothing is touched before griddepcontrol.wait then (w_early)
+    cfg.numAttrs = g_call_boundary && !g_call_overlaps ? 1 : 2;
     g_call_boundary = false;
     ++g_launch_count;
     return cudaLaunchKernelEx(&cfg, kernel, d, maps...);
@@ -904,7 +904,7 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.out = p.out; d.out_f32 = p.out_f32; d.ldo = p.ldo;
     d.vec_out = ((uintptr_t)p.out % 16) == 0 && (p.ldo * (p.out_f32 ? 4 : 2)) % 16 == 0;
     d.d_status = p.d_status;
-    d.w_early = !g_call_boundary;
+    d.w_early = !g_call_boundary;       // not as a call of its own (g_call_overlaps)
     const size_t smem = (size_t)d.stages * d.stage_bytes + fixed;
     CUtensorMap tm_x, tm_w;
     if (!x_tensor_map(p, d.x_rows, &tm_x)) return cudaErrorNotSupported;

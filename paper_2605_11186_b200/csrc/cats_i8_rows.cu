@@ -277,34 +277,41 @@ __global__ void __launch_bounds__(256) k_i8_dequantize(const int8_t* __restrict_
 
 // The QKV projection's rows [3 * D] fp32 to what the tree attention reads: q rotated, bf16; k rotated and v appended to cache
 // rows prefix_len + t (rotate-half pairs (i, i + hd / 2), angle pos[t] * base^(-2i/hd) in fp64 so that far positions lose
-// nothing; every value is rounded once, from the unrounded sums).  One block per (node, eighth of the heads).
+// nothing; every value is rounded once, from the unrounded sums).  Grid (nodes, shares of the heads); a thread takes four
+// pairs of q, k and v.  The angles need only pos, which was there before the call: they are computed before the wait for
+// the projection (the fp64 sine is what would take longest here).
 __global__ void __launch_bounds__(256) k_i8_qkv(const float* __restrict__ qkv, const int32_t* __restrict__ pos, int nh, int hd,
                                                 float rope_base, int prefix_len, uint16_t* __restrict__ q, uint16_t* __restrict__ kc,
                                                 uint16_t* __restrict__ vc) {
-    __shared__ float2 cs[64];
+    __shared__ __align__(16) float cos_s[64], sin_s[64];
     pdl_launch_dependents();
-    pdl_wait();
     const int t = blockIdx.x, half = hd / 2, D = nh * hd;
     if ((int)threadIdx.x < half) {
         const double inv_freq = pow((double)rope_base, -2.0 * (double)threadIdx.x / (double)hd);
         double s, c;
         sincos((double)pos[t] * inv_freq, &s, &c);
-        cs[threadIdx.x] = make_float2((float)c, (float)s);
+        cos_s[threadIdx.x] = (float)c;
+        sin_s[threadIdx.x] = (float)s;
     }
     __syncthreads();
+    pdl_wait();
     const float* const row = qkv + (size_t)t * 3 * D;
     const size_t cache_row = (size_t)(prefix_len + t) * D;
-    const int pairs = nh * half;
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < pairs; i += gridDim.y * 256) {
-        const int h = i / half, r = i - h * half, lo = h * hd + r, hi = lo + half;
-        const float2 f = cs[r];
-        const float q0 = row[lo], q1 = row[hi], k0 = row[D + lo], k1 = row[D + hi];
-        q[(size_t)t * D + lo] = float_to_bf16_bits(q0 * f.x - q1 * f.y);
-        q[(size_t)t * D + hi] = float_to_bf16_bits(q1 * f.x + q0 * f.y);
-        kc[cache_row + lo] = float_to_bf16_bits(k0 * f.x - k1 * f.y);
-        kc[cache_row + hi] = float_to_bf16_bits(k1 * f.x + k0 * f.y);
-        vc[cache_row + lo] = float_to_bf16_bits(row[2 * D + lo]);
-        vc[cache_row + hi] = float_to_bf16_bits(row[2 * D + hi]);
+    const int quads = nh * half / 4;
+    auto load4 = [](const float* p) { return __ldcg(reinterpret_cast<const float4*>(p)); };
+    auto store4 = [](uint16_t* p, float a, float b, float c, float d) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d)); };
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < quads; i += gridDim.y * 256) {
+        const int h = i * 4 / half, r = i * 4 - h * half, lo = h * hd + r, hi = lo + half;
+        const float4 c = *reinterpret_cast<const float4*>(cos_s + r), s = *reinterpret_cast<const float4*>(sin_s + r);
+        const float4 q0 = load4(row + lo), q1 = load4(row + hi), k0 = load4(row + D + lo), k1 = load4(row + D + hi);
+        const float4 v0 = load4(row + 2 * D + lo), v1 = load4(row + 2 * D + hi);
+        uint16_t* const qo = q + (size_t)t * D;
+        store4(qo + lo, q0.x * c.x - q1.x * s.x, q0.y * c.y - q1.y * s.y, q0.z * c.z - q1.z * s.z, q0.w * c.w - q1.w * s.w);
+        store4(qo + hi, q1.x * c.x + q0.x * s.x, q1.y * c.y + q0.y * s.y, q1.z * c.z + q0.z * s.z, q1.w * c.w + q0.w * s.w);
+        store4(kc + cache_row + lo, k0.x * c.x - k1.x * s.x, k0.y * c.y - k1.y * s.y, k0.z * c.z - k1.z * s.z, k0.w * c.w - k1.w * s.w);
+        store4(kc + cache_row + hi, k1.x * c.x + k0.x * s.x, k1.y * c.y + k0.y * s.y, k1.z * c.z + k0.z * s.z, k1.w * c.w + k0.w * s.w);
+        store4(vc + cache_row + lo, v0.x, v0.y, v0.z, v0.w);
+        store4(vc + cache_row + hi, v1.x, v1.y, v1.z, v1.w);
     }
 }
 
@@ -346,7 +353,7 @@ cudaError_t launch_i8_rows(int op, const I8RowsDev& p, cudaStream_t st) {
 
 cudaError_t launch_i8_qkv(const float* qkv, const int32_t* pos, int T, int nh, int hd, float rope_base, int prefix_len, void* q, void* kc,
                           void* vc, cudaStream_t st) {
-    return launch_i8(k_i8_qkv, dim3(T, 8), dim3(256), 0, st, qkv, pos, nh, hd, rope_base, prefix_len, (uint16_t*)q, (uint16_t*)kc,
+    return launch_i8(k_i8_qkv, dim3(T, (nh * hd / 8 + 255) / 256), dim3(256), 0, st, qkv, pos, nh, hd, rope_base, prefix_len, (uint16_t*)q, (uint16_t*)kc,
                       (uint16_t*)vc);
 }
 

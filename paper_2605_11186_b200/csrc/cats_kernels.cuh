@@ -41,11 +41,14 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-// The same for kernels that touch no memory at all before their griddepcontrol.wait: they may also overlap the tail of whatever
-// ran before the call.  (Every thread block waits, so a later kernel that waits for this one waits for all before it too.)
+// Set by the calls that are ONE launch of a kernel that then touches no memory before its griddepcontrol.wait: the launch may
+// overlap the tail of whatever ran before the call.  (All of its blocks wait, so whoever waits for it waits for everything
+// before it too.)  Calls of several launches leave it unset: their later kernels read weights and cache rows early, which is
+// only safe behind a first kernel with full stream ordering.
+extern thread_local bool g_call_overlaps;
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_i8(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
-    g_call_boundary = false;
+    if (g_call_overlaps) g_call_boundary = false;
     return launch_pdl(kernel, grid, block, smem, st, args...);
 }
 
