@@ -15,24 +15,86 @@ namespace {
 
 constexpr float kTinyMax = 7.888609052210118e-31f;    // 2^-100: the smallest maximum a scale is made from
 
-// One vector of V elements as it lies in memory: V == 8 in 16-byte pieces, V == 1 a single element.  Loads and conversion
-// are apart so that a thread can have all its loads in flight before it uses the first.  Rows are read once and marked so:
-// left to age among them, the int8 rows were written back to HBM and fetched again by the kernel that reads them
-// (SwiGLU of 4096 x 11008 and its values: 71 -> 56 us).
-template <typename T, int V> struct Raw;
-template <> struct Raw<float, 8> {
-    float4 a, b;
-    __device__ __forceinline__ void load(const float* p) { a = __ldcs(reinterpret_cast<const float4*>(p)); b = __ldcs(reinterpret_cast<const float4*>(p) + 1); }
+// Eight elements of a row as they lie in memory, 16 bytes each.  Loads and conversion are apart so that a thread can have all
+// its loads in flight before it uses the first.  Rows are read once and marked so: left to age among them, the int8 rows
+// were written back to HBM and fetched again by the kernel that reads them (SwiGLU of 4096 x 11008 and its values: 71 -> 56 us).
+//
+// load_any: for rows that start off the 16-byte grid or end inside a vector.  The 16-byte words around a vector are shifted into
+// place; those of the row's first and last vector would hold bytes outside the row, which are not read: there the elements
+// are loaded one by one, zeros behind the last column.
+__device__ __forceinline__ uint32_t word_of(const uint4& a, int i) { return i == 0 ? a.x : (i == 1 ? a.y : (i == 2 ? a.z : a.w)); }
+// words [m / 4 ...] of the NW words w, shifted right by m % 4 bytes (0 or 2); m the same for all lanes
+template <int NW> __device__ __forceinline__ void shift_words(uint32_t* w, int m) {
+    if (m & 8) {
+#pragma unroll
+        for (int i = 0; i + 2 < NW; ++i) w[i] = w[i + 2];
+    }
+    if (m & 4) {
+#pragma unroll
+        for (int i = 0; i + 1 < NW; ++i) w[i] = w[i + 1];
+    }
+    if (m & 2) {
+#pragma unroll
+        for (int i = 0; i + 1 < NW; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+}
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const float* p) {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { w[i] = word_of(a, i); w[4 + i] = word_of(b, i); }
+    }
+    __device__ __forceinline__ void load_any(const float* row, int c, int cols) {
+        const int m = (int)((uintptr_t)row & 15);
+        if (m == 0 && c + 8 <= cols) return load(row + c);
+        if (c > 0 && c + 12 - m / 4 <= cols) {
+            const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + c) - m);
+            const uint4 a = q[0], b = q[1], d = q[2];
+            uint32_t v[12];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = word_of(a, i); v[4 + i] = word_of(b, i); v[8 + i] = word_of(d, i); }
+            shift_words<12>(v, m);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = c + i < cols ? __float_as_uint(row[c + i]) : 0u;
+        }
+    }
     __device__ __forceinline__ void get(float* v) const {
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
     }
 };
-template <> struct Raw<uint16_t, 8> {     // bf16 bits
-    uint4 a;
-    __device__ __forceinline__ void load(const uint16_t* p) { a = __ldcs(reinterpret_cast<const uint4*>(p)); }
-    __device__ __forceinline__ void load_shared(const uint16_t* p) { a = __ldg(reinterpret_cast<const uint4*>(p)); }      // by all rows
+template <> struct Raw<uint16_t> {     // bf16 bits
+    uint32_t w[4];
+    __device__ __forceinline__ void put(const uint4& a) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = word_of(a, i);
+    }
+    __device__ __forceinline__ void load(const uint16_t* p) { put(__ldcs(reinterpret_cast<const uint4*>(p))); }
+    __device__ __forceinline__ void load_shared(const uint16_t* p) { put(__ldg(reinterpret_cast<const uint4*>(p))); }      // by all rows
+    __device__ __forceinline__ void load_any(const uint16_t* row, int c, int cols) {
+        const int m = (int)((uintptr_t)row & 15);
+        if (m == 0 && c + 8 <= cols) return load(row + c);
+        if (c > 0 && c + 16 - m / 2 <= cols) {
+            const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + c) - m);
+            const uint4 a = q[0], b = q[1];
+            uint32_t v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = word_of(a, i); v[4 + i] = word_of(b, i); }
+            shift_words<8>(v, m);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = (c + 2 * i < cols ? (uint32_t)row[c + 2 * i] : 0u) | (c + 2 * i + 1 < cols ? (uint32_t)row[c + 2 * i + 1] << 16 : 0u);
+        }
+    }
     __device__ __forceinline__ void get(float* v) const {
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[2 * i] = __uint_as_float(w[i] << 16);
@@ -40,47 +102,44 @@ template <> struct Raw<uint16_t, 8> {     // bf16 bits
         }
     }
 };
-template <> struct Raw<float, 1> {
-    float a;
-    __device__ __forceinline__ void load(const float* p) { a = *p; }
-    __device__ __forceinline__ void get(float* v) const { v[0] = a; }
-};
-template <> struct Raw<uint16_t, 1> {
-    uint16_t a;
-    __device__ __forceinline__ void load(const uint16_t* p) { a = *p; }
-    __device__ __forceinline__ void load_shared(const uint16_t* p) { a = __ldg(p); }
-    __device__ __forceinline__ void get(float* v) const { v[0] = bf16_bits_to_float(a); }
-};
-template <int V> __device__ __forceinline__ void store_v(float* p, const float* v) {
-    if (V == 8) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void store_vec(float* p, const float* v) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store_vec(uint16_t* p, const float* v) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+__device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_one(uint16_t* p, float v) { *p = float_to_bf16_bits(v); }
+// GRID: the vector is whole and on the 16-byte grid; else `vec` says so for whole vectors
+template <bool GRID, typename T> __device__ __forceinline__ void store_v(T* row, int c, int cols, bool vec, const float* v) {
+    if (GRID || (vec && c + 8 <= cols)) {
+        store_vec(row + c, v);
     } else {
-        p[0] = v[0];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < cols) store_one(row + c + i, v[i]);
     }
 }
-template <int V> __device__ __forceinline__ void store_v(uint16_t* p, const float* v) {
-    if (V == 8)
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-    else
-        p[0] = float_to_bf16_bits(v[0]);
-}
+
 // rint((y rs) inv) as bytes.  (y rs) inv and not y (rs inv): |y rs| <= a, so the result is finite and within
 // 127 (1 + 2^-23) whatever rs and a are.  The fused product and sum with 1.5 * 2^23 leaves the whole number (ties to even) in
 // the low bits of the result: the conversion instruction has a sixteenth of the FMA rate and shares its unit with ex2 and rcp.
 constexpr float kRintMagic = 12582912.f;
-template <int V, bool RS> __device__ __forceinline__ void store_q(int8_t* p, const float* y, float rs, float inv) {
-    uint32_t w[V];
+template <bool GRID, bool RS> __device__ __forceinline__ void store_q(int8_t* row, int c, int cols, bool vec, const float* y, float rs, float inv) {
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = __float_as_uint(fmaf(RS ? y[i] * rs : y[i], inv, kRintMagic));
-    if (V == 8) {
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(fmaf(RS ? y[i] * rs : y[i], inv, kRintMagic));
+    if (GRID || (vec && c + 8 <= cols)) {
         uint32_t o[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            o[h] = __byte_perm(__byte_perm(w[h * 4 % V], w[(h * 4 + 1) % V], 0x0040), __byte_perm(w[(h * 4 + 2) % V], w[(h * 4 + 3) % V], 0x0040), 0x5410);
-        *reinterpret_cast<uint2*>(p) = make_uint2(o[0], o[1]);
+            o[h] = __byte_perm(__byte_perm(w[h * 4], w[h * 4 + 1], 0x0040), __byte_perm(w[h * 4 + 2], w[h * 4 + 3], 0x0040), 0x5410);
+        *reinterpret_cast<uint2*>(row + c) = make_uint2(o[0], o[1]);
     } else {
-        p[0] = (int8_t)(w[0] & 0xFFu);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < cols) row[c + i] = (int8_t)(w[i] & 0xFFu);
     }
 }
 
@@ -90,9 +149,9 @@ __device__ __forceinline__ float max_abs(float m, float a, float b) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
     return m;
 }
-template <int V> __device__ __forceinline__ float max_abs(float m, const float* y) {
+__device__ __forceinline__ float max_abs(float m, const float* y) {
 #pragma unroll
-    for (int i = 0; i < V; i += 2) m = max_abs(m, y[i], y[(i + 1) % V]);
+    for (int i = 0; i < 8; i += 2) m = max_abs(m, y[i], y[i + 1]);
     return m;
 }
 // silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.  Flushing
@@ -105,68 +164,72 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
 }
 
 struct NoDelta {};        // the norm without a delta
-template <typename T, int V> struct MaybeRaw : Raw<T, V> { static constexpr bool has = true; };
-template <int V> struct MaybeRaw<NoDelta, V> {
+template <typename T> struct MaybeRaw : Raw<T> { static constexpr bool has = true; };
+template <> struct MaybeRaw<NoDelta> {
     static constexpr bool has = false;
     __device__ __forceinline__ void load(const void*) {}
+    __device__ __forceinline__ void load_any(const void*, int, int) {}
     __device__ __forceinline__ void get(float*) const {}
 };
 
-// One vector of a row at column c, and from it the values y (before the norm's row factor).
-// TD: SWIGLU's up values (TX), the norm's delta, or NoDelta.
-template <int OP, typename TX, typename TD, int V> struct RowVec {
-    Raw<TX, V> x;
-    MaybeRaw<TD, V> d;
-    Raw<uint16_t, V> g;
+// Eight elements of a row at column c, and from them the values y (before the norm's row factor).
+// TD: SWIGLU's up values (TX), the norm's delta, or NoDelta.  GRID: every vector is whole and on the 16-byte grid.
+template <int OP, typename TX, typename TD, bool GRID> struct RowVec {
+    Raw<TX> x;
+    MaybeRaw<TD> d;
+    Raw<uint16_t> g;
     __device__ __forceinline__ void load(const I8RowsDev& p, long long row, int c) {
-        x.load((const TX*)p.x + row * p.ldx + c);
-        if (OP == I8_SWIGLU) d.load((const TD*)p.x + row * p.ldx + p.cols + c);
-        if (OP == I8_NORM) {
-            d.load((const TD*)p.delta + row * p.ldd + c);
-            g.load_shared((const uint16_t*)p.gain + c);
+        const TX* const xr = (const TX*)p.x + row * p.ldx;
+        const TD* const dr = OP == I8_SWIGLU ? (const TD*)p.x + row * p.ldx + p.cols : (const TD*)p.delta + row * p.ldd;
+        if (GRID) {
+            x.load(xr + c);
+            if (OP != I8_QUANTIZE) d.load(dr + c);
+            if (OP == I8_NORM) g.load_shared((const uint16_t*)p.gain + c);
+        } else {
+            x.load_any(xr, c, p.cols);
+            if (OP != I8_QUANTIZE) d.load_any(dr, c, p.cols);
+            if (OP == I8_NORM) g.load_any((const uint16_t*)p.gain, c, p.cols);
         }
     }
     __device__ __forceinline__ void values(const I8RowsDev& p, long long row, int c, float* y, float& ss, bool write_resid) const {
         x.get(y);
         if (OP == I8_NORM) {
-            float t[V];
-            if (MaybeRaw<TD, V>::has) {
+            float t[8];
+            if (MaybeRaw<TD>::has) {
                 d.get(t);
 #pragma unroll
-                for (int i = 0; i < V; ++i) y[i] += t[i];
-                if (write_resid && p.resid_out != nullptr) store_v<V>((TX*)p.resid_out + row * p.ldo + c, y);
-            } else if (write_resid && p.resid_out != nullptr && p.resid_out != p.x) {
-                store_v<V>((TX*)p.resid_out + row * p.ldo + c, y);
+                for (int i = 0; i < 8; ++i) y[i] += t[i];
             }
+            if (write_resid && p.resid_out != nullptr && (MaybeRaw<TD>::has || p.resid_out != p.x))
+                store_v<GRID>((TX*)p.resid_out + row * p.ldo, c, p.cols, p.resid_vec, y);
             g.get(t);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 ss = fmaf(y[i], y[i], ss);
                 y[i] *= t[i];
             }
         } else if (OP == I8_SWIGLU) {
-            float u[V];
+            float u[8];
             d.get(u);
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = silu_mul(y[i], u[i]);
+            for (int i = 0; i < 8; ++i) y[i] = silu_mul(y[i], u[i]);
         }
     }
 };
-
-template <int V> __device__ __forceinline__ void zero(float* y, float& rs) {      // a row that is not finite is stored as zeros
+__device__ __forceinline__ void zero(float* y, float& rs) {      // a row that is not finite is stored as zeros
     rs = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) y[i] = 0.f;
+    for (int i = 0; i < 8; ++i) y[i] = 0.f;
 }
 
-// Largest block: two vectors of 8 of a single input fit the 64 registers of 1024 threads, the norm's three inputs do not.
-template <int OP, int V, int NV> __host__ __device__ constexpr int row_threads() { return V == 8 && NV <= 2 && OP != I8_NORM ? 1024 : 512; }
+// Largest block: two vectors of a single input fit the 64 registers of 1024 threads, the norm's three inputs do not.
+template <int OP, int NV> __host__ __device__ constexpr int row_threads() { return NV <= 2 && OP != I8_NORM ? 1024 : 512; }
 
-// A block per row, NV vectors of V elements per thread (NV * V * blockDim.x >= cols): the row is read once and stays in
+// A block per row, NV vectors of 8 elements per thread (NV * 8 * blockDim.x >= cols): the row is read once and stays in
 // registers.  LONG: any length, the row is read twice.  WARP: blocks of 128 threads hold four rows, one per warp, and need
 // no barrier.
-template <int OP, typename TX, typename TD, int V, int NV, bool WARP, bool LONG>
-__global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_rows(const I8RowsDev p) {
+template <int OP, typename TX, typename TD, bool GRID, int NV, bool WARP, bool LONG>
+__global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(const I8RowsDev p) {
     __shared__ float red_s[32];
     __shared__ uint32_t red_m[32];
     pdl_launch_dependents();
@@ -175,30 +238,30 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
     const int NT = WARP ? 32 : (int)blockDim.x;
     pdl_wait();
     if (WARP && row >= p.rows) return;
-    float y[NV][V];
+    float y[NV][8];
     float ss = 0.f;
     float am = 0.f;                 // max |y| of this thread, NaN if any is
     if (!LONG) {
-        RowVec<OP, TX, TD, V> in[NV];
+        RowVec<OP, TX, TD, GRID> in[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (k * NT + tid) * V;
+            const int c = (k * NT + tid) * 8;
             if (c < p.cols) in[k].load(p, row, c);
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (k * NT + tid) * V;
+            const int c = (k * NT + tid) * 8;
             if (c < p.cols) {
                 in[k].values(p, row, c, y[k], ss, true);
-                am = max_abs<V>(am, y[k]);
+                am = max_abs(am, y[k]);
             }
         }
     } else {
-        for (int c = tid * V; c < p.cols; c += NT * V) {
-            RowVec<OP, TX, TD, V> in;
+        for (int c = tid * 8; c < p.cols; c += NT * 8) {
+            RowVec<OP, TX, TD, GRID> in;
             in.load(p, row, c);
             in.values(p, row, c, y[0], ss, false);
-            am = max_abs<V>(am, y[0]);
+            am = max_abs(am, y[0]);
         }
     }
     uint32_t mx = __reduce_max_sync(0xffffffffu, abs_bits(am));      // the bits of non-negative values are in their order, NaN on top
@@ -232,27 +295,28 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, V, NV>()) k_i8_ro
     if (!LONG) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (k * NT + tid) * V;
+            const int c = (k * NT + tid) * 8;
             if (c < p.cols) {
-                if (!finite) zero<V>(y[k], rs);
-                store_q<V, OP == I8_NORM>(q + c, y[k], rs, inv);
+                if (!finite) zero(y[k], rs);
+                store_q<GRID, OP == I8_NORM>(q, c, p.cols, p.q_vec, y[k], rs, inv);
             }
         }
     } else {
-        for (int c = tid * V; c < p.cols; c += NT * V) {
-            RowVec<OP, TX, TD, V> in;
+        for (int c = tid * 8; c < p.cols; c += NT * 8) {
+            RowVec<OP, TX, TD, GRID> in;
             in.load(p, row, c);
             in.values(p, row, c, y[0], ss, true);
-            if (!finite) zero<V>(y[0], rs);
-            store_q<V, OP == I8_NORM>(q + c, y[0], rs, inv);
+            if (!finite) zero(y[0], rs);
+            store_q<GRID, OP == I8_NORM>(q, c, p.cols, p.q_vec, y[0], rs, inv);
         }
     }
 }
 
-// q * scale, rounded to bf16 or as fp32.  One block per (row, 4096 columns); V elements per thread and step.
-template <int V>
+// q * scale, rounded to bf16 or as fp32.  One block per (row, 4096 columns); GRID: eight elements per thread and step, else one.
+template <bool GRID>
 __global__ void __launch_bounds__(256) k_i8_dequantize(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale,
                                                        int cols, void* __restrict__ out, int out_f32, long long ldo) {
+    constexpr int V = GRID ? 8 : 1;
     pdl_launch_dependents();
     pdl_wait();
     const long long row = blockIdx.x;
@@ -260,18 +324,20 @@ __global__ void __launch_bounds__(256) k_i8_dequantize(const int8_t* __restrict_
     const int c_end = min(cols, ((int)blockIdx.y + 1) * 4096);
 #pragma unroll 2
     for (int c = blockIdx.y * 4096 + threadIdx.x * V; c < c_end; c += 256 * V) {
-        float v[V];
-        if (V == 8) {
+        if (GRID) {
             // a byte b as the float 2^23 + (b + 128), then minus 2^23 + 128: exact, and no conversion instruction
             const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + row * ldq + c));
+            float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                v[i % V] = (__uint_as_float(__byte_perm((i < 4 ? w.x : w.y) ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s;
+                v[i] = (__uint_as_float(__byte_perm((i < 4 ? w.x : w.y) ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s;
+            if (out_f32) store_vec((float*)out + row * ldo + c, v);
+            else store_vec((uint16_t*)out + row * ldo + c, v);
         } else {
-            v[0] = (float)q[row * ldq + c] * s;
+            const float v = (float)q[row * ldq + c] * s;
+            if (out_f32) store_one((float*)out + row * ldo + c, v);
+            else store_one((uint16_t*)out + row * ldo + c, v);
         }
-        if (out_f32) store_v<V>((float*)out + row * ldo + c, v);
-        else store_v<V>((uint16_t*)out + row * ldo + c, v);
     }
 }
 
@@ -317,27 +383,28 @@ __global__ void __launch_bounds__(256) k_i8_qkv(const float* __restrict__ qkv, c
 
 constexpr int kMinRowsMany = 148 * 4;     // rows from which on throughput counts, not the latency of one row
 
-template <int OP, typename TX, typename TD, int V>
+template <int OP, typename TX, typename TD, bool GRID>
 cudaError_t launch_rows_v(const I8RowsDev& p, cudaStream_t st) {
-    const int vecs = (p.cols + V - 1) / V;          // vectors of a row
-    constexpr int N = V == 8 ? 1 : (OP == I8_NORM ? 4 : 8);     // single elements: more of them per thread, as registers allow
-    if (vecs <= 32 * 4 * N) return launch_i8(k_i8_rows<OP, TX, TD, V, 4 * N, true, false>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, st, p);
+    const int vecs = (p.cols + 7) / 8;              // vectors of a row
+    if (vecs <= 32 * 4) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, true, false>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, st, p);
     const dim3 grid((unsigned)p.rows);
     auto threads = [&](int nv) { return dim3((unsigned)((vecs + nv * 32 - 1) / (nv * 32) * 32)); };
     const bool many = p.rows >= kMinRowsMany;
-    if (vecs <= 512 * N && !many) return launch_i8(k_i8_rows<OP, TX, TD, V, N, false, false>, grid, threads(N), 0, st, p);
-    if (vecs <= 2 * N * row_threads<OP, V, 2 * N>() && !many) return launch_i8(k_i8_rows<OP, TX, TD, V, 2 * N, false, false>, grid, threads(2 * N), 0, st, p);
-    if (vecs <= 2048 * N) return launch_i8(k_i8_rows<OP, TX, TD, V, 4 * N, false, false>, grid, threads(4 * N), 0, st, p);
-    return launch_i8(k_i8_rows<OP, TX, TD, V, N, false, true>, grid, dim3(512), 0, st, p);
+    if (vecs <= 512 && !many) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, false>, grid, threads(1), 0, st, p);
+    // few rows: the shorter chain; off the grid also for many, where a thread holds twice the words until they are shifted
+    if (vecs <= 2 * row_threads<OP, 2>() && (!many || !GRID)) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 2, false, false>, grid, threads(2), 0, st, p);
+    if (vecs <= 2048) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, false, false>, grid, threads(4), 0, st, p);
+    return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, true>, grid, dim3(512), 0, st, p);
 }
 
 template <int OP, typename TX, typename TD>
-cudaError_t launch_rows_t(const I8RowsDev& p, cudaStream_t st) {
-    // vectors of 8 elements where every row of every operand starts on a vector
-    auto vec = [](const void* q, long long ld, size_t size) { return q == nullptr || (((uintptr_t)q % 16) == 0 && (ld * (long long)size) % 16 == 0); };
-    const bool v8 = p.cols % 8 == 0 && vec(p.x, p.ldx, sizeof(TX)) && vec(p.delta, p.ldd, p.d_f32 ? 4 : 2) && vec(p.resid_out, p.ldo, sizeof(TX)) &&
-                    ((uintptr_t)p.gain % 16) == 0 && ((uintptr_t)p.q % 8) == 0 && p.ldq % 8 == 0;
-    return v8 ? launch_rows_v<OP, TX, TD, 8>(p, st) : launch_rows_v<OP, TX, TD, 1>(p, st);
+cudaError_t launch_rows_t(I8RowsDev p, cudaStream_t st) {
+    auto on_grid = [](const void* q, long long ld, size_t size) { return q == nullptr || (((uintptr_t)q % 16) == 0 && (ld * (long long)size) % 16 == 0); };
+    p.q_vec = ((uintptr_t)p.q % 8) == 0 && p.ldq % 8 == 0;
+    p.resid_vec = on_grid(p.resid_out, p.ldo, sizeof(TX));
+    const bool grid = p.cols % 8 == 0 && p.q_vec && p.resid_vec && on_grid(p.x, p.ldx, sizeof(TX)) && on_grid(p.delta, p.ldd, p.d_f32 ? 4 : 2) &&
+                      ((uintptr_t)p.gain % 16) == 0;
+    return grid ? launch_rows_v<OP, TX, TD, true>(p, st) : launch_rows_v<OP, TX, TD, false>(p, st);
 }
 
 }  // namespace
@@ -362,8 +429,8 @@ cudaError_t launch_i8_dequantize(const int8_t* q, long long ldq, const float* sc
     const bool v8 = cols % 8 == 0 && ((uintptr_t)q % 8) == 0 && ldq % 8 == 0 && ((uintptr_t)out % 16) == 0 &&
                     (ldo * (out_f32 ? 4 : 2)) % 16 == 0;
     const dim3 grid((unsigned)rows, (unsigned)((cols + 4095) / 4096));
-    return v8 ? launch_i8(k_i8_dequantize<8>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo)
-              : launch_i8(k_i8_dequantize<1>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo);
+    return v8 ? launch_i8(k_i8_dequantize<true>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo)
+              : launch_i8(k_i8_dequantize<false>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo);
 }
 
 }  // namespace cats
