@@ -109,17 +109,32 @@ __device__ __forceinline__ void store_vec(float* p, const float* v) {
 __device__ __forceinline__ void store_vec(uint16_t* p, const float* v) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
-__device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_one(uint16_t* p, float v) { *p = float_to_bf16_bits(v); }
-// GRID: the vector is whole and on the 16-byte grid; else `vec` says so for whole vectors
-template <bool GRID, typename T> __device__ __forceinline__ void store_v(T* row, int c, int cols, bool vec, const float* v) {
-    if (GRID || (vec && c + 8 <= cols)) {
-        store_vec(row + c, v);
-    } else {
+// The same for rows off the grid: the 256 elements from column c0 on that a warp holds, eight per lane, go through its staging
+// tile so that every store instruction covers a contiguous run (a lane storing its own eight elements one by one leaves a
+// sector of its own each time).  bf16 in pairs from the first 4-byte boundary on.  All lanes take part.
+__device__ __forceinline__ void stage_vec(float* stage, int lane, const float* v) {
+    store_vec(stage + lane * 8, v);
+    __syncwarp();
+}
+__device__ __forceinline__ void warp_store(float* row, int c0, int cols, float* stage, int lane, const float* v) {
+    stage_vec(stage, lane, v);
+    const int n = min(256, cols - c0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < cols) store_one(row + c + i, v[i]);
+    for (int i = 0; i < 8; ++i)
+        if (i * 32 + lane < n) row[c0 + i * 32 + lane] = stage[i * 32 + lane];
+    __syncwarp();
+}
+__device__ __forceinline__ void warp_store(uint16_t* row, int c0, int cols, float* stage, int lane, const float* v) {
+    stage_vec(stage, lane, v);
+    const int n = min(256, cols - c0), head = (int)(((uintptr_t)(row + c0) >> 1) & 1);
+    if (head && lane == 0) row[c0] = float_to_bf16_bits(stage[0]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = head + 2 * (i * 32 + lane);
+        if (e + 1 < n) *reinterpret_cast<uint32_t*>(row + c0 + e) = pack_bf16x2(stage[e], stage[e + 1]);
+        else if (e < n) row[c0 + e] = float_to_bf16_bits(stage[e]);
     }
+    __syncwarp();
 }
 
 // rint((y rs) inv) as bytes.  (y rs) inv and not y (rs inv): |y rs| <= a, so the result is finite and within
@@ -191,17 +206,18 @@ template <int OP, typename TX, typename TD, bool GRID> struct RowVec {
             if (OP == I8_NORM) g.load_any((const uint16_t*)p.gain, c, p.cols);
         }
     }
-    __device__ __forceinline__ void values(const I8RowsDev& p, long long row, int c, float* y, float& ss, bool write_resid) const {
+    __device__ __forceinline__ void sum(float* y) const {        // the norm: residual + delta; else the input
         x.get(y);
+        if (OP == I8_NORM && MaybeRaw<TD>::has) {
+            float t[8];
+            d.get(t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] += t[i];
+        }
+    }
+    __device__ __forceinline__ void values(float* y, float& ss) const {
         if (OP == I8_NORM) {
             float t[8];
-            if (MaybeRaw<TD>::has) {
-                d.get(t);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] += t[i];
-            }
-            if (write_resid && p.resid_out != nullptr && (MaybeRaw<TD>::has || p.resid_out != p.x))
-                store_v<GRID>((TX*)p.resid_out + row * p.ldo, c, p.cols, p.resid_vec, y);
             g.get(t);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -216,6 +232,14 @@ template <int OP, typename TX, typename TD, bool GRID> struct RowVec {
         }
     }
 };
+// The norm's sums to the residual stream: in place and without a delta they are there already.
+template <typename TX, typename TD, bool GRID>
+__device__ __forceinline__ void store_resid(const I8RowsDev& p, long long row, int c, int c0, float* stage, int lane, const float* y) {
+    if (p.resid_out == nullptr || (!MaybeRaw<TD>::has && p.resid_out == p.x)) return;
+    TX* const out = (TX*)p.resid_out + row * p.ldo;
+    if (!GRID) warp_store(out, c0, p.cols, stage, lane, y);
+    else if (c < p.cols) store_vec(out + c, y);
+}
 __device__ __forceinline__ void zero(float* y, float& rs) {      // a row that is not finite is stored as zeros
     rs = 0.f;
 #pragma unroll
@@ -232,6 +256,9 @@ template <int OP, typename TX, typename TD, bool GRID, int NV, bool WARP, bool L
 __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(const I8RowsDev p) {
     __shared__ float red_s[32];
     __shared__ uint32_t red_m[32];
+    __shared__ __align__(16) float stage_s[OP == I8_NORM && !GRID ? (WARP ? 4 : 16) * 256 : 4];      // a staging tile per warp
+    const int lane = threadIdx.x & 31;
+    float* const stage = stage_s + (OP == I8_NORM && !GRID ? (threadIdx.x >> 5) * 256 : 0);
     pdl_launch_dependents();
     const long long row = WARP ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : (long long)blockIdx.x;
     const int tid = WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
@@ -250,9 +277,11 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (k * NT + tid) * 8;
+            const int c = (k * NT + tid) * 8, c0 = c - lane * 8;
+            if (c < p.cols) in[k].sum(y[k]);
+            if (OP == I8_NORM && c0 < p.cols) store_resid<TX, TD, GRID>(p, row, c, c0, stage, lane, y[k]);
             if (c < p.cols) {
-                in[k].values(p, row, c, y[k], ss, true);
+                in[k].values(y[k], ss);
                 am = max_abs(am, y[k]);
             }
         }
@@ -260,7 +289,8 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
         for (int c = tid * 8; c < p.cols; c += NT * 8) {
             RowVec<OP, TX, TD, GRID> in;
             in.load(p, row, c);
-            in.values(p, row, c, y[0], ss, false);
+            in.sum(y[0]);
+            in.values(y[0], ss);
             am = max_abs(am, y[0]);
         }
     }
@@ -302,42 +332,72 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
             }
         }
     } else {
-        for (int c = tid * 8; c < p.cols; c += NT * 8) {
+        for (int c0 = (tid - lane) * 8; c0 < p.cols; c0 += NT * 8) {
+            const int c = c0 + lane * 8;
             RowVec<OP, TX, TD, GRID> in;
-            in.load(p, row, c);
-            in.values(p, row, c, y[0], ss, true);
-            if (!finite) zero(y[0], rs);
-            store_q<GRID, OP == I8_NORM>(q, c, p.cols, p.q_vec, y[0], rs, inv);
+            if (c < p.cols) {
+                in.load(p, row, c);
+                in.sum(y[0]);
+            }
+            if (OP == I8_NORM) store_resid<TX, TD, GRID>(p, row, c, c0, stage, lane, y[0]);
+            if (c < p.cols) {
+                in.values(y[0], ss);
+                if (!finite) zero(y[0], rs);
+                store_q<GRID, OP == I8_NORM>(q, c, p.cols, p.q_vec, y[0], rs, inv);
+            }
         }
     }
 }
 
-// q * scale, rounded to bf16 or as fp32.  One block per (row, 4096 columns); GRID: eight elements per thread and step, else one.
-template <bool GRID>
+// q * scale, rounded to bf16 or as fp32.  One block per (row, 4096 columns), eight elements per thread and step.  The second
+// kernel is for rows off the grid and ragged ends; q_vec says whether rows of q start on 8 bytes.
+__device__ __forceinline__ void eight_values(const uint2& w, float s, float* v) {
+    // a byte b as the float 2^23 + (b + 128), then minus 2^23 + 128: exact, and no conversion instruction
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = (__uint_as_float(__byte_perm((i < 4 ? w.x : w.y) ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s;
+}
 __global__ void __launch_bounds__(256) k_i8_dequantize(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale,
                                                        int cols, void* __restrict__ out, int out_f32, long long ldo) {
-    constexpr int V = GRID ? 8 : 1;
     pdl_launch_dependents();
     pdl_wait();
     const long long row = blockIdx.x;
     const float s = __ldg(scale + row);
     const int c_end = min(cols, ((int)blockIdx.y + 1) * 4096);
 #pragma unroll 2
-    for (int c = blockIdx.y * 4096 + threadIdx.x * V; c < c_end; c += 256 * V) {
-        if (GRID) {
-            // a byte b as the float 2^23 + (b + 128), then minus 2^23 + 128: exact, and no conversion instruction
-            const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + row * ldq + c));
-            float v[8];
+    for (int c = blockIdx.y * 4096 + threadIdx.x * 8; c < c_end; c += 2048) {
+        float v[8];
+        eight_values(__ldg(reinterpret_cast<const uint2*>(q + row * ldq + c)), s, v);
+        if (out_f32) store_vec((float*)out + row * ldo + c, v);
+        else store_vec((uint16_t*)out + row * ldo + c, v);
+    }
+}
+__global__ void __launch_bounds__(256) k_i8_dequantize_any(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale,
+                                                           int cols, int q_vec, void* __restrict__ out, int out_f32, long long ldo) {
+    __shared__ __align__(16) float stage_s[8 * 256];
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long row = blockIdx.x;
+    const int lane = threadIdx.x & 31;
+    float* const stage = stage_s + (threadIdx.x >> 5) * 256;
+    const float s = __ldg(scale + row);
+    const int8_t* const qr = q + row * ldq;
+    const int c_end = min(cols, ((int)blockIdx.y + 1) * 4096);
+#pragma unroll 2
+    for (int c0 = blockIdx.y * 4096 + (threadIdx.x - lane) * 8; c0 < c_end; c0 += 2048) {
+        const int c = c0 + lane * 8;
+        uint2 w = make_uint2(0, 0);
+        if (q_vec && c + 8 <= c_end) {
+            w = __ldg(reinterpret_cast<const uint2*>(qr + c));
+        } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                v[i] = (__uint_as_float(__byte_perm((i < 4 ? w.x : w.y) ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s;
-            if (out_f32) store_vec((float*)out + row * ldo + c, v);
-            else store_vec((uint16_t*)out + row * ldo + c, v);
-        } else {
-            const float v = (float)q[row * ldq + c] * s;
-            if (out_f32) store_one((float*)out + row * ldo + c, v);
-            else store_one((uint16_t*)out + row * ldo + c, v);
+                if (c + i < c_end) (i < 4 ? w.x : w.y) |= (uint32_t)(uint8_t)__ldg(qr + c + i) << (8 * (i & 3));
         }
+        float v[8];
+        eight_values(w, s, v);
+        if (out_f32) warp_store((float*)out + row * ldo, c0, c_end, stage, lane, v);
+        else warp_store((uint16_t*)out + row * ldo, c0, c_end, stage, lane, v);
     }
 }
 
@@ -401,8 +461,7 @@ template <int OP, typename TX, typename TD>
 cudaError_t launch_rows_t(I8RowsDev p, cudaStream_t st) {
     auto on_grid = [](const void* q, long long ld, size_t size) { return q == nullptr || (((uintptr_t)q % 16) == 0 && (ld * (long long)size) % 16 == 0); };
     p.q_vec = ((uintptr_t)p.q % 8) == 0 && p.ldq % 8 == 0;
-    p.resid_vec = on_grid(p.resid_out, p.ldo, sizeof(TX));
-    const bool grid = p.cols % 8 == 0 && p.q_vec && p.resid_vec && on_grid(p.x, p.ldx, sizeof(TX)) && on_grid(p.delta, p.ldd, p.d_f32 ? 4 : 2) &&
+    const bool grid = p.cols % 8 == 0 && p.q_vec && on_grid(p.resid_out, p.ldo, sizeof(TX)) && on_grid(p.x, p.ldx, sizeof(TX)) && on_grid(p.delta, p.ldd, p.d_f32 ? 4 : 2) &&
                       ((uintptr_t)p.gain % 16) == 0;
     return grid ? launch_rows_v<OP, TX, TD, true>(p, st) : launch_rows_v<OP, TX, TD, false>(p, st);
 }
@@ -426,11 +485,11 @@ cudaError_t launch_i8_qkv(const float* qkv, const int32_t* pos, int T, int nh, i
 
 cudaError_t launch_i8_dequantize(const int8_t* q, long long ldq, const float* scale, int rows, int cols, void* out, int out_f32,
                                  long long ldo, cudaStream_t st) {
-    const bool v8 = cols % 8 == 0 && ((uintptr_t)q % 8) == 0 && ldq % 8 == 0 && ((uintptr_t)out % 16) == 0 &&
-                    (ldo * (out_f32 ? 4 : 2)) % 16 == 0;
+    const bool q_vec = ((uintptr_t)q % 8) == 0 && ldq % 8 == 0;
+    const bool on_grid = cols % 8 == 0 && q_vec && ((uintptr_t)out % 16) == 0 && (ldo * (out_f32 ? 4 : 2)) % 16 == 0;
     const dim3 grid((unsigned)rows, (unsigned)((cols + 4095) / 4096));
-    return v8 ? launch_i8(k_i8_dequantize<true>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo)
-              : launch_i8(k_i8_dequantize<false>, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo);
+    return on_grid ? launch_i8(k_i8_dequantize, grid, dim3(256), 0, st, q, ldq, scale, cols, out, out_f32, ldo)
+                   : launch_i8(k_i8_dequantize_any, grid, dim3(256), 0, st, q, ldq, scale, cols, q_vec, out, out_f32, ldo);
 }
 
 }  // namespace cats

@@ -193,7 +193,7 @@ struct I8RowsDev {
     int rows, cols;
     int x_f32, d_f32;
     float eps;
-    int q_vec, resid_vec;   // filled by launch_i8_rows: whole vectors of q and resid_out may be stored at once
+    int q_vec;              // filled by launch_i8_rows: rows of q start on 8 bytes
 };
 cudaError_t launch_i8_rows(int op, const I8RowsDev& p, cudaStream_t st);
 cudaError_t launch_i8_dequantize(const int8_t* q, long long ldq, const float* scale, int rows, int cols, void* out, int out_f32,
