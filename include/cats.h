@@ -358,8 +358,9 @@ int cats_tp_argmax_merge(const float *d_max, const int32_t *d_idx, int32_t n_sha
  * Matrices are row-major with a row stride (ld*) in ELEMENTS, at least cols;
  * columns behind cols are neither read nor written.  Rows may start anywhere
  * their element type may; 16-byte starts (8 for int8) and column counts that are
- * multiples of 8 are the fast case.  Types are CATS_F32 or CATS_BF16.  rows == 0
- * launches nothing.  Except where a parameter says so, outputs must not overlap
+ * multiples of 8 are the fast case.  cols <= 131071 (the product's sums of more
+ * could overflow): CATS_ERR_UNSUPPORTED.  Types are CATS_F32 or CATS_BF16.
+ * rows == 0 launches nothing.  Except where a parameter says so, outputs must not overlap
  * inputs.  Calls need no workspace and may run on any streams at once. */
 enum { CATS_F32 = 0, CATS_BF16 = 1 };
 
@@ -395,7 +396,8 @@ int cats_pack_weights_i8(const int8_t *d_src, int64_t ld, int32_t rows, int32_t 
  * the sums are exact 32-bit integers, both scales are applied in fp32 in this
  * order, the product is rounded once to out_type.  x must start on 16 bytes and
  * ldx be a multiple of 16.  d_w: cats_pack_weights_i8 of w [outs][cols];
- * cols <= 131071 (more could overflow the sums): CATS_ERR_UNSUPPORTED. */
+ * rows, outs <= 2^30.  A bounded wait that expires sets CATS_ERR_TIMEOUT in
+ * *d_status; the output is then unspecified. */
 int cats_linear_i8(const int8_t *d_x, int64_t ldx, const float *d_x_scale, const void *d_w, const float *d_w_scale, int32_t rows,
                    int32_t cols, int32_t outs, void *d_out, int32_t out_type, int64_t ldo, int32_t *d_status, void *stream);
 

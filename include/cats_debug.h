@@ -48,7 +48,9 @@ int cats_debug_wait_limit_ns(unsigned long long ns);
  *   1 projection kernel: CTAs that contribute a partial tile to a tile another
  *     CTA owns do not raise their ready flag;
  *   2 tcgen05 attention kernel: the loader announces the query tile on its
- *     barrier but never copies it.
+ *     barrier but never copies it;
+ *   3 8-bit product (the kernels on the tensor cores): the last copy of x is
+ *     announced on its barrier but never made.
  * Set a short wait limit first, or each expiry takes a second. */
 void cats_debug_inject_fault(int which);
 

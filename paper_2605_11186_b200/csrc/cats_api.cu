@@ -268,7 +268,7 @@ int cats_debug_timeline(int kernel, void* host, size_t bytes) {
     if (e == cudaErrorNotSupported) return CATS_ERR_UNSUPPORTED;
     return e == cudaSuccess ? CATS_OK : (e == cudaErrorInvalidValue ? CATS_ERR_INVALID_ARG : CATS_ERR_CUDA);
 }
-void cats_debug_inject_fault(int which) { g_debug_fault = (which == 1 || which == 2) ? which : 0; }
+void cats_debug_inject_fault(int which) { g_debug_fault = which >= 1 && which <= 3 ? which : 0; }
 int cats_debug_wait_limit_ns(unsigned long long ns) {
     if (ns == 0) ns = kWaitLimitNs;
     if (set_wait_limit_gemm(ns) != cudaSuccess || set_wait_limit_attn(ns) != cudaSuccess || set_wait_limit_small(ns) != cudaSuccess ||
@@ -596,7 +596,7 @@ static inline int type_size(int32_t type) { return type == CATS_F32 ? 4 : 2; }
 static inline bool bad_type(int32_t type) { return type != CATS_F32 && type != CATS_BF16; }
 
 size_t cats_packed_weight_i8_bytes(int32_t rows, int32_t cols) {
-    if (rows < 1 || cols < 1 || cols > kMaxI8Cols) return 0;
+    if (rows < 1 || cols < 1 || rows > kMaxI8Rows || cols > kMaxI8Cols) return 0;
     return packed_weight_i8_bytes(rows, cols);
 }
 
@@ -617,6 +617,7 @@ int cats_quantize_i8(const void* d_x, int32_t x_type, int64_t ldx, int32_t rows,
     g_call_boundary = true;
     g_call_overlaps = true;
     if (rows < 0 || cols < 1 || bad_type(x_type) || ldx < cols || ldq < cols) return CATS_ERR_INVALID_ARG;
+    if (cols > kMaxI8Cols) return CATS_ERR_UNSUPPORTED;
     if (rows == 0) return CATS_OK;
     if (!d_x || !d_q || !d_scale || misaligned(d_x, type_size(x_type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
     I8RowsDev p = {};
@@ -632,6 +633,7 @@ int cats_dequantize_i8(const int8_t* d_q, int64_t ldq, const float* d_scale, int
     g_call_boundary = true;
     g_call_overlaps = true;
     if (rows < 0 || cols < 1 || bad_type(out_type) || ldq < cols || ldo < cols) return CATS_ERR_INVALID_ARG;
+    if (cols > kMaxI8Cols) return CATS_ERR_UNSUPPORTED;
     if (rows == 0) return CATS_OK;
     if (!d_q || !d_scale || !d_out || misaligned(d_out, type_size(out_type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
     CATS_CUDA(launch_i8_dequantize(d_q, ldq, d_scale, rows, cols, d_out, out_type == CATS_F32, ldo, (cudaStream_t)stream));
@@ -649,6 +651,7 @@ int cats_rmsnorm_i8(const void* d_resid, int32_t resid_type, int64_t ldr, const 
     if (d_delta && (bad_type(delta_type) || ldd < cols || misaligned(d_delta, type_size(delta_type)))) return CATS_ERR_INVALID_ARG;
     if (d_resid_out && (ldo < cols || misaligned(d_resid_out, type_size(resid_type)))) return CATS_ERR_INVALID_ARG;
     if (d_resid_out == d_resid && d_resid_out && ldo != ldr) return CATS_ERR_INVALID_ARG;     // in place means the same rows
+    if (cols > kMaxI8Cols) return CATS_ERR_UNSUPPORTED;
     if (rows == 0) return CATS_OK;
     if (!d_resid || !d_gain || !d_q || !d_scale) return CATS_ERR_INVALID_ARG;
     if (misaligned(d_resid, type_size(resid_type)) || misaligned(d_gain, 2) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
@@ -667,6 +670,7 @@ int cats_swiglu_i8(const void* d_gate_up, int32_t type, int64_t ld, int32_t rows
     g_call_boundary = true;
     g_call_overlaps = true;
     if (rows < 0 || cols < 1 || bad_type(type) || ld < 2 * (int64_t)cols || ldq < cols) return CATS_ERR_INVALID_ARG;
+    if (cols > kMaxI8Cols) return CATS_ERR_UNSUPPORTED;
     if (rows == 0) return CATS_OK;
     if (!d_gate_up || !d_q || !d_scale || misaligned(d_gate_up, type_size(type)) || misaligned(d_scale, 4)) return CATS_ERR_INVALID_ARG;
     I8RowsDev p = {};
@@ -682,7 +686,7 @@ int cats_linear_i8(const int8_t* d_x, int64_t ldx, const float* d_x_scale, const
     g_call_boundary = true;
     g_call_overlaps = true;
     if (rows < 0 || cols < 1 || outs < 1 || bad_type(out_type) || ldx < cols || ldx % 16 || ldo < outs) return CATS_ERR_INVALID_ARG;
-    if (cols > kMaxI8Cols) return CATS_ERR_UNSUPPORTED;
+    if (cols > kMaxI8Cols || rows > kMaxI8Rows || outs > kMaxI8Rows) return CATS_ERR_UNSUPPORTED;
     if (rows == 0) return CATS_OK;
     if (!d_x || !d_x_scale || !d_w || !d_w_scale || !d_out || !d_status) return CATS_ERR_INVALID_ARG;
     if (misaligned(d_x, 16) || misaligned(d_w, 1024) || misaligned(d_out, type_size(out_type)) || misaligned(d_x_scale, 4) ||

@@ -55,6 +55,7 @@ struct LinearDev {
     int out_f32, vec_out;   // vec_out: rows and columns allow 16-byte stores
     long long ldo;
     int w_early;            // w may be read before the kernel in front has finished
+    int drop_x;             // fault injection: the x copy of a CTA's last stage is announced but never made
     int32_t* d_status;
 };
 
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
                         for (int j = 0; j < nk; ++j) bulk_copy(stage + j * p.w_chunk, w_tile + (size_t)(kb + j) * kb_stride, w_bytes, &ctrl->full[s], pol);
                     } else {
                         mbar_expect_tx(&ctrl->full[s], p.x_chunk * nk);
-                        for (int j = 0; j < nk; ++j)
+                        for (int j = 0; j < nk && !(p.drop_x && i == n_units - 1); ++j)
                             tma_load_2d(stage + p.unit * p.w_chunk + j * p.x_chunk, &tm_x, (kb0 + kb + j) * kKb, mb * 128, &ctrl->full[s], pol);
                     }
                 }
@@ -523,7 +524,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
                         tma_load_pair(stage + p.x_chunk, &tm_w, 0, kb * n8 + w_row, &ctrl->full[s], pol);
                     } else {
                         if (rank == 0) mbar_expect_tx(&ctrl->full[s], 2 * p.x_chunk);
-                        tma_load_pair(stage, &tm_x, kb * kKb, x_row, &ctrl->full[s], pol);
+                        if (!(p.drop_x && kb == p.n_kb - 1)) tma_load_pair(stage, &tm_x, kb * kKb, x_row, &ctrl->full[s], pol);
                     }
                 }
                 __syncwarp();
@@ -708,7 +709,10 @@ __global__ void __launch_bounds__(256) k_pack_weights_i8(const int8_t* __restric
     uint32_t w[4] = {0, 0, 0, 0};
     if (row < rows) {
         const int8_t* s = src + row * ld + col;
-        for (int i = 0; i < 16 && col + i < cols; ++i) w[i >> 2] |= ((uint32_t)(uint8_t)s[i]) << (8 * (i & 3));
+        if (col + 16 <= cols && ((uintptr_t)s & 15) == 0) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(s));
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else for (int i = 0; i < 16 && col + i < cols; ++i) w[i >> 2] |= ((uint32_t)(uint8_t)s[i]) << (8 * (i & 3));
     }
     dst[group * 64 + r * 8 + (c ^ r)] = make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -792,7 +796,7 @@ Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&cl
         }
     }
     // CTA pairs on 256 tokens: half the channels to take in, and 2 R clocks of the tensor cores
-    if (p.rows > 128)
+    if (p.rows > 128 && clusters[1] > 0)
         for (int R = 256; R >= 64; R -= 32) {
             const long long tiles = (long long)ceil_div(p.rows, 256) * ceil_div(p.outs, R);
             const float waves = (float)((tiles + clusters[1] - 1) / clusters[1]);
@@ -904,6 +908,7 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.out = p.out; d.out_f32 = p.out_f32; d.ldo = p.ldo;
     d.vec_out = ((uintptr_t)p.out % 16) == 0 && (p.ldo * (p.out_f32 ? 4 : 2)) % 16 == 0;
     d.d_status = p.d_status;
+    d.drop_x = g_debug_fault == 3;
     d.w_early = !g_call_boundary;       // not as a call of its own (g_call_overlaps)
     const size_t smem = (size_t)d.stages * d.stage_bytes + fixed;
     CUtensorMap tm_x, tm_w;

@@ -446,7 +446,7 @@ constexpr int kMinRowsMany = 148 * 4;     // rows from which on throughput count
 template <int OP, typename TX, typename TD, bool GRID>
 cudaError_t launch_rows_v(const I8RowsDev& p, cudaStream_t st) {
     const int vecs = (p.cols + 7) / 8;              // vectors of a row
-    if (vecs <= 32 * 4) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, true, false>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, st, p);
+    if (vecs <= 32 * 4) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, true, false>, dim3(((unsigned)p.rows + 3u) / 4u), dim3(128), 0, st, p);
     const dim3 grid((unsigned)p.rows);
     auto threads = [&](int nv) { return dim3((unsigned)((vecs + nv * 32 - 1) / (nv * 32) * 32)); };
     const bool many = p.rows >= kMinRowsMany;

@@ -17,7 +17,8 @@ extern thread_local bool g_call_boundary;
 // Measurement / fault-injection state set through the cats_debug_* hooks (include/cats_debug.h); process-wide.
 extern int g_debug_attn_kernel;   // -1: attention kernel chosen by shape; 0: mma.sync kernel; 1: tcgen05 kernel; 2: tcgen05 kernel,
                                   // two softmax threads per query row instead of four
-extern int g_debug_fault;         // 0: none; 1: a helper CTA of a projection never publishes; 2: the attention loader drops Q
+extern int g_debug_fault;         // 0: none; 1: a helper CTA of a projection never publishes; 2: the attention loader drops Q;
+                                  // 3: the 8-bit product drops the last copy of x
 cudaError_t set_wait_limit_gemm(unsigned long long ns);
 cudaError_t set_wait_limit_attn(unsigned long long ns);
 cudaError_t set_wait_limit_small(unsigned long long ns);
@@ -180,6 +181,8 @@ size_t attn_plan(AttnProblem& p);
 cudaError_t launch_tree_attention(const AttnProblem& p, cudaStream_t st);
 
 // ---- 8-bit integer path ----------------------------------------------------------------------------
+constexpr int kMaxI8Cols = 131071;     // columns * 128 * 128 fits the int32 sums of the product
+constexpr int kMaxI8Rows = 1 << 30;    // tokens or channels of the product: tile arithmetic in 32 bits
 enum I8RowsOp : int { I8_NORM = 0, I8_SWIGLU = 1, I8_QUANTIZE = 2 };
 // Rows to int8 with one scale each.  Strides in elements; types: fp32 or (x_f32 == 0, d_f32 == 0) bf16.
 struct I8RowsDev {
@@ -204,7 +207,6 @@ cudaError_t launch_i8_qkv(const float* qkv, const int32_t* pos, int T, int nh, i
                           void* vc, cudaStream_t st);
 
 // out[t][n] = (sum_k x[t][k] w[n][k]) * sx[t] * sw[n], int8 operands, w packed by launch_pack_weights_i8.
-constexpr int kMaxI8Cols = 131071;     // K * 128 * 128 fits the int32 sums
 struct I8Linear {
     const int8_t* x;        // rows of ldx bytes (a multiple of 16)
     long long ldx;

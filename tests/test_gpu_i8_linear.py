@@ -139,6 +139,69 @@ def test_captured_and_replayed(cats):
     assert int(st.item()) == 0
 
 
+def test_captured_between_copies_and_on_two_branches(cats):
+    """In a graph whose nodes in front are copies, fills and another stream's kernels, not only kernels of this library."""
+    T, K, N = 70, 640, 1000
+    src = torch.randn(T, K, device="cuda")
+    x, out_a, out_b = torch.empty_like(src), torch.empty(T, N, device="cuda"), torch.empty(T, N, device="cuda")
+    (qa, sa), (qb, sb) = cats.new_i8(T, K), cats.new_i8(T, K)
+    w, sw = cats.quantize_weights_i8(torch.randn(N, K, device="cuda"))
+    st, side = cats.new_status(), torch.cuda.Stream()
+
+    def run():
+        main = torch.cuda.current_stream()
+        x.copy_(src)
+        qa.zero_()
+        side.wait_stream(main)
+        cats.cats_quantize_i8(x, qa, sa)
+        with torch.cuda.stream(side):
+            cats.cats_quantize_i8(x * -2, qb, sb)
+            cats.cats_linear_i8(qb, sb, w, sw, out_b, st)
+        out_a.fill_(7)
+        cats.cats_linear_i8(qa, sa, w, sw, out_a, st)
+        main.wait_stream(side)
+        cats.cats_dequantize_i8(qb, sb, x)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(3):
+        src.copy_(torch.randn(T, K, device="cuda"))
+        run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (out_a, out_b, x)]
+        for t in (out_a, out_b, x):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((out_a, out_b, x), want))
+    assert int(st.item()) == 0
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(64, 4096, 12288), (37, 1024, 50000), (64, 11008, 4096), (1000, 2048, 4096), (3000, 1024, 8192)])
+def test_a_wait_that_runs_out(cats, rows, cols, outs):
+    """Whole tiles, tiles shared by a cluster, CTA pairs: the last copy of x is announced but withheld by the host's order.  The
+    call returns, says so, writes nothing beside its output, and the next call is right."""
+    x, w, sx, sw = _whole(rows, cols, 26), _whole(outs, cols, 27), _scales(rows, 28), _scales(outs, 29)
+    packed = cats.pack_weights_i8(w)
+    want = _run(cats, x, sx, w, sw, torch.float32).clone()
+    buf, st = torch.full((rows + 2, outs), 3.0, device="cuda"), cats.new_status()
+    cats.wait_limit_ns(2_000_000)
+    try:
+        cats.inject_fault(3)
+        cats.cats_linear_i8(x, sx, packed, sw, buf[1:-1], st)
+        torch.cuda.synchronize()
+    finally:
+        cats.inject_fault(0)
+        cats.wait_limit_ns(0)
+    assert int(st.item()) == -6 and (buf[0] == 3).all() and (buf[-1] == 3).all()
+    st.zero_()
+    cats.cats_linear_i8(x, sx, packed, sw, buf[1:-1], st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0 and torch.equal(buf[1:-1], want)
+
+
 def test_wrong_shapes_and_types_are_refused(cats):
     x, w, sx, sw = _whole(4, 64, 1), _whole(32, 64, 2), _scales(4, 3), _scales(32, 4)
     p, out, st = cats.pack_weights_i8(w), torch.empty(4, 32, device="cuda"), cats.new_status()

@@ -78,6 +78,19 @@ def test_pack(lib):
     assert lib.cats_pack_weights_i8(A, 64, 0, 64, A, None) == INVALID
 
 
+def test_sizes_that_are_not_supported(lib):
+    n = 131072
+    assert lib.cats_quantize_i8(A, F32, n, 2, n, A, n, A, None) == UNSUPPORTED
+    assert lib.cats_dequantize_i8(A, n, A, 2, n, A, F32, n, None) == UNSUPPORTED
+    assert lib.cats_rmsnorm_i8(A, F32, n, None, F32, 0, A, 1e-5, 2, n, None, 0, A, n, A, None) == UNSUPPORTED
+    assert lib.cats_swiglu_i8(A, F32, 2 * n, 2, n, A, n, A, None) == UNSUPPORTED
+    big = (1 << 30) + 1
+    assert lib.cats_linear_i8(A, 64, A, A, A, big, 64, 8, A, F32, 8, A, None) == UNSUPPORTED
+    assert lib.cats_linear_i8(A, 64, A, A, A, 2, 64, big, A, F32, big, A, None) == UNSUPPORTED
+    assert lib.cats_packed_weight_i8_bytes(big, 64) == 0
+    assert lib.cats_last_launch_count() == 0
+
+
 def test_no_rows_is_no_work(lib):
     """Zero rows: accepted, nothing launched, no pointer looked at."""
     assert lib.cats_quantize_i8(None, F32, 64, 0, 64, None, 64, None, None) == 0
