@@ -246,8 +246,8 @@ __device__ __forceinline__ void zero(float* y, float& rs) {      // a row that i
     for (int i = 0; i < 8; ++i) y[i] = 0.f;
 }
 
-// Largest block: two vectors of a single input fit the 64 registers of 1024 threads, the norm's three inputs do not.
-template <int OP, int NV> __host__ __device__ constexpr int row_threads() { return NV <= 2 && OP != I8_NORM ? 1024 : 512; }
+// Largest block: what fits the 64 registers of 1024 threads is one vector, or two of a single input (the norm has three).
+template <int OP, int NV> __host__ __device__ constexpr int row_threads() { return NV == 1 || (NV == 2 && OP != I8_NORM) ? 1024 : 512; }
 
 // A block per row, NV vectors of 8 elements per thread (NV * 8 * blockDim.x >= cols): the row is read once and stays in
 // registers.  LONG: any length, the row is read twice.  WARP: blocks of 128 threads hold four rows, one per warp, and need
@@ -256,7 +256,7 @@ template <int OP, typename TX, typename TD, bool GRID, int NV, bool WARP, bool L
 __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(const I8RowsDev p) {
     __shared__ float red_s[32];
     __shared__ uint32_t red_m[32];
-    __shared__ __align__(16) float stage_s[OP == I8_NORM && !GRID ? (WARP ? 4 : 16) * 256 : 4];      // a staging tile per warp
+    __shared__ __align__(16) float stage_s[OP == I8_NORM && !GRID ? (WARP ? 4 : row_threads<OP, NV>() / 32) * 256 : 4];      // a staging tile per warp
     const int lane = threadIdx.x & 31;
     float* const stage = stage_s + (OP == I8_NORM && !GRID ? (threadIdx.x >> 5) * 256 : 0);
     pdl_launch_dependents();
@@ -450,7 +450,7 @@ cudaError_t launch_rows_v(const I8RowsDev& p, cudaStream_t st) {
     const dim3 grid((unsigned)p.rows);
     auto threads = [&](int nv) { return dim3((unsigned)((vecs + nv * 32 - 1) / (nv * 32) * 32)); };
     const bool many = p.rows >= kMinRowsMany;
-    if (vecs <= 512 && !many) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, false>, grid, threads(1), 0, st, p);
+    if (vecs <= 1024 && !many) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, false>, grid, threads(1), 0, st, p);
     // few rows: the shorter chain; off the grid also for many, where a thread holds twice the words until they are shifted
     if (vecs <= 2 * row_threads<OP, 2>() && (!many || !GRID)) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 2, false, false>, grid, threads(2), 0, st, p);
     if (vecs <= 2048) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, false, false>, grid, threads(4), 0, st, p);

@@ -42,6 +42,7 @@ SIZES = [(1, 1, 1), (1, 16, 8), (1, 128, 16), (2, 127, 15), (3, 129, 17), (8, 25
          (37, 256, 1376), (64, 4096, 4096), (77, 5120, 1536), (128, 11008, 4096), (127, 640, 40000), (129, 384, 300), (200, 2048, 512),
          (256, 256, 256), (300, 512, 2000), (513, 1024, 1111), (1000, 128, 8000), (1, 11008, 4096), (5, 40000, 48), (2500, 320, 2500),
          (257, 2048, 12296), (1024, 4096, 4096), (2049, 200, 5000), (4093, 130, 300),
+         (700, 2001, 5003), (1500, 1000, 6001), (391, 8000, 3500), (2047, 1111, 7777), (513, 6000, 2000),
          (1, 4096, 22016), (1, 131, 5003), (3, 4096, 4100), (4, 1000, 77), (4, 8192, 4096), (2, 17, 9)]
 
 
