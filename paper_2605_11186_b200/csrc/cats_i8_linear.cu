@@ -325,7 +325,24 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             if (elect_one()) umma_commit(&ctrl->acc_full[b]);      // also on abort, so that the epilogue warps wake up
             __syncwarp();
         }
-    } else if (warp >= 4) {
+    } else if (warp == 3) {
+        // A call of its own may not read w before the kernel in front has finished (it may be what writes w), but HBM need not
+        // idle until then: the first copies' bytes are requested into L2, which is where any later write of theirs lands too
+        // (64 x 4096 x 22016, calls back to back: 17.3 -> 16.2 us).
+        if (!p.w_early && p.m_blocks == 1 && first < p.n_tiles) {
+            const int n0 = first * p.R;
+            const uint32_t w_bytes = (uint32_t)min(p.R, (p.outs - n0 + 7) / 8 * 8) * kKb;
+            const size_t kb_stride = (size_t)((p.outs + 7) / 8) * 1024;
+            const uint8_t* const w_tile = p.w + (size_t)kb0 * kb_stride + (size_t)(n0 >> 3) * 1024;
+            if (elect_one())
+                for (int i = 0, u = u_first; i < min(S, n_units); ++i) {
+                    for (int j = 0; j < p.unit && u * p.unit + j < n_kb; ++j)
+                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(w_tile + (size_t)(u * p.unit + j) * kb_stride), "r"(w_bytes) : "memory");
+                    if (++u == n_units) u = 0;
+                }
+            __syncwarp();
+        }
+    } else {
         pdl_wait();
         const int q4 = warp & 3, group = (warp - 4) >> 2;         // TMEM lane quadrant; two warps share it and take turns
         uint32_t* const stage = stage_s + (warp - 4) * 1024;
@@ -649,6 +666,12 @@ template <int T> __global__ void __launch_bounds__(256) k_linear_i8_few(const Fe
     const size_t kb_stride = (size_t)gridDim.x * 1024;
     const uint8_t* const w0 = p.w + (size_t)blockIdx.x * 1024 + r * 128 + ((c ^ r) << 4);
     const uint8_t* const w1 = p.w + (size_t)blockIdx.x * 1024 + (r + 4) * 128 + ((c ^ (r + 4)) << 4);
+    // into L2 while the kernel in front finishes, as in k_linear_i8 (1 x 4096 x 4096, calls back to back: 4.2 -> 3.7 us)
+    if (c == 0)
+        for (int u = 0; u < 4 && warp + 8 * u < p.n_kb; ++u) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(w0 + (warp + 8 * u) * kb_stride));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(w1 + (warp + 8 * u) * kb_stride));
+        }
     pdl_wait();
     int acc[2][T] = {};
     for (int kb = warp; kb < p.n_kb; kb += 8 * U) {
