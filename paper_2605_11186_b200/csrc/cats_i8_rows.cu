@@ -315,11 +315,17 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
         }
     }
     float rs = 1.f;
-    if (OP == I8_NORM) rs = rsqrtf(ss / (float)p.cols + p.eps);
+    if (OP == I8_NORM) rs = __frsqrt_rn(ss / (float)p.cols + p.eps);
     float a = __uint_as_float(mx) * rs;
     const bool finite = abs_bits(a) < 0x7F800000u;
+    // 127 y / a: the norm's row factor is in both, so where a is the row's own maximum the quotient is taken without it, two
+    // roundings fewer.  (Below 2^-90 the reciprocal could overflow.)
+    float inv = 127.f / fmaxf(a, kTinyMax);
+    if (OP == I8_NORM && a >= kTinyMax && __uint_as_float(mx) >= 8.077935669463161e-28f) {
+        inv = 127.f / __uint_as_float(mx);
+        rs = 1.f;
+    }
     a = fmaxf(a, kTinyMax);
-    const float inv = 127.f / a;
     if (tid == 0) p.scale[row] = finite ? a / 127.f : __int_as_float(0x7FC00000);
     int8_t* const q = p.q + row * p.ldq;
     if (!LONG) {
