@@ -218,6 +218,34 @@ def test_wrong_shapes_and_types_are_refused(cats):
         assert e.value.status == -1
 
 
+def test_weights_past_4_gb(cats):
+    """Byte offsets into the packed weights past 2^32, in each of the kernels; the last and some other channels are checked."""
+    cols, outs = 12288, 360000
+    g = torch.Generator(device="cuda").manual_seed(30)
+    w = torch.randint(-127, 128, (outs, cols), generator=g, device="cuda", dtype=torch.int8)
+    packed, sw, st = cats.pack_weights_i8(w), _scales(outs, 31), cats.new_status()
+    assert packed.numel() > 1 << 32
+    some = torch.cat([torch.arange(0, outs, 997, device="cuda"), torch.arange(outs - 600, outs, device="cuda")])
+    for rows in (1, 16, 300):
+        x, sx = _whole(rows, cols, 32), _scales(rows, 33)
+        out = torch.empty(rows, outs, device="cuda")
+        cats.cats_linear_i8(x, sx, packed, sw, out, st)
+        ref.check_linear(out[:, some], ref.linear(x, sx, w[some], sw[some]))
+    assert int(st.item()) == 0
+
+
+@pytest.mark.parametrize("cols", [64, 640])
+def test_outputs_past_2_31_elements(cats, cols):
+    rows, outs = 4100, 530000
+    x, w, sx, sw, st = _whole(rows, cols, 34), _whole(outs, cols, 35), _scales(rows, 36), _scales(outs, 37), cats.new_status()
+    out = torch.empty(rows, outs, dtype=torch.bfloat16, device="cuda")
+    assert out.numel() > 1 << 31
+    cats.cats_linear_i8(x, sx, cats.pack_weights_i8(w), sw, out, st)
+    for some in (torch.arange(0, rows, 411, device="cuda"), torch.arange(rows - 5, rows, device="cuda")):
+        ref.check_linear(out[some], ref.linear(x[some], sx[some], w, sw))
+    assert int(st.item()) == 0
+
+
 def test_a_token_does_not_depend_on_its_batch(cats):
     """Whole-number sums have no order: any share of the tokens, whatever tiles it runs in, gives the same bits."""
     x, w, sx, sw = _whole(400, 1536, 22), _whole(2000, 1536, 23), _scales(400, 24), _scales(2000, 25)

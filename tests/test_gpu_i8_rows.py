@@ -153,8 +153,7 @@ def test_no_rows(cats):
 
 
 def test_offsets_past_32_bits(cats):
-    """Row strides that take the last rows' element offsets past 2^31 and 2^32 (bf16 rows 2^31 elements apart would be
-    8 GB; three rows of one 5 GB buffer)."""
+    """A row stride that takes the last row past 2^31 elements and 2^32 bytes (three rows of one 5 GB buffer)."""
     stride, cols = (1 << 30) + (1 << 28), 264
     buf = torch.empty(2 * stride + cols, dtype=torch.bfloat16, device="cuda")
     x = buf.as_strided((3, cols), (stride, 1))
