@@ -10,8 +10,9 @@
 //   * x is row-major as the row kernels leave it; TMA boxes of 128 bytes x ceil8(tokens) rows bring it in, zeros beyond the
 //     last row and column.
 // Warp 0 copies w, warp 1 copies x into a ring of shared-memory stages with mbarrier completion; warp 2 issues tcgen05.mma
-// into one of two TMEM accumulators; warps 4-11 drain the other one: int32 -> fp32 * sx * sw -> bf16 or fp32 rows.  Rows of a stage that no copy writes (tokens beyond the last, channels beyond the last) hold
-// leftovers; they only reach accumulator rows and columns that are not stored.
+// into one of two TMEM accumulators; warps 4-11 drain the other one: int32 -> fp32 * sx * sw -> bf16 or fp32 rows.  Rows of
+// a stage that no copy writes (tokens beyond the last, channels beyond the last) hold leftovers; they only reach accumulator
+// rows and columns that are not stored.
 // With few tiles the K blocks are cut into `split` shares, one CTA of a cluster each.  The partial sums meet in distributed
 // shared memory: the accumulator's 16-channel groups are dealt out to the CTAs, every CTA stores its int32 partial of a group
 // into the memory of the group's owner (each sender has its own place there), one cluster barrier publishes them, and the
@@ -253,7 +254,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
         // many token blocks read the same rows of w soon after one another; a tree reads them once
         const uint64_t pol = is_w && p.m_blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
         const size_t kb_stride = (size_t)((p.outs + 7) / 8) * 1024;       // packed bytes of one K block
-        // x comes from the kernel before; w does not where this launch follows others of the same call
+        // x comes from the kernel before; w does not where this launch follows others of the same call: the ring is filled with
+        // it at once.  No clock of a bounded wait starts before the kernel in front has finished.
         if (!is_w || !p.w_early) pdl_wait();
         int s = 0, issued = 0;
         uint32_t par = 1;
@@ -264,6 +266,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             const uint32_t w_bytes = (uint32_t)min(p.R, (p.outs - n0 + 7) / 8 * 8) * kKb;
             const uint8_t* const w_tile = p.w + (size_t)kb0 * kb_stride + (size_t)(n0 >> 3) * 1024;
             for (int i = 0, u = u_first; i < n_units; ++i) {
+                if (issued == S) pdl_wait();
                 if (issued >= S && !warp_wait(&ctrl->empty[s], par, abort_flag)) { ok = false; break; }
                 uint8_t* const stage = smem + (size_t)s * p.stage_bytes;
                 const int kb = u * p.unit, nk = min(p.unit, n_kb - kb);
@@ -288,6 +291,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             for (int j = max(0, issued - S); j < issued; ++j) mbar_wait(&ctrl->full[j % S], (j / S) & 1, &ignore);
         }
     } else if (warp == 2) {
+        pdl_wait();
         const uint32_t idesc = idesc_i8_m128(p.R);
         int s = 0, seg = 0;
         uint32_t par = 0;
@@ -447,8 +451,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
 // The same product for many tokens, where it is bound by the tensor cores and by what an SM takes in: a pair of CTAs on two
 // SMs works on one tile of 256 tokens x R channels (tcgen05 cta_group::2).  Each CTA brings its 128 tokens and half of the
 // tile's channels, (128 + R / 2) rows per K block for 128 x R sums, where a CTA on its own takes in 128 + R; that is what lets
-// the tensor cores keep up their rate (4093 x 4096 x 22016: 219 us, 3370 TOP/s; single CTAs on 128 x 256 tiles 301 us).  Copies of both CTAs
-// count on the first CTA's barrier, whose warp 2 issues the MMAs for both; commits arrive at both.
+// the tensor cores keep up their rate (4093 x 4096 x 22016: 219 us, 3370 TOP/s; single CTAs on 128 x 256 tiles 301 us).
+// Copies of both CTAs count on the first CTA's barrier, whose warp 2 issues the MMAs for both; commits arrive at both.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr uint32_t kFirstOfPair = 0xFEFFFFFFu;       // a shared-memory address in the pair's first CTA
 
@@ -533,6 +537,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
             const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
             const int w_row = nt * p.R / 8 + rank * (p.R / 16), x_row = mb * 256 + rank * 128;
             for (int kb = 0; kb < p.n_kb; ++kb) {
+                if (issued == S) pdl_wait();
                 if (issued >= S && !warp_wait(&ctrl->empty[s], par, abort_flag)) { ok = false; break; }
                 uint8_t* const stage = smem + (size_t)s * p.stage_bytes;
                 if (elect_one()) {
@@ -558,6 +563,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
         }
     } else if (warp == 2) {
         if (rank == 0) {
+            pdl_wait();
             const uint32_t idesc = idesc_i8_m256(p.R);
             int s = 0, seg = 0;
             uint32_t par = 0;
