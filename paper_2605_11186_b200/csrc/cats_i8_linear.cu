@@ -147,9 +147,8 @@ __device__ __forceinline__ void bulk_copy(void* smem_dst, const void* gsrc, uint
 
 // The way of NC accumulator columns of a warp's 32 tokens (one per lane) to out[t0 + lane][n0 .. n0 + NC), through the warp's
 // staging tile: a store instruction then covers whole runs of a few rows (from the lanes directly, every lane's 16 bytes are a
-// cache line of their own).  The sums are staged as they are and scaled on the way out, in short loops: the epilogue runs
-// once or twice per launch, and unrolled it spent its time fetching instructions.  16-byte pieces are permuted by row so that
-// neither side has bank conflicts.
+// cache line of their own).  The sums are staged as they are and scaled on the way out, where a lane keeps its columns' scales.
+// 16-byte pieces are permuted by row so that neither side has bank conflicts.
 template <int NC> __device__ __forceinline__ uint32_t* staged(uint32_t* stage, int row, int piece) {
     return stage + row * NC + ((piece ^ (NC == 32 ? row & 7 : (row >> 1) & 3)) << 2);
 }
@@ -162,30 +161,48 @@ template <int NC> __device__ __forceinline__ void stage_cols(const uint32_t* acc
 // n_tokens: valid tokens from t0 on; n_cols <= NC: valid columns; sx: the 32 token scales; sw: scales of the columns.
 template <int NC>
 __device__ __forceinline__ void store_cols(const LinearDev& p, long long t0, int n_tokens, int n0, int n_cols, const float* sx, const float* sw,
-                                           uint32_t* stage, int lane) {
+                                           const uint32_t* stage, int lane) {
     constexpr int NP = NC / 4;                       // pieces of 4 columns per row
-    auto scaled = [&](int row, int piece, const float4& w) {
-        const uint4 a = *reinterpret_cast<const uint4*>(staged<NC>(stage, row, piece));
-        const float s = sx[row];
+    auto scale4 = [](const uint4& a, float s, const float4& w) {
         return make_float4((float)(int)a.x * s * w.x, (float)(int)a.y * s * w.y, (float)(int)a.z * s * w.z, (float)(int)a.w * s * w.w);
     };
     if (p.vec_out && n_cols % 8 == 0) {
+        // A lane keeps its columns and steps through the rows: the permutation of its pieces repeats every 8 rows.
         if (p.out_f32) {
-            const int piece = lane % NP;
+            constexpr int RI = 32 / NP;              // rows per instruction
+            const int r0 = lane / NP, piece = lane % NP;
             const float4 w = *reinterpret_cast<const float4*>(sw + piece * 4);
-            float* o = (float*)p.out + (t0 + lane / NP) * p.ldo + n0 + piece * 4;
+            float* o = (float*)p.out + (t0 + r0) * p.ldo + n0 + piece * 4;
+            uint4 a[NP];                             // all loads before the first store: the compiler keeps their order
+            float s[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                a[i] = *reinterpret_cast<const uint4*>(staged<NC>(const_cast<uint32_t*>(stage), r0 + i * RI, piece));
+                s[i] = sx[r0 + i * RI];
+            }
             if (piece * 4 < n_cols)
-#pragma unroll 2
-                for (int row = lane / NP; row < n_tokens; row += 32 / NP, o += (32 / NP) * p.ldo) *reinterpret_cast<float4*>(o) = scaled(row, piece, w);
+#pragma unroll
+                for (int i = 0; i < NP; ++i, o += RI * p.ldo)
+                    if (r0 + i * RI < n_tokens) *reinterpret_cast<float4*>(o) = scale4(a[i], s[i], w);
         } else {
-            const int piece = lane % (NP / 2) * 2;
+            constexpr int RI = 64 / NP;
+            const int r0 = lane / (NP / 2), piece = lane % (NP / 2) * 2;
             const float4 w0 = *reinterpret_cast<const float4*>(sw + piece * 4), w1 = *reinterpret_cast<const float4*>(sw + piece * 4 + 4);
-            uint16_t* o = (uint16_t*)p.out + (t0 + lane / (NP / 2)) * p.ldo + n0 + piece * 4;
+            uint16_t* o = (uint16_t*)p.out + (t0 + r0) * p.ldo + n0 + piece * 4;
+            uint4 a[NP / 2], b[NP / 2];
+            float s[NP / 2];
+#pragma unroll
+            for (int i = 0; i < NP / 2; ++i) {
+                a[i] = *reinterpret_cast<const uint4*>(staged<NC>(const_cast<uint32_t*>(stage), r0 + i * RI, piece));
+                b[i] = *reinterpret_cast<const uint4*>(staged<NC>(const_cast<uint32_t*>(stage), r0 + i * RI, piece + 1));
+                s[i] = sx[r0 + i * RI];
+            }
             if (piece * 4 < n_cols)
-#pragma unroll 2
-                for (int row = lane / (NP / 2); row < n_tokens; row += 64 / NP, o += (64 / NP) * p.ldo) {
-                    const float4 a = scaled(row, piece, w0), b = scaled(row, piece + 1, w1);
-                    *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w));
+#pragma unroll
+                for (int i = 0; i < NP / 2; ++i, o += RI * p.ldo) {
+                    const float4 u = scale4(a[i], s[i], w0), v = scale4(b[i], s[i], w1);
+                    if (r0 + i * RI < n_tokens)
+                        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(u.x, u.y), pack_bf16x2(u.z, u.w), pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
                 }
         }
     } else {
@@ -193,15 +210,51 @@ __device__ __forceinline__ void store_cols(const LinearDev& p, long long t0, int
         if (col < n_cols) {
             const float w = sw[col];
             long long o = (t0 + lane / NC) * p.ldo + n0 + col;
-#pragma unroll 2
+#pragma unroll 4
             for (int row = lane / NC; row < n_tokens; row += 32 / NC, o += (32 / NC) * p.ldo) {
-                const float v = (float)(int)staged<NC>(stage, row, col >> 2)[col & 3] * sx[row] * w;
+                const float v = (float)(int)staged<NC>(const_cast<uint32_t*>(stage), row, col >> 2)[col & 3] * sx[row] * w;
                 if (p.out_f32) ((float*)p.out)[o] = v;
                 else ((uint16_t*)p.out)[o] = float_to_bf16_bits(v);
             }
         }
     }
     __syncwarp();
+}
+
+// The scales of a tile, fetched a tile ahead into registers and from there to the warp's copy in shared memory.
+struct TileScales {
+    float w[8], x;
+    __device__ __forceinline__ void fetch(const LinearDev& p, int n0, long long t0, int lane) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = lane + 32 * j < p.R && n0 + lane + 32 * j < p.outs ? __ldg(p.sw + n0 + lane + 32 * j) : 0.f;
+        x = t0 + lane < p.rows ? __ldg(p.sx + t0 + lane) : 0.f;
+    }
+    __device__ __forceinline__ void put(float* sw, float* sx, int lane) const {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sw[lane + 32 * j] = w[j];
+        sx[lane] = x;
+        __syncwarp();
+    }
+};
+
+// This warp's share (32 columns, every other time) of a whole accumulator: the next columns are on their way while these are
+// scaled and stored.  n_tokens > 0.  release(): called once when the warp has read its last columns.
+template <typename F>
+__device__ __forceinline__ void store_tile(const LinearDev& p, uint32_t taddr, int group, long long t0, int n_tokens, int n0, const float* sx,
+                                           const float* sw, uint32_t* stage, int lane, F release) {
+    uint32_t acc[32];
+    const int n_cols = min(p.R, p.outs - n0);
+    if (group * 32 < n_cols) tmem_load<32>(taddr + group * 32, acc);
+    else release();
+#pragma unroll 1
+    for (int c = group * 32; c < n_cols; c += 64) {
+        tmem_loaded<32>(acc);
+        stage_cols<32>(acc, stage, lane);
+        if (c + 64 < n_cols) tmem_load<32>(taddr + c + 64, acc);
+        else release();
+        store_cols<32>(p, t0, n_tokens, n0 + c, min(32, n_cols - c), sx, sw + c, stage, lane);
+    }
 }
 
 __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const __grid_constant__ CUtensorMap tm_x) {
@@ -222,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             mbar_init(&ctrl->empty[lane], 1);
         } else if (lane >= 30) {
             mbar_init(&ctrl->acc_full[lane - 30], 1);
-            mbar_init(&ctrl->acc_empty[lane - 30], 32 * kEpiWarps);
+            mbar_init(&ctrl->acc_empty[lane - 30], kEpiWarps);
         }
         if (lane == 0) ctrl->abort_flag = 0;
         mbar_fence_init();
@@ -352,18 +405,33 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
         uint32_t* const stage = stage_s + (warp - 4) * 1024;
         float* const sw = sw_s + (warp - 4) * 288;                // a copy of the tile's scales per warp: no barrier needed
         float* const sx = sw + 256;
+        const int tl = q4 * 32 + lane;
         int seg = 0;
         bool ok = true;
+        TileScales scales;
+        auto place = [&](int tile, int& n0, long long& t0) {
+            const int nt = p.m_blocks == 1 ? tile : tile / p.m_blocks;
+            n0 = nt * p.R;
+            t0 = (long long)(tile - nt * p.m_blocks) * 128 + q4 * 32;
+        };
+        int n0 = 0;
+        long long t0 = 0;
+        if (first < p.n_tiles) {
+            place(first, n0, t0);
+            scales.fetch(p, n0, t0, lane);
+        }
         for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
-            const int nt = p.m_blocks == 1 ? tile : tile / p.m_blocks, mb = tile - nt * p.m_blocks;
-            const int n0 = nt * p.R, b = seg & 1;
-            const int tl = q4 * 32 + lane;
-            const long long t0 = (long long)mb * 128 + q4 * 32, t = t0 + lane;
+            const int b = seg & 1;
+            place(tile, n0, t0);
+            const long long t = t0 + lane;
             const int n_tokens = (int)min(32ll, p.rows - t0);      // valid tokens of this warp (negative: none)
-            __syncwarp();
-            for (int i = lane; i < p.R; i += 32) sw[i] = n0 + i < p.outs ? __ldg(p.sw + n0 + i) : 0.f;
-            sx[lane] = t < p.rows ? __ldg(p.sx + t) : 0.f;
-            __syncwarp();
+            scales.put(sw, sx, lane);
+            if (tile + G < p.n_tiles) {
+                int n1;
+                long long t1;
+                place(tile + G, n1, t1);
+                scales.fetch(p, n1, t1, lane);
+            }
             ok = warp_wait(&ctrl->acc_full[b], (seg >> 1) & 1, abort_flag) && !__any_sync(0xffffffffu, *abort_flag);
             tc_fence_after_sync();
             const bool busy = n_tokens > 0;
@@ -414,21 +482,14 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
                         store_cols<16>(p, t0, n_tokens, n0 + g * 16, min(16, p.outs - n0 - g * 16), sx, sw + g * 16, stage, lane);
                     }
                 }
-            } else if (ok && busy) {
-                // the next columns are on their way while these are scaled and stored
-                uint32_t acc[32];
-                const int n_cols = min(p.R, p.outs - n0);
-                if (group * 32 < n_cols) tmem_load<32>(taddr + group * 32, acc);
-#pragma unroll 1
-                for (int c = group * 32; c < n_cols; c += 64) {
-                    tmem_loaded<32>(acc);
-                    stage_cols<32>(acc, stage, lane);
-                    if (c + 64 < n_cols) tmem_load<32>(taddr + c + 64, acc);
-                    store_cols<32>(p, t0, n_tokens, n0 + c, min(32, n_cols - c), sx, sw + c, stage, lane);
-                }
             }
-            tc_fence_before_sync();
-            mbar_arrive(&ctrl->acc_empty[b]);
+            auto release = [&] {                                   // the accumulator may be overwritten as far as this warp goes
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctrl->acc_empty[b]);
+            };
+            if (p.split == 1 && ok && busy) store_tile(p, taddr, group, t0, n_tokens, n0, sx, sw, stage, lane, release);
+            else release();
         }
     }
     if (p.split > 1 && warp < 4) {            // the other warps' part in the two phases of the cluster barrier
@@ -599,33 +660,39 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
         float* const sx = sw + 256;
         int seg = 0;
         bool ok = true;
+        TileScales scales;
+        auto place = [&](int tile, int& n0, long long& t0) {
+            const int nt = tile / p.m_blocks;
+            n0 = nt * p.R;
+            t0 = (long long)(tile - nt * p.m_blocks) * 256 + rank * 128 + q4 * 32;
+        };
+        int n0 = 0;
+        long long t0 = 0;
+        if (first < p.n_tiles) {
+            place(first, n0, t0);
+            scales.fetch(p, n0, t0, lane);
+        }
         for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
-            const int nt = tile / p.m_blocks, mb = tile - nt * p.m_blocks;
-            const int n0 = nt * p.R, b = seg & 1;
-            const long long t0 = (long long)mb * 256 + rank * 128 + q4 * 32;
+            const int b = seg & 1;
+            place(tile, n0, t0);
             const int n_tokens = (int)min(32ll, p.rows - t0);      // valid tokens of this warp (negative: none)
-            __syncwarp();
-            for (int i = lane; i < p.R; i += 32) sw[i] = n0 + i < p.outs ? __ldg(p.sw + n0 + i) : 0.f;
-            sx[lane] = lane < n_tokens ? __ldg(p.sx + t0 + lane) : 0.f;
-            __syncwarp();
+            scales.put(sw, sx, lane);
+            if (tile + G < p.n_tiles) {
+                int n1;
+                long long t1;
+                place(tile + G, n1, t1);
+                scales.fetch(p, n1, t1, lane);
+            }
             ok = warp_wait(&ctrl->acc_full[b], (seg >> 1) & 1, abort_flag) && !__any_sync(0xffffffffu, *abort_flag);
             tc_fence_after_sync();
             const uint32_t taddr = tmem + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(b * p.R);
-            if (ok && n_tokens > 0) {
-                uint32_t acc[32];
-                const int n_cols = min(p.R, p.outs - n0);
-                if (group * 32 < n_cols) tmem_load<32>(taddr + group * 32, acc);
-#pragma unroll 1
-                for (int c = group * 32; c < n_cols; c += 64) {
-                    tmem_loaded<32>(acc);
-                    stage_cols<32>(acc, stage, lane);
-                    if (c + 64 < n_cols) tmem_load<32>(taddr + c + 64, acc);
-                    store_cols<32>(p, t0, n_tokens, n0 + c, min(32, n_cols - c), sx, sw + c, stage, lane);
-                }
-            }
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) arrive_first(&ctrl->acc_empty[b]);
+            auto release = [&] {
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) arrive_first(&ctrl->acc_empty[b]);
+            };
+            if (ok && n_tokens > 0) store_tile(p, taddr, group, t0, n_tokens, n0, sx, sw, stage, lane, release);
+            else release();
         }
     }
     tc_fence_before_sync();
@@ -799,7 +866,8 @@ struct Tiling {
 // per ns (128 x 11008 x 4096, from L2), all of them together 6500 bytes of w per ns (from HBM); the four MMAs of a K block
 // cost their issuing warp 0.15 us however small they are (1 x 4096 x 4096 as 128 whole tiles 8.4 us, as 32 tiles in four
 // shares 6.5); exchanging partial sums costs 1.2 us and 1 ns per 40 bytes sent (77 x 5120 x 15360: whole tiles 15.8, halves
-// 17.2 us; 128 x 11008 x 4096: whole tiles 18.9, halves 15.6, quarters 13.4 us); a pair takes 1 us more to set up and gains
+// 17.2 us; 128 x 11008 x 4096: whole tiles 18.9, halves 15.6, quarters 13.4 us); an epilogue takes 6 ns per channel and
+// CTA (what is left of it when a call ends); a pair takes 1 us more to set up and gains
 // from a few hundred tokens on (160 x 4096 x 4096: 10.6 against 9.5 us, 300: 12.0 against 11.5, 1000: 17.1 against 20.5;
 // 4093 x 4096 x 22016: 219 against 301).  clusters[i]: clusters of 2^i CTAs that fit the device at once.
 Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&clusters)[4]) {
@@ -820,7 +888,7 @@ Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&cl
             const float sent_ns = c > 1 ? 1200.f + (float)(R * (c - 1) / c) * (float)x_rows * (4.f / 40.f) : 0.f;
             const float sm_ns = waves * (float)share * kb_ns;
             // the two overlap, but not quite: of tilings that HBM bounds, the one that leaves the SMs the most slack is best
-            const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + sent_ns;
+            const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + sent_ns + 6.f * R / c;
             if (ns < best_ns) { best_ns = ns; best = {R, c, 0}; }
         }
     }
@@ -830,7 +898,7 @@ Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&cl
             const long long tiles = (long long)ceil_div(p.rows, 256) * ceil_div(p.outs, R);
             const float waves = (float)((tiles + clusters[1] - 1) / clusters[1]);
             const float sm_ns = waves * (float)n_kb * fmaxf(fmaxf((float)(R / 2 + 128) * (kKb / 95.f), 2.f * R / 1.7f), 150.f);
-            const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + 1000.f;
+            const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + 1000.f + 6.f * R;
             if (ns < best_ns) { best_ns = ns; best = {R, 1, 1}; }
         }
     return best;
