@@ -221,6 +221,13 @@ __device__ __forceinline__ void store_cols(const LinearDev& p, long long t0, int
     __syncwarp();
 }
 
+// "The accumulator has been read": its loads have completed (tcgen05.wait::ld) before this is issued, and nothing else is handed
+// over.  A releasing arrive would wait for the output stores in flight as well (in a pair, whose barrier is a cluster away:
+// 4096 x 1024 x 8192 35.8 instead of 32.0 us).
+__device__ __forceinline__ void arrive_read(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 // The scales of a tile, fetched a tile ahead into registers and from there to the warp's copy in shared memory.
 struct TileScales {
     float w[8], x;
@@ -486,7 +493,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
             auto release = [&] {                                   // the accumulator may be overwritten as far as this warp goes
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ctrl->acc_empty[b]);
+                if (lane == 0) arrive_read(&ctrl->acc_empty[b]);
             };
             if (p.split == 1 && ok && busy) store_tile(p, taddr, group, t0, n_tokens, n0, sx, sw, stage, lane, release);
             else release();
@@ -542,8 +549,8 @@ __device__ __forceinline__ void tma_load_pair(void* smem_dst, const void* tmap, 
         ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(smem_u32(bar) & kFirstOfPair), "l"(policy)
         : "memory");
 }
-__device__ __forceinline__ void arrive_first(uint64_t* bar) {     // at the first CTA's barrier
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(smem_u32(bar) & kFirstOfPair) : "memory");
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {     // at the first CTA's barrier; relaxed as arrive_read
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(smem_u32(bar) & kFirstOfPair) : "memory");
 }
 
 __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, const __grid_constant__ CUtensorMap tm_x,
@@ -708,8 +715,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
 
 // ---------------------------------------------------------------------------------------------------------------------
 // The same product for very few tokens (one-token passes): there the tensor-core kernel above is a chain of latencies -- set-up,
-// copy, MMA, exchange, store -- around a copy of 2 to 3 us.  Here a block of eight warps takes one 8-row group of w; its warps
-// take the K blocks in turn, a lane one 16-byte piece of rows r and r + 4 per K block straight into registers, four-way
+// copy, MMA, exchange, store -- around a copy of 2 to 3 us.  Here a block of eight warps takes one 8-row group of w (several, if
+// there are fewer K blocks than warps); its warps take the K blocks in turn, a lane one 16-byte piece of rows r and r + 4 per K block straight into registers, four-way
 // products on the ordinary cores (dp4a), T times as many as there are tokens.
 // ---------------------------------------------------------------------------------------------------------------------
 struct FewDev {
@@ -718,6 +725,7 @@ struct FewDev {
     const float *sx, *sw;
     const uint8_t* w;
     int rows, cols, outs, n_kb;
+    int kw;                 // warps that share a group's K blocks: 1, 2, 4 or 8
     void* out;
     int out_f32;
     long long ldo;
@@ -736,23 +744,26 @@ template <int T> __global__ void __launch_bounds__(256) k_linear_i8_few(const Fe
     __shared__ int red[8][8][T];
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 7, r = lane >> 3;
-    const size_t kb_stride = (size_t)gridDim.x * 1024;
-    const uint8_t* const w0 = p.w + (size_t)blockIdx.x * 1024 + r * 128 + ((c ^ r) << 4);
-    const uint8_t* const w1 = p.w + (size_t)blockIdx.x * 1024 + (r + 4) * 128 + ((c ^ (r + 4)) << 4);
+    const int kw = p.kw, groups = 8 / kw, n8 = (p.outs + 7) / 8;
+    const int group = (int)blockIdx.x * groups + warp / kw, first = warp % kw;
+    const size_t kb_stride = (size_t)n8 * 1024;
+    const int n_kb = group < n8 ? p.n_kb : 0;
+    const uint8_t* const w0 = p.w + (size_t)group * 1024 + r * 128 + ((c ^ r) << 4);
+    const uint8_t* const w1 = p.w + (size_t)group * 1024 + (r + 4) * 128 + ((c ^ (r + 4)) << 4);
     // into L2 while the kernel in front finishes, as in k_linear_i8 (1 x 4096 x 4096, calls back to back: 4.2 -> 3.7 us)
     if (c == 0)
-        for (int u = 0; u < 4 && warp + 8 * u < p.n_kb; ++u) {
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(w0 + (warp + 8 * u) * kb_stride));
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(w1 + (warp + 8 * u) * kb_stride));
+        for (int u = 0; u < 4 && first + kw * u < n_kb; ++u) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(w0 + (first + kw * u) * kb_stride));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(w1 + (first + kw * u) * kb_stride));
         }
     pdl_wait();
     int acc[2][T] = {};
-    for (int kb = warp; kb < p.n_kb; kb += 8 * U) {
+    for (int kb = first; kb < n_kb; kb += kw * U) {
         int4 a[U][2], b[U][T];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int k = kb + 8 * u;
-            const bool in = k < p.n_kb;
+            const int k = kb + kw * u;
+            const bool in = k < n_kb;
             a[u][0] = in ? __ldcs(reinterpret_cast<const int4*>(w0 + k * kb_stride)) : make_int4(0, 0, 0, 0);
             a[u][1] = in ? __ldcs(reinterpret_cast<const int4*>(w1 + k * kb_stride)) : make_int4(0, 0, 0, 0);
 #pragma unroll
@@ -780,11 +791,10 @@ template <int T> __global__ void __launch_bounds__(256) k_linear_i8_few(const Fe
             if (c == 0) red[warp][r + 4 * h][t] = acc[h][t];
         }
     __syncthreads();
-    if (threadIdx.x < 8 * T) {
-        const int row = threadIdx.x & 7, t = threadIdx.x >> 3, n = (int)blockIdx.x * 8 + row;
+    if (threadIdx.x < 8 * T * groups) {       // consecutive threads: consecutive channels of one token
+        const int ch = threadIdx.x % (8 * groups), t = threadIdx.x / (8 * groups), n = (int)blockIdx.x * 8 * groups + ch;
         int sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += red[i][row][t];
+        for (int i = 0; i < kw; ++i) sum += red[(ch >> 3) * kw + i][ch & 7][t];
         if (t < p.rows && n < p.outs) {
             const float v = (float)sum * p.sx[t] * p.sw[n];
             if (p.out_f32) ((float*)p.out)[t * p.ldo + n] = v;
@@ -853,28 +863,24 @@ bool w_tensor_map(const I8Linear& p, int box_groups, CUtensorMap* out) {
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// When the kernel for few tokens is the faster one.  Measured, it against the tensor cores, us: one token 3.0 / 6.4 (4096 x
-// 4096), 7.9 / 10.7 (11008 x 4096), 15.0 / 16.1 (4096 x 22016), 15.3 / 14.2 (5120 x 15360); two tokens 4.5 / 6.5, 10.4 / 10.7,
-// 22.5 / 16.2, 21.5 / 14.2; four tokens 6.2 / 6.5, 14.5 / 10.8, 22.2 / 16.2; eight tokens of 4096 x 4096 9.8 / 6.4.
-bool linear_few(const I8Linear& p) { return p.rows == 1 || (p.rows <= 4 && (long long)p.outs * p.cols <= 1 << 24); }
-
 struct Tiling {
     int R, split, pair;
+    float ns;
 };
 
 // Channels per tile, CTAs per tile, or CTA pairs, by the time of the busiest SM.  Measured: an SM takes in 95 bytes of w and x
-// per ns (128 x 11008 x 4096, from L2), all of them together 6500 bytes of w per ns (from HBM); the four MMAs of a K block
-// cost their issuing warp 0.15 us however small they are (1 x 4096 x 4096 as 128 whole tiles 8.4 us, as 32 tiles in four
-// shares 6.5); exchanging partial sums costs 1.2 us and 1 ns per 40 bytes sent (77 x 5120 x 15360: whole tiles 15.8, halves
-// 17.2 us; 128 x 11008 x 4096: whole tiles 18.9, halves 15.6, quarters 13.4 us); an epilogue takes 6 ns per channel and
-// CTA (what is left of it when a call ends); a pair takes 1 us more to set up and gains
+// per ns (128 x 11008 x 4096, from L2), all of them together move 6500 bytes of w and out per ns (HBM); the four MMAs of a K
+// block cost their issuing warp 0.15 us however small they are (1 x 4096 x 4096 as 128 whole tiles 8.4 us, as 32 tiles in
+// four shares 6.5); exchanging partial sums costs 1.2 us and 1 ns per 40 bytes sent (77 x 5120 x 15360: whole tiles 15.8,
+// halves 17.2 us; 128 x 11008 x 4096: whole tiles 18.9, halves 15.6, quarters 13.4 us); a call ends 6 ns per channel of a tile
+// after its last sum; a tile cannot follow another in less than its epilogue takes (4096 x 128 x 8192: 32, 64, 128, 256
+// channels 67.9, 40.1, 30.3, 25.5 us, in pairs of 64, 128, 256 35.3, 28.4, 25.2); a pair takes 1 us more to set up and gains
 // from a few hundred tokens on (160 x 4096 x 4096: 10.6 against 9.5 us, 300: 12.0 against 11.5, 1000: 17.1 against 20.5;
 // 4093 x 4096 x 22016: 219 against 301).  clusters[i]: clusters of 2^i CTAs that fit the device at once.
 Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&clusters)[4]) {
     const int n_kb = ceil_div(p.cols, kKb);
-    const float hbm_ns = (float)p.outs * p.cols / 6500.f;
-    Tiling best = {256, 1, 0};
-    float best_ns = 1e30f;
+    const float hbm_ns = ((float)p.outs * p.cols + (float)p.rows * p.outs * (p.out_f32 ? 4 : 2)) / 6500.f;
+    Tiling best = {256, 1, 0, 1e30f};
     for (int i = 0; i < 4; ++i) {
         const int c = 1 << i;
         const int share = ceil_div(n_kb, c);
@@ -886,10 +892,11 @@ Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&cl
             const float waves = (float)((tiles + clusters[i] - 1) / clusters[i]);
             const float kb_ns = fmaxf((float)(R + x_rows) * (kKb / 95.f), 150.f);
             const float sent_ns = c > 1 ? 1200.f + (float)(R * (c - 1) / c) * (float)x_rows * (4.f / 40.f) : 0.f;
-            const float sm_ns = waves * (float)share * kb_ns;
+            const float tile_ns = (float)share * kb_ns;
+            const float sm_ns = tile_ns + (waves - 1.f) * fmaxf(tile_ns, 950.f + 10.5f * R);
             // the two overlap, but not quite: of tilings that HBM bounds, the one that leaves the SMs the most slack is best
             const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + sent_ns + 6.f * R / c;
-            if (ns < best_ns) { best_ns = ns; best = {R, c, 0}; }
+            if (ns < best.ns) best = {R, c, 0, ns};
         }
     }
     // CTA pairs on 256 tokens: half the channels to take in, and 2 R clocks of the tensor cores
@@ -897,11 +904,35 @@ Tiling linear_tiling(const I8Linear& p, int m_blocks, int x_rows, const int (&cl
         for (int R = 256; R >= 64; R -= 32) {
             const long long tiles = (long long)ceil_div(p.rows, 256) * ceil_div(p.outs, R);
             const float waves = (float)((tiles + clusters[1] - 1) / clusters[1]);
-            const float sm_ns = waves * (float)n_kb * fmaxf(fmaxf((float)(R / 2 + 128) * (kKb / 95.f), 2.f * R / 1.7f), 150.f);
+            const float tile_ns = (float)n_kb * fmaxf(fmaxf((float)(R / 2 + 128) * (kKb / 95.f), 2.f * R / 1.7f), 150.f);
+            const float sm_ns = tile_ns + (waves - 1.f) * fmaxf(tile_ns, 500.f + 12.f * R);
             const float ns = fmaxf(sm_ns, hbm_ns) + 0.25f * fminf(sm_ns, hbm_ns) + 1000.f + 6.f * R;
-            if (ns < best_ns) { best_ns = ns; best = {R, 1, 1}; }
+            if (ns < best.ns) best = {R, 1, 1, ns};
         }
     return best;
+}
+
+// The same for the kernel for few tokens; the tensor cores' kernels take 1.5 us more than linear_tiling counts.  A block
+// takes the time of its weights at 6500 bytes per ns for all blocks together, or of its instructions, about 2 ns.  Measured, it
+// against the tensor cores, us: one token 3.8 / 6.7 (4096 x 4096), 8.5 / 10.3 (11008 x 4096), 14.1 / 16.2 (4096 x 22016), 10.5 /
+// 8.0 (1024 x 32000), 26.6 / 11.9 (640 x 100000); two tokens 4.1 / 6.7, 8.6 / 10.4 (11008 x 4096), 10.0 / 10.3 (4096 x 12288);
+// four tokens 5.0 / 6.8, 10.5 / 10.3, 12.5 / 10.2.
+inline int few_warps(int n_kb) { return n_kb > 4 ? 8 : (n_kb > 2 ? 4 : n_kb); }     // that share a group's K blocks
+float few_ns(const I8Linear& p) {
+    if (p.rows > 4) return 1e30f;
+    const int n_kb = ceil_div(p.cols, kKb), groups = 8 / few_warps(n_kb);
+    const float blocks = (float)ceil_div(ceil_div(p.outs, 8), groups);
+    const float work = 1.8f + 0.25f * p.rows + (p.cols % 16 ? 1.5f * p.rows : 0.f);
+    const float bytes = (float)n_kb * groups * (1024.f / 6500.f) * (1.f + 0.13f * (p.rows - 1));
+    return 1500.f + blocks * fmaxf(work, bytes);
+}
+cudaError_t launch_few(const I8Linear& p, cudaStream_t st) {
+    const int n_kb = ceil_div(p.cols, kKb), kw = few_warps(n_kb);
+    const FewDev f = {p.x, p.ldx, p.sx, p.sw, (const uint8_t*)p.w, p.rows, p.cols, p.outs, n_kb, kw, p.out, p.out_f32, p.ldo};
+    const dim3 grid((unsigned)ceil_div(ceil_div(p.outs, 8), 8 / kw));
+    if (p.rows == 1) return launch_i8(k_linear_i8_few<1>, grid, dim3(256), 0, st, f);
+    if (p.rows == 2) return launch_i8(k_linear_i8_few<2>, grid, dim3(256), 0, st, f);
+    return launch_i8(k_linear_i8_few<4>, grid, dim3(256), 0, st, f);
 }
 
 template <typename... Maps>
@@ -967,13 +998,6 @@ cudaError_t launch_pack_weights_i8(const int8_t* src, long long ld, int rows, in
 }
 
 cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
-    if (linear_few(p)) {
-        const FewDev f = {p.x, p.ldx, p.sx, p.sw, (const uint8_t*)p.w, p.rows, p.cols, p.outs, ceil_div(p.cols, kKb), p.out, p.out_f32, p.ldo};
-        const dim3 grid((unsigned)ceil_div(p.outs, 8));
-        if (p.rows == 1) return launch_i8(k_linear_i8_few<1>, grid, dim3(256), 0, st, f);
-        if (p.rows == 2) return launch_i8(k_linear_i8_few<2>, grid, dim3(256), 0, st, f);
-        return launch_i8(k_linear_i8_few<4>, grid, dim3(256), 0, st, f);
-    }
     const int(*clusters)[4];
     cudaError_t e = linear_device(&clusters);
     if (e != cudaSuccess) return e;
@@ -982,6 +1006,7 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.m_blocks = ceil_div(p.rows, 128);
     d.x_rows = p.rows >= 128 ? 128 : ceil_div(p.rows, 8) * 8;
     const Tiling tiling = linear_tiling(p, d.m_blocks, d.x_rows, *clusters);
+    if (few_ns(p) < tiling.ns + 1500.f) return launch_few(p, st);
     d.R = tiling.R;
     d.split = tiling.split;
     d.kb_share = ceil_div(d.n_kb, d.split);
