@@ -774,6 +774,8 @@ int cats_verify_layer_i8(const cats_model_cfg* cfg, const cats_layer_weights_i8*
     a.hd = cfg->head_dim; a.kv_stride = D; a.scale = 1.0f / sqrtf((float)cfg->head_dim); a.out = ws.o;
     a.part_o = ws.attn_o; a.part_ml = ws.attn_ml; a.d_status = d_status;
     attn_plan(a);
+    // as in the 16-bit layer: the attention kernel leaves HBM idle and requests a share of the gate and up matrices into L2
+    a.warm[1] = warm_policy(1, w->w_gate_up, packed_weight_i8_bytes(2 * F, H));
     CATS_CUDA(launch_tree_attention(a, st));
     I8RowsDev r = {};                                       // attention output
     r.x = ws.o; r.ldx = D; r.rows = T; r.cols = D; r.q = ws.x; r.ldq = ws.ldx; r.scale = ws.scale;
