@@ -102,6 +102,33 @@ def test_same_bits_every_time_and_on_other_streams(cats):
     assert all(torch.equal(o, want) for o in outs) and int(st.item()) == 0
 
 
+def test_several_threads_at_once(cats):
+    """Four host threads, a stream each, different sizes (few tokens, whole tiles, clusters, pairs): each gets its own bits."""
+    import threading
+    jobs = []
+    for i, (rows, cols, outs) in enumerate([(1, 4096, 4096), (64, 1024, 4096), (64, 11008, 2048), (700, 2048, 4096)]):
+        x, w, sx, sw = _whole(rows, cols, 40 + i), _whole(outs, cols, 50 + i), _scales(rows, 60 + i), _scales(outs, 70 + i)
+        jobs.append((x, sx, cats.pack_weights_i8(w), sw, _run(cats, x, sx, w, sw, torch.float32).clone()))
+    wrong = []
+
+    def work(x, sx, packed, sw, want):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            outs, st = [torch.empty_like(want) for _ in range(20)], cats.new_status()
+            for o in outs:
+                cats.cats_linear_i8(x, sx, packed, sw, o, st)
+        stream.synchronize()
+        if int(st.item()) or not all(torch.equal(o, want) for o in outs):
+            wrong.append(tuple(want.shape))
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 def test_captured_and_replayed(cats):
     """norm -> product -> SwiGLU -> product -> norm in a graph, replayed on other inputs: the bits of the calls themselves."""
     T, H, F = 21, 512, 1376
