@@ -447,19 +447,25 @@ __global__ void __launch_bounds__(256) k_i8_qkv(const float* __restrict__ qkv, c
     }
 }
 
-constexpr int kMinRowsMany = 148 * 4;     // rows from which on throughput counts, not the latency of one row
+// Few vectors per thread make the shortest chain for a row, many keep more bytes in flight and fewer threads waiting: the
+// former while all rows are on the SMs at once.  Measured, one or two against four vectors, us: norm of 64 / 592 / 1024 / 8192 x
+// 4096 2.2 / 4.0 / 6.7 / 42.6 against 2.7 / 5.2 / 6.5 / 38.9; quantise 1.6 / 2.2 / 3.2 / 23.1 against 1.8 / 2.6 / 3.0 / 17.4; SwiGLU of
+// 64 / 148 / 300 / 8192 x 11008 2.5 / 2.7 / 6.3 / 124 against 3.0 / 2.9 / 5.3 / 67.6.
+inline bool rows_fit(const I8RowsDev& p, int threads) { return p.rows <= 148 * (2048 / threads); }
 
 template <int OP, typename TX, typename TD, bool GRID>
 cudaError_t launch_rows_v(const I8RowsDev& p, cudaStream_t st) {
     const int vecs = (p.cols + 7) / 8;              // vectors of a row
+    // up to 1024 columns a warp holds a row: no barrier (64 x 1000: 1.6 us)
     if (vecs <= 32 * 4) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, true, false>, dim3(((unsigned)p.rows + 3u) / 4u), dim3(128), 0, st, p);
     const dim3 grid((unsigned)p.rows);
-    auto threads = [&](int nv) { return dim3((unsigned)((vecs + nv * 32 - 1) / (nv * 32) * 32)); };
-    const bool many = p.rows >= kMinRowsMany;
-    if (vecs <= 1024 && !many) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, false>, grid, threads(1), 0, st, p);
-    // few rows: the shorter chain; off the grid also for many, where a thread holds twice the words until they are shifted
-    if (vecs <= 2 * row_threads<OP, 2>() && (!many || !GRID)) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 2, false, false>, grid, threads(2), 0, st, p);
-    if (vecs <= 2048) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, false, false>, grid, threads(4), 0, st, p);
+    auto threads = [&](int nv) { return (vecs + nv * 32 - 1) / (nv * 32) * 32; };
+    if (threads(1) <= row_threads<OP, 1>() && rows_fit(p, threads(1)))
+        return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, false>, grid, dim3(threads(1)), 0, st, p);
+    // off the grid also for many rows: a thread holds twice the words until they are shifted
+    if (threads(2) <= row_threads<OP, 2>() && (!GRID || rows_fit(p, threads(2))))
+        return launch_i8(k_i8_rows<OP, TX, TD, GRID, 2, false, false>, grid, dim3(threads(2)), 0, st, p);
+    if (threads(4) <= row_threads<OP, 4>()) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, false, false>, grid, dim3(threads(4)), 0, st, p);
     return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, true>, grid, dim3(512), 0, st, p);
 }
 
