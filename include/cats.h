@@ -352,7 +352,9 @@ int cats_tp_argmax_merge(const float *d_max, const int32_t *d_idx, int32_t n_sha
  * A row y of `cols` values is held as
  *     a = max(max_c |y[c]|, 2^-100),  q[c] = rint(127 y[c] / a) (ties to even),
  *     scale = a / 127,                so that y[c] ~ q[c] * scale;
- * y, a and the quotient are fp32.  A row with an infinity or a NaN gets a NaN
+ * y and a are fp32; the quotient is rounded once to fp32, so that an exact half
+ * is a tie.  (SwiGLU's, whose y is rounded several times before, is taken with
+ * fl(127 / a), 2^-24 of it off.)  A row with an infinity or a NaN gets a NaN
  * scale and zeros, and so makes NaN of whatever is computed from it.
  *
  * Matrices are row-major with a row stride (ld*) in ELEMENTS, at least cols;

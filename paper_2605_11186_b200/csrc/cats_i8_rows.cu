@@ -137,14 +137,27 @@ __device__ __forceinline__ void warp_store(uint16_t* row, int c0, int cols, floa
     __syncwarp();
 }
 
-// rint((y rs) inv) as bytes.  (y rs) inv and not y (rs inv): |y rs| <= a, so the result is finite and within
-// 127 (1 + 2^-23) whatever rs and a are.  The fused product and sum with 1.5 * 2^23 leaves the whole number (ties to even) in
-// the low bits of the result: the conversion instruction has a sixteenth of the FMA rate and shares its unit with ex2 and rcp.
+// rint(127 v / a) as bytes, v = y rs; |v| <= a, so the result is within 127 whatever rs and a are.
+// One bf16 element in a thousand is a tie, 127 v / a an exact half, and v fl(127 / a) puts it on either side of the half (one in 1900
+// elements a step off).  So the factor is kept in two parts, hi + lo = 127 / a to 2^-29 or better, and fma(v, hi, v lo) rounds the
+// quotient once: one that fp32 holds, a tie among them, is exact.  SwiGLU's values have several roundings behind them and
+// no exact ties: they take hi alone (4096 x 11008 and its values 56 us, with the second part 63).  Two instructions per element
+// more than hi alone: 22016 x 4096 bf16 and its values 82.6 -> 84.6 us, norm of 8191 x 4096 53.3 -> 53.7.
+// Rounding to a whole number: the sum with 1.5 * 2^23 leaves it (ties to even) in the low bits; the conversion instruction has
+// a sixteenth of the FMA rate and shares its unit with ex2 and rcp.
 constexpr float kRintMagic = 12582912.f;
-template <bool GRID, bool RS> __device__ __forceinline__ void store_q(int8_t* row, int c, int cols, bool vec, const float* y, float rs, float inv) {
+struct Factor { float hi, lo; };
+__device__ __forceinline__ Factor factor_127_over(float a) {
+    const float hi = 127.f / a;
+    return {hi, fmaf(-hi, a, 127.f) * (hi * (1.f / 127.f))};      // the remainder of the division, over a
+}
+template <int OP, bool GRID> __device__ __forceinline__ void store_q(int8_t* row, int c, int cols, bool vec, const float* y, float rs, const Factor& f) {
     uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(fmaf(RS ? y[i] * rs : y[i], inv, kRintMagic));
+    for (int i = 0; i < 8; ++i) {
+        const float v = OP == I8_NORM ? __fmul_rn(y[i], rs) : y[i];
+        w[i] = __float_as_uint(OP == I8_SWIGLU ? fmaf(v, f.hi, kRintMagic) : __fadd_rn(fmaf(v, f.hi, __fmul_rn(v, f.lo)), kRintMagic));
+    }
     if (GRID || (vec && c + 8 <= cols)) {
         uint32_t o[2];
 #pragma unroll
@@ -320,11 +333,12 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
     const bool finite = abs_bits(a) < 0x7F800000u;
     // 127 y / a: the norm's row factor is in both, so where a is the row's own maximum the quotient is taken without it, two
     // roundings fewer.  (Below 2^-90 the reciprocal could overflow.)
-    float inv = 127.f / fmaxf(a, kTinyMax);
+    float by = fmaxf(a, kTinyMax);
     if (OP == I8_NORM && a >= kTinyMax && __uint_as_float(mx) >= 8.077935669463161e-28f) {
-        inv = 127.f / __uint_as_float(mx);
+        by = __uint_as_float(mx);
         rs = 1.f;
     }
+    const Factor factor = factor_127_over(finite ? by : 1.f);
     a = fmaxf(a, kTinyMax);
     if (tid == 0) p.scale[row] = finite ? a / 127.f : __int_as_float(0x7FC00000);
     int8_t* const q = p.q + row * p.ldq;
@@ -334,7 +348,7 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
             const int c = (k * NT + tid) * 8;
             if (c < p.cols) {
                 if (!finite) zero(y[k], rs);
-                store_q<GRID, OP == I8_NORM>(q, c, p.cols, p.q_vec, y[k], rs, inv);
+                store_q<OP, GRID>(q, c, p.cols, p.q_vec, y[k], rs, factor);
             }
         }
     } else {
@@ -349,7 +363,7 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
             if (c < p.cols) {
                 in.values(y[0], ss);
                 if (!finite) zero(y[0], rs);
-                store_q<GRID, OP == I8_NORM>(q, c, p.cols, p.q_vec, y[0], rs, inv);
+                store_q<OP, GRID>(q, c, p.cols, p.q_vec, y[0], rs, factor);
             }
         }
     }
