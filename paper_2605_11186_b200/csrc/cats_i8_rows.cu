@@ -182,13 +182,32 @@ __device__ __forceinline__ float max_abs(float m, const float* y) {
     for (int i = 0; i < 8; i += 2) m = max_abs(m, y[i], y[i + 1]);
     return m;
 }
-// silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.  Flushing
-// forms of 2^x and 1/x: a quotient below 2^-126 is zero at any scale, and the others need twice the instructions.
-__device__ __forceinline__ float silu_mul(float g, float u) {
-    float e, r;
+// silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.  Flushing forms of
+// 2^x and 1/x, which need half the instructions: for gates from kFarGate up every intermediate is a normal number.
+constexpr float kFarGate = -80.f, kFarExp = 1.2089258196146292e24f;      // 2^80: below e^80, so that no gate below kFarGate is missed
+constexpr uint32_t kFarMark = 0x80000000u;
+__device__ __forceinline__ float silu_mul(float g, float u, float& e) {
+    float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return g * r * u;
+}
+// The same below kFarGate, where 1 + e^-g is e^-g and its reciprocal leaves the fp32 range (at -87) before the product with a large up
+// value does: e^g as the square of h = e^(g/2), one factor for g and one for u.  h is zero below -175, where no up value
+// brings the product to the 2^-108 that half a step of the smallest scale is.
+__device__ __forceinline__ float silu_mul_far(float g, float u) {
+    float h;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(h) : "f"(g * 0.72134752044448170f));
+    return (g * h) * (h * u);
+}
+// The largest of the row's threads' values, to all of them; for a block's row the barrier in front of the first write to red_m is here
+template <bool WARP> __device__ __forceinline__ uint32_t row_max(uint32_t m, int tid, int NT, uint32_t* red_m) {
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (WARP) return m;
+    __syncthreads();
+    if ((tid & 31) == 0) red_m[tid >> 5] = m;
+    __syncthreads();
+    return __reduce_max_sync(0xffffffffu, (tid & 31) < (NT >> 5) ? red_m[tid & 31] : 0u);
 }
 
 struct NoDelta {};        // the norm without a delta
@@ -228,21 +247,34 @@ template <int OP, typename TX, typename TD, bool GRID> struct RowVec {
             for (int i = 0; i < 8; ++i) y[i] += t[i];
         }
     }
-    __device__ __forceinline__ void values(float* y, float& ss) const {
+    // acc: SWIGLU: the largest e^-gate so far (or NaN); the norm: the sum of squares so far
+    __device__ __forceinline__ void values(float* y, float& acc) const {
         if (OP == I8_NORM) {
             float t[8];
             g.get(t);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                ss = fmaf(y[i], y[i], ss);
+                acc = fmaf(y[i], y[i], acc);
                 y[i] *= t[i];
             }
         } else if (OP == I8_SWIGLU) {
             float u[8];
             d.get(u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = silu_mul(y[i], u[i]);
+            for (int i = 0; i < 8; i += 2) {
+                float e0, e1;
+                y[i] = silu_mul(y[i], u[i], e0);
+                y[i + 1] = silu_mul(y[i + 1], u[i + 1], e1);
+                acc = max_abs(acc, e0, e1);
+            }
         }
+    }
+    // SWIGLU's values in a vector that has, or may have, gates below kFarGate; y: as sum() leaves it
+    __device__ __forceinline__ void far_values(float* y) const {
+        float u[8], e;
+        d.get(u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = y[i] < kFarGate ? silu_mul_far(y[i], u[i]) : silu_mul(y[i], u[i], e);
     }
 };
 // The norm's sums to the residual stream: in place and without a delta they are there already.
@@ -259,6 +291,34 @@ __device__ __forceinline__ void zero(float* y, float& rs) {      // a row that i
     for (int i = 0; i < 8; ++i) y[i] = 0.f;
 }
 
+// A row of SwiGLU with gates below kFarGate, by all threads that hold it.  They are rare: the row is read again, twice, a vector at a
+// time, in a function of its own.  The pass over 4096 x 11008 and its values went from 56 to 60.5 us with this, to 64 with the choice
+// per element inside values(), and to 70 with a second try over the vectors in registers, which leaves two blocks per SM of three.
+template <typename TX, bool GRID, bool WARP>
+__device__ __noinline__ void far_row(const I8RowsDev& p, long long row, int tid, int NT, uint32_t* red_m) {
+    RowVec<I8_SWIGLU, TX, TX, GRID> in;
+    float y[8], am = 0.f;
+    for (int c = tid * 8; c < p.cols; c += NT * 8) {
+        in.load(p, row, c);
+        in.sum(y);
+        in.far_values(y);
+        am = max_abs(am, y);
+    }
+    const uint32_t mx = row_max<WARP>(abs_bits(am), tid, NT, red_m);
+    const float a = fmaxf(__uint_as_float(mx), kTinyMax);
+    const bool finite = mx < 0x7F800000u;
+    const Factor factor = factor_127_over(finite ? a : 1.f);
+    if (tid == 0) p.scale[row] = finite ? a / 127.f : __int_as_float(0x7FC00000);
+    for (int c = tid * 8; c < p.cols; c += NT * 8) {
+        in.load(p, row, c);
+        in.sum(y);
+        in.far_values(y);
+        float rs;
+        if (!finite) zero(y, rs);
+        store_q<I8_SWIGLU, GRID>(p.q + row * p.ldq, c, p.cols, p.q_vec, y, 1.f, factor);
+    }
+}
+
 // Largest block: what fits the 64 registers of 1024 threads is one vector, or two of a single input (the norm has three).
 template <int OP, int NV> __host__ __device__ constexpr int row_threads() { return NV == 1 || (NV == 2 && OP != I8_NORM) ? 1024 : 512; }
 
@@ -266,7 +326,7 @@ template <int OP, int NV> __host__ __device__ constexpr int row_threads() { retu
 // registers.  LONG: any length, the row is read twice.  WARP: blocks of 128 threads hold four rows, one per warp, and need
 // no barrier.
 template <int OP, typename TX, typename TD, bool GRID, int NV, bool WARP, bool LONG>
-__global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(const I8RowsDev p) {
+__global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(const __grid_constant__ I8RowsDev p) {
     __shared__ float red_s[32];
     __shared__ uint32_t red_m[32];
     __shared__ __align__(16) float stage_s[OP == I8_NORM && !GRID ? (WARP ? 4 : row_threads<OP, NV>() / 32) * 256 : 4];      // a staging tile per warp
@@ -279,7 +339,7 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
     pdl_wait();
     if (WARP && row >= p.rows) return;
     float y[NV][8];
-    float ss = 0.f;
+    float ss = 0.f;                 // the norm: sum of squares; SwiGLU: the largest e^-gate
     float am = 0.f;                 // max |y| of this thread, NaN if any is
     if (!LONG) {
         RowVec<OP, TX, TD, GRID> in[NV];
@@ -303,11 +363,15 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
             RowVec<OP, TX, TD, GRID> in;
             in.load(p, row, c);
             in.sum(y[0]);
-            in.values(y[0], ss);
+            if (OP == I8_SWIGLU) in.far_values(y[0]);
+            else in.values(y[0], ss);
             am = max_abs(am, y[0]);
         }
     }
-    uint32_t mx = __reduce_max_sync(0xffffffffu, abs_bits(am));      // the bits of non-negative values are in their order, NaN on top
+    // the bits of non-negative values are in their order, NaN on top, and above them the mark of a row with gates below kFarGate
+    uint32_t mx = abs_bits(am);
+    if (OP == I8_SWIGLU && !LONG && !(ss < kFarExp)) mx = kFarMark;
+    mx = __reduce_max_sync(0xffffffffu, mx);
     if (OP == I8_NORM) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
@@ -327,6 +391,7 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
             for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         }
     }
+    if (OP == I8_SWIGLU && !LONG && mx == kFarMark) return far_row<TX, GRID, WARP>(p, row, tid, NT, red_m);
     float rs = 1.f;
     if (OP == I8_NORM) rs = __frsqrt_rn(ss / (float)p.cols + p.eps);
     float a = __uint_as_float(mx) * rs;
@@ -361,7 +426,8 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
             }
             if (OP == I8_NORM) store_resid<TX, TD, GRID>(p, row, c, c0, stage, lane, y[0]);
             if (c < p.cols) {
-                in.values(y[0], ss);
+                if (OP == I8_SWIGLU) in.far_values(y[0]);
+                else in.values(y[0], ss);
                 if (!finite) zero(y[0], rs);
                 store_q<OP, GRID>(q, c, p.cols, p.q_vec, y[0], rs, factor);
             }
