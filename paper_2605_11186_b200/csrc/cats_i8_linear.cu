@@ -233,8 +233,8 @@ struct TileScales {
     float w[8], x;
     __device__ __forceinline__ void fetch(const LinearDev& p, int n0, long long t0, int lane) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = lane + 32 * j < p.R && n0 + lane + 32 * j < p.outs ? __ldg(p.sw + n0 + lane + 32 * j) : 0.f;
-        x = t0 + lane < p.rows ? __ldg(p.sx + t0 + lane) : 0.f;
+        for (int j = 0; j < 8; ++j) w[j] = lane + 32 * j < p.R && n0 + lane + 32 * j < p.outs ? __ldcg(p.sw + n0 + lane + 32 * j) : 0.f;
+        x = t0 + lane < p.rows ? __ldcg(p.sx + t0 + lane) : 0.f;
     }
     __device__ __forceinline__ void put(float* sw, float* sx, int lane) const {
         __syncwarp();

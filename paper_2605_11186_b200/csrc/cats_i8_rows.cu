@@ -75,7 +75,7 @@ template <> struct Raw<uint16_t> {     // bf16 bits
         for (int i = 0; i < 4; ++i) w[i] = word_of(a, i);
     }
     __device__ __forceinline__ void load(const uint16_t* p) { put(__ldcs(reinterpret_cast<const uint4*>(p))); }
-    __device__ __forceinline__ void load_shared(const uint16_t* p) { put(__ldg(reinterpret_cast<const uint4*>(p))); }      // by all rows
+    __device__ __forceinline__ void load_shared(const uint16_t* p) { put(*reinterpret_cast<const uint4*>(p)); }      // by all rows
     __device__ __forceinline__ void load_any(const uint16_t* row, int c, int cols) {
         const int m = (int)((uintptr_t)row & 15);
         if (m == 0 && c + 8 <= cols) return load(row + c);
@@ -435,53 +435,67 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
     }
 }
 
-// q * scale, rounded to bf16 or as fp32.  One block per (row, 4096 columns), eight elements per thread and step.  The second
-// kernel is for rows off the grid and ragged ends; q_vec says whether rows of q start on 8 bytes.
+// q * scale, rounded to bf16 or as fp32.  One block per (row, 4096 columns), eight elements per thread and step, both steps loaded
+// before the first is stored.  The second kernel is for rows off the grid and ragged ends; q_vec says whether rows of q start on
+// 8 bytes.  q and scale come from the kernel in front, which may still run when this one starts: no read-only loads (__ldg, const
+// __restrict__), here and wherever a kernel of this path waits for the one in front.
 __device__ __forceinline__ void eight_values(const uint2& w, float s, float* v) {
     // a byte b as the float 2^23 + (b + 128), then minus 2^23 + 128: exact, and no conversion instruction
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         v[i] = (__uint_as_float(__byte_perm((i < 4 ? w.x : w.y) ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s;
 }
-__global__ void __launch_bounds__(256) k_i8_dequantize(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale,
-                                                       int cols, void* __restrict__ out, int out_f32, long long ldo) {
+__global__ void __launch_bounds__(256) k_i8_dequantize(const int8_t* q, long long ldq, const float* scale, int cols, void* out, int out_f32,
+                                                       long long ldo) {
     pdl_launch_dependents();
     pdl_wait();
     const long long row = blockIdx.x;
-    const float s = __ldg(scale + row);
-    const int c_end = min(cols, ((int)blockIdx.y + 1) * 4096);
-#pragma unroll 2
-    for (int c = blockIdx.y * 4096 + threadIdx.x * 8; c < c_end; c += 2048) {
+    const float s = scale[row];
+    const int c_end = min(cols, ((int)blockIdx.y + 1) * 4096), c0 = blockIdx.y * 4096 + threadIdx.x * 8;
+    uint2 w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (c0 + k * 2048 < c_end) w[k] = __ldcg(reinterpret_cast<const uint2*>(q + row * ldq + c0 + k * 2048));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = c0 + k * 2048;
+        if (c >= c_end) break;
         float v[8];
-        eight_values(__ldg(reinterpret_cast<const uint2*>(q + row * ldq + c)), s, v);
+        eight_values(w[k], s, v);
         if (out_f32) store_vec((float*)out + row * ldo + c, v);
         else store_vec((uint16_t*)out + row * ldo + c, v);
     }
 }
-__global__ void __launch_bounds__(256) k_i8_dequantize_any(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale,
-                                                           int cols, int q_vec, void* __restrict__ out, int out_f32, long long ldo) {
+__global__ void __launch_bounds__(256) k_i8_dequantize_any(const int8_t* q, long long ldq, const float* scale, int cols, int q_vec, void* out,
+                                                           int out_f32, long long ldo) {
     __shared__ __align__(16) float stage_s[8 * 256];
     pdl_launch_dependents();
     pdl_wait();
     const long long row = blockIdx.x;
     const int lane = threadIdx.x & 31;
     float* const stage = stage_s + (threadIdx.x >> 5) * 256;
-    const float s = __ldg(scale + row);
+    const float s = scale[row];
     const int8_t* const qr = q + row * ldq;
-    const int c_end = min(cols, ((int)blockIdx.y + 1) * 4096);
-#pragma unroll 2
-    for (int c0 = blockIdx.y * 4096 + (threadIdx.x - lane) * 8; c0 < c_end; c0 += 2048) {
-        const int c = c0 + lane * 8;
-        uint2 w = make_uint2(0, 0);
+    const int c_end = min(cols, ((int)blockIdx.y + 1) * 4096), c_warp = blockIdx.y * 4096 + (threadIdx.x - lane) * 8;
+    uint2 w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = c_warp + k * 2048 + lane * 8;
+        w[k] = make_uint2(0, 0);
         if (q_vec && c + 8 <= c_end) {
-            w = __ldg(reinterpret_cast<const uint2*>(qr + c));
+            w[k] = __ldcg(reinterpret_cast<const uint2*>(qr + c));
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (c + i < c_end) (i < 4 ? w.x : w.y) |= (uint32_t)(uint8_t)__ldg(qr + c + i) << (8 * (i & 3));
+                if (c + i < c_end) (i < 4 ? w[k].x : w[k].y) |= (uint32_t)(uint8_t)qr[c + i] << (8 * (i & 3));
         }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c0 = c_warp + k * 2048;
+        if (c0 >= c_end) break;
         float v[8];
-        eight_values(w, s, v);
+        eight_values(w[k], s, v);
         if (out_f32) warp_store((float*)out + row * ldo, c0, c_end, stage, lane, v);
         else warp_store((uint16_t*)out + row * ldo, c0, c_end, stage, lane, v);
     }
@@ -492,9 +506,8 @@ __global__ void __launch_bounds__(256) k_i8_dequantize_any(const int8_t* __restr
 // nothing; every value is rounded once, from the unrounded sums).  Grid (nodes, shares of the heads); a thread takes four
 // pairs of q, k and v.  The angles need only pos, which was there before the call: they are computed before the wait for
 // the projection (the fp64 sine is what would take longest here).
-__global__ void __launch_bounds__(256) k_i8_qkv(const float* __restrict__ qkv, const int32_t* __restrict__ pos, int nh, int hd,
-                                                float rope_base, int prefix_len, uint16_t* __restrict__ q, uint16_t* __restrict__ kc,
-                                                uint16_t* __restrict__ vc) {
+__global__ void __launch_bounds__(256) k_i8_qkv(const float* qkv, const int32_t* pos, int nh, int hd, float rope_base, int prefix_len,
+                                                uint16_t* q, uint16_t* kc, uint16_t* vc) {
     __shared__ __align__(16) float cos_s[64], sin_s[64];
     pdl_launch_dependents();
     const int t = blockIdx.x, half = hd / 2, D = nh * hd;
