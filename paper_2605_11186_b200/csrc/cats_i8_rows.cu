@@ -326,7 +326,7 @@ template <int OP, int NV> __host__ __device__ constexpr int row_threads() { retu
 // registers.  LONG: any length, the row is read twice.  WARP: blocks of 128 threads hold four rows, one per warp, and need
 // no barrier.
 template <int OP, typename TX, typename TD, bool GRID, int NV, bool WARP, bool LONG>
-__global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(const __grid_constant__ I8RowsDev p) {
+__device__ __forceinline__ void i8_rows(const I8RowsDev& p) {
     __shared__ float red_s[32];
     __shared__ uint32_t red_m[32];
     __shared__ __align__(16) float stage_s[OP == I8_NORM && !GRID ? (WARP ? 4 : row_threads<OP, NV>() / 32) * 256 : 4];      // a staging tile per warp
@@ -433,6 +433,20 @@ __global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(
             }
         }
     }
+}
+
+// SwiGLU's parameters stay where the launch put them, for far_row to read; with __grid_constant__ the others are slower (quantise
+// 22016 x 4096 and its values 90.5 instead of 84.6 us).
+template <int OP, typename TX, typename TD, bool GRID, int NV, bool WARP, bool LONG>
+__global__ void __launch_bounds__(WARP ? 128 : row_threads<OP, NV>()) k_i8_rows(const I8RowsDev p) { i8_rows<OP, TX, TD, GRID, NV, WARP, LONG>(p); }
+template <typename TX, bool GRID, int NV, bool WARP, bool LONG>
+__global__ void __launch_bounds__(WARP ? 128 : row_threads<I8_SWIGLU, NV>()) k_i8_swiglu_rows(const __grid_constant__ I8RowsDev p) {
+    i8_rows<I8_SWIGLU, TX, TX, GRID, NV, WARP, LONG>(p);
+}
+template <int OP, typename TX, typename TD, bool GRID, int NV, bool WARP, bool LONG>
+cudaError_t launch_rows_k(dim3 grid, int threads, cudaStream_t st, const I8RowsDev& p) {
+    if constexpr (OP == I8_SWIGLU) return launch_i8(k_i8_swiglu_rows<TX, GRID, NV, WARP, LONG>, grid, dim3(threads), 0, st, p);
+    else return launch_i8(k_i8_rows<OP, TX, TD, GRID, NV, WARP, LONG>, grid, dim3(threads), 0, st, p);
 }
 
 // q * scale, rounded to bf16 or as fp32.  One block per (row, 4096 columns), eight elements per thread and step, both steps loaded
@@ -550,16 +564,16 @@ template <int OP, typename TX, typename TD, bool GRID>
 cudaError_t launch_rows_v(const I8RowsDev& p, cudaStream_t st) {
     const int vecs = (p.cols + 7) / 8;              // vectors of a row
     // up to 1024 columns a warp holds a row: no barrier (64 x 1000: 1.6 us)
-    if (vecs <= 32 * 4) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, true, false>, dim3(((unsigned)p.rows + 3u) / 4u), dim3(128), 0, st, p);
+    if (vecs <= 32 * 4) return launch_rows_k<OP, TX, TD, GRID, 4, true, false>(dim3(((unsigned)p.rows + 3u) / 4u), 128, st, p);
     const dim3 grid((unsigned)p.rows);
     auto threads = [&](int nv) { return (vecs + nv * 32 - 1) / (nv * 32) * 32; };
     if (threads(1) <= row_threads<OP, 1>() && rows_fit(p, threads(1)))
-        return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, false>, grid, dim3(threads(1)), 0, st, p);
+        return launch_rows_k<OP, TX, TD, GRID, 1, false, false>(grid, threads(1), st, p);
     // off the grid also for many rows: a thread holds twice the words until they are shifted
     if (threads(2) <= row_threads<OP, 2>() && (!GRID || rows_fit(p, threads(2))))
-        return launch_i8(k_i8_rows<OP, TX, TD, GRID, 2, false, false>, grid, dim3(threads(2)), 0, st, p);
-    if (threads(4) <= row_threads<OP, 4>()) return launch_i8(k_i8_rows<OP, TX, TD, GRID, 4, false, false>, grid, dim3(threads(4)), 0, st, p);
-    return launch_i8(k_i8_rows<OP, TX, TD, GRID, 1, false, true>, grid, dim3(512), 0, st, p);
+        return launch_rows_k<OP, TX, TD, GRID, 2, false, false>(grid, threads(2), st, p);
+    if (threads(4) <= row_threads<OP, 4>()) return launch_rows_k<OP, TX, TD, GRID, 4, false, false>(grid, threads(4), st, p);
+    return launch_rows_k<OP, TX, TD, GRID, 1, false, true>(grid, 512, st, p);
 }
 
 template <int OP, typename TX, typename TD>
