@@ -50,7 +50,9 @@ int cats_debug_wait_limit_ns(unsigned long long ns);
  *   2 tcgen05 attention kernel: the loader announces the query tile on its
  *     barrier but never copies it;
  *   3 8-bit product (the kernels on the tensor cores): the last copy of x is
- *     announced on its barrier but never made.
+ *     announced on its barrier but never made;
+ *   4 the same kernels: the warps that issue the MMAs give up in place of their
+ *     first wait, while the copies are on their way as usual.
  * Set a short wait limit first, or each expiry takes a second. */
 void cats_debug_inject_fault(int which);
 

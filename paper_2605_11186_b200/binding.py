@@ -204,7 +204,7 @@ def wait_limit_ns(ns: int) -> None:
 
 def inject_fault(which: int) -> None:
     """cats_debug_inject_fault: 0 none, 1 a projection's contributors keep their ready flags, 2 the attention loader
-    never copies Q, 3 the 8-bit product's last copy of x is never made."""
+    never copies Q, 3 the 8-bit product's last copy of x is never made, 4 its MMA warps give up at once."""
     lib.cats_debug_inject_fault(C.c_int(which))
 
 

@@ -268,7 +268,7 @@ int cats_debug_timeline(int kernel, void* host, size_t bytes) {
     if (e == cudaErrorNotSupported) return CATS_ERR_UNSUPPORTED;
     return e == cudaSuccess ? CATS_OK : (e == cudaErrorInvalidValue ? CATS_ERR_INVALID_ARG : CATS_ERR_CUDA);
 }
-void cats_debug_inject_fault(int which) { g_debug_fault = which >= 1 && which <= 3 ? which : 0; }
+void cats_debug_inject_fault(int which) { g_debug_fault = which >= 1 && which <= 4 ? which : 0; }
 int cats_debug_wait_limit_ns(unsigned long long ns) {
     if (ns == 0) ns = kWaitLimitNs;
     if (set_wait_limit_gemm(ns) != cudaSuccess || set_wait_limit_attn(ns) != cudaSuccess || set_wait_limit_small(ns) != cudaSuccess ||

@@ -17,7 +17,7 @@
 // shared memory: the accumulator's 16-channel groups are dealt out to the CTAs, every CTA stores its int32 partial of a group
 // into the memory of the group's owner (each sender has its own place there), one cluster barrier publishes them, and the
 // owners add and store.  Whole numbers: the order of the sums does not matter, and nothing is left in global memory.
-// Every wait is bounded; on expiry the CTA reports CATS_ERR_TIMEOUT, lets its copies land, frees its TMEM and returns.
+// Every wait is bounded; on expiry the CTA reports CATS_ERR_TIMEOUT, lets its copies land and its MMAs end, frees its TMEM and returns.
 #include <cuda.h>
 
 #include <mutex>
@@ -57,6 +57,7 @@ struct LinearDev {
     long long ldo;
     int w_early;            // w may be read before the kernel in front has finished
     int drop_x;             // fault injection: the x copy of a CTA's last stage is announced but never made
+    int give_up;            // fault injection: the MMA warp raises the abort flag in place of its first wait
     int32_t* d_status;
 };
 
@@ -64,6 +65,7 @@ struct Ctrl {
     uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
     uint32_t tmem_base;
     int abort_flag;
+    int issued[4], segs;      // after an abort: stages issued by each copying warp (a pair: of both CTAs), accumulators committed
 };
 static_assert(sizeof(Ctrl) <= kCtrl, "control block too large");
 
@@ -119,6 +121,9 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t local_smem, int rank) 
 }
 __device__ __forceinline__ void st_cluster_v4(uint32_t addr, const uint32_t* v) {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -228,6 +233,32 @@ __device__ __forceinline__ void arrive_read(uint64_t* bar) {
     asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// After an abort: what is still in flight into this CTA's memories ends before the CTA goes away.  By all threads, when none of them
+// waits on a barrier of the pipeline any more, so that nothing is issued after this.  Copies: the stages issued last, at most S of them,
+// are waited for on their barriers.  A copying warp that gave up before the other one arrives in its place, without bytes
+// (it is less than S stages behind: the other one's stage j needed stage j - S whole).  MMAs: the last commit.  The limit is for
+// what never comes, such as a withheld copy; copies and MMAs take microseconds.
+constexpr unsigned long long kDrainNs = 10000000ull;
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, unsigned long long t0) {
+    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - t0 < kDrainNs) {}
+}
+__device__ __noinline__ void drain(Ctrl* ctrl, int S, int issued, int segs) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned long long t0 = globaltimer_ns();
+    if (warp <= 1 && lane == 0) ctrl->issued[warp] = issued;
+    __syncthreads();
+    if (warp <= 1) {
+        const int last = max(ctrl->issued[0], ctrl->issued[1]);
+        if (lane == 0)
+            for (int j = issued; j < last; ++j) mbar_arrive(&ctrl->full[j % S]);
+        __syncwarp();
+        for (int j = max(0, last - S); j < last; ++j) drain_wait(&ctrl->full[j % S], (j / S) & 1, t0);
+    } else if (warp == 2 && segs > 0) {
+        drain_wait(&ctrl->acc_full[(segs - 1) & 1], ((segs - 1) >> 1) & 1, t0);
+    }
+    __syncthreads();
+}
+
 // The scales of a tile, fetched a tile ahead into registers and from there to the warp's copy in shared memory.
 struct TileScales {
     float w[8], x;
@@ -305,6 +336,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = ctrl->tmem_base;
+    int issued = 0, segs = 0;                 // stages issued by this copying warp; tiles whose accumulator the MMA warp has committed
     if (p.split > 1) cluster_arrive();        // waited for before the first store into a peer: every CTA of the cluster has started
     pdl_launch_dependents();
     // stage layout: unit chunks of w, then unit chunks of x.  All lanes of a role's warp run its loop and one of them issues:
@@ -317,7 +349,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
         // x comes from the kernel before; w does not where this launch follows others of the same call: the ring is filled with
         // it at once.  No clock of a bounded wait starts before the kernel in front has finished.
         if (!is_w || !p.w_early) pdl_wait();
-        int s = 0, issued = 0;
+        int s = 0;
         uint32_t par = 1;
         bool ok = true;
         for (int tile = first; tile < p.n_tiles && ok; tile += G) {
@@ -346,19 +378,16 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
                 if (++u == n_units) u = 0;
             }
         }
-        if (*abort_flag) {                    // let the copies in flight land before the CTA goes away
-            volatile int ignore = 0;
-            for (int j = max(0, issued - S); j < issued; ++j) mbar_wait(&ctrl->full[j % S], (j / S) & 1, &ignore);
-        }
     } else if (warp == 2) {
         pdl_wait();
         const uint32_t idesc = idesc_i8_m128(p.R);
-        int s = 0, seg = 0;
+        int s = 0;
         uint32_t par = 0;
-        bool ok = true;
-        for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
-            const int b = seg & 1;
-            if (seg >= 2) ok = warp_wait(&ctrl->acc_empty[b], ((seg >> 1) - 1) & 1, abort_flag);
+        bool ok = !p.give_up;
+        if (!ok) *abort_flag = 1;
+        for (int tile = first; tile < p.n_tiles && ok; tile += G, ++segs) {
+            const int b = segs & 1;
+            if (segs >= 2) ok = warp_wait(&ctrl->acc_empty[b], ((segs >> 1) - 1) & 1, abort_flag);
             tc_fence_after_sync();
             const uint32_t d = tmem + (uint32_t)(b * p.R);
             uint32_t more = 0;                // the first MMA of a tile overwrites the accumulator
@@ -507,6 +536,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
     }
     tc_fence_before_sync();
     __syncthreads();
+    if (*abort_flag) drain(ctrl, S, issued, segs);      // whoever raised the flag did so before this barrier
     if (warp == 2) {
         __syncwarp();
         tc_fence_after_sync();
@@ -553,6 +583,47 @@ __device__ __forceinline__ void arrive_first(uint64_t* bar) {     // at the firs
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(smem_u32(bar) & kFirstOfPair) : "memory");
 }
 
+__device__ __forceinline__ void mbar_complete_tx(uint64_t* bar, uint32_t bytes) {      // as if a copy of so many bytes had landed
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+// As drain, for a pair.  The barriers of all copies are the first CTA's, whose two copying warps announce both CTAs' bytes.  They
+// make up for stages that not all four copying warps came to issue: an arrival with the bytes that the other CTA
+// did ask for, or the bytes that it did not ask for.  (All four have issued whatever stage was consumed, so again less than S stages.)
+__device__ __noinline__ void drain_pair(Ctrl* ctrl, int S, int rank, int issued, int segs, uint32_t w_chunk, uint32_t x_chunk) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned long long t0 = globaltimer_ns();
+    if (lane == 0 && warp <= 1) st_cluster(cluster_addr(smem_u32(&ctrl->issued[2 * rank + warp]), 0), (uint32_t)issued);
+    if (lane == 0 && warp == 2 && rank == 0)
+        for (int r = 0; r < 2; ++r) st_cluster(cluster_addr(smem_u32(&ctrl->segs), r), (uint32_t)segs);
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    if (rank == 0 && warp <= 1) {
+        const volatile int* const n = ctrl->issued;
+        const int peer = n[2 + warp], last = max(max(n[0], n[1]), max(n[2], n[3]));
+        const uint32_t chunk = warp == 0 ? w_chunk : x_chunk;
+        if (lane == 0)
+            for (int j = max(0, last - S); j < last; ++j) {
+                uint64_t* const bar = &ctrl->full[j % S];
+                if (j < issued) {
+                    if (j >= peer) mbar_complete_tx(bar, chunk);
+                } else if (j < peer) {
+                    mbar_expect_tx(bar, chunk);
+                } else {
+                    mbar_arrive(bar);
+                }
+            }
+        __syncwarp();
+        for (int j = max(0, last - S); j < last; ++j) drain_wait(&ctrl->full[j % S], (j / S) & 1, t0);
+    } else if (warp == 2) {                   // commits arrive at both CTAs
+        segs = *(const volatile int*)&ctrl->segs;
+        if (segs > 0) drain_wait(&ctrl->acc_full[(segs - 1) & 1], ((segs - 1) >> 1) & 1, t0);
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+}
+
 __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, const __grid_constant__ CUtensorMap tm_x,
                                                              const __grid_constant__ CUtensorMap tm_w) {
     extern __shared__ __align__(1024) uint8_t smem[];      // [stages][128 tokens, R / 2 channels], staging tiles, scales, control block
@@ -594,11 +665,12 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
     pdl_launch_dependents();
     const int S = p.stages, G = (int)gridDim.x / 2, first = (int)cluster_id();
     const int n8 = (p.outs + 7) / 8;
+    int issued = 0, segs = 0;                 // as in k_linear_i8
     if (warp <= 1) {
         const bool is_w = warp == 0;
         const uint64_t pol = l2_policy_evict_last();
         if (!is_w || !p.w_early) pdl_wait();
-        int s = 0, issued = 0;
+        int s = 0;
         uint32_t par = 1;
         bool ok = true;
         for (int tile = first; tile < p.n_tiles && ok; tile += G) {
@@ -622,23 +694,17 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
                 if (++s == S) { s = 0; par ^= 1u; }
             }
         }
-        if (*abort_flag) {                    // let the copies in flight land before the CTA goes away
-            volatile int ignore = 0;
-            if (rank == 0)
-                for (int j = max(0, issued - S); j < issued; ++j) mbar_wait(&ctrl->full[j % S], (j / S) & 1, &ignore);
-            // the second CTA's copies count on barriers that it cannot wait for: a thousand times a copy's latency instead
-            for (const unsigned long long t0 = globaltimer_ns(); globaltimer_ns() - t0 < 1000000ull;) {}
-        }
     } else if (warp == 2) {
         if (rank == 0) {
             pdl_wait();
             const uint32_t idesc = idesc_i8_m256(p.R);
-            int s = 0, seg = 0;
+            int s = 0;
             uint32_t par = 0;
-            bool ok = true;
-            for (int tile = first; tile < p.n_tiles && ok; tile += G, ++seg) {
-                const int b = seg & 1;
-                if (seg >= 2) ok = warp_wait(&ctrl->acc_empty[b], ((seg >> 1) - 1) & 1, abort_flag);
+            bool ok = !p.give_up;
+            if (!ok) *abort_flag = 1;
+            for (int tile = first; tile < p.n_tiles && ok; tile += G, ++segs) {
+                const int b = segs & 1;
+                if (segs >= 2) ok = warp_wait(&ctrl->acc_empty[b], ((segs >> 1) - 1) & 1, abort_flag);
                 tc_fence_after_sync();
                 const uint32_t d = tmem + (uint32_t)(b * p.R);
                 for (int kb = 0; kb < p.n_kb && ok; ++kb) {
@@ -702,10 +768,13 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8_pair(const LinearDev p, 
             else release();
         }
     }
+    // An abort concerns both CTAs: the warp that raised the flag, if no other, sees it here and raises the peer's too.
+    if (lane == 0 && *abort_flag) st_cluster(cluster_addr(smem_u32(&ctrl->abort_flag), rank ^ 1), 1);
     tc_fence_before_sync();
     __syncwarp();
     cluster_arrive();                         // nobody leaves while its peer may still reach into its memory
     cluster_wait();
+    if (*abort_flag) drain_pair(ctrl, S, rank, issued, segs, p.w_chunk, p.x_chunk);
     if (warp == 2) {
         tc_fence_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
@@ -1031,6 +1100,7 @@ cudaError_t launch_linear_i8(const I8Linear& p, cudaStream_t st) {
     d.vec_out = ((uintptr_t)p.out % 16) == 0 && (p.ldo * (p.out_f32 ? 4 : 2)) % 16 == 0;
     d.d_status = p.d_status;
     d.drop_x = g_debug_fault == 3;
+    d.give_up = g_debug_fault == 4;
     d.w_early = !g_call_boundary;       // not as a call of its own (g_call_overlaps)
     const size_t smem = (size_t)d.stages * d.stage_bytes + fixed;
     CUtensorMap tm_x, tm_w;
