@@ -6,6 +6,8 @@ status.  There is no fallback: if the library cannot be loaded, importing this m
 """
 import ctypes as C
 import os
+import subprocess
+import threading
 
 import torch
 
@@ -370,12 +372,23 @@ lib.cats_workspace_i8_bytes.argtypes = [C.POINTER(ModelCfg), _i32]
 lib.cats_verify_layer_i8.argtypes = [C.POINTER(ModelCfg), C.POINTER(LayerWeightsI8), _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp,
                                      C.c_size_t, _vp, _vp]
 
-# Checks and marshals the operands of the calls below (csrc/cats_py.cpp).
-if not os.path.exists(_build.PY_EXT):
-    _build.build_python()
-from . import _cats_py  # noqa: E402
+_ext = None
+_ext_lock = threading.Lock()
 
-_cats_py.bind(*[C.cast(getattr(lib, "cats_%s_i8" % n), _vp).value for n in ("quantize", "dequantize", "rmsnorm", "swiglu", "linear")])
+
+def _marshal():
+    """Checks and marshals the operands of the calls below: csrc/cats_py.cpp, built and loaded with the first of them."""
+    global _ext
+    with _ext_lock:
+        if _ext is None:
+            try:
+                _build.build_python()
+                from . import _cats_py
+            except (ImportError, OSError, subprocess.CalledProcessError) as e:
+                raise RuntimeError("the extension of the 8-bit calls (csrc/cats_py.cpp) cannot be built or loaded: %s" % e) from e
+            _cats_py.bind(*[C.cast(getattr(lib, "cats_%s_i8" % n), _vp).value for n in ("quantize", "dequantize", "rmsnorm", "swiglu", "linear")])
+            _ext = _cats_py
+    return _ext
 
 
 def new_i8(rows: int, cols: int, device="cuda"):
@@ -387,28 +400,28 @@ def new_i8(rows: int, cols: int, device="cuda"):
 def cats_quantize_i8(x, q, scale):
     """x fp32 or bf16 [rows][cols] -> q int8 [rows][cols], scale fp32 [rows].  Like every call below: tensors on the current
     device, rows contiguous and any row stride; ValueError for operands that do not fit each other."""
-    rc = _cats_py.quantize_i8(x, q, scale)
+    rc = (_ext or _marshal()).quantize_i8(x, q, scale)
     if rc:
         raise CatsError(rc, "cats_quantize_i8")
 
 
 def cats_dequantize_i8(q, scale, out):
     """out fp32 or bf16 [rows][cols]."""
-    rc = _cats_py.dequantize_i8(q, scale, out)
+    rc = (_ext or _marshal()).dequantize_i8(q, scale, out)
     if rc:
         raise CatsError(rc, "cats_dequantize_i8")
 
 
 def cats_rmsnorm_i8(resid, delta, gain, eps, resid_out, q, scale):
     """delta and resid_out may be None; resid_out may be resid itself."""
-    rc = _cats_py.rmsnorm_i8(resid, delta, gain, eps, resid_out, q, scale)
+    rc = (_ext or _marshal()).rmsnorm_i8(resid, delta, gain, eps, resid_out, q, scale)
     if rc:
         raise CatsError(rc, "cats_rmsnorm_i8")
 
 
 def cats_swiglu_i8(gate_up, q, scale):
     """gate_up fp32 or bf16 [rows][2 * cols]."""
-    rc = _cats_py.swiglu_i8(gate_up, q, scale)
+    rc = (_ext or _marshal()).swiglu_i8(gate_up, q, scale)
     if rc:
         raise CatsError(rc, "cats_swiglu_i8")
 
@@ -429,7 +442,7 @@ def pack_weights_i8(w: torch.Tensor) -> torch.Tensor:
 
 def cats_linear_i8(x, x_scale, w_packed, w_scale, out, status):
     """x int8 [rows][cols], rows starting on 16 bytes (see new_i8); w_packed: pack_weights_i8 of [outs][cols]; out [rows][outs]."""
-    rc = _cats_py.linear_i8(x, x_scale, w_packed, w_scale, out, status)
+    rc = (_ext or _marshal()).linear_i8(x, x_scale, w_packed, w_scale, out, status)
     if rc:
         raise CatsError(rc, "cats_linear_i8")
 

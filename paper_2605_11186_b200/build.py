@@ -19,22 +19,40 @@ def _stale(lib=LIB) -> bool:
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
 
 
-def build_python(force: bool = False) -> str:
-    """The CPython extension that marshals the 8-bit calls' tensors (csrc/cats_py.cpp), for the torch that is installed."""
+def _python_stamp() -> str:
+    """What the extension depends on: its sources, the interpreter and the installed torch."""
+    import hashlib
     import sysconfig
 
     import torch
-    src = os.path.join(CSRC, "cats_py.cpp")
-    deps = [src, os.path.join(HERE, "..", "include", "cats.h"), torch.__file__]
-    if not force and os.path.exists(PY_EXT) and all(os.path.getmtime(f) <= os.path.getmtime(PY_EXT) for f in deps):
-        return PY_EXT
+    h = hashlib.sha256()
+    for f in (os.path.join(CSRC, "cats_py.cpp"), os.path.join(HERE, "..", "include", "cats.h")):
+        with open(f, "rb") as src:
+            h.update(src.read())
+    h.update(("%s %s %s" % (torch.__version__, torch._C._GLIBCXX_USE_CXX11_ABI, sysconfig.get_config_var("SOABI"))).encode())
+    return "cats_py_stamp:" + h.hexdigest()
+
+
+def build_python(force: bool = False) -> str:
+    """The CPython extension that marshals the 8-bit calls' tensors (csrc/cats_py.cpp), for the torch that is installed.  Built if
+    there is none that carries the stamp of its sources and that torch (not by the files' times, which a copy may set at will)."""
+    import sysconfig
+
+    import torch
+    stamp = _python_stamp()
+    if not force and os.path.exists(PY_EXT):
+        with open(PY_EXT, "rb") as f:
+            if stamp.encode() in f.read():
+                return PY_EXT
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     tmp = PY_EXT + ".tmp.%d" % os.getpid()
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                           '-DCATS_PY_STAMP="%s"' % stamp,
                            "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(root, "include"),
                            "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
-                           src, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", tmp])
+                           os.path.join(CSRC, "cats_py.cpp"), "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+                           "-lc10_cuda", "-o", tmp])
     os.replace(tmp, PY_EXT)
     return PY_EXT
 

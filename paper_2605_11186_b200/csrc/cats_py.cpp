@@ -204,4 +204,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cats_py", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__cats_py(void) { return PyModule_Create(&module); }
+// What this was built from and for (build.py): looked for in the file before it is loaded.
+PyMODINIT_FUNC PyInit__cats_py(void) {
+    PyObject* const m = PyModule_Create(&module);
+    if (m != nullptr && PyModule_AddStringConstant(m, "stamp", CATS_PY_STAMP) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
