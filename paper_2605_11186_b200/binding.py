@@ -426,17 +426,41 @@ def cats_swiglu_i8(gate_up, q, scale):
         raise CatsError(rc, "cats_swiglu_i8")
 
 
+def _device():
+    return torch.device("cuda", torch.cuda.current_device() if torch.cuda.is_initialized() else 0)
+
+
+def _need(where, name, t, dtypes, n=None):
+    """``t``: a contiguous tensor of one of ``dtypes`` with at least n elements on the current device, else ValueError."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError("%s: %s must be a tensor" % (where, name))
+    if t.device != _device():
+        raise ValueError("%s: %s is not on the current device" % (where, name))
+    if t.dtype not in dtypes:
+        raise ValueError("%s: %s must be %s" % (where, name, " or ".join(str(d).split(".")[-1] for d in dtypes)))
+    if not t.is_contiguous():
+        raise ValueError("%s: %s must be contiguous" % (where, name))
+    if n is not None and t.numel() < n:
+        raise ValueError("%s: %s has %d elements, %d are wanted" % (where, name, t.numel(), n))
+
+
 def pack_weights_i8(w: torch.Tensor) -> torch.Tensor:
     """cats_pack_weights_i8: int8 [outs][cols] -> packed buffer (uint8 CUDA tensor, 1024-byte aligned)."""
+    where = "cats_pack_weights_i8"
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.dtype != torch.int8:
+        raise ValueError("%s: w must be an int8 matrix" % where)
+    if w.device != _device():
+        raise ValueError("%s: w is not on the current device" % where)
     rows, cols = w.shape
-    assert w.is_cuda and w.dtype == torch.int8 and w.stride(1) == 1
+    if cols > 1 and w.stride(1) != 1:
+        raise ValueError("%s: w must have contiguous rows" % where)
     n = int(lib.cats_packed_weight_i8_bytes(rows, cols))
     if n == 0:
         raise CatsError(-3, "cats_packed_weight_i8_bytes")
     buf = torch.empty(n + 1024, dtype=torch.uint8, device=w.device)
     off = (-buf.data_ptr()) % 1024
     out = buf[off:off + n]
-    _check(lib.cats_pack_weights_i8(w.data_ptr(), w.stride(0) if rows > 1 else cols, rows, cols, out.data_ptr(), _stream()), "cats_pack_weights_i8")
+    _check(lib.cats_pack_weights_i8(w.data_ptr(), w.stride(0) if rows > 1 else cols, rows, cols, out.data_ptr(), _stream()), where)
     return out
 
 
@@ -464,12 +488,22 @@ def pack_layer_i8(w: dict) -> dict:
 
 
 def layer_weights_i8(w: dict) -> LayerWeightsI8:
-    """``w``: a packed 8-bit layer (see pack_layer_i8)."""
-    s = LayerWeightsI8()
+    """``w``: a packed 8-bit layer (see pack_layer_i8).  The struct holds addresses; its ``tensors`` keep what they point to, its
+    ``shape`` is (hidden, n_heads * head_dim, ffn).  ValueError for tensors that are not the weights of one layer."""
+    where = "layer_weights_i8"
+    if any(n not in w for n, _ in LayerWeightsI8._fields_):
+        raise ValueError("%s: a weight is missing" % where)
     for n, _ in LayerWeightsI8._fields_:
-        t = w[n]
-        assert t.is_cuda and t.is_contiguous(), n
-        setattr(s, n, t.data_ptr())
+        _need(where, n, w[n], (torch.float32,) if n.startswith("s_") else (torch.bfloat16,) if n.endswith("_norm") else (torch.uint8,))
+    H, D, F = w["attn_norm"].numel(), w["s_qkv"].numel() // 3, w["s_gate_up"].numel() // 2
+    lengths = {"mlp_norm": H, "s_qkv": 3 * D, "s_o": H, "s_gate_up": 2 * F, "s_down": H}
+    for n, outs, cols in (("wqkv", 3 * D, H), ("wo", H, D), ("w_gate_up", 2 * F, H), ("w_down", H, F)):
+        lengths[n] = int(lib.cats_packed_weight_i8_bytes(outs, cols))
+    for n, length in lengths.items():
+        if w[n].numel() != length:
+            raise ValueError("%s: %s has %d elements, %d are wanted" % (where, n, w[n].numel(), length))
+    s = LayerWeightsI8(*[w[n].data_ptr() for n, _ in LayerWeightsI8._fields_])
+    s.tensors, s.shape = [w[n] for n, _ in LayerWeightsI8._fields_], (H, D, F)
     return s
 
 
@@ -483,8 +517,19 @@ def new_workspace_i8(cfg: ModelCfg, T: int, device="cuda") -> torch.Tensor:
 
 
 def cats_verify_layer_i8(cfg, w: LayerWeightsI8, resid, kcache, vcache, mask, pos, T, prefix_len, ws, status):
+    """``w``: layer_weights_i8 of the layer.  ValueError for operands that do not fit cfg and T."""
+    where, D = "cats_verify_layer_i8", cfg.n_heads * cfg.head_dim
+    if getattr(w, "shape", (cfg.hidden, D, cfg.ffn)) != (cfg.hidden, D, cfg.ffn):
+        raise ValueError("%s: the weights are another model's" % where)
+    _need(where, "resid", resid, (torch.float32,), T * cfg.hidden)
+    for name, t in (("kcache", kcache), ("vcache", vcache)):
+        _need(where, name, t, (torch.bfloat16,), cfg.max_seq * D)
+    _need(where, "mask", mask, (torch.int64, torch.uint64), 2 * T)
+    _need(where, "pos", pos, (torch.int32,), T)
+    _need(where, "ws", ws, (torch.uint8,))
+    _need(where, "status", status, (torch.int32,), 1)
     _check(lib.cats_verify_layer_i8(C.byref(cfg), C.byref(w), _ptr(resid), _ptr(kcache), _ptr(vcache), _ptr(mask), _ptr(pos), T,
-                                    prefix_len, _ptr(ws), ws.numel(), _ptr(status), _stream()), "cats_verify_layer_i8")
+                                    prefix_len, _ptr(ws), ws.numel(), _ptr(status), _stream()), where)
 
 
 class VerifyForward:
