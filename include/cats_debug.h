@@ -31,6 +31,14 @@ void cats_debug_stage_mask(unsigned mask);
  * out: HOST array of 8 size_t. */
 int cats_debug_workspace_layout(const cats_model_cfg *cfg, int32_t T, size_t *out);
 
+/* The same for the workspace of cats_workspace_i8_bytes: out[0..5] = the int8
+ * rows in front of the projection at hand (row stride out[6] bytes), their fp32
+ * scales, the fp32 output of the QKV or gate/up projection ([T][outs]), of the O
+ * or down projection ([T][hidden]), the rotated q and the attention output (bf16
+ * [T][n_heads*head_dim]).  After a call they hold what its last user left.
+ * out: HOST array of 7 size_t. */
+int cats_debug_workspace_i8_layout(const cats_model_cfg *cfg, int32_t T, size_t *out);
+
 /* Attention kernel used for head_dim 128: -1 (default) chosen by shape, 0 the
  * mma.sync kernel (the fallback when the driver offers no tensor maps), 1 the
  * tcgen05 kernel, 2 the tcgen05 kernel with two softmax threads per query row

@@ -516,6 +516,13 @@ def new_workspace_i8(cfg: ModelCfg, T: int, device="cuda") -> torch.Tensor:
     return buf[off:off + n]
 
 
+def workspace_i8_layout(cfg: ModelCfg, T: int) -> dict:
+    """cats_debug_workspace_i8_layout: byte offsets of the intermediate buffers inside the workspace (for tests that inspect them)."""
+    out = (C.c_size_t * 7)()
+    _check(lib.cats_debug_workspace_i8_layout(C.byref(cfg), T, out), "cats_debug_workspace_i8_layout")
+    return dict(x=out[0], scale=out[1], wide=out[2], delta=out[3], q=out[4], o=out[5], ldx=out[6])
+
+
 def cats_verify_layer_i8(cfg, w: LayerWeightsI8, resid, kcache, vcache, mask, pos, T, prefix_len, ws, status):
     """``w``: layer_weights_i8 of the layer.  ValueError for operands that do not fit cfg and T."""
     where, D = "cats_verify_layer_i8", cfg.n_heads * cfg.head_dim

@@ -734,6 +734,15 @@ size_t cats_workspace_i8_bytes(const cats_model_cfg* cfg, int32_t T) {
     return carve_i8(cfg, T, nullptr).bytes;
 }
 
+int cats_debug_workspace_i8_layout(const cats_model_cfg* cfg, int32_t T, size_t* out) {
+    if (check_cfg(cfg) != CATS_OK || T < 1 || T > CATS_MAX_TREE || !out) return CATS_ERR_INVALID_ARG;
+    const WorkspaceI8 w = carve_i8(cfg, T, nullptr);
+    const void* at[] = {w.x, w.scale, w.wide, w.delta, w.q, w.o};
+    for (int i = 0; i < 6; ++i) out[i] = (size_t)((const uint8_t*)at[i] - (const uint8_t*)nullptr);
+    out[6] = (size_t)w.ldx;
+    return CATS_OK;
+}
+
 int cats_verify_layer_i8(const cats_model_cfg* cfg, const cats_layer_weights_i8* w, float* d_resid, void* d_kcache, void* d_vcache,
                          const uint64_t* d_mask, const int32_t* d_pos, int32_t T, int32_t prefix_len, void* d_ws, size_t ws_bytes,
                          int32_t* d_status, void* stream) {
