@@ -549,7 +549,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_i8(const LinearDev p, const
 // The same product for many tokens, where it is bound by the tensor cores and by what an SM takes in: a pair of CTAs on two
 // SMs works on one tile of 256 tokens x R channels (tcgen05 cta_group::2).  Each CTA brings its 128 tokens and half of the
 // tile's channels, (128 + R / 2) rows per K block for 128 x R sums, where a CTA on its own takes in 128 + R; that is what lets
-// the tensor cores keep up their rate (4093 x 4096 x 22016: 219 us, 3370 TOP/s; single CTAs on 128 x 256 tiles 301 us).
+// the tensor cores keep up their rate (4093 x 4096 x 22016: 220 to 240 us, 3360 to 3080 TOP/s as the power limit allows; single CTAs on
+// 128 x 256 tiles 301 us beside the former).
 // Copies of both CTAs count on the first CTA's barrier, whose warp 2 issues the MMAs for both; commits arrive at both.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr uint32_t kFirstOfPair = 0xFEFFFFFFu;       // a shared-memory address in the pair's first CTA

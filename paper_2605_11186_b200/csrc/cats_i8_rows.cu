@@ -556,8 +556,8 @@ __global__ void __launch_bounds__(256) k_i8_qkv(const float* qkv, const int32_t*
 
 // Few vectors per thread make the shortest chain for a row, many keep more bytes in flight and fewer threads waiting: the
 // former while all rows are on the SMs at once.  Measured, one or two against four vectors, us: norm of 64 / 592 / 1024 / 8192 x
-// 4096 2.2 / 4.0 / 6.7 / 42.6 against 2.7 / 5.2 / 6.5 / 38.9; quantise 1.6 / 2.2 / 3.2 / 23.1 against 1.8 / 2.6 / 3.0 / 17.4; SwiGLU of
-// 64 / 148 / 300 / 8192 x 11008 2.5 / 2.7 / 6.3 / 124 against 3.0 / 2.9 / 5.3 / 67.6.
+// 4096 2.3 / 4.2 / 7.1 / 44.1 against 2.8 / 5.5 / 6.8 / 39.4; quantise 1.6 / 2.4 / 3.4 / 25.0 against 1.9 / 3.0 / 3.4 / 18.3; SwiGLU of
+// 64 / 148 / 300 / 8192 x 11008 2.6 / 2.7 / 6.3 / 122 against 3.2 / 3.0 / 5.2 / 75.5.
 inline bool rows_fit(const I8RowsDev& p, int threads) { return p.rows <= 148 * (2048 / threads); }
 
 template <int OP, typename TX, typename TD, bool GRID>
