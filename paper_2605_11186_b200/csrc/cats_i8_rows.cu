@@ -184,7 +184,7 @@ __device__ __forceinline__ float max_abs(float m, const float* y) {
 }
 // silu(g) u = g u / (1 + e^-g): for g -> -inf the quotient goes to -0 (e^-g reaches infinity), for g -> inf to g.  Flushing forms of
 // 2^x and 1/x, which need half the instructions: for gates from kFarGate up every intermediate is a normal number.
-constexpr float kFarGate = -80.f, kFarExp = 1.2089258196146292e24f;      // 2^80: below e^80, so that no gate below kFarGate is missed
+constexpr float kFarGate = -80.f, kFarExp = 4.1538374868278621e34f;      // 2^115: just below e^80, so that no gate below kFarGate is missed
 constexpr uint32_t kFarMark = 0x80000000u;
 __device__ __forceinline__ float silu_mul(float g, float u, float& e) {
     float r;
