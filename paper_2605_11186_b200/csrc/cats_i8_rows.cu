@@ -141,8 +141,8 @@ __device__ __forceinline__ void warp_store(uint16_t* row, int c0, int cols, floa
 // One bf16 element in a thousand is a tie, 127 v / a an exact half, and v fl(127 / a) puts it on either side of the half (one in 1900
 // elements a step off).  So the factor is kept in two parts, hi + lo = 127 / a to 2^-29 or better, and fma(v, hi, v lo) rounds the
 // quotient once: one that fp32 holds, a tie among them, is exact.  SwiGLU's values have several roundings behind them and
-// no exact ties: they take hi alone (4096 x 11008 and its values 56 us, with the second part 63).  Two instructions per element
-// more than hi alone: 22016 x 4096 bf16 and its values 82.6 -> 84.6 us, norm of 8191 x 4096 53.3 -> 53.7.
+// no exact ties: they take hi alone (the second part took 7 us more for 4096 x 11008 and its values).  Two instructions per element
+// more than hi alone: 22016 x 4096 bf16 and its values 82.6 -> 84.2 us, norm of 8191 x 4096 53.3 either way.
 // Rounding to a whole number: the sum with 1.5 * 2^23 leaves it (ties to even) in the low bits; the conversion instruction has
 // a sixteenth of the FMA rate and shares its unit with ex2 and rcp.
 constexpr float kRintMagic = 12582912.f;
