@@ -16,7 +16,8 @@
  *     The library allocates no device memory.  The state it keeps is host-side
  *     and derived from arguments only: kernel attributes set once per process,
  *     a cache of up to 256 encoded tensor maps keyed by (pointer, shape) for
- *     the attention kernel, the per-device address of the scratch array of
+ *     the attention kernel, the rotary frequencies of each thread's last
+ *     cats_paged_append, the per-device address of the scratch array of
  *     cats_tree_attention_static, and the switches of include/cats_debug.h
  *     (all at their defaults unless a test or a benchmark sets them).  No
  *     environment variable is read.
@@ -420,6 +421,94 @@ size_t cats_workspace_i8_bytes(const cats_model_cfg *cfg, int32_t T);
 int cats_verify_layer_i8(const cats_model_cfg *cfg, const cats_layer_weights_i8 *w, float *d_resid, void *d_kcache,
                          void *d_vcache, const uint64_t *d_mask, const int32_t *d_pos, int32_t T, int32_t prefix_len, void *d_ws,
                          size_t ws_bytes, int32_t *d_status, void *stream);
+
+/* ---- Paged cache -------------------------------------------------------------
+ * (The paper decodes one sequence over a contiguous cache; these calls are this
+ * library's.)  K and V of one layer, of many sequences, in pages of page_size rows.
+ * Row p of sequence s is row p % page_size of page
+ * d_table[s * ld_table + p / page_size]; entries behind a sequence's last page are
+ * not read.  The element at (page, row, head, c) lies
+ * page * page_stride + row * row_stride + head * head_stride + c elements behind k
+ * (and v): any order of pages, rows and heads; rows of one head of a page that lie
+ * together are the fast case.  A contiguous cache [max_seq][n_heads*head_dim] is one
+ * page of max_seq rows.
+ *   type CATS_BF16: bf16 elements, k_scale and v_scale NULL.
+ *   type CATS_I8: int8 elements, one fp32 scale per (page, row, head) at
+ *     page * s_page_stride + row * s_row_stride + head * s_head_stride, of K and of V;
+ *     a row of one head is held as the 8-bit path holds a row (above).
+ * head_dim 64 or 128 (else CATS_ERR_UNSUPPORTED); k and v start on 16 bytes, strides
+ * are not negative and whole multiples of 16 bytes (8 elements of bf16, 16 of int8;
+ * the scales' any); a page holds at most 2^26 rows, K (and V) spans at most 2^36 bytes
+ * and its scales 2^32 elements (CATS_ERR_UNSUPPORTED).
+ * A sequence, position or page outside the tables' ranges sets
+ * CATS_ERR_INVALID_ARG in *d_status; nothing is read or written there. */
+enum { CATS_I8 = 2 };
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int32_t type, n_pages, page_size, n_kv_heads, head_dim;
+    int64_t page_stride, row_stride, head_stride;
+    int64_t s_page_stride, s_row_stride, s_head_stride;
+} cats_paged_kv;
+
+/* Row i of the inputs becomes row d_pos[i] of sequence d_seq[i] (d_seq NULL: of
+ * sequence i).  d_pos[i] < 0: row i is left out, and its outputs as they are.  No two
+ * rows of a call may name the same cache row.
+ *   d_k, d_v [rows][n_kv_heads*head_dim], d_q [rows][n_heads*head_dim] (NULL: none) of
+ *     `type` CATS_F32 or CATS_BF16, row strides in elements; a row may start anywhere.
+ *   rope_base > 0: q and k are rotated to d_pos[i] (rotate-half pairs
+ *     (i, i + head_dim/2), angle pos * base^(-2i/head_dim) reduced in fp64), 0: not.
+ *   d_q_out bf16 [rows][n_heads*head_dim]; may not overlap d_q.
+ * All arithmetic is fp32; every value is rounded once into the cache or to bf16. */
+int cats_paged_append(const cats_paged_kv *kv, const int32_t *d_table, int64_t ld_table, int32_t table_width, int32_t n_seqs,
+                      const int32_t *d_seq, const int32_t *d_pos, int32_t rows, const void *d_q, int64_t ldq, int32_t n_heads,
+                      const void *d_k, int64_t ldk, const void *d_v, int64_t ldv, int32_t type, float rope_base, void *d_q_out,
+                      int64_t ldqo, int32_t *d_status, void *stream);
+
+/* The same rows back: d_k_out, d_v_out [rows][n_kv_heads*head_dim] of out_type CATS_F32
+ * or CATS_BF16 (a bf16 cache's rows come back as they are).  The contiguous bf16 caches
+ * that cats_verify_layer reads are such matrices. */
+int cats_paged_read(const cats_paged_kv *kv, const int32_t *d_table, int64_t ld_table, int32_t table_width, int32_t n_seqs,
+                    const int32_t *d_seq, const int32_t *d_pos, int32_t rows, void *d_k_out, int64_t ldk, void *d_v_out, int64_t ldv,
+                    int32_t out_type, int32_t *d_status, void *stream);
+
+/* One query row per sequence over that sequence's rows 0 .. d_len[s] - 1:
+ *   out[s][h] = sum_t softmax_t(q[s][h] . k[t][g] * scale) v[t][g],  g = h / (n_heads / n_kv_heads)
+ * q [n_seqs][n_heads*head_dim] bf16 (rotated: cats_paged_append's d_q_out), out likewise;
+ * q starts on 16 bytes and ldq is a multiple of 8, out on 4 and ldo of 2.
+ * n_heads is a multiple of n_kv_heads.  d_len[s] <= 0: the row of out is zeros.  Lengths
+ * past table_width * page_size are cut there and reported.  Scores and softmax are fp32, the
+ * probabilities enter the second product with 16 significant bits over a bf16 cache and with 11
+ * over an int8 cache.  Rows behind a sequence's length are not read.
+ * Workspace: cats_paged_workspace_bytes (0 for arguments that are refused), 1024-byte
+ * aligned, one per stream, ZEROED once by the caller; a call leaves it fit for the next of
+ * any size that it is large enough for. */
+size_t cats_paged_workspace_bytes(int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+int cats_paged_attention(const cats_paged_kv *kv, const int32_t *d_table, int64_t ld_table, int32_t table_width, const int32_t *d_len,
+                         int32_t n_seqs, const void *d_q, int64_t ldq, int32_t n_heads, float scale, void *d_out, int64_t ldo,
+                         void *d_ws, size_t ws_bytes, int32_t *d_status, void *stream);
+
+/* ---- Sampling ----------------------------------------------------------------
+ * One token per draw, from a row of logits (fp32 or bf16) and a given random number.
+ * Draw i reads row d_row[i] (d_row NULL: row i; d_row[i] < 0: the draw is left out).
+ * Tokens are ordered by falling logit, equal ones by rising index, and weigh
+ *     w = exp((logit - largest) / temperature).
+ * Kept are, one after the other: the first top_k of the order (0 or less: all); of
+ * those the shortest run from the front whose w add up to top_p of theirs, at least
+ * one token (top_p >= 1: all); of those the ones with w >= min_p, and the largest.  The token is the
+ * first in INDEX order at which the sum of the kept w exceeds u times their whole sum
+ * (u < 0 counts as 0, u >= 1 takes the last kept token); d_prob its share of that sum.
+ * temperature 0: the first token of the order, d_prob 1.  temperature inf: equal weights.
+ * d_temperature, d_top_p, d_min_p, d_u fp32 [rows], d_top_k int32 [rows]; NULL:
+ * temperature 1, no top-k, no top-p, no min-p; d_u is always needed.  d_prob may be NULL.
+ * w is a whole multiple of 2^-44 (from an fp64 exponential), so every sum is exact and the
+ * token does not depend on how the work is split; -0 equals 0; -inf weighs nothing.
+ * A row with a NaN, an infinity or nothing finite, a NaN setting, a negative temperature
+ * or a row index past logit_rows: token -1, prob 0 and CATS_ERR_INVALID_ARG in *d_status.
+ * vocab <= 262144 (CATS_ERR_UNSUPPORTED). */
+int cats_sample(const void *d_logits, int32_t type, int64_t ld, int32_t logit_rows, int32_t vocab, const int32_t *d_row, int32_t rows,
+                const float *d_temperature, const int32_t *d_top_k, const float *d_top_p, const float *d_min_p, const float *d_u,
+                int32_t *d_token, float *d_prob, int32_t *d_status, void *stream);
 
 /* Number of kernel launches the last call of this thread issued (for reports). */
 int cats_last_launch_count(void);

@@ -386,7 +386,9 @@ def _marshal():
                 from . import _cats_py
             except (ImportError, OSError, subprocess.CalledProcessError) as e:
                 raise RuntimeError("the extension of the 8-bit calls (csrc/cats_py.cpp) cannot be built or loaded: %s" % e) from e
-            _cats_py.bind(*[C.cast(getattr(lib, "cats_%s_i8" % n), _vp).value for n in ("quantize", "dequantize", "rmsnorm", "swiglu", "linear")])
+            _cats_py.bind(*[C.cast(getattr(lib, "cats_" + n), _vp).value for n in
+                            ("quantize_i8", "dequantize_i8", "rmsnorm_i8", "swiglu_i8", "linear_i8", "paged_append", "paged_read",
+                             "paged_attention", "sample")])
             _ext = _cats_py
     return _ext
 
@@ -537,6 +539,116 @@ def cats_verify_layer_i8(cfg, w: LayerWeightsI8, resid, kcache, vcache, mask, po
     _need(where, "status", status, (torch.int32,), 1)
     _check(lib.cats_verify_layer_i8(C.byref(cfg), C.byref(w), _ptr(resid), _ptr(kcache), _ptr(vcache), _ptr(mask), _ptr(pos), T,
                                     prefix_len, _ptr(ws), ws.numel(), _ptr(status), _stream()), where)
+
+
+class PagedKVDesc(C.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("type", _i32), ("n_pages", _i32), ("page_size", _i32),
+                ("n_kv_heads", _i32), ("head_dim", _i32), ("page_stride", _i64), ("row_stride", _i64), ("head_stride", _i64),
+                ("s_page_stride", _i64), ("s_row_stride", _i64), ("s_head_stride", _i64)]
+
+
+I8 = 2
+_kvp = C.POINTER(PagedKVDesc)
+lib.cats_paged_append.argtypes = [_kvp, _vp, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _i32, C.c_float, _vp,
+                                  _i64, _vp, _vp]
+lib.cats_paged_read.argtypes = [_kvp, _vp, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _i32, _vp, _vp]
+lib.cats_paged_workspace_bytes.restype = C.c_size_t
+lib.cats_paged_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32]
+lib.cats_paged_attention.argtypes = [_kvp, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _i32, C.c_float, _vp, _i64, _vp, C.c_size_t, _vp, _vp]
+lib.cats_sample.argtypes = [_vp, _i32, _i64, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+
+
+class PagedKV:
+    """The pages of one layer's cache (cats_paged_kv): k, v bf16 or int8 [n_pages][page_size][n_kv_heads][head_dim] in any order of
+    memory in which a head's elements lie together, and for int8 k_scale, v_scale fp32 [n_pages][page_size][n_kv_heads].  Keeps the
+    tensors; their addresses and strides are taken here.  ValueError for tensors that do not fit each other."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        where = "PagedKV"
+
+        def pair(names, a, b, dim, dtypes):
+            for name, t in zip(names, (a, b)):
+                if not isinstance(t, torch.Tensor) or t.dim() != dim or t.dtype not in dtypes:
+                    raise ValueError("%s: %s must be a tensor of %d dimensions, %s" % (where, name, dim, " or ".join(str(d).split(".")[-1] for d in dtypes)))
+                if t.device != k.device:
+                    raise ValueError("%s: %s is on another device" % (where, name))
+            strides = [[st if n > 1 else 0 for n, st in zip(t.shape, t.stride())] for t in (a, b)]
+            if a.dtype != b.dtype or a.shape != b.shape or strides[0] != strides[1]:
+                raise ValueError("%s: %s and %s must have one type, shape and layout" % (where, names[0], names[1]))
+            return strides[0]
+
+        if not isinstance(k, torch.Tensor):
+            raise ValueError("%s: k must be a tensor" % where)
+        st = pair(("k", "v"), k, v, 4, (torch.bfloat16, torch.int8))
+        if max(k.shape) > 2 ** 31 - 1:
+            raise ValueError("%s: k is too large" % where)
+        if k.shape[3] > 1 and st[3] != 1:
+            raise ValueError("%s: the elements of a head must be contiguous" % where)
+        i8, ss = k.dtype == torch.int8, [0, 0, 0]
+        if i8 != (k_scale is not None) or i8 != (v_scale is not None):
+            raise ValueError("%s: scales belong to int8 pages, and to those alone" % where)
+        if i8:
+            ss = pair(("k_scale", "v_scale"), k_scale, v_scale, 3, (torch.float32,))
+            if k_scale.shape != k.shape[:3]:
+                raise ValueError("%s: the scales must be [n_pages][page_size][n_kv_heads]" % where)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        n = [t.data_ptr() if t is not None else None for t in (k, v, k_scale, v_scale)]
+        self.struct = PagedKVDesc(*n, I8 if i8 else BF16, *k.shape, *st[:3], *ss)
+        self.desc = bytes(self.struct)
+
+
+def new_paged_kv(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype=torch.int8, device="cuda") -> PagedKV:
+    """A cache of zeros in the order that the attention reads fastest: the rows of one head of a page together."""
+    def pages(*shape, **kw):
+        return torch.zeros(n_pages, n_kv_heads, page_size, *shape, device=device, **kw).transpose(1, 2)
+    scales = [pages(dtype=torch.float32) for _ in range(2)] if dtype == torch.int8 else []
+    return PagedKV(pages(head_dim, dtype=dtype), pages(head_dim, dtype=dtype), *scales)
+
+
+def _paged(where, kv):
+    if not isinstance(kv, PagedKV):
+        raise ValueError("%s: cache must be a PagedKV" % where)
+    return kv
+
+
+def cats_paged_append(kv, table, seq, pos, q, k, v, rope_base, q_out, status):
+    """Rows k, v (fp32 or bf16 [rows][n_kv_heads * head_dim], or [rows][n_kv_heads][head_dim]) become rows pos[i] of the sequences seq[i]
+    (None: of sequence i); q and q_out (bf16) may be None.  table: int32 [n_seqs][pages].  rope_base 0: no rotation."""
+    rc = (_ext or _marshal()).paged_append(_paged("cats_paged_append", kv).k, kv.desc, table, seq, pos, q, k, v, rope_base, q_out, status)
+    if rc:
+        raise CatsError(rc, "cats_paged_append")
+
+
+def cats_paged_read(kv, table, seq, pos, k_out, v_out, status):
+    """Rows pos[i] of the sequences seq[i] (None: of sequence i) to k_out, v_out, fp32 or bf16 [rows][n_kv_heads * head_dim]."""
+    rc = (_ext or _marshal()).paged_read(_paged("cats_paged_read", kv).k, kv.desc, table, seq, pos, k_out, v_out, status)
+    if rc:
+        raise CatsError(rc, "cats_paged_read")
+
+
+def new_workspace_paged(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """Zeroed workspace of cats_paged_attention, one per stream."""
+    n = int(lib.cats_paged_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim))
+    if n == 0:
+        raise CatsError(-3, "cats_paged_workspace_bytes")
+    buf = torch.zeros(n + 1024, dtype=torch.uint8, device=device)
+    off = (-buf.data_ptr()) % 1024
+    return buf[off:off + n]
+
+
+def cats_paged_attention(kv, table, lens, q, scale, out, ws, status):
+    """q, out: bf16 [n_seqs][n_heads * head_dim] or [n_seqs][n_heads][head_dim]; lens: int32 [n_seqs]; ws: new_workspace_paged."""
+    rc = (_ext or _marshal()).paged_attention(_paged("cats_paged_attention", kv).k, kv.desc, table, lens, q, scale, out, ws, status)
+    if rc:
+        raise CatsError(rc, "cats_paged_attention")
+
+
+def cats_sample(logits, row, temperature, top_k, top_p, min_p, u, token, prob, status):
+    """logits: fp32 or bf16 [logit_rows][vocab]; row (int32), temperature, top_k (int32), top_p, min_p and prob may be None; u, token
+    (int32): one per draw."""
+    rc = (_ext or _marshal()).sample(logits, row, temperature, top_k, top_p, min_p, u, token, prob, status)
+    if rc:
+        raise CatsError(rc, "cats_sample")
 
 
 class VerifyForward:

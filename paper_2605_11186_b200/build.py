@@ -6,8 +6,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcats.so")
 PY_EXT = os.path.join(HERE, "_cats_py.so")
-SOURCES = ["cats_api.cu", "cats_small_kernels.cu", "cats_gemm.cu", "cats_attn.cu", "cats_i8_rows.cu", "cats_i8_linear.cu"]
-HEADERS = ["cats_common.cuh", "cats_kernels.cuh", os.path.join("..", "..", "include", "cats.h")]
+SOURCES = ["cats_api.cu", "cats_small_kernels.cu", "cats_gemm.cu", "cats_attn.cu", "cats_i8_rows.cu", "cats_i8_linear.cu", "cats_paged.cu",
+           "cats_paged_attn.cu", "cats_sample.cu"]
+HEADERS = ["cats_common.cuh", "cats_i8.cuh", "cats_paged.cuh", "cats_kernels.cuh", os.path.join("..", "..", "include", "cats.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--shared", "-cudart", "static"]
 

@@ -4,7 +4,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
-#include "cats_kernels.cuh"
+#include "cats_paged.cuh"
 
 namespace cats {
 
@@ -799,6 +799,146 @@ int cats_verify_layer_i8(const cats_model_cfg* cfg, const cats_layer_weights_i8*
     CATS_CUDA(linear(w->w_down, w->s_down, F, H, ws.delta));
     CATS_CUDA(launch_rmsnorm(d_resid, nullptr, ws.delta, 1, (size_t)T * H, nullptr, T, H, cfg->rms_eps, nullptr, nullptr, nullptr, nullptr,
                              cfg->head_dim, cfg->rope_base, nullptr, 0, st, d_status));
+    return CATS_OK;
+}
+
+// ---- paged cache ---------------------------------------------------------------------------------
+
+namespace {
+// Checks the cache and its table, and makes what the kernels take of them.
+int paged_dev(const cats_paged_kv* kv, const int32_t* d_table, int64_t ld_table, int32_t width, int32_t n_seqs, PagedDev& c) {
+    if (!kv || (kv->type != CATS_BF16 && kv->type != CATS_I8)) return CATS_ERR_INVALID_ARG;
+    const bool i8 = kv->type == CATS_I8;
+    if (kv->n_pages < 1 || kv->page_size < 1 || kv->n_kv_heads < 1 || width < 1 || n_seqs < 0 || ld_table < width) return CATS_ERR_INVALID_ARG;
+    if (kv->head_dim != 64 && kv->head_dim != 128) return CATS_ERR_UNSUPPORTED;
+    if (kv->page_size > (1 << 26)) return CATS_ERR_UNSUPPORTED;
+    const int64_t n[3] = {kv->n_pages, kv->page_size, kv->n_kv_heads};
+    int64_t st[3] = {kv->page_stride, kv->row_stride, kv->head_stride}, ss[3] = {kv->s_page_stride, kv->s_row_stride, kv->s_head_stride};
+    const int64_t unit = i8 ? 16 : 8;           // elements of 16 bytes
+    unsigned __int128 span = (unsigned)kv->head_dim, s_span = 1;
+    for (int d = 0; d < 3; ++d) {
+        if (n[d] == 1) st[d] = ss[d] = 0;       // a stride over one element means nothing
+        if (st[d] < 0 || st[d] % unit || (i8 && ss[d] < 0)) return CATS_ERR_INVALID_ARG;
+        if (!i8) ss[d] = 0;
+        span += (unsigned __int128)(n[d] - 1) * (uint64_t)st[d];
+        s_span += (unsigned __int128)(n[d] - 1) * (uint64_t)ss[d];
+    }
+    if (span > ((uint64_t)1 << 36) / (i8 ? 1 : 2) || s_span > ((uint64_t)1 << 32)) return CATS_ERR_UNSUPPORTED;
+    if (n_seqs == 0) return CATS_OK;
+    if (!kv->k || !kv->v || misaligned(kv->k, 16) || misaligned(kv->v, 16) || !d_table || misaligned(d_table, 4)) return CATS_ERR_INVALID_ARG;
+    if (i8 && (!kv->k_scale || !kv->v_scale || misaligned(kv->k_scale, 4) || misaligned(kv->v_scale, 4))) return CATS_ERR_INVALID_ARG;
+    c.k = (uint8_t*)kv->k; c.v = (uint8_t*)kv->v; c.ks = kv->k_scale; c.vs = kv->v_scale;
+    c.page16 = (uint32_t)(st[0] / unit); c.row16 = (uint32_t)(st[1] / unit); c.head16 = (uint32_t)(st[2] / unit);
+    c.s_page = (uint32_t)ss[0]; c.s_row = (uint32_t)ss[1]; c.s_head = (uint32_t)ss[2];
+    c.n_pages = kv->n_pages; c.page_size = kv->page_size; c.n_kv = kv->n_kv_heads;
+    c.by_page = divisor((uint32_t)kv->page_size);
+    c.table = d_table; c.ld_table = ld_table; c.width = width; c.n_seqs = n_seqs;
+    return CATS_OK;
+}
+}  // namespace
+
+int cats_paged_append(const cats_paged_kv* kv, const int32_t* d_table, int64_t ld_table, int32_t table_width, int32_t n_seqs,
+                      const int32_t* d_seq, const int32_t* d_pos, int32_t rows, const void* d_q, int64_t ldq, int32_t n_heads,
+                      const void* d_k, int64_t ldk, const void* d_v, int64_t ldv, int32_t type, float rope_base, void* d_q_out,
+                      int64_t ldqo, int32_t* d_status, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_paged_append");
+    g_call_boundary = true;
+    g_call_overlaps = true;
+    PagedDev c = {};
+    const int rc = paged_dev(kv, d_table, ld_table, table_width, n_seqs, c);
+    if (rc) return rc;
+    if (rows < 0 || bad_type(type) || !(rope_base >= 0.f) || rope_base > 3.4e38f || n_heads < 0 || (d_q && n_heads < 1)) return CATS_ERR_INVALID_ARG;
+    if (kv->n_kv_heads > (1 << 16) || n_heads > (1 << 16)) return CATS_ERR_UNSUPPORTED;
+    const int64_t kv_cols = (int64_t)kv->n_kv_heads * kv->head_dim, q_cols = (int64_t)n_heads * kv->head_dim;
+    if (ldk < kv_cols || ldv < kv_cols || (d_q && (ldq < q_cols || ldqo < q_cols)) || (!d_seq && rows > n_seqs)) return CATS_ERR_INVALID_ARG;
+    if (rows == 0 || n_seqs == 0) return rows == 0 ? CATS_OK : CATS_ERR_INVALID_ARG;
+    if (!d_pos || !d_k || !d_v || !d_status || misaligned(d_pos, 4) || misaligned(d_seq, 4) || misaligned(d_status, 4)) return CATS_ERR_INVALID_ARG;
+    if (misaligned(d_k, type_size(type)) || misaligned(d_v, type_size(type))) return CATS_ERR_INVALID_ARG;
+    if (d_q && (!d_q_out || d_q_out == d_q || misaligned(d_q, type_size(type)) || misaligned(d_q_out, 2))) return CATS_ERR_INVALID_ARG;
+    PagedRows r = {};
+    r.seq = d_seq; r.pos = d_pos; r.rows = rows; r.n_heads = d_q ? n_heads : 0; r.f32 = type == CATS_F32;
+    r.q = d_q; r.k = d_k; r.v = d_v; r.ldq = ldq; r.ldk = ldk; r.ldv = ldv; r.q_out = (uint16_t*)d_q_out; r.ldqo = ldqo;
+    r.rope_base = rope_base; r.d_status = d_status;
+    CATS_CUDA(launch_paged_append(c, r, kv->type == CATS_I8, kv->head_dim, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+int cats_paged_read(const cats_paged_kv* kv, const int32_t* d_table, int64_t ld_table, int32_t table_width, int32_t n_seqs,
+                    const int32_t* d_seq, const int32_t* d_pos, int32_t rows, void* d_k_out, int64_t ldk, void* d_v_out, int64_t ldv,
+                    int32_t out_type, int32_t* d_status, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_paged_read");
+    g_call_boundary = true;
+    g_call_overlaps = true;
+    PagedDev c = {};
+    const int rc = paged_dev(kv, d_table, ld_table, table_width, n_seqs, c);
+    if (rc) return rc;
+    const int64_t kv_cols = (int64_t)kv->n_kv_heads * kv->head_dim;
+    if (rows < 0 || bad_type(out_type) || ldk < kv_cols || ldv < kv_cols || (!d_seq && rows > n_seqs)) return CATS_ERR_INVALID_ARG;
+    if (kv->n_kv_heads > (1 << 16)) return CATS_ERR_UNSUPPORTED;
+    if (rows == 0 || n_seqs == 0) return rows == 0 ? CATS_OK : CATS_ERR_INVALID_ARG;
+    if (!d_pos || !d_k_out || !d_v_out || !d_status || misaligned(d_pos, 4) || misaligned(d_seq, 4) || misaligned(d_status, 4)) return CATS_ERR_INVALID_ARG;
+    if (misaligned(d_k_out, type_size(out_type)) || misaligned(d_v_out, type_size(out_type))) return CATS_ERR_INVALID_ARG;
+    PagedRows r = {};
+    r.seq = d_seq; r.pos = d_pos; r.rows = rows; r.f32 = out_type == CATS_F32; r.k_out = d_k_out; r.v_out = d_v_out; r.ldk = ldk; r.ldv = ldv;
+    r.d_status = d_status;
+    CATS_CUDA(launch_paged_read(c, r, kv->type == CATS_I8, kv->head_dim, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+static bool paged_heads_ok(int32_t n_seqs, int32_t n_heads, int32_t n_kv, int32_t hd) {
+    return n_seqs >= 0 && n_heads >= 1 && n_kv >= 1 && n_heads % n_kv == 0 && n_heads <= (1 << 16) && (hd == 64 || hd == 128) &&
+           (int64_t)n_seqs * n_heads <= (1 << 24);
+}
+
+size_t cats_paged_workspace_bytes(int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+    return paged_heads_ok(n_seqs, n_heads, n_kv_heads, head_dim) ? align_up(paged_attn_workspace(n_seqs, n_heads, n_kv_heads, head_dim), 1024) : 0;
+}
+
+int cats_paged_attention(const cats_paged_kv* kv, const int32_t* d_table, int64_t ld_table, int32_t table_width, const int32_t* d_len,
+                         int32_t n_seqs, const void* d_q, int64_t ldq, int32_t n_heads, float scale, void* d_out, int64_t ldo, void* d_ws,
+                         size_t ws_bytes, int32_t* d_status, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_paged_attention");
+    g_call_boundary = true;
+    g_call_overlaps = true;
+    PagedDev c = {};
+    const int rc = paged_dev(kv, d_table, ld_table, table_width, n_seqs, c);
+    if (rc) return rc;
+    if (n_heads < 1 || n_heads % kv->n_kv_heads) return CATS_ERR_INVALID_ARG;
+    if (!paged_heads_ok(n_seqs, n_heads, kv->n_kv_heads, kv->head_dim)) return CATS_ERR_UNSUPPORTED;
+    const int64_t cols = (int64_t)n_heads * kv->head_dim;
+    if (ldq < cols || ldo < cols || ldq % 8 || ldo % 2 || !(scale >= -3.4e38f && scale <= 3.4e38f)) return CATS_ERR_INVALID_ARG;
+    if (n_seqs == 0) return CATS_OK;
+    if (!d_len || !d_q || !d_out || !d_ws || !d_status || misaligned(d_len, 4) || misaligned(d_q, 16) || misaligned(d_out, 4) || misaligned(d_status, 4))
+        return CATS_ERR_INVALID_ARG;
+    if (misaligned(d_ws, 1024) || ws_bytes < cats_paged_workspace_bytes(n_seqs, n_heads, kv->n_kv_heads, kv->head_dim)) return CATS_ERR_WORKSPACE;
+    PagedAttn a = {d_len, (const uint16_t*)d_q, ldq, n_heads, scale, (uint16_t*)d_out, ldo, d_ws, d_status};
+    CATS_CUDA(launch_paged_attn(c, a, kv->type == CATS_I8, kv->head_dim, (cudaStream_t)stream));
+    return CATS_OK;
+}
+
+// ---- sampling ------------------------------------------------------------------------------------
+
+int cats_sample(const void* d_logits, int32_t type, int64_t ld, int32_t logit_rows, int32_t vocab, const int32_t* d_row, int32_t rows,
+                const float* d_temperature, const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, const float* d_u,
+                int32_t* d_token, float* d_prob, int32_t* d_status, void* stream) {
+    g_launch_count = 0;
+    NvtxRange nvtx_range("cats_sample");
+    g_call_boundary = true;
+    g_call_overlaps = true;
+    if (bad_type(type) || logit_rows < 0 || vocab < 1 || ld < vocab || rows < 0 || (!d_row && rows > logit_rows)) return CATS_ERR_INVALID_ARG;
+    if (vocab > kMaxSampleVocab) return CATS_ERR_UNSUPPORTED;
+    if (rows == 0) return CATS_OK;
+    if (!d_logits || !d_u || !d_token || !d_status || misaligned(d_logits, type_size(type))) return CATS_ERR_INVALID_ARG;
+    const void* words[] = {d_row, d_temperature, d_top_k, d_top_p, d_min_p, d_u, d_token, d_prob, d_status};
+    for (const void* w : words) if (misaligned(w, 4)) return CATS_ERR_INVALID_ARG;
+    SampleDev p = {};
+    p.logits = d_logits; p.f32 = type == CATS_F32; p.ld = ld; p.logit_rows = logit_rows; p.vocab = vocab; p.row = d_row; p.rows = rows;
+    p.temperature = d_temperature; p.top_k = d_top_k; p.top_p = d_top_p; p.min_p = d_min_p; p.u = d_u; p.token = d_token; p.prob = d_prob;
+    p.d_status = d_status;
+    CATS_CUDA(launch_sample(p, (cudaStream_t)stream));
     return CATS_OK;
 }
 

@@ -8,12 +8,11 @@
 // Bound by HBM for many rows and by latency (one trip to memory, one block-wide reduction) for the few rows of a tree.
 // A row is read once and stays in registers; the norm needs sum x^2 and max|x g|, which are independent of each other, so
 // both go through ONE reduction: y = (x g) r with r > 0 has its maximum where |x g| has.  The maxima keep NaNs.
+#include "cats_i8.cuh"
 #include "cats_kernels.cuh"
 
 namespace cats {
 namespace {
-
-constexpr float kTinyMax = 7.888609052210118e-31f;    // 2^-100: the smallest maximum a scale is made from
 
 // Eight elements of a row as they lie in memory, 16 bytes each.  Loads and conversion are apart so that a thread can have all
 // its loads in flight before it uses the first.  Rows are read once and marked so: left to age among them, the int8 rows
@@ -137,20 +136,6 @@ __device__ __forceinline__ void warp_store(uint16_t* row, int c0, int cols, floa
     __syncwarp();
 }
 
-// rint(127 v / a) as bytes, v = y rs; |v| <= a, so the result is within 127 whatever rs and a are.
-// One bf16 element in a thousand is a tie, 127 v / a an exact half, and v fl(127 / a) puts it on either side of the half (one in 1900
-// elements a step off).  So the factor is kept in two parts, hi + lo = 127 / a to 2^-29 or better, and fma(v, hi, v lo) rounds the
-// quotient once: one that fp32 holds, a tie among them, is exact.  SwiGLU's values have several roundings behind them and
-// no exact ties: they take hi alone (the second part took 7 us more for 4096 x 11008 and its values).  Two instructions per element
-// more than hi alone: 22016 x 4096 bf16 and its values 82.6 -> 84.2 us, norm of 8191 x 4096 53.3 either way.
-// Rounding to a whole number: the sum with 1.5 * 2^23 leaves it (ties to even) in the low bits; the conversion instruction has
-// a sixteenth of the FMA rate and shares its unit with ex2 and rcp.
-constexpr float kRintMagic = 12582912.f;
-struct Factor { float hi, lo; };
-__device__ __forceinline__ Factor factor_127_over(float a) {
-    const float hi = 127.f / a;
-    return {hi, fmaf(-hi, a, 127.f) * (hi * (1.f / 127.f))};      // the remainder of the division, over a
-}
 template <int OP, bool GRID> __device__ __forceinline__ void store_q(int8_t* row, int c, int cols, bool vec, const float* y, float rs, const Factor& f) {
     uint32_t w[8];
 #pragma unroll
@@ -171,7 +156,6 @@ template <int OP, bool GRID> __device__ __forceinline__ void store_q(int8_t* row
     }
 }
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 // max(m, |a|, |b|), NaN if any of them is
 __device__ __forceinline__ float max_abs(float m, float a, float b) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));

@@ -224,4 +224,50 @@ size_t packed_weight_i8_bytes(int rows, int cols);
 cudaError_t launch_pack_weights_i8(const int8_t* src, long long ld, int rows, int cols, void* dst, cudaStream_t st);
 cudaError_t set_wait_limit_i8(unsigned long long ns);
 
+// ---- paged cache -----------------------------------------------------------------------------------
+struct PagedDev;        // cats_paged.cuh
+struct PagedRows {      // rows in (append) or out (read): rows of heads, row strides in elements
+    const int32_t *seq, *pos;
+    int rows, n_heads, f32;             // f32: type of q, k and v, or of what is read back; else bf16
+    const void *q, *k, *v;
+    long long ldq, ldk, ldv;
+    uint16_t* q_out;
+    long long ldqo;
+    float rope_base;
+    void *k_out, *v_out;
+    int32_t* d_status;
+};
+cudaError_t launch_paged_append(const PagedDev& c, const PagedRows& r, int i8, int hd, cudaStream_t st);
+cudaError_t launch_paged_read(const PagedDev& c, const PagedRows& r, int i8, int hd, cudaStream_t st);
+struct PagedAttn {
+    const int32_t* len;
+    const uint16_t* q;
+    long long ldq;
+    int n_heads;
+    float scale;
+    uint16_t* out;
+    long long ldo;
+    void* ws;
+    int32_t* d_status;
+};
+size_t paged_attn_workspace(int n_seqs, int n_heads, int n_kv, int hd);
+cudaError_t launch_paged_attn(const PagedDev& c, const PagedAttn& a, int i8, int hd, cudaStream_t st);
+
+// ---- sampling --------------------------------------------------------------------------------------
+constexpr int kMaxSampleVocab = 1 << 18;
+struct SampleDev {
+    const void* logits;
+    int f32;
+    long long ld;
+    int logit_rows, vocab;
+    const int32_t* row;
+    int rows;
+    const float *temperature, *top_p, *min_p, *u;
+    const int32_t* top_k;
+    int32_t* token;
+    float* prob;
+    int32_t* d_status;
+};
+cudaError_t launch_sample(const SampleDev& p, cudaStream_t st);
+
 }  // namespace cats
