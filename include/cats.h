@@ -477,7 +477,7 @@ int cats_paged_read(const cats_paged_kv *kv, const int32_t *d_table, int64_t ld_
  * q [n_seqs][n_heads*head_dim] bf16 (rotated: cats_paged_append's d_q_out), out likewise;
  * q starts on 16 bytes and ldq is a multiple of 8, out on 4 and ldo of 2.
  * n_heads is a multiple of n_kv_heads.  d_len[s] <= 0: the row of out is zeros.  Lengths
- * past table_width * page_size are cut there and reported.  Scores and softmax are fp32, the
+ * past table_width * page_size, or 2^31 - 1024, are cut there and reported.  Scores and softmax are fp32, the
  * probabilities enter the second product with 16 significant bits over a bf16 cache and with 11
  * over an int8 cache.  Rows behind a sequence's length are not read.
  * Workspace: cats_paged_workspace_bytes (0 for arguments that are refused), 1024-byte

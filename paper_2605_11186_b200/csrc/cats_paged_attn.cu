@@ -1,80 +1,601 @@
 // Attention of one new token per sequence over the paged cache (include/cats.h: cats_paged_attention):
 //   out[s][h] = sum_t softmax_t(q[s][h] . k[t][g] scale) v[t][g],   g = h / (n_heads / n_kv_heads)
-// A block per (sequence, query head); its warps take the rows in turn, one pass with a running maximum and sum each, and join at the end.
+//
+// Bound by reading K and V once.  The query heads of a group share every row, so both products are matrix products whose small
+// side is the group: S^T = K Q^T (16 rows x head_dim x 8 heads per instruction) and O^T = V^T P^T.  mma.sync takes the cache's
+// rows as its 16-row operand straight from the registers they were loaded into, 16 bytes at a time: both products may run over
+// channels and rows in any order, so a thread's 16 bytes are 8 (int8: 16) neighbouring channels of a row, and nothing of K or V
+// passes through shared memory.  (tcgen05 would want a tile of 128 rows in shared memory for 8 columns of work; at the rate
+// HBM delivers rows the 8-column products take a tenth of the issue slots.)
+//
+// One pass with a running maximum and sum per head and warp.  Probabilities enter the second product as two bf16 parts (16
+// bits) over a bf16 cache.  An int8 cache's bytes are whole numbers in fp16, exact; the row's scale is part of the weight
+// w = p scale_v, which is rounded to fp16: the running maximum is that of score + log2 scale_v, so that w is at most 1, times 2^15, and
+// what is 2^-28 of the largest is still a normal number (a long flat tail behind one large row keeps its bits).
+//
+// Work: the rows of every (sequence, head group) are cut into units of 4 tiles; all units in one line are dealt out evenly to the
+// blocks, three per SM (12 warps with 8 KB of rows in flight each; HBM needs about 45 KB per SM).  A block of four warps takes
+// its units sequence by sequence, the warps tile by tile, and joins its warps through shared memory.  What one block has of a
+// head group that others have rows of goes to the workspace; the last to arrive (a counter) adds the parts in order of their rows,
+// so the result does not depend on who that is.  More than kGroup parts are added in two steps.  No block ever waits for another.
 #include "cats_paged.cuh"
 
 namespace cats {
 namespace {
 
-template <int HD, bool I8> __device__ __forceinline__ void row_values(const uint8_t* p, int lane, float* v) {
-    constexpr int N = HD / 32;
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = I8 ? (float)reinterpret_cast<const int8_t*>(p)[lane * N + i] : bf16_bits_to_float(reinterpret_cast<const uint16_t*>(p)[lane * N + i]);
-}
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kBlocksPerSm = 3, kMaxBlocks = 148 * kBlocksPerSm;
+constexpr int kGroup = 24;          // parts added at once; kGroup^2 >= kMaxBlocks
+constexpr int kMaxHeads = 16;       // query heads per block
+constexpr int kMaxLen = INT32_MAX - 1023;       // a tile's rows behind the last one are still numbers
+constexpr uint32_t kNoRow = 0xFFFFFFFFu;
+static_assert(kGroup * kGroup >= kMaxBlocks, "two steps have to do");
 
-template <int HD, bool I8> __global__ void __launch_bounds__(128) k_paged_attn(const PagedDev c, const PagedAttn a) {
-    constexpr int N = HD / 32;
-    __shared__ float m_s[4], l_s[4], o_s[4][HD];
+// Workspace: two part slots per block (a head group that began before its first unit, one that goes on behind its last), then counters.  A
+// block is the first of at most one head group that goes on in the next, and a later one of at most one: a counter each.
+constexpr size_t kSlotFloats = (size_t)kMaxHeads * (128 + 2);
+struct Slots {
+    float* part;
+    int* counters;              // zero between calls
+    __device__ __forceinline__ int* first(int block) const { return counters + block; }                       // parts that begin with a first block's
+    __device__ __forceinline__ int* later(int block) const { return counters + kMaxBlocks + block; }          // with a later one's
+    __device__ __forceinline__ int* groups(int block) const { return counters + 2 * kMaxBlocks + block; }     // sums of kGroup parts, by first block
+    __device__ __forceinline__ float* o(int slot) const { return part + (size_t)slot * kSlotFloats; }
+    __device__ __forceinline__ float2* ml(int slot) const { return reinterpret_cast<float2*>(part + (size_t)slot * kSlotFloats + kMaxHeads * 128); }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+template <bool I8> __device__ __forceinline__ void mma(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (I8)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Bytes 0 and 1 (which = 0x4140) or 2 and 3 (0x4342) of w, each 128 more than the number it stands for, as fp16: 0x6400 + b is 1024 + b
+__device__ __forceinline__ uint32_t f16_of_bytes(uint32_t w, uint32_t which) {
+    uint32_t r, x = __byte_perm(w, 0x64646464u, which);
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x64806480u));
+    return r;
+}
+__device__ __forceinline__ uint32_t word_of(const uint4& a, int i) { return i == 0 ? a.x : (i == 1 ? a.y : (i == 2 ? a.z : a.w)); }
+
+template <int HD, bool I8, int NT> struct Attn {
+    static constexpr int kTile = I8 ? (NT == 1 ? 32 : 16) : (HD == 128 ? 16 : (NT == 1 ? 32 : 16));      // rows per warp and step
+    static constexpr int kUnit = kTile * kWarps;
+    static constexpr int kBlk = kTile / 16;
+    static constexpr int KI = HD * (I8 ? 1 : 2) / 64;       // 16-byte pieces of a K row per thread
+    static constexpr int VI = I8 ? 1 : HD / 64;             // and of a V row (int8, 64 channels: 8 bytes)
+    static constexpr int MT = HD / 16;                      // 16-channel tiles of O^T
+    static constexpr int QV = HD / 32;                      // 16-byte pieces of the queries per thread and 8 heads
+    static constexpr int kPad = HD + 4;
+    struct Shared {
+        uint4 q[NT][QV][32];
+        float o[kWarps][NT * 8][kPad];
+        float2 ml[kWarps][NT * 8];
+        float2 parts[kGroup][NT * 8];
+        long long total, before;        // units of all sequences, and of those in front of `seq`
+        int seq, last;
+        long long warp_sum[kWarps];
+    };
+
+    const PagedDev& c;
+    const PagedAttn& a;
+    Shared& sh;
+    const int lane, warp, g, j;
+    float acc[NT][MT][4];
+    float m[NT][2], l[NT][2], qf[NT][2];       // heads 2j and 2j + 1 of each 8: reference, sum, factor of the scores
+    uint4 kr[kBlk * 2][KI], vr[kBlk * 4][VI];
+
+    __device__ __forceinline__ Attn(const PagedDev& c_, const PagedAttn& a_, Shared& s_)
+        : c(c_), a(a_), sh(s_), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), g((threadIdx.x & 31) >> 2), j(threadIdx.x & 3) {}
+
+    // A row of the tile per lane: where it lies, and (int8) its scales.
+    struct Rows {
+        uint32_t at;
+        float ks, vs;
+    };
+    __device__ __forceinline__ Rows rows_of(int s, int kvh, int t, int t1) const {
+        Rows r = {kNoRow, 0.f, 0.f};
+        PagedDev::Row p;
+        if ((kTile == 32 || lane < kTile) && t + lane < t1) {
+            if (c.locate(s, t + lane, p)) {
+                r.at = p.at;
+                if (I8) {
+                    r.ks = __ldcg(c.ks + (size_t)p.s + (size_t)kvh * c.s_head);
+                    r.vs = __ldcg(c.vs + (size_t)p.s + (size_t)kvh * c.s_head);
+                }
+            } else {
+                report(a.d_status, CATS_ERR_INVALID_ARG);
+            }
+        }
+        return r;
+    }
+    __device__ __forceinline__ void load_k(const uint8_t* k, uint32_t at) {
+#pragma unroll
+        for (int b = 0; b < kBlk * 2; ++b) {
+            const uint32_t r = __shfl_sync(0xffffffffu, at, b * 8 + g);
+            const uint8_t* const p = k + (size_t)r * 16 + j * 16;
+#pragma unroll
+            for (int i = 0; i < KI; ++i) kr[b][i] = r != kNoRow ? __ldcg(reinterpret_cast<const uint4*>(p + i * 64)) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void load_v(const uint8_t* v, uint32_t at) {
+#pragma unroll
+        for (int n = 0; n < kBlk * 4; ++n) {
+            const uint32_t r = __shfl_sync(0xffffffffu, at, (n >> 2) * 16 + ((n & 2) ? 8 : 0) + 2 * j + (n & 1));
+            const uint8_t* const p = v + (size_t)r * 16;
+            if (I8 && HD == 64) {
+                uint2 w = make_uint2(0, 0);
+                if (r != kNoRow) w = __ldcg(reinterpret_cast<const uint2*>(p + g * 8));
+                vr[n][0] = make_uint4(w.x, w.y, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VI; ++i) vr[n][i] = r != kNoRow ? __ldcg(reinterpret_cast<const uint4*>(p + g * 16 + i * 128)) : make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
+
+    // The queries of `heads` heads from `head0` on, as the second operand of K Q^T: thread (g, j) holds of head g the channels that
+    // thread (any, j) holds of a K row.  int8: as fp16, times a power of two that brings the head's largest to 2^14: exact down to 2^-28 of it.
+    __device__ __forceinline__ void load_q(int s, int head0, int heads) {
+        const float base = a.scale * 1.4426950408889634f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int h = nt * 8 + g;
+            const uint16_t* const q = a.q + s * a.ldq + (size_t)(head0 + h) * HD;
+            uint4 x[QV];
+#pragma unroll
+            for (int i = 0; i < QV; ++i) {
+                const int ch = I8 ? (i >> 1) * 64 + j * 16 + (i & 1) * 8 : i * 32 + j * 8;
+                x[i] = h < heads ? __ldcg(reinterpret_cast<const uint4*>(q + ch)) : make_uint4(0, 0, 0, 0);
+            }
+            float mine = base;
+            if (I8) {
+                uint32_t mx = 0;
+#pragma unroll
+                for (int i = 0; i < QV; ++i)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) mx = max(mx, max((word_of(x[i], w) << 16) & 0x7FFF0000u, word_of(x[i], w) & 0x7FFF0000u));
+                mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                const int e = (int)(mx >> 23);                      // biased exponent; zero and subnormals, infinities and NaN: factor 1
+                const int up = e > 0 && e < 255 ? 141 - e : 0;      // e - 127 + up = 14
+                // 2^up in two factors: up reaches 140
+                const float f0 = __int_as_float((127 + up / 2) << 23), f1 = __int_as_float((127 + up - up / 2) << 23);
+#pragma unroll
+                for (int i = 0; i < QV; ++i) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t y = word_of(x[i], w);
+                        o[w] = pack_f16x2(__uint_as_float(y << 16) * f0 * f1, __uint_as_float(y & 0xFFFF0000u) * f0 * f1);
+                    }
+                    x[i] = make_uint4(o[0], o[1], o[2], o[3]);
+                }
+                mine = base / f0 / f1;
+            }
+            if (warp == (nt & (kWarps - 1))) {
+#pragma unroll
+                for (int i = 0; i < QV; ++i) sh.q[nt][i][lane] = x[i];
+            }
+            qf[nt][0] = __shfl_sync(0xffffffffu, mine, (2 * j) * 4);
+            qf[nt][1] = __shfl_sync(0xffffffffu, mine, (2 * j + 1) * 4);
+        }
+    }
+
+    // One tile: scores, weights, O^T.  next: where the next tile's rows lie; its K is requested as soon as this one's is used up.
+    __device__ __forceinline__ void step(const Rows& r, const uint8_t* k, const uint8_t* v, uint32_t next, bool more) {
+        float s[NT][kBlk][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nt][b][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < KI; ++i) {
+            if (I8) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+#pragma unroll
+                    for (int b = 0; b < kBlk; ++b) {
+                        const uint32_t x = word_of(kr[2 * b][i], w) ^ 0x80808080u, y = word_of(kr[2 * b + 1][i], w) ^ 0x80808080u;
+                        const uint32_t a0 = f16_of_bytes(x, 0x4140), a1 = f16_of_bytes(y, 0x4140), a2 = f16_of_bytes(x, 0x4342), a3 = f16_of_bytes(y, 0x4342);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint4 q = sh.q[nt][i * 2 + (w >> 1)][lane];
+                            mma<I8>(s[nt][b], a0, a1, a2, a3, w & 1 ? q.z : q.x, w & 1 ? q.w : q.y);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint4 q = sh.q[nt][i][lane];
+#pragma unroll
+                    for (int b = 0; b < kBlk; ++b) {
+                        mma<I8>(s[nt][b], kr[2 * b][i].x, kr[2 * b + 1][i].x, kr[2 * b][i].y, kr[2 * b + 1][i].y, q.x, q.y);
+                        mma<I8>(s[nt][b], kr[2 * b][i].z, kr[2 * b + 1][i].z, kr[2 * b][i].w, kr[2 * b + 1][i].w, q.z, q.w);
+                    }
+                }
+            }
+        }
+        if (more) load_k(k, next);
+        // scores in log2, and what the running reference is the maximum of: for int8 with the row's log2 scale_v (no less than the scale of a row of zeros)
+        float vs[kBlk][2], ref[kBlk][2];
+        const float lv = I8 ? lg2(fmaxf(fabsf(r.vs), 6.2e-33f)) : 0.f, bias = r.at == kNoRow ? -INFINITY : 0.f;
+#pragma unroll
+        for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = b * 16 + h * 8 + g;
+                const float ks = I8 ? __shfl_sync(0xffffffffu, r.ks, row) : 1.f, none = __shfl_sync(0xffffffffu, bias, row);
+                vs[b][h] = I8 ? __shfl_sync(0xffffffffu, r.vs * 32768.f, row) : 1.f;
+                ref[b][h] = I8 ? __shfl_sync(0xffffffffu, lv, row) : 0.f;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) s[nt][b][h * 2 + e] = s[nt][b][h * 2 + e] * qf[nt][e] * ks + none;
+            }
+        bool moved = false;
+        float keep[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x = s[nt][0][e] + ref[0][0];
+#pragma unroll
+                for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) x = fmaxf(x, s[nt][b][h * 2 + e] + ref[b][h]);
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                x = fmaxf(x, m[nt][e]);
+                keep[nt][e] = 1.f;
+                if (x != m[nt][e]) {
+                    keep[nt][e] = ex2(m[nt][e] - x);
+                    m[nt][e] = x;
+                    moved = true;
+                }
+            }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[nt][t][e] *= keep[nt][e & 1];
+                l[nt][0] *= keep[nt][0];
+                l[nt][1] *= keep[nt][1];
+            }
+        }
+        // weights, turned into the second operand of V^T P^T: heads along the lanes' groups, rows along a thread
+        uint32_t p[NT][kBlk][2], lo[NT][kBlk][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+#pragma unroll
+            for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float p0 = ex2(s[nt][b][h * 2] - m0), p1 = ex2(s[nt][b][h * 2 + 1] - m1);
+                    l[nt][0] += p0;
+                    l[nt][1] += p1;
+                    if (I8) {
+                        p[nt][b][h] = transpose8x8(pack_f16x2(p0 * vs[b][h], p1 * vs[b][h]));
+                    } else {
+                        const uint32_t hi = pack_bf16x2(p0, p1);
+                        lo[nt][b][h] = transpose8x8(pack_bf16x2(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xFFFF0000u)));
+                        p[nt][b][h] = transpose8x8(hi);
+                    }
+                }
+        }
+#pragma unroll
+        for (int b = 0; b < kBlk; ++b) {
+            if (I8) {
+#pragma unroll
+                for (int w = 0; w < HD / 32; ++w) {
+                    uint32_t x[2], y[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t t0 = word_of(vr[b * 4 + h * 2][0], w) ^ 0x80808080u, t1 = word_of(vr[b * 4 + h * 2 + 1][0], w) ^ 0x80808080u;
+                        x[h] = __byte_perm(t0, t1, 0x5140);
+                        y[h] = __byte_perm(t0, t1, 0x7362);
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t z0 = half ? y[0] : x[0], z1 = half ? y[1] : x[1];
+                        const uint32_t a0 = f16_of_bytes(z0, 0x4140), a1 = f16_of_bytes(z0, 0x4342), a2 = f16_of_bytes(z1, 0x4140), a3 = f16_of_bytes(z1, 0x4342);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma<I8>(acc[nt][w * 2 + half], a0, a1, a2, a3, p[nt][b][0], p[nt][b][1]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VI; ++i)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t t0 = word_of(vr[b * 4][i], w), t1 = word_of(vr[b * 4 + 1][i], w), t2 = word_of(vr[b * 4 + 2][i], w), t3 = word_of(vr[b * 4 + 3][i], w);
+                        const uint32_t a0 = __byte_perm(t0, t1, 0x5410), a1 = __byte_perm(t0, t1, 0x7632), a2 = __byte_perm(t2, t3, 0x5410), a3 = __byte_perm(t2, t3, 0x7632);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma<I8>(acc[nt][i * 4 + w], a0, a1, a2, a3, p[nt][b][0], p[nt][b][1]);
+                            mma<I8>(acc[nt][i * 4 + w], a0, a1, a2, a3, lo[nt][b][0], lo[nt][b][1]);
+                        }
+                    }
+            }
+        }
+        if (more) load_v(v, next);
+    }
+    // Channel of row g of tile t of O^T; row g + 8 is the next one.
+    __device__ __forceinline__ int channel(int t) const { return I8 ? g * (HD / 8) + 2 * t : (t >> 2) * 64 + g * 8 + (t & 3) * 2; }
+
+    // Rows t0 .. t1 - 1 of a sequence for `heads` heads: leaves what the block has of them in sh.o and sh.ml, one entry per warp that had rows.
+    __device__ __forceinline__ int rows(int s, int kvh, int head0, int heads, int t0, int t1) {
+        const uint8_t* const k = c.k + (size_t)kvh * c.head16 * 16;
+        const uint8_t* const v = c.v + (size_t)kvh * c.head16 * 16;
+        load_q(s, head0, heads);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[nt][t][e] = 0.f;
+        }
+        const int active = min(kWarps, (t1 - t0 + kTile - 1) / kTile);
+        int t = t0 + warp * kTile;
+        Rows now = rows_of(s, kvh, t, t1);
+        if (t < t1) {
+            load_k(k, now.at);
+            load_v(v, now.at);
+        }
+        Rows next = rows_of(s, kvh, t + kUnit, t1);
+        __syncthreads();            // the queries are there
+        for (; t < t1; t += kUnit) {
+            const bool more = t + kUnit < t1;
+            const Rows after = rows_of(s, kvh, t + 2 * kUnit, t1);
+            step(now, k, v, next.at, more);
+            now = next;
+            next = after;
+        }
+        if (warp < active) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], o);
+                if (g == 0) {
+                    sh.ml[warp][nt * 8 + 2 * j] = make_float2(m[nt][0], l[nt][0]);
+                    sh.ml[warp][nt * 8 + 2 * j + 1] = make_float2(m[nt][1], l[nt][1]);
+                }
+#pragma unroll
+                for (int t2 = 0; t2 < MT; ++t2) {
+                    *reinterpret_cast<float2*>(&sh.o[warp][nt * 8 + 2 * j][channel(t2)]) = make_float2(acc[nt][t2][0], acc[nt][t2][2]);
+                    *reinterpret_cast<float2*>(&sh.o[warp][nt * 8 + 2 * j + 1][channel(t2)]) = make_float2(acc[nt][t2][1], acc[nt][t2][3]);
+                }
+            }
+        }
+        __syncthreads();
+        return active;
+    }
+
+    __device__ __forceinline__ static float factor(float mi, float top) { return ex2(mi - (top == -INFINITY ? 0.f : top)); }
+    __device__ __forceinline__ void store_out(int s, int head, int ch, const float4& x, float sum, bool empty) {
+        const float f = empty ? 0.f : (I8 ? 1.f / 32768.f : 1.f) / sum;
+        uint32_t* const o = reinterpret_cast<uint32_t*>(a.out + s * a.ldo + (size_t)head * HD + ch);
+        o[0] = empty ? 0u : pack_bf16x2(x.x * f, x.y * f);
+        o[1] = empty ? 0u : pack_bf16x2(x.z * f, x.w * f);
+    }
+    static __device__ __forceinline__ void add(float4& x, const float4& y, float f) {
+        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+    }
+
+    // The block's warps joined: to `slot`, or (slot < 0) to the output.
+    __device__ __forceinline__ void join(int s, int head0, int heads, int active, const Slots& w, int slot) {
+        for (int i = threadIdx.x; i < heads * (HD / 4); i += kThreads) {
+            const int h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
+            float top = -INFINITY, sum = 0.f;
+            for (int k = 0; k < active; ++k) top = fmaxf(top, sh.ml[k][h].x);
+            float4 x = make_float4(0, 0, 0, 0);
+            for (int k = 0; k < active; ++k) {
+                const float f = factor(sh.ml[k][h].x, top);
+                sum = fmaf(sh.ml[k][h].y, f, sum);
+                add(x, *reinterpret_cast<const float4*>(&sh.o[k][h][ch]), f);
+            }
+            if (slot < 0) {
+                store_out(s, head0 + h, ch, x, sum, active == 0);
+            } else {
+                *reinterpret_cast<float4*>(w.o(slot) + h * HD + ch) = x;
+                if (ch == 0) w.ml(slot)[h] = make_float2(top, sum);
+            }
+        }
+        __syncthreads();            // the next rows may use sh.o
+    }
+
+    // Parts at slots slot_of(0) .. slot_of(n - 1) added in this order: to slot `to`, or (to < 0) to the output.
+    template <typename F> __device__ __forceinline__ void add_parts(int s, int head0, int heads, int n, F slot_of, const Slots& w, int to) {
+        for (int i = threadIdx.x; i < n * heads; i += kThreads) sh.parts[i / heads][i % heads] = __ldcg(w.ml(slot_of(i / heads)) + i % heads);
+        __syncthreads();
+        for (int i = threadIdx.x; i < heads * (HD / 4); i += kThreads) {
+            const int h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
+            float top = -INFINITY, sum = 0.f;
+            for (int k = 0; k < n; ++k) top = fmaxf(top, sh.parts[k][h].x);
+            float4 x = make_float4(0, 0, 0, 0);
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) {
+                const float f = factor(sh.parts[k][h].x, top);
+                sum = fmaf(sh.parts[k][h].y, f, sum);
+                add(x, __ldcg(reinterpret_cast<const float4*>(w.o(slot_of(k)) + h * HD + ch)), f);
+            }
+            if (to < 0) {
+                store_out(s, head0 + h, ch, x, sum, false);
+            } else {
+                *reinterpret_cast<float4*>(w.o(to) + h * HD + ch) = x;
+                if (ch == 0) w.ml(to)[h] = make_float2(top, sum);
+            }
+        }
+        __syncthreads();
+    }
+    // Whether this block is the last of n to come here; it then sees what the others wrote, and the counter is zero again.
+    __device__ __forceinline__ bool arrive(int* counter, int n) {
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            __threadfence();
+            const bool last = atomicAdd(counter, 1) == n - 1;
+            if (last) *counter = 0;
+            __threadfence();
+            sh.last = last;
+        }
+        __syncthreads();
+        return sh.last != 0;
+    }
+
+    __device__ __forceinline__ int length(int s) const {
+        const int asked = a.len[s];
+        const long long most = min((long long)c.width * c.page_size, (long long)kMaxLen);
+        if (asked > most) report(a.d_status, CATS_ERR_INVALID_ARG);
+        return (int)min((long long)max(asked, 0), most);
+    }
+    static __device__ __forceinline__ int units_of(int len) { return len > 0 ? (len - 1) / kUnit + 1 : 1; }
+
+    // The sequence that unit `first(total)` lies in, to sh.seq; sh.before: units per head group of those in front of it, sh.total: of all.
+    template <typename F> __device__ __forceinline__ void find(int groups, F first) {
+        const int each = (c.n_seqs + kThreads - 1) / kThreads, s0 = min(c.n_seqs, (int)threadIdx.x * each), s1 = min(c.n_seqs, s0 + each);
+        long long mine = 0;
+        for (int s = s0; s < s1; ++s) mine += units_of(length(s));
+        long long upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long t = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += t;
+        }
+        if (lane == 31) sh.warp_sum[warp] = upto;
+        __syncthreads();
+        long long total = 0;
+        for (int k = 0; k < kWarps; ++k) {
+            if (k < warp) upto += sh.warp_sum[k];
+            total += sh.warp_sum[k];
+        }
+        long long before = upto - mine;
+        const long long want = first(total * groups);
+        if (want >= before * groups && want < upto * groups) {
+            int s = s0;
+            for (;; ++s) {
+                const int n = units_of(length(s));
+                if (want < (before + n) * groups) break;
+                before += n;
+            }
+            sh.seq = s;
+            sh.before = before;
+        }
+        if (threadIdx.x == 0) sh.total = total * groups;
+        __syncthreads();
+    }
+
+    __device__ __forceinline__ void run() {
+        const int per_kv = a.n_heads / c.n_kv, chunks = (per_kv + NT * 8 - 1) / (NT * 8), groups = c.n_kv * chunks;
+        const int me = blockIdx.x;
+        // block b of the first min(blocks, units) has units [b units / blocks, (b + 1) units / blocks)
+        auto blocks_for = [&](long long units) { return (long long)min((long long)gridDim.x, units); };
+        find(groups, [&](long long units) {
+            const long long n = blocks_for(units);
+            return me < n ? me * units / n : -1;
+        });
+        const long long units = sh.total, n_blocks = blocks_for(units);
+        if (me >= n_blocks) return;
+        long long u = me * units / n_blocks;
+        const long long u_end = (me + 1) * units / n_blocks;
+        auto block_of = [&](long long unit) { return (int)(((unit + 1) * n_blocks - 1) / units); };
+        const Slots w = {(float*)a.ws, (int*)((float*)a.ws + 2 * kMaxBlocks * kSlotFloats)};
+        int s = sh.seq;
+        long long base = sh.before * groups;         // first unit of sequence s
+        int len = length(s), n = units_of(len);
+        while (u < u_end) {
+            while (u >= base + (long long)n * groups) {
+                base += (long long)n * groups;
+                len = length(++s);
+                n = units_of(len);
+            }
+            const int group = (int)((u - base) / n), unit = (int)(u - base - (long long)group * n);
+            const int mine = (int)min((long long)(n - unit), u_end - u);
+            const int kvh = group / chunks, chunk = group % chunks, head0 = kvh * per_kv + chunk * NT * 8, heads = min(NT * 8, per_kv - chunk * NT * 8);
+            const int t0 = unit * kUnit, t1 = min((long long)len, (long long)(unit + mine) * kUnit);
+            const int active = rows(s, kvh, head0, heads, t0, t1);
+            if (mine == n) {
+                join(s, head0, heads, active, w, -1);
+            } else {
+                // blocks first .. last have rows of this head group; the first of them in its second slot
+                const int first = block_of(u - unit), last = block_of(u - unit + n - 1), parts = last - first + 1;
+                auto slot_of = [&](int k) { return 2 * (first + k) + (k == 0 ? 1 : 0); };
+                join(s, head0, heads, active, w, slot_of(me - first));
+                if (parts <= kGroup) {
+                    if (arrive(w.first(first), parts)) add_parts(s, head0, heads, parts, slot_of, w, -1);
+                } else {
+                    const int mine0 = (me - first) / kGroup * kGroup, size = min(kGroup, parts - mine0), n_groups = (parts + kGroup - 1) / kGroup;
+                    if (arrive(mine0 == 0 ? w.first(first) : w.later(first + mine0), size)) {
+                        add_parts(s, head0, heads, size, [&](int k) { return slot_of(mine0 + k); }, w, slot_of(mine0));
+                        if (arrive(w.groups(first), n_groups)) add_parts(s, head0, heads, n_groups, [&](int k) { return slot_of(k * kGroup); }, w, -1);
+                    }
+                }
+            }
+            u += mine;
+        }
+    }
+};
+
+template <int HD, bool I8, int NT> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_paged_attn(const __grid_constant__ PagedDev c, const __grid_constant__ PagedAttn a) {
+    __shared__ __align__(16) typename Attn<HD, I8, NT>::Shared sh;
     pdl_launch_dependents();
     pdl_wait();
-    const int s = blockIdx.x, h = blockIdx.y, g = h / (a.n_heads / c.n_kv), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const float scale = a.scale * 1.4426950408889634f;
-    const long long most = (long long)c.width * c.page_size;
-    const int asked = a.len[s], len = (int)min((long long)max(asked, 0), most);
-    if (asked > most && threadIdx.x == 0 && h == 0) report(a.d_status, CATS_ERR_INVALID_ARG);
-    float q[N], o[N], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        q[i] = bf16_bits_to_float(a.q[s * a.ldq + h * HD + lane * N + i]) * scale;
-        o[i] = 0.f;
-    }
-    for (int t = warp; t < len; t += 4) {
-        PagedDev::Row at;
-        if (!c.locate(s, t, at)) {
-            if (lane == 0) report(a.d_status, CATS_ERR_INVALID_ARG);
-            continue;
-        }
-        const size_t off = ((size_t)at.at + (size_t)g * c.head16) * 16, so = (size_t)at.s + (size_t)g * c.s_head;
-        float k[N], v[N], x = 0.f;
-        row_values<HD, I8>(c.k + off, lane, k);
-        row_values<HD, I8>(c.v + off, lane, v);
-#pragma unroll
-        for (int i = 0; i < N; ++i) x = fmaf(q[i], k[i], x);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        if (I8) x *= c.ks[so];
-        const float m1 = fmaxf(m, x), base = m1 == -INFINITY ? 0.f : m1, keep = exp2f(m - base), p = exp2f(x - base);
-        const float w = I8 ? p * c.vs[so] : p;
-        l = l * keep + p;
-#pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = fmaf(w, v[i], o[i] * keep);
-        m = m1;
-    }
-    if (lane == 0) { m_s[warp] = m; l_s[warp] = l; }
-#pragma unroll
-    for (int i = 0; i < N; ++i) o_s[warp][lane * N + i] = o[i];
-    __syncthreads();
-    if ((int)threadIdx.x < HD) {
-        const float top = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3])), base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f, acc = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = exp2f(m_s[w] - base);
-            sum += l_s[w] * f;
-            acc += o_s[w][threadIdx.x] * f;
-        }
-        a.out[s * a.ldo + h * HD + threadIdx.x] = float_to_bf16_bits(len > 0 ? acc / sum : 0.f);
-    }
+    Attn<HD, I8, NT>(c, a, sh).run();
+}
+
+template <int HD, bool I8, int NT> cudaError_t launch_k(const PagedDev& c, const PagedAttn& a, cudaStream_t st) {
+    typedef Attn<HD, I8, NT> A;
+    const long long per_kv = a.n_heads / c.n_kv, groups = c.n_kv * ((per_kv + NT * 8 - 1) / (NT * 8));
+    const long long most = (long long)c.width * c.page_size, units = (most - 1) / A::kUnit + 1;
+    const long long blocks = units >= kMaxBlocks ? kMaxBlocks : min((long long)kMaxBlocks, units * groups * c.n_seqs);
+    return launch_i8(k_paged_attn<HD, I8, NT>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, a);
 }
 
 }  // namespace
 
-size_t paged_attn_workspace(int n_seqs, int n_heads, int n_kv, int hd) { return 1024; }
+size_t paged_attn_workspace(int, int, int, int) { return 2 * kMaxBlocks * kSlotFloats * 4 + 3 * kMaxBlocks * sizeof(int); }
 
 cudaError_t launch_paged_attn(const PagedDev& c, const PagedAttn& a, int i8, int hd, cudaStream_t st) {
-    const dim3 grid((unsigned)c.n_seqs, (unsigned)a.n_heads);
-    if (hd == 128) return i8 ? launch_i8(k_paged_attn<128, true>, grid, dim3(128), 0, st, c, a) : launch_i8(k_paged_attn<128, false>, grid, dim3(128), 0, st, c, a);
-    return i8 ? launch_i8(k_paged_attn<64, true>, grid, dim3(128), 0, st, c, a) : launch_i8(k_paged_attn<64, false>, grid, dim3(128), 0, st, c, a);
+    // eight heads at a time while the group has no more: the accumulators of sixteen leave registers for half the rows in flight
+    const bool one = a.n_heads / c.n_kv <= 8;
+    if (hd == 128) {
+        if (i8) return one ? launch_k<128, true, 1>(c, a, st) : launch_k<128, true, 2>(c, a, st);
+        return one ? launch_k<128, false, 1>(c, a, st) : launch_k<128, false, 2>(c, a, st);
+    }
+    if (i8) return one ? launch_k<64, true, 1>(c, a, st) : launch_k<64, true, 2>(c, a, st);
+    return one ? launch_k<64, false, 1>(c, a, st) : launch_k<64, false, 2>(c, a, st);
 }
 
 }  // namespace cats
