@@ -89,9 +89,16 @@ template <int HD, bool I8, int NT> struct Attn {
     static constexpr int MT = HD / 16;                      // 16-channel tiles of O^T
     static constexpr int QV = HD / 32;                      // 16-byte pieces of the queries per thread and 8 heads
     static constexpr int kPad = HD + 4;
+    // A stage of a warp's ring: the 16-byte pieces in the order [piece][lane], then (int8) a scale of K and of V per row.
+    static constexpr int kVBytes = I8 && HD == 64 ? 8 : 16;
+    static constexpr int kV = kBlk * 2 * KI * 512, kScales = kV + kBlk * 4 * VI * 32 * kVBytes, kStage = kScales + (I8 ? 256 : 0);
+    static constexpr int kStages = kStage > 6000 ? 2 : 4;
     struct Shared {
+        union {
+            uint8_t ring[kWarps][kStages][kStage];
+            float o[kWarps][NT * 8][kPad];              // after the last row
+        };
         uint4 q[NT][QV][32];
-        float o[kWarps][NT * 8][kPad];
         float2 ml[kWarps][NT * 8];
         float2 parts[kGroup][NT * 8];
         long long total, before;        // units of all sequences, and of those in front of `seq`
@@ -105,55 +112,65 @@ template <int HD, bool I8, int NT> struct Attn {
     const int lane, warp, g, j;
     float acc[NT][MT][4];
     float m[NT][2], l[NT][2], qf[NT][2];       // heads 2j and 2j + 1 of each 8: reference, sum, factor of the scores
-    uint4 kr[kBlk * 2][KI], vr[kBlk * 4][VI];
 
     __device__ __forceinline__ Attn(const PagedDev& c_, const PagedAttn& a_, Shared& s_)
         : c(c_), a(a_), sh(s_), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), g((threadIdx.x & 31) >> 2), j(threadIdx.x & 3) {}
 
-    // A row of the tile per lane: where it lies, and (int8) its scales.
-    struct Rows {
+    // A row of a tile per lane: where it lies; kNoRow: nowhere, zeros are taken for it.
+    struct Row {
         uint32_t at;
-        float ks, vs;
+        uint32_t s;
     };
-    __device__ __forceinline__ Rows rows_of(int s, int kvh, int t, int t1) const {
-        Rows r = {kNoRow, 0.f, 0.f};
+    __device__ __forceinline__ Row row_of(int s, int t, int t1) const {
+        Row r = {kNoRow, 0};
         PagedDev::Row p;
         if ((kTile == 32 || lane < kTile) && t + lane < t1) {
-            if (c.locate(s, t + lane, p)) {
-                r.at = p.at;
-                if (I8) {
-                    r.ks = __ldcg(c.ks + (size_t)p.s + (size_t)kvh * c.s_head);
-                    r.vs = __ldcg(c.vs + (size_t)p.s + (size_t)kvh * c.s_head);
-                }
-            } else {
-                report(a.d_status, CATS_ERR_INVALID_ARG);
-            }
+            if (c.locate(s, t + lane, p)) r = {p.at, p.s};
+            else report(a.d_status, CATS_ERR_INVALID_ARG);
         }
         return r;
     }
-    __device__ __forceinline__ void load_k(const uint8_t* k, uint32_t at) {
+    template <int N> static __device__ __forceinline__ void copy(uint32_t to, const void* from, bool there) {
+        if (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(N), "r"(there ? N : 0) : "memory");
+    }
+    // Requests a tile.  What a thread copies of K and V is what it reads itself.
+    __device__ __forceinline__ void request(uint32_t stage, const Row& row, const uint8_t* k, const uint8_t* v, const float* ks, const float* vs) const {
 #pragma unroll
         for (int b = 0; b < kBlk * 2; ++b) {
-            const uint32_t r = __shfl_sync(0xffffffffu, at, b * 8 + g);
-            const uint8_t* const p = k + (size_t)r * 16 + j * 16;
+            const uint32_t r = __shfl_sync(0xffffffffu, row.at, b * 8 + g);
+            const uint8_t* const p = k + (r != kNoRow ? (size_t)r * 16 : 0) + j * 16;
 #pragma unroll
-            for (int i = 0; i < KI; ++i) kr[b][i] = r != kNoRow ? __ldcg(reinterpret_cast<const uint4*>(p + i * 64)) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < KI; ++i) copy<16>(stage + (b * KI + i) * 512 + lane * 16, p + i * 64, r != kNoRow);
         }
-    }
-    __device__ __forceinline__ void load_v(const uint8_t* v, uint32_t at) {
 #pragma unroll
         for (int n = 0; n < kBlk * 4; ++n) {
-            const uint32_t r = __shfl_sync(0xffffffffu, at, (n >> 2) * 16 + ((n & 2) ? 8 : 0) + 2 * j + (n & 1));
-            const uint8_t* const p = v + (size_t)r * 16;
-            if (I8 && HD == 64) {
-                uint2 w = make_uint2(0, 0);
-                if (r != kNoRow) w = __ldcg(reinterpret_cast<const uint2*>(p + g * 8));
-                vr[n][0] = make_uint4(w.x, w.y, 0, 0);
-            } else {
+            const uint32_t r = __shfl_sync(0xffffffffu, row.at, (n >> 2) * 16 + ((n & 2) ? 8 : 0) + 2 * j + (n & 1));
+            const uint8_t* const p = v + (r != kNoRow ? (size_t)r * 16 : 0) + g * kVBytes;
 #pragma unroll
-                for (int i = 0; i < VI; ++i) vr[n][i] = r != kNoRow ? __ldcg(reinterpret_cast<const uint4*>(p + g * 16 + i * 128)) : make_uint4(0, 0, 0, 0);
-            }
+            for (int i = 0; i < VI; ++i) copy<kVBytes>(stage + kV + ((n * VI + i) * 32 + lane) * kVBytes, p + i * 128, r != kNoRow);
         }
+        if (I8 && lane < kTile) {
+            copy<4>(stage + kScales + lane * 4, ks + row.s, row.at != kNoRow);
+            copy<4>(stage + kScales + 128 + lane * 4, vs + row.s, row.at != kNoRow);
+        }
+    }
+    static __device__ __forceinline__ uint4 lds16(uint32_t p) {
+        uint4 x;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(p) : "memory");
+        return x;
+    }
+    static __device__ __forceinline__ float lds_float(uint32_t p) {
+        float x;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(p) : "memory");
+        return x;
+    }
+    __device__ __forceinline__ uint4 k_piece(uint32_t stage, int b, int i) const { return lds16(stage + (b * KI + i) * 512 + lane * 16); }
+    __device__ __forceinline__ uint4 v_piece(uint32_t stage, int n, int i) const {
+        if (kVBytes == 16) return lds16(stage + kV + ((n * VI + i) * 32 + lane) * 16);
+        uint4 x = make_uint4(0, 0, 0, 0);
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(stage + kV + (n * 32 + lane) * 8) : "memory");
+        return x;
     }
 
     // The queries of `heads` heads from `head0` on, as the second operand of K Q^T: thread (g, j) holds of head g the channels that
@@ -204,8 +221,8 @@ template <int HD, bool I8, int NT> struct Attn {
         }
     }
 
-    // One tile: scores, weights, O^T.  next: where the next tile's rows lie; its K is requested as soon as this one's is used up.
-    __device__ __forceinline__ void step(const Rows& r, const uint8_t* k, const uint8_t* v, uint32_t next, bool more) {
+    // One tile: scores, weights, O^T.  left: rows of the sequence from the tile's first on.
+    __device__ __forceinline__ void step(uint32_t stage, int left) {
         float s[NT][kBlk][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -215,12 +232,15 @@ template <int HD, bool I8, int NT> struct Attn {
                 for (int e = 0; e < 4; ++e) s[nt][b][e] = 0.f;
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
+            uint4 kr[kBlk * 2];
+#pragma unroll
+            for (int b = 0; b < kBlk * 2; ++b) kr[b] = k_piece(stage, b, i);
             if (I8) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
 #pragma unroll
                     for (int b = 0; b < kBlk; ++b) {
-                        const uint32_t x = word_of(kr[2 * b][i], w) ^ 0x80808080u, y = word_of(kr[2 * b + 1][i], w) ^ 0x80808080u;
+                        const uint32_t x = word_of(kr[2 * b], w) ^ 0x80808080u, y = word_of(kr[2 * b + 1], w) ^ 0x80808080u;
                         const uint32_t a0 = f16_of_bytes(x, 0x4140), a1 = f16_of_bytes(y, 0x4140), a2 = f16_of_bytes(x, 0x4342), a3 = f16_of_bytes(y, 0x4342);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
@@ -235,24 +255,29 @@ template <int HD, bool I8, int NT> struct Attn {
                     const uint4 q = sh.q[nt][i][lane];
 #pragma unroll
                     for (int b = 0; b < kBlk; ++b) {
-                        mma<I8>(s[nt][b], kr[2 * b][i].x, kr[2 * b + 1][i].x, kr[2 * b][i].y, kr[2 * b + 1][i].y, q.x, q.y);
-                        mma<I8>(s[nt][b], kr[2 * b][i].z, kr[2 * b + 1][i].z, kr[2 * b][i].w, kr[2 * b + 1][i].w, q.z, q.w);
+                        mma<I8>(s[nt][b], kr[2 * b].x, kr[2 * b + 1].x, kr[2 * b].y, kr[2 * b + 1].y, q.x, q.y);
+                        mma<I8>(s[nt][b], kr[2 * b].z, kr[2 * b + 1].z, kr[2 * b].w, kr[2 * b + 1].w, q.z, q.w);
                     }
                 }
             }
         }
-        if (more) load_k(k, next);
         // scores in log2, and what the running reference is the maximum of: for int8 with the row's log2 scale_v (no less than the scale of a row of zeros)
         float vs[kBlk][2], ref[kBlk][2];
-        const float lv = I8 ? lg2(fmaxf(fabsf(r.vs), 6.2e-33f)) : 0.f, bias = r.at == kNoRow ? -INFINITY : 0.f;
 #pragma unroll
         for (int b = 0; b < kBlk; ++b)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = b * 16 + h * 8 + g;
-                const float ks = I8 ? __shfl_sync(0xffffffffu, r.ks, row) : 1.f, none = __shfl_sync(0xffffffffu, bias, row);
-                vs[b][h] = I8 ? __shfl_sync(0xffffffffu, r.vs * 32768.f, row) : 1.f;
-                ref[b][h] = I8 ? __shfl_sync(0xffffffffu, lv, row) : 0.f;
+                const float none = row < left ? 0.f : -INFINITY;
+                float ks = 1.f;
+                vs[b][h] = 1.f;
+                ref[b][h] = 0.f;
+                if (I8) {
+                    ks = lds_float(stage + kScales + row * 4);
+                    const float sv = lds_float(stage + kScales + 128 + row * 4);
+                    ref[b][h] = lg2(fmaxf(fabsf(sv), 6.2e-33f));
+                    vs[b][h] = sv * 32768.f;
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -315,12 +340,15 @@ template <int HD, bool I8, int NT> struct Attn {
 #pragma unroll
         for (int b = 0; b < kBlk; ++b) {
             if (I8) {
+                uint4 vr[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) vr[n] = v_piece(stage, b * 4 + n, 0);
 #pragma unroll
                 for (int w = 0; w < HD / 32; ++w) {
                     uint32_t x[2], y[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint32_t t0 = word_of(vr[b * 4 + h * 2][0], w) ^ 0x80808080u, t1 = word_of(vr[b * 4 + h * 2 + 1][0], w) ^ 0x80808080u;
+                        const uint32_t t0 = word_of(vr[h * 2], w) ^ 0x80808080u, t1 = word_of(vr[h * 2 + 1], w) ^ 0x80808080u;
                         x[h] = __byte_perm(t0, t1, 0x5140);
                         y[h] = __byte_perm(t0, t1, 0x7362);
                     }
@@ -334,10 +362,13 @@ template <int HD, bool I8, int NT> struct Attn {
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < VI; ++i)
+                for (int i = 0; i < VI; ++i) {
+                    uint4 vr[4];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) vr[n] = v_piece(stage, b * 4 + n, i);
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const uint32_t t0 = word_of(vr[b * 4][i], w), t1 = word_of(vr[b * 4 + 1][i], w), t2 = word_of(vr[b * 4 + 2][i], w), t3 = word_of(vr[b * 4 + 3][i], w);
+                        const uint32_t t0 = word_of(vr[0], w), t1 = word_of(vr[1], w), t2 = word_of(vr[2], w), t3 = word_of(vr[3], w);
                         const uint32_t a0 = __byte_perm(t0, t1, 0x5410), a1 = __byte_perm(t0, t1, 0x7632), a2 = __byte_perm(t2, t3, 0x5410), a3 = __byte_perm(t2, t3, 0x7632);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
@@ -345,9 +376,9 @@ template <int HD, bool I8, int NT> struct Attn {
                             mma<I8>(acc[nt][i * 4 + w], a0, a1, a2, a3, lo[nt][b][0], lo[nt][b][1]);
                         }
                     }
+                }
             }
         }
-        if (more) load_v(v, next);
     }
     // Channel of row g of tile t of O^T; row g + 8 is the next one.
     __device__ __forceinline__ int channel(int t) const { return I8 ? g * (HD / 8) + 2 * t : (t >> 2) * 64 + g * 8 + (t & 3) * 2; }
@@ -356,6 +387,17 @@ template <int HD, bool I8, int NT> struct Attn {
     __device__ __forceinline__ int rows(int s, int kvh, int head0, int heads, int t0, int t1) {
         const uint8_t* const k = c.k + (size_t)kvh * c.head16 * 16;
         const uint8_t* const v = c.v + (size_t)kvh * c.head16 * 16;
+        const float* const ks = c.ks + (size_t)kvh * c.s_head;
+        const float* const vs = c.vs + (size_t)kvh * c.s_head;
+        const uint32_t ring = smem_u32(sh.ring[warp]);
+        const int t = t0 + warp * kTile, tiles = t < t1 ? (t1 - t + kUnit - 1) / kUnit : 0;
+        // kStages - 1 tiles are on their way before the first is used; where the rows of one more lie is looked up a step ahead
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) {
+            if (i < tiles) request(ring + i * kStage, row_of(s, t + i * kUnit, t1), k, v, ks, vs);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        Row next = row_of(s, t + (kStages - 1) * kUnit, t1);
         load_q(s, head0, heads);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -367,21 +409,16 @@ template <int HD, bool I8, int NT> struct Attn {
                 for (int e = 0; e < 4; ++e) acc[nt][t][e] = 0.f;
         }
         const int active = min(kWarps, (t1 - t0 + kTile - 1) / kTile);
-        int t = t0 + warp * kTile;
-        Rows now = rows_of(s, kvh, t, t1);
-        if (t < t1) {
-            load_k(k, now.at);
-            load_v(v, now.at);
-        }
-        Rows next = rows_of(s, kvh, t + kUnit, t1);
         __syncthreads();            // the queries are there
-        for (; t < t1; t += kUnit) {
-            const bool more = t + kUnit < t1;
-            const Rows after = rows_of(s, kvh, t + 2 * kUnit, t1);
-            step(now, k, v, next.at, more);
-            now = next;
-            next = after;
+        for (int i = 0; i < tiles; ++i) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+            __syncwarp();           // also: all lanes are done with the stage that is filled next
+            if (i + kStages - 1 < tiles) request(ring + (i + kStages - 1) % kStages * kStage, next, k, v, ks, vs);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            next = row_of(s, t + (i + kStages) * kUnit, t1);
+            step(ring + i % kStages * kStage, t1 - (t + i * kUnit));
         }
+        __syncthreads();            // the ring is now sh.o
         if (warp < active) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -434,7 +471,7 @@ template <int HD, bool I8, int NT> struct Attn {
                 if (ch == 0) w.ml(slot)[h] = make_float2(top, sum);
             }
         }
-        __syncthreads();            // the next rows may use sh.o
+        __syncthreads();            // the ring is free
     }
 
     // Parts at slots slot_of(0) .. slot_of(n - 1) added in this order: to slot `to`, or (to < 0) to the output.
@@ -569,7 +606,8 @@ template <int HD, bool I8, int NT> struct Attn {
 };
 
 template <int HD, bool I8, int NT> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_paged_attn(const __grid_constant__ PagedDev c, const __grid_constant__ PagedAttn a) {
-    __shared__ __align__(16) typename Attn<HD, I8, NT>::Shared sh;
+    extern __shared__ __align__(16) uint8_t smem[];
+    typename Attn<HD, I8, NT>::Shared& sh = *reinterpret_cast<typename Attn<HD, I8, NT>::Shared*>(smem);
     pdl_launch_dependents();
     pdl_wait();
     Attn<HD, I8, NT>(c, a, sh).run();
@@ -580,7 +618,10 @@ template <int HD, bool I8, int NT> cudaError_t launch_k(const PagedDev& c, const
     const long long per_kv = a.n_heads / c.n_kv, groups = c.n_kv * ((per_kv + NT * 8 - 1) / (NT * 8));
     const long long most = (long long)c.width * c.page_size, units = (most - 1) / A::kUnit + 1;
     const long long blocks = units >= kMaxBlocks ? kMaxBlocks : min((long long)kMaxBlocks, units * groups * c.n_seqs);
-    return launch_i8(k_paged_attn<HD, I8, NT>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, a);
+    constexpr size_t smem = sizeof(typename A::Shared);
+    static const cudaError_t set = cudaFuncSetAttribute(k_paged_attn<HD, I8, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (set != cudaSuccess) return set;
+    return launch_i8(k_paged_attn<HD, I8, NT>, dim3((unsigned)blocks), dim3(kThreads), smem, st, c, a);
 }
 
 }  // namespace
