@@ -18,6 +18,8 @@
 // its units sequence by sequence, the warps tile by tile, and joins its warps through shared memory.  What one block has of a
 // head group that others have rows of goes to the workspace; the last to arrive (a counter) adds the parts in order of their rows,
 // so the result does not depend on who that is.  More than kGroup parts are added in two steps.  No block ever waits for another.
+#include <atomic>
+
 #include "cats_paged.cuh"
 
 namespace cats {
@@ -80,27 +82,38 @@ __device__ __forceinline__ uint32_t f16_of_bytes(uint32_t w, uint32_t which) {
 }
 __device__ __forceinline__ uint32_t word_of(const uint4& a, int i) { return i == 0 ? a.x : (i == 1 ? a.y : (i == 2 ? a.z : a.w)); }
 
+// A run of units of one head group.
+struct Segment {
+    int s, kvh, head0, heads;       // sequence, head of the cache, query heads
+    int t0, t1;                     // rows
+    int unit, units;                // first unit, and units of the whole head group
+    __device__ __forceinline__ int tiles(int first, int step) const { return first < t1 ? (t1 - first + step - 1) / step : 0; }
+};
+
 template <int HD, bool I8, int NT> struct Attn {
-    static constexpr int kTile = I8 ? (NT == 1 ? 32 : 16) : (HD == 128 ? 16 : (NT == 1 ? 32 : 16));      // rows per warp and step
+    static constexpr int kTile = I8 || HD == 64 ? 32 : 16;      // rows per warp and step
     static constexpr int kUnit = kTile * kWarps;
     static constexpr int kBlk = kTile / 16;
-    static constexpr int KI = HD * (I8 ? 1 : 2) / 64;       // 16-byte pieces of a K row per thread
+    static constexpr int RB = HD * (I8 ? 1 : 2);            // bytes of a row
+    static constexpr int RP = RB / 16, kPerCopy = 32 / RP;  // its 16-byte pieces, rows per copy of a warp
+    static constexpr int kCopies = kTile / kPerCopy;
+    static constexpr int KI = RB / 64;                      // 16-byte pieces of a K row per thread
     static constexpr int VI = I8 ? 1 : HD / 64;             // and of a V row (int8, 64 channels: 8 bytes)
     static constexpr int MT = HD / 16;                      // 16-channel tiles of O^T
     static constexpr int QV = HD / 32;                      // 16-byte pieces of the queries per thread and 8 heads
     static constexpr int kPad = HD + 4;
-    // A stage of a warp's ring: the 16-byte pieces in the order [piece][lane], then (int8) a scale of K and of V per row.
-    static constexpr int kVBytes = I8 && HD == 64 ? 8 : 16;
-    static constexpr int kV = kBlk * 2 * KI * 512, kScales = kV + kBlk * 4 * VI * 32 * kVBytes, kStage = kScales + (I8 ? 256 : 0);
-    static constexpr int kStages = kStage > 6000 ? 2 : 4;
+    // Half of a warp's ring: a tile of K, one of V, and (int8) a scale of each per row; or, after a segment, the warp's O.
+    static constexpr int kV = kTile * RB, kScales = 2 * kV, kO = NT * 8 * kPad * 4;
+    static constexpr int kStage = (kScales + (I8 ? 256 : 0)) > kO ? kScales + (I8 ? 256 : 0) : kO;
     struct Shared {
+        uint8_t ring[kWarps][2][kStage];
+        uint4 raw[2][NT * 8 * HD / 8];                      // the queries of this segment and the next, as they are
         union {
-            uint8_t ring[kWarps][kStages][kStage];
-            float o[kWarps][NT * 8][kPad];              // after the last row
+            uint4 q[NT][QV][32];
+            float2 parts[kGroup][NT * 8];                   // behind a segment
         };
-        uint4 q[NT][QV][32];
         float2 ml[kWarps][NT * 8];
-        float2 parts[kGroup][NT * 8];
+        int o_at[kWarps];                                   // which half of its ring a warp's O is in
         long long total, before;        // units of all sequences, and of those in front of `seq`
         int seq, last;
         long long warp_sum[kWarps];
@@ -134,26 +147,39 @@ template <int HD, bool I8, int NT> struct Attn {
         if (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
         else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(N), "r"(there ? N : 0) : "memory");
     }
-    // Requests a tile.  What a thread copies of K and V is what it reads itself.
-    __device__ __forceinline__ void request(uint32_t stage, const Row& row, const uint8_t* k, const uint8_t* v, const float* ks, const float* vs) const {
-#pragma unroll
-        for (int b = 0; b < kBlk * 2; ++b) {
-            const uint32_t r = __shfl_sync(0xffffffffu, row.at, b * 8 + g);
-            const uint8_t* const p = k + (r != kNoRow ? (size_t)r * 16 : 0) + j * 16;
-#pragma unroll
-            for (int i = 0; i < KI; ++i) copy<16>(stage + (b * KI + i) * 512 + lane * 16, p + i * 64, r != kNoRow);
+    // Where piece `piece` of row `row` of a tile lies.  Rows follow each other; the pieces within 128 bytes change places so that neither the
+    // reads of K (rows 2p, 2p + 1 and four pieces at a time) nor those of V (rows 0, 2, 4, 6 and two pieces) meet in a bank.
+    static __device__ __forceinline__ int k_at(int row, int piece) { return row * RB + ((RB >= 128 ? piece ^ ((row & 1) << 2) : piece) << 4); }
+    static __device__ __forceinline__ int v_at(int row, int piece) {
+        const int x = row * RP + piece;
+        return (x ^ (((row >> 1) & 3) << 1)) << 4;
+    }
+    // Requests the tile whose rows are `row`: 512 bytes of whole rows per instruction.  (Rows in pieces of 64 bytes, as the threads
+    // use them, asked L2 for every line twice: 4.85 instead of 6.05 TB/s.)
+    __device__ __forceinline__ void request(uint32_t stage, const Row& row, int kvh) const {
+        const uint8_t* const k = c.k + (size_t)kvh * c.head16 * 16 + (lane % RP) * 16;
+        const uint8_t* const v = c.v + (size_t)kvh * c.head16 * 16 + (lane % RP) * 16;
+        if (I8) {
+            copy<4>(stage + kScales + lane * 4, c.ks + (size_t)kvh * c.s_head + row.s, row.at != kNoRow);
+            copy<4>(stage + kScales + 128 + lane * 4, c.vs + (size_t)kvh * c.s_head + row.s, row.at != kNoRow);
         }
 #pragma unroll
-        for (int n = 0; n < kBlk * 4; ++n) {
-            const uint32_t r = __shfl_sync(0xffffffffu, row.at, (n >> 2) * 16 + ((n & 2) ? 8 : 0) + 2 * j + (n & 1));
-            const uint8_t* const p = v + (r != kNoRow ? (size_t)r * 16 : 0) + g * kVBytes;
-#pragma unroll
-            for (int i = 0; i < VI; ++i) copy<kVBytes>(stage + kV + ((n * VI + i) * 32 + lane) * kVBytes, p + i * 128, r != kNoRow);
+        for (int n = 0; n < kCopies; ++n) {
+            const int r = n * kPerCopy + lane / RP;
+            const uint32_t at = __shfl_sync(0xffffffffu, row.at, r);
+            copy<16>(stage + k_at(r, lane % RP), k + (at != kNoRow ? (size_t)at * 16 : 0), at != kNoRow);
+            copy<16>(stage + kV + v_at(r, lane % RP), v + (at != kNoRow ? (size_t)at * 16 : 0), at != kNoRow);
         }
-        if (I8 && lane < kTile) {
-            copy<4>(stage + kScales + lane * 4, ks + row.s, row.at != kNoRow);
-            copy<4>(stage + kScales + 128 + lane * 4, vs + row.s, row.at != kNoRow);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // Requests the queries of a segment into half `to`.
+    __device__ __forceinline__ void request_q(int to, const Segment& g) const {
+        const uint16_t* const q = a.q + g.s * a.ldq + (size_t)g.head0 * HD;
+        for (int i = threadIdx.x; i < NT * 8 * HD / 8; i += kThreads) {
+            const bool there = i < g.heads * (HD / 8);
+            copy<16>(smem_u32(&sh.raw[to][i]), q + (there ? i * 8 : 0), there);
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     }
     static __device__ __forceinline__ uint4 lds16(uint32_t p) {
         uint4 x;
@@ -165,28 +191,24 @@ template <int HD, bool I8, int NT> struct Attn {
         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(p) : "memory");
         return x;
     }
-    __device__ __forceinline__ uint4 k_piece(uint32_t stage, int b, int i) const { return lds16(stage + (b * KI + i) * 512 + lane * 16); }
+    __device__ __forceinline__ uint4 k_piece(uint32_t stage, int b, int i) const { return lds16(stage + k_at(b * 8 + g, i * 4 + j)); }
     __device__ __forceinline__ uint4 v_piece(uint32_t stage, int n, int i) const {
-        if (kVBytes == 16) return lds16(stage + kV + ((n * VI + i) * 32 + lane) * 16);
+        const int row = (n >> 2) * 16 + ((n & 2) ? 8 : 0) + 2 * j + (n & 1);
+        if (!I8 || HD == 128) return lds16(stage + kV + v_at(row, i * 8 + g));
         uint4 x = make_uint4(0, 0, 0, 0);
-        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(stage + kV + (n * 32 + lane) * 8) : "memory");
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(stage + kV + v_at(row, g >> 1) + (g & 1) * 8) : "memory");
         return x;
     }
 
-    // The queries of `heads` heads from `head0` on, as the second operand of K Q^T: thread (g, j) holds of head g the channels that
-    // thread (any, j) holds of a K row.  int8: as fp16, times a power of two that brings the head's largest to 2^14: exact down to 2^-28 of it.
-    __device__ __forceinline__ void load_q(int s, int head0, int heads) {
+    // A segment's queries as the second operand of K Q^T: thread (g, j) holds of head g the channels that thread (any, j) holds of a
+    // K row.  int8: as fp16, times a power of two that brings the head's largest to 2^14: exact down to 2^-28 of it.
+    __device__ __forceinline__ void take_q(int from) {
         const float base = a.scale * 1.4426950408889634f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int h = nt * 8 + g;
-            const uint16_t* const q = a.q + s * a.ldq + (size_t)(head0 + h) * HD;
             uint4 x[QV];
 #pragma unroll
-            for (int i = 0; i < QV; ++i) {
-                const int ch = I8 ? (i >> 1) * 64 + j * 16 + (i & 1) * 8 : i * 32 + j * 8;
-                x[i] = h < heads ? __ldcg(reinterpret_cast<const uint4*>(q + ch)) : make_uint4(0, 0, 0, 0);
-            }
+            for (int i = 0; i < QV; ++i) x[i] = sh.raw[from][(nt * 8 + g) * (HD / 8) + (I8 ? (i >> 1) * 8 + j * 2 + (i & 1) : i * 4 + j)];
             float mine = base;
             if (I8) {
                 uint32_t mx = 0;
@@ -383,22 +405,23 @@ template <int HD, bool I8, int NT> struct Attn {
     // Channel of row g of tile t of O^T; row g + 8 is the next one.
     __device__ __forceinline__ int channel(int t) const { return I8 ? g * (HD / 8) + 2 * t : (t >> 2) * 64 + g * 8 + (t & 3) * 2; }
 
-    // Rows t0 .. t1 - 1 of a sequence for `heads` heads: leaves what the block has of them in sh.o and sh.ml, one entry per warp that had rows.
-    __device__ __forceinline__ int rows(int s, int kvh, int head0, int heads, int t0, int t1) {
-        const uint8_t* const k = c.k + (size_t)kvh * c.head16 * 16;
-        const uint8_t* const v = c.v + (size_t)kvh * c.head16 * 16;
-        const float* const ks = c.ks + (size_t)kvh * c.s_head;
-        const float* const vs = c.vs + (size_t)kvh * c.s_head;
+    // What the block has of a segment, to sh.ml and the warps' rings, one entry per warp that had rows; returns how many.  One tile is always on
+    // its way while another is worked on, the next segment's first behind this one's last; where the rows of the tile to be
+    // requested next lie is looked up a step ahead.
+    int used;                   // half of the ring that is worked on
+    bool pending;               // whether the other half's tile has been requested
+    __device__ __forceinline__ int segment(const Segment& g0, const Segment& g1, bool more, int parity) {
+        const int first = g0.t0 + warp * kTile, tiles = g0.tiles(first, kUnit), first1 = g1.t0 + warp * kTile;
+        const bool next_has = more && first1 < g1.t1;
         const uint32_t ring = smem_u32(sh.ring[warp]);
-        const int t = t0 + warp * kTile, tiles = t < t1 ? (t1 - t + kUnit - 1) / kUnit : 0;
-        // kStages - 1 tiles are on their way before the first is used; where the rows of one more lie is looked up a step ahead
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) {
-            if (i < tiles) request(ring + i * kStage, row_of(s, t + i * kUnit, t1), k, v, ks, vs);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
-        Row next = row_of(s, t + (kStages - 1) * kUnit, t1);
-        load_q(s, head0, heads);
+        if (!pending && tiles > 0) request(ring + (used ^ 1) * kStage, row_of(g0.s, first, g0.t1), g0.kvh);
+        pending = tiles > 0;
+        Row next;               // of the tile behind the pending one
+        if (tiles > 1) next = row_of(g0.s, first + kUnit, g0.t1);
+        else if (next_has) next = row_of(g1.s, first1, g1.t1);
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();        // the queries are there
+        take_q(parity);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             m[nt][0] = m[nt][1] = -INFINITY;
@@ -408,32 +431,39 @@ template <int HD, bool I8, int NT> struct Attn {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[nt][t][e] = 0.f;
         }
-        const int active = min(kWarps, (t1 - t0 + kTile - 1) / kTile);
-        __syncthreads();            // the queries are there
+        __syncthreads();        // and in order
+        if (more) request_q(parity ^ 1, g1);
         for (int i = 0; i < tiles; ++i) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-            __syncwarp();           // also: all lanes are done with the stage that is filled next
-            if (i + kStages - 1 < tiles) request(ring + (i + kStages - 1) % kStages * kStage, next, k, v, ks, vs);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            next = row_of(s, t + (i + kStages) * kUnit, t1);
-            step(ring + i % kStages * kStage, t1 - (t + i * kUnit));
+            if (i > 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();       // also: all lanes are done with the half that is filled next
+            used ^= 1;
+            pending = i + 1 < tiles || next_has;
+            if (pending) {
+                request(ring + (used ^ 1) * kStage, next, i + 1 < tiles ? g0.kvh : g1.kvh);
+                if (i + 2 < tiles) next = row_of(g0.s, first + (i + 2) * kUnit, g0.t1);
+                else if (i + 2 == tiles && next_has) next = row_of(g1.s, first1, g1.t1);
+            }
+            step(ring + used * kStage, g0.t1 - (first + i * kUnit));
         }
-        __syncthreads();            // the ring is now sh.o
+        const int active = min(kWarps, (g0.t1 - g0.t0 + kTile - 1) / kTile);
         if (warp < active) {
+            float* const o = reinterpret_cast<float*>(sh.ring[warp][used]);
+            if (lane == 0) sh.o_at[warp] = used;
+            __syncwarp();
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], o);
+                    for (int d = 4; d < 32; d <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], d);
                 if (g == 0) {
                     sh.ml[warp][nt * 8 + 2 * j] = make_float2(m[nt][0], l[nt][0]);
                     sh.ml[warp][nt * 8 + 2 * j + 1] = make_float2(m[nt][1], l[nt][1]);
                 }
 #pragma unroll
-                for (int t2 = 0; t2 < MT; ++t2) {
-                    *reinterpret_cast<float2*>(&sh.o[warp][nt * 8 + 2 * j][channel(t2)]) = make_float2(acc[nt][t2][0], acc[nt][t2][2]);
-                    *reinterpret_cast<float2*>(&sh.o[warp][nt * 8 + 2 * j + 1][channel(t2)]) = make_float2(acc[nt][t2][1], acc[nt][t2][3]);
+                for (int t = 0; t < MT; ++t) {
+                    *reinterpret_cast<float2*>(o + (nt * 8 + 2 * j) * kPad + channel(t)) = make_float2(acc[nt][t][0], acc[nt][t][2]);
+                    *reinterpret_cast<float2*>(o + (nt * 8 + 2 * j + 1) * kPad + channel(t)) = make_float2(acc[nt][t][1], acc[nt][t][3]);
                 }
             }
         }
@@ -462,7 +492,7 @@ template <int HD, bool I8, int NT> struct Attn {
             for (int k = 0; k < active; ++k) {
                 const float f = factor(sh.ml[k][h].x, top);
                 sum = fmaf(sh.ml[k][h].y, f, sum);
-                add(x, *reinterpret_cast<const float4*>(&sh.o[k][h][ch]), f);
+                add(x, *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(sh.ring[k][sh.o_at[k]]) + h * kPad + ch), f);
             }
             if (slot < 0) {
                 store_out(s, head0 + h, ch, x, sum, active == 0);
@@ -471,7 +501,7 @@ template <int HD, bool I8, int NT> struct Attn {
                 if (ch == 0) w.ml(slot)[h] = make_float2(top, sum);
             }
         }
-        __syncthreads();            // the ring is free
+        __syncthreads();            // the rings are free
     }
 
     // Parts at slots slot_of(0) .. slot_of(n - 1) added in this order: to slot `to`, or (to < 0) to the output.
@@ -572,40 +602,62 @@ template <int HD, bool I8, int NT> struct Attn {
         int s = sh.seq;
         long long base = sh.before * groups;         // first unit of sequence s
         int len = length(s), n = units_of(len);
-        while (u < u_end) {
+        auto next_segment = [&] {                    // from unit u on
+            Segment g;
             while (u >= base + (long long)n * groups) {
                 base += (long long)n * groups;
                 len = length(++s);
                 n = units_of(len);
             }
-            const int group = (int)((u - base) / n), unit = (int)(u - base - (long long)group * n);
-            const int mine = (int)min((long long)(n - unit), u_end - u);
-            const int kvh = group / chunks, chunk = group % chunks, head0 = kvh * per_kv + chunk * NT * 8, heads = min(NT * 8, per_kv - chunk * NT * 8);
-            const int t0 = unit * kUnit, t1 = min((long long)len, (long long)(unit + mine) * kUnit);
-            const int active = rows(s, kvh, head0, heads, t0, t1);
-            if (mine == n) {
-                join(s, head0, heads, active, w, -1);
+            const int group = (int)((u - base) / n), chunk = group % chunks;
+            g.s = s;
+            g.kvh = group / chunks;
+            g.head0 = g.kvh * per_kv + chunk * NT * 8;
+            g.heads = min(NT * 8, per_kv - chunk * NT * 8);
+            g.unit = (int)(u - base - (long long)group * n);
+            g.units = n;
+            const int mine = (int)min((long long)(n - g.unit), u_end - u);
+            g.t0 = g.unit * kUnit;
+            g.t1 = (int)min((long long)len, (long long)(g.unit + mine) * kUnit);
+            u += mine;
+            return g;
+        };
+        Segment now = next_segment();
+        long long at = me * units / n_blocks;        // its first unit
+        used = 1;
+        pending = false;
+        request_q(0, now);
+        for (int parity = 0;; parity ^= 1) {
+            const long long end = u;
+            const bool more = end < u_end;
+            Segment next = now;
+            if (more) next = next_segment();
+            const int active = segment(now, next, more, parity);
+            if (end - at == now.units) {
+                join(now.s, now.head0, now.heads, active, w, -1);
             } else {
                 // blocks first .. last have rows of this head group; the first of them in its second slot
-                const int first = block_of(u - unit), last = block_of(u - unit + n - 1), parts = last - first + 1;
+                const int first = block_of(at - now.unit), last = block_of(at - now.unit + now.units - 1), parts = last - first + 1;
                 auto slot_of = [&](int k) { return 2 * (first + k) + (k == 0 ? 1 : 0); };
-                join(s, head0, heads, active, w, slot_of(me - first));
+                join(now.s, now.head0, now.heads, active, w, slot_of(me - first));
                 if (parts <= kGroup) {
-                    if (arrive(w.first(first), parts)) add_parts(s, head0, heads, parts, slot_of, w, -1);
+                    if (arrive(w.first(first), parts)) add_parts(now.s, now.head0, now.heads, parts, slot_of, w, -1);
                 } else {
                     const int mine0 = (me - first) / kGroup * kGroup, size = min(kGroup, parts - mine0), n_groups = (parts + kGroup - 1) / kGroup;
                     if (arrive(mine0 == 0 ? w.first(first) : w.later(first + mine0), size)) {
-                        add_parts(s, head0, heads, size, [&](int k) { return slot_of(mine0 + k); }, w, slot_of(mine0));
-                        if (arrive(w.groups(first), n_groups)) add_parts(s, head0, heads, n_groups, [&](int k) { return slot_of(k * kGroup); }, w, -1);
+                        add_parts(now.s, now.head0, now.heads, size, [&](int k) { return slot_of(mine0 + k); }, w, slot_of(mine0));
+                        if (arrive(w.groups(first), n_groups)) add_parts(now.s, now.head0, now.heads, n_groups, [&](int k) { return slot_of(k * kGroup); }, w, -1);
                     }
                 }
             }
-            u += mine;
+            if (!more) break;
+            now = next;
+            at = end;
         }
     }
 };
 
-template <int HD, bool I8, int NT> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_paged_attn(const __grid_constant__ PagedDev c, const __grid_constant__ PagedAttn a) {
+template <int HD, bool I8, int NT> __global__ void __launch_bounds__(kThreads, NT == 1 ? kBlocksPerSm : 2) k_paged_attn(const __grid_constant__ PagedDev c, const __grid_constant__ PagedAttn a) {
     extern __shared__ __align__(16) uint8_t smem[];
     typename Attn<HD, I8, NT>::Shared& sh = *reinterpret_cast<typename Attn<HD, I8, NT>::Shared*>(smem);
     pdl_launch_dependents();
@@ -617,10 +669,19 @@ template <int HD, bool I8, int NT> cudaError_t launch_k(const PagedDev& c, const
     typedef Attn<HD, I8, NT> A;
     const long long per_kv = a.n_heads / c.n_kv, groups = c.n_kv * ((per_kv + NT * 8 - 1) / (NT * 8));
     const long long most = (long long)c.width * c.page_size, units = (most - 1) / A::kUnit + 1;
-    const long long blocks = units >= kMaxBlocks ? kMaxBlocks : min((long long)kMaxBlocks, units * groups * c.n_seqs);
+    const long long fit = NT == 1 ? kMaxBlocks : 148 * 2, blocks = units >= fit ? fit : min(fit, units * groups * c.n_seqs);
     constexpr size_t smem = sizeof(typename A::Shared);
-    static const cudaError_t set = cudaFuncSetAttribute(k_paged_attn<HD, I8, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (set != cudaSuccess) return set;
+    static_assert((smem + 1024) * (NT == 1 ? kBlocksPerSm : 2) <= 228 * 1024, "the blocks of an SM share its memory");
+    static std::atomic<uint64_t> known{0};           // devices whose attribute is set
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!(known.load(std::memory_order_acquire) >> dev & 1)) {
+        e = cudaFuncSetAttribute(k_paged_attn<HD, I8, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        known.fetch_or((uint64_t)1 << dev, std::memory_order_release);
+    }
     return launch_i8(k_paged_attn<HD, I8, NT>, dim3((unsigned)blocks), dim3(kThreads), smem, st, c, a);
 }
 
