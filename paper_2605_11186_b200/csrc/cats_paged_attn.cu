@@ -107,11 +107,12 @@ template <int HD, bool I8, int NT> struct Attn {
     static constexpr int kStage = (kScales + (I8 ? 256 : 0)) > kO ? kScales + (I8 ? 256 : 0) : kO;
     struct Shared {
         uint8_t ring[kWarps][2][kStage];
-        uint4 raw[2][NT * 8 * HD / 8];                      // the queries of this segment and the next, as they are
+        uint4 raw[NT * 8 * HD / 8];                         // the queries of the next segment, as they are
         union {
-            uint4 q[NT][QV][32];
-            float2 parts[kGroup][NT * 8];                   // behind a segment
-        };
+            uint4 q[NT][QV][32];                            // and as the second operand of K Q^T, of this segment and the next
+            float2 parts[kGroup][NT * 8];                   // behind a segment, in its half
+        } q[2];
+        float qf[2][NT * 8];                                // factors of the scores
         float2 ml[kWarps][NT * 8];
         int o_at[kWarps];                                   // which half of its ring a warp's O is in
         long long total, before;        // units of all sequences, and of those in front of `seq`
@@ -163,21 +164,31 @@ template <int HD, bool I8, int NT> struct Attn {
             copy<4>(stage + kScales + lane * 4, c.ks + (size_t)kvh * c.s_head + row.s, row.at != kNoRow);
             copy<4>(stage + kScales + 128 + lane * 4, c.vs + (size_t)kvh * c.s_head + row.s, row.at != kNoRow);
         }
+        const uint32_t at0 = __shfl_sync(0xffffffffu, row.at, 0);
+        if (__all_sync(0xffffffffu, (kTile < 32 && lane >= kTile) || (row.at != kNoRow && row.at == at0 + lane * RP))) {      // rows that follow each other
 #pragma unroll
-        for (int n = 0; n < kCopies; ++n) {
-            const int r = n * kPerCopy + lane / RP;
-            const uint32_t at = __shfl_sync(0xffffffffu, row.at, r);
-            copy<16>(stage + k_at(r, lane % RP), k + (at != kNoRow ? (size_t)at * 16 : 0), at != kNoRow);
-            copy<16>(stage + kV + v_at(r, lane % RP), v + (at != kNoRow ? (size_t)at * 16 : 0), at != kNoRow);
+            for (int n = 0; n < kCopies; ++n) {
+                const int r = n * kPerCopy + lane / RP;
+                copy<16>(stage + k_at(r, lane % RP), k + (size_t)at0 * 16 + lane / RP * RB + n * 512, true);
+                copy<16>(stage + kV + v_at(r, lane % RP), v + (size_t)at0 * 16 + lane / RP * RB + n * 512, true);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < kCopies; ++n) {
+                const int r = n * kPerCopy + lane / RP;
+                const uint32_t at = __shfl_sync(0xffffffffu, row.at, r);
+                copy<16>(stage + k_at(r, lane % RP), k + (at != kNoRow ? (size_t)at * 16 : 0), at != kNoRow);
+                copy<16>(stage + kV + v_at(r, lane % RP), v + (at != kNoRow ? (size_t)at * 16 : 0), at != kNoRow);
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // Requests the queries of a segment into half `to`.
-    __device__ __forceinline__ void request_q(int to, const Segment& g) const {
+    // Requests the queries of a segment.
+    __device__ __forceinline__ void request_q(const Segment& g) const {
         const uint16_t* const q = a.q + g.s * a.ldq + (size_t)g.head0 * HD;
         for (int i = threadIdx.x; i < NT * 8 * HD / 8; i += kThreads) {
             const bool there = i < g.heads * (HD / 8);
-            copy<16>(smem_u32(&sh.raw[to][i]), q + (there ? i * 8 : 0), there);
+            copy<16>(smem_u32(&sh.raw[i]), q + (there ? i * 8 : 0), there);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
@@ -200,15 +211,15 @@ template <int HD, bool I8, int NT> struct Attn {
         return x;
     }
 
-    // A segment's queries as the second operand of K Q^T: thread (g, j) holds of head g the channels that thread (any, j) holds of a
-    // K row.  int8: as fp16, times a power of two that brings the head's largest to 2^14: exact down to 2^-28 of it.
-    __device__ __forceinline__ void take_q(int from) {
+    // The queries that have arrived as the second operand of K Q^T, by one warp: thread (g, j) makes of head g the channels that thread
+    // (any, j) holds of a K row.  int8: as fp16, times a power of two that brings the head's largest to 2^14: exact down to 2^-28 of it.
+    __device__ __forceinline__ void make_q(int to) {
         const float base = a.scale * 1.4426950408889634f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             uint4 x[QV];
 #pragma unroll
-            for (int i = 0; i < QV; ++i) x[i] = sh.raw[from][(nt * 8 + g) * (HD / 8) + (I8 ? (i >> 1) * 8 + j * 2 + (i & 1) : i * 4 + j)];
+            for (int i = 0; i < QV; ++i) x[i] = sh.raw[(nt * 8 + g) * (HD / 8) + (I8 ? (i >> 1) * 8 + j * 2 + (i & 1) : i * 4 + j)];
             float mine = base;
             if (I8) {
                 uint32_t mx = 0;
@@ -234,17 +245,14 @@ template <int HD, bool I8, int NT> struct Attn {
                 }
                 mine = base / f0 / f1;
             }
-            if (warp == (nt & (kWarps - 1))) {
 #pragma unroll
-                for (int i = 0; i < QV; ++i) sh.q[nt][i][lane] = x[i];
-            }
-            qf[nt][0] = __shfl_sync(0xffffffffu, mine, (2 * j) * 4);
-            qf[nt][1] = __shfl_sync(0xffffffffu, mine, (2 * j + 1) * 4);
+            for (int i = 0; i < QV; ++i) sh.q[to].q[nt][i][lane] = x[i];
+            if (j == 0) sh.qf[to][nt * 8 + g] = mine;
         }
     }
 
     // One tile: scores, weights, O^T.  left: rows of the sequence from the tile's first on.
-    __device__ __forceinline__ void step(uint32_t stage, int left) {
+    __device__ __forceinline__ void step(uint32_t stage, int left, int parity) {
         float s[NT][kBlk][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -266,7 +274,7 @@ template <int HD, bool I8, int NT> struct Attn {
                         const uint32_t a0 = f16_of_bytes(x, 0x4140), a1 = f16_of_bytes(y, 0x4140), a2 = f16_of_bytes(x, 0x4342), a3 = f16_of_bytes(y, 0x4342);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            const uint4 q = sh.q[nt][i * 2 + (w >> 1)][lane];
+                            const uint4 q = sh.q[parity].q[nt][i * 2 + (w >> 1)][lane];
                             mma<I8>(s[nt][b], a0, a1, a2, a3, w & 1 ? q.z : q.x, w & 1 ? q.w : q.y);
                         }
                     }
@@ -274,7 +282,7 @@ template <int HD, bool I8, int NT> struct Attn {
             } else {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const uint4 q = sh.q[nt][i][lane];
+                    const uint4 q = sh.q[parity].q[nt][i][lane];
 #pragma unroll
                     for (int b = 0; b < kBlk; ++b) {
                         mma<I8>(s[nt][b], kr[2 * b].x, kr[2 * b + 1].x, kr[2 * b].y, kr[2 * b + 1].y, q.x, q.y);
@@ -419,22 +427,22 @@ template <int HD, bool I8, int NT> struct Attn {
         Row next;               // of the tile behind the pending one
         if (tiles > 1) next = row_of(g0.s, first + kUnit, g0.t1);
         else if (next_has) next = row_of(g1.s, first1, g1.t1);
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncthreads();        // the queries are there
-        take_q(parity);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            m[nt][0] = m[nt][1] = -INFINITY;
-            l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                m[nt][e] = -INFINITY;
+                l[nt][e] = 0.f;
+                qf[nt][e] = sh.qf[parity][nt * 8 + 2 * j + e];
+            }
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[nt][t][e] = 0.f;
         }
-        __syncthreads();        // and in order
-        if (more) request_q(parity ^ 1, g1);
+        if (more) request_q(g1);
         for (int i = 0; i < tiles; ++i) {
-            if (i > 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncwarp();       // also: all lanes are done with the half that is filled next
             used ^= 1;
             pending = i + 1 < tiles || next_has;
@@ -443,7 +451,7 @@ template <int HD, bool I8, int NT> struct Attn {
                 if (i + 2 < tiles) next = row_of(g0.s, first + (i + 2) * kUnit, g0.t1);
                 else if (i + 2 == tiles && next_has) next = row_of(g1.s, first1, g1.t1);
             }
-            step(ring + used * kStage, g0.t1 - (first + i * kUnit));
+            step(ring + used * kStage, g0.t1 - (first + i * kUnit), parity);
         }
         const int active = min(kWarps, (g0.t1 - g0.t0 + kTile - 1) / kTile);
         if (warp < active) {
@@ -467,7 +475,11 @@ template <int HD, bool I8, int NT> struct Attn {
                 }
             }
         }
+        // the next segment's queries; a tile requested behind them may still be on its way
+        if (pending) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncthreads();
+        if (more && warp == kWarps - 1) make_q(parity ^ 1);
         return active;
     }
 
@@ -505,18 +517,18 @@ template <int HD, bool I8, int NT> struct Attn {
     }
 
     // Parts at slots slot_of(0) .. slot_of(n - 1) added in this order: to slot `to`, or (to < 0) to the output.
-    template <typename F> __device__ __forceinline__ void add_parts(int s, int head0, int heads, int n, F slot_of, const Slots& w, int to) {
-        for (int i = threadIdx.x; i < n * heads; i += kThreads) sh.parts[i / heads][i % heads] = __ldcg(w.ml(slot_of(i / heads)) + i % heads);
+    template <typename F> __device__ __forceinline__ void add_parts(int s, int head0, int heads, int n, F slot_of, const Slots& w, int to, float2 (*parts)[NT * 8]) {
+        for (int i = threadIdx.x; i < n * heads; i += kThreads) parts[i / heads][i % heads] = __ldcg(w.ml(slot_of(i / heads)) + i % heads);
         __syncthreads();
         for (int i = threadIdx.x; i < heads * (HD / 4); i += kThreads) {
             const int h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
             float top = -INFINITY, sum = 0.f;
-            for (int k = 0; k < n; ++k) top = fmaxf(top, sh.parts[k][h].x);
+            for (int k = 0; k < n; ++k) top = fmaxf(top, parts[k][h].x);
             float4 x = make_float4(0, 0, 0, 0);
 #pragma unroll 8
             for (int k = 0; k < n; ++k) {
-                const float f = factor(sh.parts[k][h].x, top);
-                sum = fmaf(sh.parts[k][h].y, f, sum);
+                const float f = factor(parts[k][h].x, top);
+                sum = fmaf(parts[k][h].y, f, sum);
                 add(x, __ldcg(reinterpret_cast<const float4*>(w.o(slot_of(k)) + h * HD + ch)), f);
             }
             if (to < 0) {
@@ -599,40 +611,54 @@ template <int HD, bool I8, int NT> struct Attn {
         const long long u_end = (me + 1) * units / n_blocks;
         auto block_of = [&](long long unit) { return (int)(((unit + 1) * n_blocks - 1) / units); };
         const Slots w = {(float*)a.ws, (int*)((float*)a.ws + 2 * kMaxBlocks * kSlotFloats)};
-        int s = sh.seq;
-        long long base = sh.before * groups;         // first unit of sequence s
-        int len = length(s), n = units_of(len);
+        // the sequence at hand, its length and the next one's, and how far the segments have come in it
+        int s = sh.seq, len = length(s), len1 = s + 1 < c.n_seqs ? length(s + 1) : 0, n = units_of(len);
+        const int group0 = (int)((u - sh.before * groups) / n);
+        int kvh = group0 / chunks, chunk = group0 % chunks, unit = (int)(u - sh.before * groups - (long long)group0 * n);
         auto next_segment = [&] {                    // from unit u on
-            Segment g;
-            while (u >= base + (long long)n * groups) {
-                base += (long long)n * groups;
-                len = length(++s);
-                n = units_of(len);
+            if (unit == n) {
+                unit = 0;
+                if (++chunk == chunks) {
+                    chunk = 0;
+                    if (++kvh == c.n_kv) {
+                        kvh = 0;
+                        ++s;
+                        len = len1;
+                        len1 = s + 1 < c.n_seqs ? length(s + 1) : 0;
+                        n = units_of(len);
+                    }
+                }
             }
-            const int group = (int)((u - base) / n), chunk = group % chunks;
+            Segment g;
             g.s = s;
-            g.kvh = group / chunks;
-            g.head0 = g.kvh * per_kv + chunk * NT * 8;
+            g.kvh = kvh;
+            g.head0 = kvh * per_kv + chunk * NT * 8;
             g.heads = min(NT * 8, per_kv - chunk * NT * 8);
-            g.unit = (int)(u - base - (long long)group * n);
+            g.unit = unit;
             g.units = n;
-            const int mine = (int)min((long long)(n - g.unit), u_end - u);
-            g.t0 = g.unit * kUnit;
-            g.t1 = (int)min((long long)len, (long long)(g.unit + mine) * kUnit);
+            const int mine = (int)min((long long)(n - unit), u_end - u);
+            g.t0 = unit * kUnit;
+            g.t1 = (int)min((long long)len, (long long)(unit + mine) * kUnit);
             u += mine;
+            unit += mine;
             return g;
         };
         Segment now = next_segment();
         long long at = me * units / n_blocks;        // its first unit
         used = 1;
         pending = false;
-        request_q(0, now);
+        request_q(now);
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+        if (warp == kWarps - 1) make_q(0);
+        __syncthreads();
         for (int parity = 0;; parity ^= 1) {
             const long long end = u;
             const bool more = end < u_end;
             Segment next = now;
             if (more) next = next_segment();
             const int active = segment(now, next, more, parity);
+            auto spare = sh.q[parity].parts;
             if (end - at == now.units) {
                 join(now.s, now.head0, now.heads, active, w, -1);
             } else {
@@ -641,12 +667,12 @@ template <int HD, bool I8, int NT> struct Attn {
                 auto slot_of = [&](int k) { return 2 * (first + k) + (k == 0 ? 1 : 0); };
                 join(now.s, now.head0, now.heads, active, w, slot_of(me - first));
                 if (parts <= kGroup) {
-                    if (arrive(w.first(first), parts)) add_parts(now.s, now.head0, now.heads, parts, slot_of, w, -1);
+                    if (arrive(w.first(first), parts)) add_parts(now.s, now.head0, now.heads, parts, slot_of, w, -1, spare);
                 } else {
                     const int mine0 = (me - first) / kGroup * kGroup, size = min(kGroup, parts - mine0), n_groups = (parts + kGroup - 1) / kGroup;
                     if (arrive(mine0 == 0 ? w.first(first) : w.later(first + mine0), size)) {
-                        add_parts(now.s, now.head0, now.heads, size, [&](int k) { return slot_of(mine0 + k); }, w, slot_of(mine0));
-                        if (arrive(w.groups(first), n_groups)) add_parts(now.s, now.head0, now.heads, n_groups, [&](int k) { return slot_of(k * kGroup); }, w, -1);
+                        add_parts(now.s, now.head0, now.heads, size, [&](int k) { return slot_of(mine0 + k); }, w, slot_of(mine0), spare);
+                        if (arrive(w.groups(first), n_groups)) add_parts(now.s, now.head0, now.heads, n_groups, [&](int k) { return slot_of(k * kGroup); }, w, -1, spare);
                     }
                 }
             }
