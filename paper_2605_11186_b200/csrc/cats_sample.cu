@@ -6,10 +6,14 @@
 // order, and so are all decisions made from them.  (vocab <= 2^18, so no sum reaches 2^63.)  Logits 46 T log 2 and more below the largest weigh
 // nothing and are left out of everything.
 //
-// A cluster of 1 to 8 blocks holds a row in shared memory, so it is read once.  Thresholds come from histograms of the distance to the largest
-// logit (counts for top-k; counts and weights for top-p), then of the keys within the bucket that holds the threshold, until few
-// tokens are left; those are compared each with each.  Where top-k, or top-p, leaves at most kFew tokens in the buckets up to its
-// own (the usual settings), these alone are gathered and the first block does the rest with them.
+// A cluster of 1 to 8 blocks holds a row in shared memory, so it is read once.
+//   - top-k up to kFewK: the k-th largest of the threads' own maxima bounds the k-th logit from below; what reaches that bound (little more
+//     than k tokens) is gathered, and the first block does the rest with these alone, comparing each with each.
+//   - else thresholds come from a histogram of the distance to the largest logit, then of the keys within the bucket that holds the
+//     threshold, until at most kFew tokens are left.  For top-p the counts bound the weights of a bucket to 1.6 % either way, so
+//     only the buckets between those bounds get exact sums by atomics; everything above and all together are sums in registers.
+//     Where at most kFew tokens lie in the buckets up to the threshold's, these are gathered and finished as above.
+// The fp64 exponential, 12 instructions at half rate, is what rows without top-k spend their time on.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -24,7 +28,7 @@ namespace cg = cooperative_groups;
 typedef long long i64;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBuckets = 1024;
-constexpr int kFew = 256;
+constexpr int kFew = 256, kFewK = 128;
 constexpr int kMaxBlocks = 8;           // of a cluster
 constexpr float kRange = 46.f;          // log2 of the weights that count
 
@@ -39,6 +43,13 @@ template <typename T> struct Elements;
 template <> struct Elements<float> {
     static constexpr int N = 4;
     static __device__ __forceinline__ float get(const uint4& v, int e) { return __uint_as_float(e == 0 ? v.x : (e == 1 ? v.y : (e == 2 ? v.z : v.w))); }
+    // the largest of a vector, NaN if there is one
+    static __device__ __forceinline__ float top(const uint4& v) {
+        float m = __uint_as_float(v.x);
+        asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(v.w)));
+        return m;
+    }
 };
 template <> struct Elements<uint16_t> {
     static constexpr int N = 8;
@@ -46,7 +57,20 @@ template <> struct Elements<uint16_t> {
         const uint32_t w = e < 2 ? v.x : (e < 4 ? v.y : (e < 6 ? v.z : v.w));
         return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
     }
+    static __device__ __forceinline__ float top(const uint4& v) {
+        uint32_t a, b;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+        float m = __uint_as_float(a << 16);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(a & 0xFFFF0000u)));
+        return m;
+    }
 };
+__device__ __forceinline__ float max_nan(float a, float b) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
+    return a;
+}
 
 struct Candidate {
     float x;
@@ -68,7 +92,8 @@ template <typename T> struct Row {
         i64 xch[2][kMaxBlocks][2];
         i64 red[2][kWarps];
         Found found;
-        int n_mine;
+        int n_mine, n_of[kMaxBlocks + 1];
+        int window[2];
         uint32_t tau;
         i64 above;
         int same, index;
@@ -98,30 +123,29 @@ template <typename T> struct Row {
             for (int e = 0; e < N; ++e) f(Elements<T>::get(x, e), first + v * N + e);
         }
     }
-    // 2^44 times the weight, by 2^y = 2^(i/64) 2^r with |r| <= 1/128 and the series of e^(r ln 2) up to the fifth power
-    __device__ __forceinline__ double power(float x) const {
-        const double y = fma((double)x - (double)top, c, 44.0);
+    // 2^44 times the weight = 2^y, by 2^(i/64) 2^r with |r| <= 1/128 and the series of 2^r up to the fourth power (4e-14 off)
+    __device__ __forceinline__ double power(double y) const {
         const double z = fma(y, 64.0, 6755399441055744.0);          // 1.5 2^52: 64 y as a whole number in the low bits
         const int i = __double2loint(z);
-        const double r = fma(z - 6755399441055744.0, -0.015625, y) * 0.69314718055994530942;
-        double s = fma(r, 1.0 / 120.0, 1.0 / 24.0);
-        s = fma(s, r, 1.0 / 6.0);
-        s = fma(s, r, 0.5);
-        s = fma(s, r, 1.0);
+        const double r = fma(z - 6755399441055744.0, -0.015625, y);
+        double s = fma(r, 9.6181291076284772e-3, 5.5504108664821580e-2);        // (ln 2)^n / n!
+        s = fma(s, r, 2.4022650695910071e-1);
+        s = fma(s, r, 6.9314718055994531e-1);
         s = fma(s, r, 1.0) * sh.table[i & 63];
         return __hiloint2double(__double2hiint(s) + ((i >> 6) << 20), __double2loint(s));
     }
+    __device__ __forceinline__ double power_of(float x) const { return fma((double)x - (double)top, c, 44.0); }
     __device__ __forceinline__ i64 weight(float x) const {
-        if (!(((double)x - (double)top) * c > -46.0)) return 0;     // -inf too
-        return __double_as_longlong(power(x) + 4503599627370496.0) & 0xFFFFFFFFFFFFFll;      // + 2^52: rounded to a whole number
+        const double y = power_of(x);
+        const i64 w = __double_as_longlong(power(y) + 4503599627370496.0) & 0xFFFFFFFFFFFFFll;      // + 2^52: rounded to a whole number
+        return y > -2.0 ? w : 0;                                    // -inf too
     }
-    // Bucket by distance to the largest; kBuckets or more: weighs nothing (x = -inf at temperature inf: NaN)
+    // Bucket by distance to the largest (a sum with 2^23 rounds it); false: weighs nothing (x = -inf at temperature inf: NaN)
     __device__ __forceinline__ bool bucket_of(float x, int& b) const {
         const float t = (0.5f * top - 0.5f * x) * bucket_scale;       // halves: the difference of two large logits is still a number
-        b = (int)t;
-        return t < (float)kBuckets;
+        b = (int)(__float_as_uint(t + 8388608.f) & 0x7FFu);
+        return t < (float)kBuckets - 0.5f;
     }
-
     // a and b of this block to every block's sh.xch[parity ^ 1][rank]
     __device__ __forceinline__ void exchange(i64 a, i64 b) {
         if ((int)threadIdx.x < blocks) {
@@ -154,45 +178,74 @@ template <typename T> struct Row {
         }
     }
 
-    __device__ __forceinline__ void add_to(int b, i64 w) {
-        atomicAdd(&sh.cnt[b], 1u);
-        if (w) {
-            const uint32_t lo = (uint32_t)w, hi = (uint32_t)(w >> 32), old = atomicAdd(&sh.lo[b], lo);
-            const uint32_t carry = old + lo < old;
-            if (hi + carry) atomicAdd(&sh.hi[b], hi + carry);
+    // f(x, ...) for all elements that are at least x0, most vectors by their largest alone
+    template <typename F> __device__ __forceinline__ void each_from(float x0, F f) const {
+        for (int v = threadIdx.x; v < vecs; v += kThreads) {
+            const uint4 x = data[v];
+            if (Elements<T>::top(x) >= x0) {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (Elements<T>::get(x, e) >= x0) f(Elements<T>::get(x, e), first + v * N + e);
+            }
         }
     }
-    // Histogram of what f puts into a bucket (f(x, index, b): whether it does), by counts alone or with the weights
-    template <bool MASS, typename F> __device__ __forceinline__ void histogram(F f) {
+    __device__ __forceinline__ void add_weight(int b, i64 w) {
+        const uint32_t lo = (uint32_t)w, old = atomicAdd(&sh.lo[b], lo), hi = (uint32_t)(w >> 32) + (old + lo < old);
+        if (hi) atomicAdd(&sh.hi[b], hi);
+    }
+    __device__ __forceinline__ void clear() {
         sync();                     // nobody reads the last one any more
         for (int i = threadIdx.x; i < kBuckets; i += kThreads) sh.cnt[i] = sh.lo[i] = sh.hi[i] = 0;
         __syncthreads();
-        each([&](float x, int index) {
+    }
+    // Histogram of what f puts into a bucket (f(x, b): whether it does) among the logits from x0 on, by counts alone or with the weights
+    template <bool MASS, typename F> __device__ __forceinline__ void histogram(float x0, F f) {
+        clear();
+        auto one = [&](float x, int) {
             int b;
-            if (f(x, index, b)) {
-                const i64 w = MASS ? weight(x) : 0;
-                // all lanes at one bucket (equal logits): one of them adds for all
-                const unsigned at = __activemask();
-                const int b0 = __shfl_sync(at, b, __ffs(at) - 1);
-                if (at == 0xffffffffu && __all_sync(at, b == b0)) {
-                    i64 s = w;
-                    if (MASS) {
+            if (!f(x, b)) return;
+            // all lanes at one bucket (equal logits): one of them adds for all
+            const unsigned at = __activemask();
+            const int b0 = __shfl_sync(at, b, __ffs(at) - 1);
+            i64 w = MASS ? weight(x) : 0;
+            if (at == 0xffffffffu && __all_sync(at, b == b0)) {
+                if (MASS) {
 #pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                    }
-                    if (lane == 0) {
-                        atomicAdd(&sh.cnt[b], 32u);
-                        if (MASS && s) {
-                            const uint32_t lo = (uint32_t)s, old = atomicAdd(&sh.lo[b], lo);
-                            atomicAdd(&sh.hi[b], (uint32_t)(s >> 32) + (old + lo < old));
-                        }
-                    }
-                } else {
-                    add_to(b, w);
+                    for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+                }
+                if (lane == 0) {
+                    atomicAdd(&sh.cnt[b], 32u);
+                    if (MASS && w) add_weight(b, w);
+                }
+            } else {
+                atomicAdd(&sh.cnt[b], 1u);
+                if (MASS && w) add_weight(b, w);
+            }
+        };
+        if (x0 > -INFINITY) each_from(x0, one);
+        else each(one);
+        sync();
+    }
+    // Counts and weights of bucket b in all blocks
+    template <bool MASS> __device__ __forceinline__ void bucket_sums(int b, i64& n, i64& w) {
+        uint32_t cnt[kMaxBlocks], lo[kMaxBlocks], hi[kMaxBlocks];
+#pragma unroll
+        for (int r = 0; r < kMaxBlocks; ++r) {
+            cnt[r] = lo[r] = hi[r] = 0;
+            if (r < blocks) {
+                cnt[r] = blocks > 1 ? cluster.map_shared_rank(sh.cnt, r)[b] : sh.cnt[b];
+                if (MASS) {
+                    lo[r] = blocks > 1 ? cluster.map_shared_rank(sh.lo, r)[b] : sh.lo[b];
+                    hi[r] = blocks > 1 ? cluster.map_shared_rank(sh.hi, r)[b] : sh.hi[b];
                 }
             }
-        });
-        sync();
+        }
+        n = w = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxBlocks; ++r) {
+            n += cnt[r];
+            if (MASS) w += ((i64)hi[r] << 32) + lo[r];
+        }
     }
     // The first bucket at which the running sum of the counts (or weights) over all blocks reaches what target(total) says
     template <bool MASS, typename F> __device__ __forceinline__ Found find(F target, i64& total) {
@@ -200,12 +253,7 @@ template <typename T> struct Row {
         i64 val[each_has], cnt[each_has], a = 0, n = 0;
 #pragma unroll
         for (int i = 0; i < each_has; ++i) {
-            const int b = threadIdx.x * each_has + i;
-            val[i] = cnt[i] = 0;
-            for (int r = 0; r < blocks; ++r) {
-                cnt[i] += blocks > 1 ? cluster.map_shared_rank(sh.cnt, r)[b] : sh.cnt[b];
-                if (MASS) val[i] += blocks > 1 ? ((i64)cluster.map_shared_rank(sh.hi, r)[b] << 32) + cluster.map_shared_rank(sh.lo, r)[b] : ((i64)sh.hi[b] << 32) + sh.lo[b];
-            }
+            bucket_sums<MASS>(threadIdx.x * each_has + i, cnt[i], val[i]);
             if (!MASS) val[i] = cnt[i];
             a += val[i];
             n += cnt[i];
@@ -226,26 +274,28 @@ template <typename T> struct Row {
         return f;
     }
 
-    // Tokens that f takes, of all blocks, to sh.all of this block (every block, or the first alone).  There are at most kFew of them.
-    template <typename F> __device__ __forceinline__ int gather(bool first_only, F f) {
+    // Tokens from x0 on that f takes, of all blocks, to sh.all of this block (every block, or the first alone).  Returns how many there are: if more than kFew, none
+    // have been taken.
+    template <typename F> __device__ __forceinline__ int gather(bool first_only, float x0, F f) {
         if (threadIdx.x == 0) sh.n_mine = 0;
         sync();                     // and nobody reads sh.mine any more
-        each([&](float x, int index) {
-            if (f(x, index)) {
+        auto one = [&](float x, int index) {
+            if (f(x)) {
                 const int at = atomicAdd(&sh.n_mine, 1);
                 if (at < kFew) sh.mine[at] = {x, index, 0};
             }
-        });
+        };
+        if (x0 > -INFINITY) each_from(x0, one);
+        else each(one);
         sync();
-        int n = 0;
-        if (!first_only || rank == 0) {
-            for (int r = 0; r < blocks; ++r) {
-                const int m = min(kFew - n, blocks > 1 ? *cluster.map_shared_rank(&sh.n_mine, r) : sh.n_mine);
-                const Candidate* const from = blocks > 1 ? cluster.map_shared_rank(sh.mine, r) : sh.mine;
-                for (int i = threadIdx.x; i < m; i += kThreads) sh.all[n + i] = from[i];
-                n += m;
-            }
+        if ((int)threadIdx.x < blocks) sh.n_of[threadIdx.x + 1] = blocks > 1 ? *cluster.map_shared_rank(&sh.n_mine, threadIdx.x) : sh.n_mine;
+        __syncthreads();
+        int n = 0, r = 0, at = 0;   // this thread's candidate: the at-th of block r
+        for (int k = 0; k < blocks; ++k) {
+            if ((int)threadIdx.x >= n) { r = k; at = threadIdx.x - n; }
+            n += sh.n_of[k + 1];
         }
+        if (n <= kFew && (int)threadIdx.x < n && (!first_only || rank == 0)) sh.all[threadIdx.x] = (blocks > 1 ? cluster.map_shared_rank(sh.mine, r) : sh.mine)[at];
         return n;
     }
     // f(i, j) for all pairs of n candidates, the j of an i spread over lanes of a warp; done(i, on the first of these lanes) after sums a and b of what f
@@ -317,7 +367,7 @@ template <typename T> struct Row {
             int s = 0;
             while (((n1 - n0) >> s) >= (uint32_t)kBuckets) ++s;
             // keys between the least and the most of a bucket are all in it
-            histogram<MASS>([&](float x, int, int& b) {
+            histogram<MASS>(value_of(n0), [&](float x, int& b) {
                 const uint32_t k = key_of(x);
                 b = (int)((n1 - k) >> s);
                 return k >= n0 && k <= n1 && weighs(x, f);
@@ -329,7 +379,7 @@ template <typename T> struct Row {
             got = find<MASS>([&](i64) { return want - skipped; }, total);
             skipped += got.before;
         }
-        const int n = gather(false, [&](float x, int) { return in(x) && (shift == 32 || weighs(x, f)); });
+        const int n = gather(false, -INFINITY, [&](float x) { return in(x) && (shift == 32 || weighs(x, f)); });
         __syncthreads();
         for (int i = threadIdx.x; i < n; i += kThreads) sh.all[i].w = MASS ? weight(sh.all[i].x) : 1;
         __syncthreads();
@@ -353,7 +403,7 @@ template <typename T> struct Row {
     // The first index at which the running sum of f over the row exceeds `target`, to sh.index of every block that asks; total: the whole sum.  A warp takes
     // a run of neighbouring vectors.
     template <typename F, typename G> __device__ __forceinline__ void walk(F f, G target, i64& total) {
-        const int run = ((vecs + kWarps - 1) / kWarps + 31) / 32 * 32, v0 = min(vecs, warp * run), v1 = min(vecs, v0 + run);
+        const int run = ((vecs + kWarps - 1) / kWarps + 31) / 32 * 32, v0 = min(vecs, warp * run), v1 = min(vecs, v0 + run);      // at most 32 strips of 32 vectors
         auto of_vec = [&](int v) {
             i64 s = 0;
             if (v < v1) {
@@ -363,10 +413,23 @@ template <typename T> struct Row {
             }
             return s;
         };
-        i64 mine = 0;
-        for (int v = v0 + lane; v < v1; v += 32) mine += of_vec(v);
+        i64 strip = 0;              // of lane i: the sum of strip i
+        for (int v = v0, i = 0; v < v1; v += 32, ++i) {
+            i64 one = of_vec(v + lane);
+            if (__any_sync(0xffffffffu, one != 0)) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+                for (int o = 16; o > 0; o >>= 1) one += __shfl_xor_sync(0xffffffffu, one, o);
+                if (lane == i) strip = one;
+            }
+        }
+        i64 mine = strip;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const i64 t = __shfl_up_sync(0xffffffffu, mine, o);
+            if (lane >= o) mine += t;
+        }
+        const i64 strips = mine;    // up to and with strip i
+        mine = __shfl_sync(0xffffffffu, mine, 31);
         __syncthreads();
         if (lane == 0) sh.red[0][warp] = mine;
         __syncthreads();
@@ -386,32 +449,26 @@ template <typename T> struct Row {
         }
         const i64 want = target(total);
         if (at <= want && want < at + mine) {
-            for (int v = v0; v < v1; v += 32) {
-                const i64 s = of_vec(v + lane);
-                i64 upto = s;
+            const int i = __ffs(__ballot_sync(0xffffffffu, want < at + strips)) - 1, v = v0 + i * 32 + lane;
+            const i64 s = of_vec(v);
+            i64 upto = s;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const i64 t = __shfl_up_sync(0xffffffffu, upto, o);
-                    if (lane >= o) upto += t;
-                }
-                const i64 all = __shfl_sync(0xffffffffu, upto, 31);
-                if (want < at + all) {
-                    i64 sum = at + upto - s;
-                    if (sum <= want && want < sum + s) {
-                        const uint4 x = data[v + lane];
+            for (int o = 1; o < 32; o <<= 1) {
+                const i64 t = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += t;
+            }
+            i64 sum = at + __shfl_sync(0xffffffffu, strips - strip, i) + upto - s;
+            if (sum <= want && want < sum + s) {
+                const uint4 x = data[v];
 #pragma unroll
-                        for (int e = 0; e < N; ++e) {
-                            const int index = first + (v + lane) * N + e;
-                            const i64 one = f(Elements<T>::get(x, e), index);
-                            if (sum <= want && want < sum + one) {
-                                for (int r = 0; r < blocks; ++r) *(blocks > 1 ? cluster.map_shared_rank(&sh.index, r) : &sh.index) = index;
-                            }
-                            sum += one;
-                        }
+                for (int e = 0; e < N; ++e) {
+                    const int index = first + v * N + e;
+                    const i64 one = f(Elements<T>::get(x, e), index);
+                    if (sum <= want && want < sum + one) {
+                        for (int r = 0; r < blocks; ++r) *(blocks > 1 ? cluster.map_shared_rank(&sh.index, r) : &sh.index) = index;
                     }
-                    break;
+                    sum += one;
                 }
-                at += all;
             }
         }
         sync();
@@ -462,7 +519,7 @@ template <typename T> struct Row {
         pairs(n, [&](int i, int j, i64& a, int&) {
             if (sh.all[j].index < sh.all[i].index) a += sh.all[j].w;
         }, [&](int i, i64 a, int) {
-            if (a <= r && r < a + sh.all[i].w) answer(d, sh.all[i].index, (float)(power(sh.all[i].x) / (double)kept));
+            if (a <= r && r < a + sh.all[i].w) answer(d, sh.all[i].index, (float)(power(power_of(sh.all[i].x)) / (double)kept));
         });
     }
     __device__ __forceinline__ void block_sum(i64& a) {
@@ -474,6 +531,87 @@ template <typename T> struct Row {
         a = 0;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) a += sh.red[0][w];
+    }
+
+    // Top-p over the whole row: the bucket in which the weights reach `want` = top_p of all of them (`total`).
+    __device__ __forceinline__ Found by_weight(float top_p, i64& want, i64& total) {
+        histogram<false>(-INFINITY, [&](float x, int& b) { return bucket_of(x, b); });
+        // Between b - 1/2 and b + 1/2 buckets from the largest, n tokens weigh n 2^(-b width) to within half a bucket; the sums below are in units of 2^44 and
+        // rounded by far less than the rest of a bucket that is added.
+        constexpr int each_has = kBuckets / kThreads;
+        constexpr float width = kRange / ((float)kBuckets - 0.5f);
+        float most = 0.f, least = 0.f, up[each_has], down[each_has];
+#pragma unroll
+        for (int i = 0; i < each_has; ++i) {
+            const int b = threadIdx.x * each_has + i;
+            i64 n, w;
+            bucket_sums<false>(b, n, w);
+            up[i] = (float)n * exp2f(-((float)b - 0.75f) * width);
+            down[i] = (float)n * exp2f(-((float)b + 0.75f) * width);
+            most += up[i];
+            least += down[i];
+        }
+        float a = most, z = least;          // up to and with this thread
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const float s = __shfl_up_sync(0xffffffffu, a, o), t = __shfl_up_sync(0xffffffffu, z, o);
+            if (lane >= o) { a += s; z += t; }
+        }
+        __syncthreads();
+        if (lane == 31) { sh.red[0][warp] = __float_as_uint(a); sh.red[1][warp] = __float_as_uint(z); }
+        if (threadIdx.x == 0) { sh.window[0] = kBuckets; sh.window[1] = kBuckets; }
+        __syncthreads();
+        float all_most = 0.f, all_least = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w == warp) { a += all_most; z += all_least; }
+            all_most += __uint_as_float((uint32_t)sh.red[0][w]);
+            all_least += __uint_as_float((uint32_t)sh.red[1][w]);
+        }
+        a -= most;
+        z -= least;
+#pragma unroll
+        for (int i = 0; i < each_has; ++i) {        // the first bucket that may reach it, and the first that surely has
+            a += up[i];
+            z += down[i];
+            if (a * 1.0001f >= top_p * all_least) atomicMin(&sh.window[0], (int)threadIdx.x * each_has + i);
+            if (z >= top_p * all_most * 1.0001f) atomicMin(&sh.window[1], (int)threadIdx.x * each_has + i);
+        }
+        __syncthreads();
+        const bool bounded = bucket_scale < 3e38f;      // else the buckets are wider than that
+        const int b0 = bounded ? sh.window[0] : 0, b1 = bounded ? sh.window[1] : kBuckets;
+        i64 above = 0, all = 0;
+        each([&](float x, int) {
+            int b;
+            if (bucket_of(x, b)) {
+                const i64 w = weight(x);
+                all += w;
+                if (b < b0) above += w;
+                else if (b <= b1 && w) add_weight(b, w);
+            }
+        });
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            all += __shfl_xor_sync(0xffffffffu, all, o);
+            above += __shfl_xor_sync(0xffffffffu, above, o);
+        }
+        __syncthreads();
+        if (lane == 0) { sh.red[0][warp] = all; sh.red[1][warp] = above; }
+        __syncthreads();
+        all = above = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) { all += sh.red[0][w]; above += sh.red[1][w]; }
+        if (blocks > 1) {
+            exchange(all, above);
+            all = above = 0;
+            for (int r = 0; r < blocks; ++r) { all += sh.xch[parity ^ 1][r][0]; above += sh.xch[parity ^ 1][r][1]; }
+        }
+        total = all;
+        want = share(top_p, all);
+        i64 in_window;
+        Found f = find<true>([&](i64) { return want - above; }, in_window);
+        f.before += above;
+        return f;
     }
 
     // The smallest logit whose weight is at least min_p, the largest among them always
@@ -500,8 +638,7 @@ template <typename T> struct Row {
         if (threadIdx.x < 64) sh.table[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
         // this block's vectors: of 16 bytes on their grid; what of them lies outside the row counts as -inf
         const bool unseen = bad;
-        float low = INFINITY;
-        top = -INFINITY;
+        float own = -INFINITY;              // this thread's largest
         if (!bad) {
             const T* const x = (const T*)p.logits + row * p.ld;
             const int shift = (int)(((uintptr_t)x & 15) / sizeof(T)), all_vecs = (shift + V + N - 1) / N, per = (all_vecs + blocks - 1) / blocks;
@@ -509,7 +646,7 @@ template <typename T> struct Row {
             vecs = min(per, all_vecs - v0);
             first = v0 * N - shift;
             const uint4* const from = reinterpret_cast<const uint4*>(x - shift) + v0;
-            constexpr int kAtOnce = 4;
+            constexpr int kAtOnce = 8;
             for (int va = threadIdx.x; va < vecs; va += kThreads * kAtOnce) {
                 uint4 w[kAtOnce];
 #pragma unroll
@@ -535,33 +672,21 @@ template <typename T> struct Row {
                     const int v = va + k * kThreads;
                     if (v < vecs) {
                         store[v] = w[k];
-#pragma unroll
-                        for (int e = 0; e < N; ++e) {
-                            const float y = Elements<T>::get(w[k], e);
-                            asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(y));
-                            low = fminf(low, y == -INFINITY ? INFINITY : y);
-                        }
+                        own = max_nan(own, Elements<T>::top(w[k]));
                     }
                 }
             }
+            top = own;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(__shfl_xor_sync(0xffffffffu, top, o)));
-                low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-            }
-            if (lane == 0) { sh.red[0][warp] = __float_as_uint(top); sh.red[1][warp] = __float_as_uint(low); }
+            for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if (lane == 0) sh.red[0][warp] = __float_as_uint(top);
             __syncthreads();
-            for (int w = 0; w < kWarps; ++w) {
-                asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(__uint_as_float((uint32_t)sh.red[0][w])));
-                low = fminf(low, __uint_as_float((uint32_t)sh.red[1][w]));
-            }
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) top = max_nan(top, __uint_as_float((uint32_t)sh.red[0][w]));
             if (blocks > 1) {
                 cluster.barrier_wait(std::move(started));       // the others' shared memory is there
-                exchange(__float_as_uint(top), __float_as_uint(low));
-                for (int r = 0; r < blocks; ++r) {
-                    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(__uint_as_float((uint32_t)sh.xch[parity ^ 1][r][0])));
-                    low = fminf(low, __uint_as_float((uint32_t)sh.xch[parity ^ 1][r][1]));
-                }
+                exchange(__float_as_uint(top), 0);
+                for (int r = 0; r < blocks; ++r) top = max_nan(top, __uint_as_float((uint32_t)sh.xch[parity ^ 1][r][0]));
             }
             bad = !(top < INFINITY) || top == -INFINITY;
         }
@@ -580,22 +705,34 @@ template <typename T> struct Row {
             return;
         }
         c = 1.4426950408889634074 / (double)temp;
-        {
-            const double range = fmin(((double)top - (double)low) * c, (double)kRange);
-            bucket_scale = range > 0.0 ? (float)fmin(2.0 * c * ((double)kBuckets - 0.5) / range, 3e38) : 0.f;
-        }
+        bucket_scale = (float)fmin(2.0 * c * ((double)kBuckets - 0.5) / (double)kRange, 3e38);
         const float least = least_of(min_p);
         auto weighed = [&](float x, int& b) { return bucket_of(x, b); };
         uint32_t tau = 0;               // kept: keys above tau, and at tau the ones up to index `last`
         i64 ties = -1;                  // how many at tau; -1: all
         int same = 0;
         bool by_k = top_k > 0 && top_k < V;
+        if (by_k && top_k <= kFewK) {
+            int b;
+            clear();
+            if (bucket_of(own, b)) atomicAdd(&sh.cnt[b], 1u);
+            sync();
+            const Found f = find<false>([&](i64) { return (i64)top_k; }, total);
+            if (f.bucket >= 0) {        // half a bucket and what fp32 rounds below its end
+                const float x0 = (top - ((float)f.bucket + 1.f) * 2.f / bucket_scale) - fabsf(top) * 2e-7f;
+                const int n = gather(true, x0, [](float) { return true; });
+                if (n <= kFew) {
+                    if (rank == 0) finish(d, n, top_k, top_p, least, u, -1);
+                    return sync();
+                }
+            }
+        }
         if (by_k) {
-            histogram<false>([&](float x, int, int& b) { return bucket_of(x, b); });
+            histogram<false>(-INFINITY, [&](float x, int& b) { return bucket_of(x, b); });
             const Found f = find<false>([&](i64) { return (i64)top_k; }, total);
             by_k = f.bucket >= 0;       // else fewer than top_k weigh anything
             if (by_k && f.count_before + f.count <= kFew) {
-                const int n = gather(true, [&](float x, int) { int b; return bucket_of(x, b) && b <= f.bucket; });
+                const int n = gather(true, -INFINITY, [&](float x) { int b; return bucket_of(x, b) && b <= f.bucket; });
                 if (rank == 0) finish(d, n, top_k, top_p, least, u, -1);
                 return sync();
             }
@@ -607,12 +744,17 @@ template <typename T> struct Row {
             }
         }
         if (top_p < 1.f) {
-            histogram<true>([&](float x, int, int& b) { return bucket_of(x, b) && key_of(x) > tau; });
             const i64 at_tau = by_k ? ties * weight(value_of(tau)) : 0;
             i64 want = 0;
-            const Found f = find<true>([&](i64 above) { return want = share(top_p, above + at_tau); }, total);
+            Found f;
+            if (by_k) {                 // few tokens
+                histogram<true>(value_of(tau), [&](float x, int& b) { return bucket_of(x, b) && key_of(x) > tau; });
+                f = find<true>([&](i64 above) { return want = share(top_p, above + at_tau); }, total);
+            } else {
+                f = by_weight(top_p, want, total);
+            }
             if (f.bucket >= 0 && f.count_before + f.count <= kFew) {
-                const int n = gather(true, [&](float x, int) { int b; return bucket_of(x, b) && key_of(x) > tau && b <= f.bucket; });
+                const int n = gather(true, -INFINITY, [&](float x) { int b; return bucket_of(x, b) && key_of(x) > tau && b <= f.bucket; });
                 if (rank == 0) finish(d, n, INT_MAX, top_p, least, u, total + at_tau);
                 return sync();
             }
@@ -645,12 +787,12 @@ template <typename T> struct Row {
             const int i = sh.index;
             const T v = ((const T*)p.logits + row * p.ld)[i];
             const float x = sizeof(T) == 4 ? *reinterpret_cast<const float*>(&v) : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(&v) << 16);
-            answer(d, i, (float)(power(x) / (double)total));
+            answer(d, i, (float)(power(power_of(x)) / (double)total));
         }
     }
 };
 
-template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ SampleDev p) {
+template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ SampleDev p) {
     __shared__ __align__(16) typename Row<T>::Shared sh;
     extern __shared__ __align__(16) uint4 data[];
     pdl_launch_dependents();
@@ -659,10 +801,10 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
 }
 
 template <typename T> cudaError_t launch_t(const SampleDev& p, cudaStream_t st) {
-    constexpr int kMost = 200 * 1024, kUsual = 56 * 1024;      // bytes of a row per block: what fits, and with what three share an SM
+    constexpr int kMost = 200 * 1024, kUsual = 88 * 1024;      // bytes of a row per block: what fits, and with what two share an SM
     const long long bytes = (long long)p.vocab * sizeof(T) + 32;
-    int blocks = 1;
-    while (blocks < kMaxBlocks && (bytes / blocks > kUsual || ((long long)p.rows * blocks * 2 <= 148 && bytes / blocks > 16 * 1024))) blocks *= 2;
+    int blocks = (int)min((long long)kMaxBlocks, (bytes + kUsual - 1) / kUsual);
+    while (blocks < kMaxBlocks && (long long)p.rows * (blocks + 1) <= 148 && bytes / blocks > 16 * 1024) ++blocks;      // SMs that no row has
     const size_t smem = (size_t)((bytes / 16 + 2 + blocks - 1) / blocks) * 16;
     static std::atomic<uint64_t> known{0};           // devices whose attribute is set
     int dev = 0;
