@@ -7,13 +7,16 @@
 // nothing and are left out of everything.
 //
 // A cluster of 1 to 8 blocks holds a row in shared memory, so it is read once.
-//   - top-k up to kFewK: the k-th largest of the threads' own maxima bounds the k-th logit from below; what reaches that bound (little more
-//     than k tokens) is gathered, and the first block does the rest with these alone, comparing each with each.
-//   - else thresholds come from a histogram of the distance to the largest logit, then of the keys within the bucket that holds the
-//     threshold, until at most kFew tokens are left.  For top-p the counts bound the weights of a bucket to 1.6 % either way, so
-//     only the buckets between those bounds get exact sums by atomics; everything above and all together are sums in registers.
-//     Where at most kFew tokens lie in the buckets up to the threshold's, these are gathered and finished as above.
-// The fp64 exponential, 12 instructions at half rate, is what rows without top-k spend their time on.
+//   - top-k up to kFewK: with b blocks, every block looks for a bound that at least k / b of its threads' own largest logits reach, and not many more; the
+//     lowest of the bounds is below the k-th logit.  What reaches it (little more than k tokens) is gathered, and the first block does
+//     the rest with these alone, comparing each with each.
+//   - larger top-k: a histogram of the distance to the largest logit by counts, then a list of the tokens in the bucket that holds the threshold.
+//   - top-p over the whole row: the counts bound the weights of a bucket to 1.6 % either way, so only what lies between those bounds (the
+//     window) gets a histogram of exact weights, in bins of 1/256 of a factor of two; what lies above is summed per strip of 512 tokens and
+//     all together per thread, in one pass.  The tokens of the window that turn out to be kept are added to their strips at the end.
+//   - the draw looks for the strip in which the sum passes u times the whole, and goes through that strip alone.
+// The fp64 exponential is 12 instructions at half rate and as many for its integers.  The functions that pass over a row are not
+// inlined and work on variables at fixed places of shared memory: together in one body they were fetched as slowly as they ran.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -26,11 +29,58 @@ namespace {
 
 namespace cg = cooperative_groups;
 typedef long long i64;
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBuckets = 1024;
-constexpr int kFew = 256, kFewK = 128;
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kBuckets = kThreads;
+constexpr int kFew = 256, kFewK = 128, kList = 2048;
 constexpr int kMaxBlocks = 8;           // of a cluster
+constexpr int kStrip = 512, kStrips = 8; // tokens, and how many of them a warp has at most
+constexpr int kInside = 24;             // elements of a thread inside the window, of up to 256
 constexpr float kRange = 46.f;          // log2 of the weights that count
+constexpr float kWidth = kRange / ((float)kBuckets - 0.5f);      // of a bucket
+
+struct Candidate {
+    unsigned long long order;       // key of the logit, then the lower index first
+    i64 w;
+    __device__ __forceinline__ int index() const { return 0x7FFFFFFF - (int)(uint32_t)order; }
+};
+struct Found {
+    i64 before, total;      // counts or weights in front of the bucket, and all
+    int bucket;             // -1: what was asked for is not reached
+    int count_before, count;
+};
+struct Row {
+    double c, top_d;        // log2 e / T; the largest logit
+    float top, scale;       // the largest logit; buckets per logit, times 2
+    int n, first;           // elements of this block (whole vectors), index of the first (negative: in front of the row)
+};
+struct Shared {
+    Row row;
+    uint32_t cnt[kBuckets];
+    union {
+        struct { uint32_t lo[kBuckets], hi[kBuckets]; };        // weights as hi 2^32 + lo
+        float list_mine[kList];                                 // logits of one bucket: this block's
+    };
+    union {
+        struct { Candidate all[kFew], mine[kFew]; };          // as they come, and in their order
+        float list[kList];                                      // and all blocks'
+    };
+    double table[256];                                          // 2^(i / 256)
+    uint32_t strip_lo[2][kWarps][kStrips], strip_hi[2][kWarps][kStrips];  // of counts and of weights
+    i64 xch[5][kMaxBlocks][2];
+    i64 red[2][kWarps];
+    int red_n[kWarps];
+    i64 front[kFew];
+    Found found;
+    int n_mine, n_all, n_of[kMaxBlocks];
+    int window[2];
+    int index, strip_at;
+    i64 strip_before;
+};
+__shared__ Shared sh;
+// Dynamic: the notes of what lies inside the window (which of a thread's elements), then this block's part of the row
+extern __shared__ __align__(16) uint8_t dynamic[];
+__device__ __forceinline__ uint8_t& noted_at(int q) { return dynamic[q * kThreads + threadIdx.x]; }
+__device__ __forceinline__ uint4* row_data() { return reinterpret_cast<uint4*>(dynamic + kInside * kThreads); }
 
 // Keys in the order of the logits; -0 as 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -38,774 +88,874 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
-
-template <typename T> struct Elements;
-template <> struct Elements<float> {
-    static constexpr int N = 4;
-    static __device__ __forceinline__ float get(const uint4& v, int e) { return __uint_as_float(e == 0 ? v.x : (e == 1 ? v.y : (e == 2 ? v.z : v.w))); }
-    // the largest of a vector, NaN if there is one
-    static __device__ __forceinline__ float top(const uint4& v) {
-        float m = __uint_as_float(v.x);
-        asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)));
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(v.w)));
-        return m;
-    }
-};
-template <> struct Elements<uint16_t> {
-    static constexpr int N = 8;
-    static __device__ __forceinline__ float get(const uint4& v, int e) {
-        const uint32_t w = e < 2 ? v.x : (e < 4 ? v.y : (e < 6 ? v.z : v.w));
-        return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
-    }
-    static __device__ __forceinline__ float top(const uint4& v) {
-        uint32_t a, b;
-        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
-        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
-        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
-        float m = __uint_as_float(a << 16);
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(a & 0xFFFF0000u)));
-        return m;
-    }
-};
 __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
     return a;
 }
 
-struct Candidate {
-    float x;
-    int index;
-    i64 w;
-};
-struct Found {
-    int bucket;             // -1: the target is not reached
-    int count_before, count;
-    i64 before;             // of what was asked for: counts or weights
-};
-
-template <typename T> struct Row {
-    static constexpr int N = Elements<T>::N;
-    struct Shared {
-        uint32_t cnt[kBuckets], lo[kBuckets], hi[kBuckets];     // counts, and weights as hi 2^32 + lo
-        Candidate all[kFew], mine[kFew];
-        double table[64];                                       // 2^(i / 64)
-        i64 xch[2][kMaxBlocks][2];
-        i64 red[2][kWarps];
-        Found found;
-        int n_mine, n_of[kMaxBlocks + 1];
-        int window[2];
-        uint32_t tau;
-        i64 above;
-        int same, index;
-    };
-    const SampleDev& p;
-    Shared& sh;
-    const uint4* data;              // this block's vectors
-    cg::cluster_group cluster;
-    const int rank, blocks, lane, warp;
-    int vecs, first;                // vectors of this block, index of its first element (negative: in front of the row)
-    int parity;
-    float top, bucket_scale;
-    double c;
-
-    __device__ __forceinline__ Row(const SampleDev& p_, Shared& s_, const uint4* d_)
-        : p(p_), sh(s_), data(d_), cluster(cg::this_cluster()), rank((int)cluster.block_rank()), blocks((int)cluster.num_blocks()), lane(threadIdx.x & 31),
-          warp(threadIdx.x >> 5), parity(0) {}
-
-    __device__ __forceinline__ void sync() {
-        if (blocks > 1) cluster.sync();
-        else __syncthreads();
+template <typename T> struct Elements;
+template <> struct Elements<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ float one(int i) { return reinterpret_cast<const float*>(row_data())[i]; }
+    // the largest of a vector, NaN if there is one
+    static __device__ __forceinline__ float top(const uint4& v) {
+        float m = __uint_as_float(v.x);
+        asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)));
+        return max_nan(m, __uint_as_float(v.w));
     }
-    template <typename F> __device__ __forceinline__ void each(F f) const {
-        for (int v = threadIdx.x; v < vecs; v += kThreads) {
-            const uint4 x = data[v];
+};
+template <> struct Elements<uint16_t> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ float one(int i) { return bf16_bits_to_float(reinterpret_cast<const uint16_t*>(row_data())[i]); }
+    static __device__ __forceinline__ float top(const uint4& v) {
+        uint32_t a, b;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+        return max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+    }
+};
+
+__device__ __forceinline__ int lane_id() { return threadIdx.x & 31; }
+__device__ __forceinline__ int warp_id() { return threadIdx.x >> 5; }
+__device__ __forceinline__ int rank_id() { return (int)cg::this_cluster().block_rank(); }
+__device__ __forceinline__ int n_blocks() { return (int)cg::this_cluster().num_blocks(); }
+__device__ __forceinline__ void sync_all() {
+    if (n_blocks() > 1) cg::this_cluster().sync();
+    else __syncthreads();
+}
+template <typename V> __device__ __forceinline__ V* of_block(V* p, int r) { return cg::this_cluster().map_shared_rank(p, r); }
+
+// Sum of non-negative 62-bit numbers over a warp, in three parts
+__device__ __forceinline__ i64 warp_sum(i64 x) {
+    const uint32_t a = __reduce_add_sync(0xffffffffu, (uint32_t)x & 0x1FFFFFu), b = __reduce_add_sync(0xffffffffu, (uint32_t)(x >> 21) & 0x1FFFFFu),
+                   c = __reduce_add_sync(0xffffffffu, (uint32_t)(x >> 42));
+    return (i64)a + ((i64)b << 21) + ((i64)c << 42);
+}
+// and over the lanes up to and with this one
+__device__ __forceinline__ i64 warp_upto(i64 x) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) f(Elements<T>::get(x, e), first + v * N + e);
-        }
+    for (int o = 1; o < 32; o <<= 1) {
+        const i64 t = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane_id() >= o) x += t;
     }
-    // 2^44 times the weight = 2^y, by 2^(i/64) 2^r with |r| <= 1/128 and the series of 2^r up to the fourth power (4e-14 off)
-    __device__ __forceinline__ double power(double y) const {
-        const double z = fma(y, 64.0, 6755399441055744.0);          // 1.5 2^52: 64 y as a whole number in the low bits
-        const int i = __double2loint(z);
-        const double r = fma(z - 6755399441055744.0, -0.015625, y);
-        double s = fma(r, 9.6181291076284772e-3, 5.5504108664821580e-2);        // (ln 2)^n / n!
-        s = fma(s, r, 2.4022650695910071e-1);
-        s = fma(s, r, 6.9314718055994531e-1);
-        s = fma(s, r, 1.0) * sh.table[i & 63];
-        return __hiloint2double(__double2hiint(s) + ((i >> 6) << 20), __double2loint(s));
+    return x;
+}
+// and over a block
+__device__ __noinline__ i64 block_sum(i64 x) {
+    x = warp_sum(x);
+    __syncthreads();
+    if (lane_id() == 0) sh.red[0][warp_id()] = x;
+    __syncthreads();
+    return warp_sum(sh.red[0][lane_id()]);
+}
+// a and b of this block to every block's sh.xch[site][rank]; a site is used again only after another exchange or sync_all
+__device__ __noinline__ void exchange(int site, i64 a, i64 b) {
+    if ((int)threadIdx.x < n_blocks()) {
+        i64* const to = of_block(&sh.xch[site][rank_id()][0], threadIdx.x);
+        to[0] = a;
+        to[1] = b;
     }
-    __device__ __forceinline__ double power_of(float x) const { return fma((double)x - (double)top, c, 44.0); }
-    __device__ __forceinline__ i64 weight(float x) const {
-        const double y = power_of(x);
-        const i64 w = __double_as_longlong(power(y) + 4503599627370496.0) & 0xFFFFFFFFFFFFFll;      // + 2^52: rounded to a whole number
-        return y > -2.0 ? w : 0;                                    // -inf too
+    cg::this_cluster().sync();
+}
+__device__ __noinline__ i64 cluster_sum(int site, i64 x) {      // x: of the block
+    const int n = n_blocks();
+    if (n == 1) return x;
+    exchange(site, x, 0);
+    x = 0;
+    for (int r = 0; r < n; ++r) x += sh.xch[site][r][0];
+    return x;
+}
+
+// 2^44 times the weight = 2^(Y/256), Y = 256 ((x - top) c + 44), by 2^(i/256) 2^(r/256) with |r| <= 1/2 and the series of 2^(r/256) up to the third
+// power (1.4e-13 off).  The constants are operands from the constant bank: as immediates, two of an instruction's took moves of their own.
+__constant__ double kMagic = 6755399441055744.0;            // 1.5 2^52: a sum with it holds the nearest whole number in the low bits
+__constant__ double kOnes = 4503599627370496.0;             // 2^52
+__constant__ double kSeries[3] = {2.7076061740622863e-3, 3.6655655969101060e-6, 3.3083026805413710e-9};      // (ln 2 / 256)^n / n!
+__constant__ double kTop = 44.0 * 256.0, kLeast = -2.0 * 256.0;
+struct Weigher {
+    double top, c;
+    __device__ __forceinline__ Weigher() : top(sh.row.top_d), c(sh.row.c * 256.0) {}
+    __device__ __forceinline__ double exponent(float x) const { return fma((double)x - top, c, kTop); }
+    static __device__ __forceinline__ double power(double y, int& i) {
+        const double z = y + kMagic;
+        i = __double2loint(z);
+        const double r = y - (z - kMagic);
+        double s = fma(r, kSeries[2], kSeries[1]);
+        s = fma(s, r, kSeries[0]);
+        s = fma(s, r, 1.0) * sh.table[i & 255];
+        return __hiloint2double(__double2hiint(s) + ((i >> 8) << 20), __double2loint(s));
     }
-    // Bucket by distance to the largest (a sum with 2^23 rounds it); false: weighs nothing (x = -inf at temperature inf: NaN)
-    __device__ __forceinline__ bool bucket_of(float x, int& b) const {
-        const float t = (0.5f * top - 0.5f * x) * bucket_scale;       // halves: the difference of two large logits is still a number
+    // i: Y rounded, where the weight is not zero
+    __device__ __forceinline__ i64 operator()(float x, int& i) const {
+        const double y = exponent(x);
+        const i64 w = __double_as_longlong(power(y, i) + kOnes) & 0xFFFFFFFFFFFFFll;      // rounded to a whole number
+        return y > kLeast ? w : 0;                                  // -inf too
+    }
+    __device__ __forceinline__ i64 operator()(float x) const {
+        int i;
+        return (*this)(x, i);
+    }
+    __device__ __forceinline__ float share_of(float x, i64 all) const {
+        int i;
+        return (float)(power(exponent(x), i) / (double)all);
+    }
+};
+// Bucket by distance to the largest (a sum with 2^23 rounds it); false: weighs nothing (x = -inf at temperature inf: NaN)
+struct Bucketer {
+    float half_top, scale;
+    __device__ __forceinline__ Bucketer() : half_top(0.5f * sh.row.top), scale(sh.row.scale) {}
+    __device__ __forceinline__ bool operator()(float x, int& b) const {
+        const float t = fmaf(x, -0.5f, half_top) * scale;           // halves: the difference of two large logits is still a number
         b = (int)(__float_as_uint(t + 8388608.f) & 0x7FFu);
         return t < (float)kBuckets - 0.5f;
     }
-    // a and b of this block to every block's sh.xch[parity ^ 1][rank]
-    __device__ __forceinline__ void exchange(i64 a, i64 b) {
-        if ((int)threadIdx.x < blocks) {
-            i64* const to = cluster.map_shared_rank(&sh.xch[parity][rank][0], threadIdx.x);
-            to[0] = a;
-            to[1] = b;
-        }
-        cluster.sync();
-        parity ^= 1;
-    }
-    // Sums of (a, b) over the threads of this block in front of this one; totals in all_a, all_b
-    __device__ __forceinline__ void before(i64& a, i64& b, i64& all_a, i64& all_b) {
-        i64 x = a, y = b;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const i64 s = __shfl_up_sync(0xffffffffu, x, o), t = __shfl_up_sync(0xffffffffu, y, o);
-            if (lane >= o) { x += s; y += t; }
-        }
-        __syncthreads();
-        if (lane == 31) { sh.red[0][warp] = x; sh.red[1][warp] = y; }
-        __syncthreads();
-        a = x - a;
-        b = y - b;
-        all_a = all_b = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w == warp) { a += all_a; b += all_b; }
-            all_a += sh.red[0][w];
-            all_b += sh.red[1][w];
-        }
-    }
-
-    // f(x, ...) for all elements that are at least x0, most vectors by their largest alone
-    template <typename F> __device__ __forceinline__ void each_from(float x0, F f) const {
-        for (int v = threadIdx.x; v < vecs; v += kThreads) {
-            const uint4 x = data[v];
-            if (Elements<T>::top(x) >= x0) {
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (Elements<T>::get(x, e) >= x0) f(Elements<T>::get(x, e), first + v * N + e);
-            }
-        }
-    }
-    __device__ __forceinline__ void add_weight(int b, i64 w) {
-        const uint32_t lo = (uint32_t)w, old = atomicAdd(&sh.lo[b], lo), hi = (uint32_t)(w >> 32) + (old + lo < old);
-        if (hi) atomicAdd(&sh.hi[b], hi);
-    }
-    __device__ __forceinline__ void clear() {
-        sync();                     // nobody reads the last one any more
-        for (int i = threadIdx.x; i < kBuckets; i += kThreads) sh.cnt[i] = sh.lo[i] = sh.hi[i] = 0;
-        __syncthreads();
-    }
-    // Histogram of what f puts into a bucket (f(x, b): whether it does) among the logits from x0 on, by counts alone or with the weights
-    template <bool MASS, typename F> __device__ __forceinline__ void histogram(float x0, F f) {
-        clear();
-        auto one = [&](float x, int) {
-            int b;
-            if (!f(x, b)) return;
-            // all lanes at one bucket (equal logits): one of them adds for all
-            const unsigned at = __activemask();
-            const int b0 = __shfl_sync(at, b, __ffs(at) - 1);
-            i64 w = MASS ? weight(x) : 0;
-            if (at == 0xffffffffu && __all_sync(at, b == b0)) {
-                if (MASS) {
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-                }
-                if (lane == 0) {
-                    atomicAdd(&sh.cnt[b], 32u);
-                    if (MASS && w) add_weight(b, w);
-                }
-            } else {
-                atomicAdd(&sh.cnt[b], 1u);
-                if (MASS && w) add_weight(b, w);
-            }
-        };
-        if (x0 > -INFINITY) each_from(x0, one);
-        else each(one);
-        sync();
-    }
-    // Counts and weights of bucket b in all blocks
-    template <bool MASS> __device__ __forceinline__ void bucket_sums(int b, i64& n, i64& w) {
-        uint32_t cnt[kMaxBlocks], lo[kMaxBlocks], hi[kMaxBlocks];
-#pragma unroll
-        for (int r = 0; r < kMaxBlocks; ++r) {
-            cnt[r] = lo[r] = hi[r] = 0;
-            if (r < blocks) {
-                cnt[r] = blocks > 1 ? cluster.map_shared_rank(sh.cnt, r)[b] : sh.cnt[b];
-                if (MASS) {
-                    lo[r] = blocks > 1 ? cluster.map_shared_rank(sh.lo, r)[b] : sh.lo[b];
-                    hi[r] = blocks > 1 ? cluster.map_shared_rank(sh.hi, r)[b] : sh.hi[b];
-                }
-            }
-        }
-        n = w = 0;
-#pragma unroll
-        for (int r = 0; r < kMaxBlocks; ++r) {
-            n += cnt[r];
-            if (MASS) w += ((i64)hi[r] << 32) + lo[r];
-        }
-    }
-    // The first bucket at which the running sum of the counts (or weights) over all blocks reaches what target(total) says
-    template <bool MASS, typename F> __device__ __forceinline__ Found find(F target, i64& total) {
-        constexpr int each_has = kBuckets / kThreads;
-        i64 val[each_has], cnt[each_has], a = 0, n = 0;
-#pragma unroll
-        for (int i = 0; i < each_has; ++i) {
-            bucket_sums<MASS>(threadIdx.x * each_has + i, cnt[i], val[i]);
-            if (!MASS) val[i] = cnt[i];
-            a += val[i];
-            n += cnt[i];
-        }
-        i64 all_n;
-        if (threadIdx.x == 0) sh.found.bucket = -1;
-        before(a, n, total, all_n);
-        const i64 want = target(total);
-#pragma unroll
-        for (int i = 0; i < each_has; ++i) {
-            if (a < want && want <= a + val[i]) sh.found = {(int)threadIdx.x * each_has + i, (int)n, (int)cnt[i], a};
-            a += val[i];
-            n += cnt[i];
-        }
-        __syncthreads();
-        const Found f = sh.found;
-        __syncthreads();
-        return f;
-    }
-
-    // Tokens from x0 on that f takes, of all blocks, to sh.all of this block (every block, or the first alone).  Returns how many there are: if more than kFew, none
-    // have been taken.
-    template <typename F> __device__ __forceinline__ int gather(bool first_only, float x0, F f) {
-        if (threadIdx.x == 0) sh.n_mine = 0;
-        sync();                     // and nobody reads sh.mine any more
-        auto one = [&](float x, int index) {
-            if (f(x)) {
-                const int at = atomicAdd(&sh.n_mine, 1);
-                if (at < kFew) sh.mine[at] = {x, index, 0};
-            }
-        };
-        if (x0 > -INFINITY) each_from(x0, one);
-        else each(one);
-        sync();
-        if ((int)threadIdx.x < blocks) sh.n_of[threadIdx.x + 1] = blocks > 1 ? *cluster.map_shared_rank(&sh.n_mine, threadIdx.x) : sh.n_mine;
-        __syncthreads();
-        int n = 0, r = 0, at = 0;   // this thread's candidate: the at-th of block r
-        for (int k = 0; k < blocks; ++k) {
-            if ((int)threadIdx.x >= n) { r = k; at = threadIdx.x - n; }
-            n += sh.n_of[k + 1];
-        }
-        if (n <= kFew && (int)threadIdx.x < n && (!first_only || rank == 0)) sh.all[threadIdx.x] = (blocks > 1 ? cluster.map_shared_rank(sh.mine, r) : sh.mine)[at];
-        return n;
-    }
-    // f(i, j) for all pairs of n candidates, the j of an i spread over lanes of a warp; done(i, on the first of these lanes) after sums a and b of what f
-    // adds to them.  All threads take part.
-    template <typename F, typename D> __device__ __forceinline__ void pairs(int n, F f, D done) {
-        int per = 1;
-        while (per < 32 && per * 2 * n <= kThreads) per *= 2;
-        for (int i0 = 0; i0 < n; i0 += kThreads / per) {
-            const int i = i0 + (int)threadIdx.x / per;
-            i64 a = 0;
-            int b = 0;
-            if (i < n)
-                for (int j = threadIdx.x % per; j < n; j += per) f(i, j, a, b);
-            for (int o = 1; o < per; o <<= 1) {
-                a += __shfl_xor_sync(0xffffffffu, a, o);
-                b += __shfl_xor_sync(0xffffffffu, b, o);
-            }
-            if (i < n && threadIdx.x % per == 0) done(i, a, b);
-        }
-    }
-    static __device__ __forceinline__ bool in_front(const Candidate& a, const Candidate& b) { return a.x > b.x || (a.x == b.x && a.index < b.index); }
-
-    // The logit at which the running sum (of counts, or of weights) in falling order reaches `want`, among the tokens that f takes (f(x, b): whether, and its bucket), after
-    // their histogram: to sh.tau its key, to sh.above the sum in front of it and to sh.same how many tokens have it.
-    template <bool MASS, typename F> __device__ __forceinline__ void threshold(Found got, i64 want, F f) {
-        i64 skipped = got.before;
-        uint32_t k0 = 0, k1 = 0xFFFFFFFFu;      // keys that are left
-        int shift = 32;                         // 32: by f; else buckets of 2^shift keys from k1 down
-        auto in = [&](float x) {
-            const uint32_t k = key_of(x);
-            int b;
-            if (k < k0 || k > k1) return false;
-            if (shift == 32) return f(x, b) && b == got.bucket;
-            return (int)((k1 - k) >> shift) == got.bucket;
-        };
-        while (got.count > kFew) {
-            // range of the keys in this bucket
-            uint32_t most = 0, least = 0xFFFFFFFFu;
-            each([&](float x, int) {
-                if (in(x)) {
-                    const uint32_t k = key_of(x);
-                    most = max(most, k);
-                    least = min(least, k);
-                }
-            });
-            most = __reduce_max_sync(0xffffffffu, most);
-            least = __reduce_min_sync(0xffffffffu, least);
-            __syncthreads();
-            if (lane == 0) { sh.red[0][warp] = most; sh.red[1][warp] = least; }
-            __syncthreads();
-            for (int w = 0; w < kWarps; ++w) {
-                most = max(most, (uint32_t)sh.red[0][w]);
-                least = min(least, (uint32_t)sh.red[1][w]);
-            }
-            if (blocks > 1) {
-                exchange(most, least);
-                for (int r = 0; r < blocks; ++r) {
-                    most = max(most, (uint32_t)sh.xch[parity ^ 1][r][0]);
-                    least = min(least, (uint32_t)sh.xch[parity ^ 1][r][1]);
-                }
-            }
-            if (most == least) {
-                __syncthreads();
-                if (threadIdx.x == 0) { sh.tau = most; sh.above = skipped; sh.same = got.count; }
-                __syncthreads();
-                return;
-            }
-            const uint32_t n0 = least, n1 = most;
-            int s = 0;
-            while (((n1 - n0) >> s) >= (uint32_t)kBuckets) ++s;
-            // keys between the least and the most of a bucket are all in it
-            histogram<MASS>(value_of(n0), [&](float x, int& b) {
-                const uint32_t k = key_of(x);
-                b = (int)((n1 - k) >> s);
-                return k >= n0 && k <= n1 && weighs(x, f);
-            });
-            k0 = n0;
-            k1 = n1;
-            shift = s;
-            i64 total;
-            got = find<MASS>([&](i64) { return want - skipped; }, total);
-            skipped += got.before;
-        }
-        const int n = gather(false, -INFINITY, [&](float x) { return in(x) && (shift == 32 || weighs(x, f)); });
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) sh.all[i].w = MASS ? weight(sh.all[i].x) : 1;
-        __syncthreads();
-        pairs(n, [&](int i, int j, i64& a, int& b) {
-            if (sh.all[j].x > sh.all[i].x) a += sh.all[j].w;
-            b += sh.all[j].x == sh.all[i].x;
-        }, [&](int i, i64 a, int b) {
-            if (skipped + a < want && want <= skipped + a + b * sh.all[i].w) {
-                sh.tau = key_of(sh.all[i].x);
-                sh.above = skipped + a;
-                sh.same = b;
-            }
-        });
-        __syncthreads();
-    }
-    template <typename F> static __device__ __forceinline__ bool weighs(float x, F f) {
-        int b;
-        return f(x, b);
-    }
-
-    // The first index at which the running sum of f over the row exceeds `target`, to sh.index of every block that asks; total: the whole sum.  A warp takes
-    // a run of neighbouring vectors.
-    template <typename F, typename G> __device__ __forceinline__ void walk(F f, G target, i64& total) {
-        const int run = ((vecs + kWarps - 1) / kWarps + 31) / 32 * 32, v0 = min(vecs, warp * run), v1 = min(vecs, v0 + run);      // at most 32 strips of 32 vectors
-        auto of_vec = [&](int v) {
-            i64 s = 0;
-            if (v < v1) {
-                const uint4 x = data[v];
-#pragma unroll
-                for (int e = 0; e < N; ++e) s += f(Elements<T>::get(x, e), first + v * N + e);
-            }
-            return s;
-        };
-        i64 strip = 0;              // of lane i: the sum of strip i
-        for (int v = v0, i = 0; v < v1; v += 32, ++i) {
-            i64 one = of_vec(v + lane);
-            if (__any_sync(0xffffffffu, one != 0)) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) one += __shfl_xor_sync(0xffffffffu, one, o);
-                if (lane == i) strip = one;
-            }
-        }
-        i64 mine = strip;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const i64 t = __shfl_up_sync(0xffffffffu, mine, o);
-            if (lane >= o) mine += t;
-        }
-        const i64 strips = mine;    // up to and with strip i
-        mine = __shfl_sync(0xffffffffu, mine, 31);
-        __syncthreads();
-        if (lane == 0) sh.red[0][warp] = mine;
-        __syncthreads();
-        i64 at = 0, block = 0;
-        for (int w = 0; w < kWarps; ++w) {
-            if (w == warp) at = block;
-            block += sh.red[0][w];
-        }
-        total = block;
-        if (blocks > 1) {
-            exchange(block, 0);
-            total = 0;
-            for (int r = 0; r < blocks; ++r) {
-                if (r == rank) at += total;
-                total += sh.xch[parity ^ 1][r][0];
-            }
-        }
-        const i64 want = target(total);
-        if (at <= want && want < at + mine) {
-            const int i = __ffs(__ballot_sync(0xffffffffu, want < at + strips)) - 1, v = v0 + i * 32 + lane;
-            const i64 s = of_vec(v);
-            i64 upto = s;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const i64 t = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += t;
-            }
-            i64 sum = at + __shfl_sync(0xffffffffu, strips - strip, i) + upto - s;
-            if (sum <= want && want < sum + s) {
-                const uint4 x = data[v];
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const int index = first + v * N + e;
-                    const i64 one = f(Elements<T>::get(x, e), index);
-                    if (sum <= want && want < sum + one) {
-                        for (int r = 0; r < blocks; ++r) *(blocks > 1 ? cluster.map_shared_rank(&sh.index, r) : &sh.index) = index;
-                    }
-                    sum += one;
-                }
-            }
-        }
-        sync();
-    }
-
-    __device__ __forceinline__ void answer(int d, int token, float prob) const {
-        p.token[d] = token;
-        if (p.prob) p.prob[d] = prob;
-    }
-    static __device__ __forceinline__ i64 drawn(float u, i64 all) {
-        const double x = u < 0.f ? 0.0 : (double)u;
-        return x >= 1.0 ? all - 1 : min(all - 1, (i64)(x * (double)all));
-    }
-    static __device__ __forceinline__ i64 share(float top_p, i64 all) {
-        const i64 want = (i64)ceil((double)top_p * (double)all);
-        return want < 1 ? 1 : want;
-    }
-
-    // Few candidates, those in front of the order among them: the rest of the filters and the draw, by the first block.  all: the weight that top-p is a share of, or
-    // (negative) that of the first top_k.
-    __device__ __forceinline__ void finish(int d, int n, int top_k, float top_p, float least, float u, i64 all) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) sh.all[i].w = weight(sh.all[i].x);
-        __syncthreads();
-        // rank and weight in front, kept in sh.mine
-        pairs(n, [&](int i, int j, i64& a, int& b) {
-            if (in_front(sh.all[j], sh.all[i])) {
-                a += sh.all[j].w;
-                ++b;
-            }
-        }, [&](int i, i64 a, int b) { sh.mine[i] = {0.f, b, a}; });
-        __syncthreads();
-        if (all < 0) {
-            i64 a = 0, b = 0;
-            for (int i = threadIdx.x; i < n; i += kThreads)
-                if (sh.mine[i].index < top_k) a += sh.all[i].w;
-            block_sum(a);
-            all = a;
-        }
-        const i64 want = top_p < 1.f ? share(top_p, all) : all + 1;
-        i64 kept = 0;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            if (sh.mine[i].index >= top_k || sh.mine[i].w >= want || !(sh.all[i].x >= least)) sh.all[i].w = 0;
-            kept += sh.all[i].w;
-        }
-        block_sum(kept);
-        const i64 r = drawn(u, kept);
-        pairs(n, [&](int i, int j, i64& a, int&) {
-            if (sh.all[j].index < sh.all[i].index) a += sh.all[j].w;
-        }, [&](int i, i64 a, int) {
-            if (a <= r && r < a + sh.all[i].w) answer(d, sh.all[i].index, (float)(power(power_of(sh.all[i].x)) / (double)kept));
-        });
-    }
-    __device__ __forceinline__ void block_sum(i64& a) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-        __syncthreads();
-        if (lane == 0) sh.red[0][warp] = a;
-        __syncthreads();
-        a = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) a += sh.red[0][w];
-    }
-
-    // Top-p over the whole row: the bucket in which the weights reach `want` = top_p of all of them (`total`).
-    __device__ __forceinline__ Found by_weight(float top_p, i64& want, i64& total) {
-        histogram<false>(-INFINITY, [&](float x, int& b) { return bucket_of(x, b); });
-        // Between b - 1/2 and b + 1/2 buckets from the largest, n tokens weigh n 2^(-b width) to within half a bucket; the sums below are in units of 2^44 and
-        // rounded by far less than the rest of a bucket that is added.
-        constexpr int each_has = kBuckets / kThreads;
-        constexpr float width = kRange / ((float)kBuckets - 0.5f);
-        float most = 0.f, least = 0.f, up[each_has], down[each_has];
-#pragma unroll
-        for (int i = 0; i < each_has; ++i) {
-            const int b = threadIdx.x * each_has + i;
-            i64 n, w;
-            bucket_sums<false>(b, n, w);
-            up[i] = (float)n * exp2f(-((float)b - 0.75f) * width);
-            down[i] = (float)n * exp2f(-((float)b + 0.75f) * width);
-            most += up[i];
-            least += down[i];
-        }
-        float a = most, z = least;          // up to and with this thread
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const float s = __shfl_up_sync(0xffffffffu, a, o), t = __shfl_up_sync(0xffffffffu, z, o);
-            if (lane >= o) { a += s; z += t; }
-        }
-        __syncthreads();
-        if (lane == 31) { sh.red[0][warp] = __float_as_uint(a); sh.red[1][warp] = __float_as_uint(z); }
-        if (threadIdx.x == 0) { sh.window[0] = kBuckets; sh.window[1] = kBuckets; }
-        __syncthreads();
-        float all_most = 0.f, all_least = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w == warp) { a += all_most; z += all_least; }
-            all_most += __uint_as_float((uint32_t)sh.red[0][w]);
-            all_least += __uint_as_float((uint32_t)sh.red[1][w]);
-        }
-        a -= most;
-        z -= least;
-#pragma unroll
-        for (int i = 0; i < each_has; ++i) {        // the first bucket that may reach it, and the first that surely has
-            a += up[i];
-            z += down[i];
-            if (a * 1.0001f >= top_p * all_least) atomicMin(&sh.window[0], (int)threadIdx.x * each_has + i);
-            if (z >= top_p * all_most * 1.0001f) atomicMin(&sh.window[1], (int)threadIdx.x * each_has + i);
-        }
-        __syncthreads();
-        const bool bounded = bucket_scale < 3e38f;      // else the buckets are wider than that
-        const int b0 = bounded ? sh.window[0] : 0, b1 = bounded ? sh.window[1] : kBuckets;
-        i64 above = 0, all = 0;
-        each([&](float x, int) {
-            int b;
-            if (bucket_of(x, b)) {
-                const i64 w = weight(x);
-                all += w;
-                if (b < b0) above += w;
-                else if (b <= b1 && w) add_weight(b, w);
-            }
-        });
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            all += __shfl_xor_sync(0xffffffffu, all, o);
-            above += __shfl_xor_sync(0xffffffffu, above, o);
-        }
-        __syncthreads();
-        if (lane == 0) { sh.red[0][warp] = all; sh.red[1][warp] = above; }
-        __syncthreads();
-        all = above = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) { all += sh.red[0][w]; above += sh.red[1][w]; }
-        if (blocks > 1) {
-            exchange(all, above);
-            all = above = 0;
-            for (int r = 0; r < blocks; ++r) { all += sh.xch[parity ^ 1][r][0]; above += sh.xch[parity ^ 1][r][1]; }
-        }
-        total = all;
-        want = share(top_p, all);
-        i64 in_window;
-        Found f = find<true>([&](i64) { return want - above; }, in_window);
-        f.before += above;
-        return f;
-    }
-
-    // The smallest logit whose weight is at least min_p, the largest among them always
-    __device__ __forceinline__ float least_of(float min_p) const {
-        if (!(min_p > 0.f)) return -INFINITY;
-        const double log_p = log2((double)min_p);
-        if (log_p >= 0.0) return top;
-        if (c == 0.0) return -3.402823466e38f;
-        auto in = [&](float x) { return ((double)x - (double)top) * c >= log_p; };
-        float x = (float)fmax((double)top + log_p / c, -3.4028234663852886e38);
-        while (in(x) && x > -3.402823466e38f) x = value_of(key_of(x) - 1);
-        while (!in(x)) x = value_of(key_of(x) + 1);
-        return fminf(x, top);
-    }
-
-    __device__ __forceinline__ void run(uint4* store) {
-        const int d = blockIdx.x / blocks, row = p.row ? p.row[d] : d, V = p.vocab;
-        if (row < 0) return;
-        const float temp = p.temperature ? p.temperature[d] : 1.f, top_p = p.top_p ? p.top_p[d] : 1.f, min_p = p.min_p ? p.min_p[d] : 0.f, u = p.u[d];
-        int top_k = p.top_k ? p.top_k[d] : 0;
-        bool bad = row >= p.logit_rows || !(temp >= 0.f) || isnan(top_p) || isnan(min_p) || isnan(u);
-        cg::cluster_group::arrival_token started;
-        if (blocks > 1) started = cluster.barrier_arrive();
-        if (threadIdx.x < 64) sh.table[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
-        // this block's vectors: of 16 bytes on their grid; what of them lies outside the row counts as -inf
-        const bool unseen = bad;
-        float own = -INFINITY;              // this thread's largest
-        if (!bad) {
-            const T* const x = (const T*)p.logits + row * p.ld;
-            const int shift = (int)(((uintptr_t)x & 15) / sizeof(T)), all_vecs = (shift + V + N - 1) / N, per = (all_vecs + blocks - 1) / blocks;
-            const int v0 = min(all_vecs, rank * per);
-            vecs = min(per, all_vecs - v0);
-            first = v0 * N - shift;
-            const uint4* const from = reinterpret_cast<const uint4*>(x - shift) + v0;
-            constexpr int kAtOnce = 8;
-            for (int va = threadIdx.x; va < vecs; va += kThreads * kAtOnce) {
-                uint4 w[kAtOnce];
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const int v = va + k * kThreads, i = first + v * N;
-                    if (v < vecs) {
-                        if (i >= 0 && i + N <= V) {
-                            w[k] = __ldcg(from + v);
-                        } else {
-                            uint32_t y[4] = {0, 0, 0, 0};
-#pragma unroll
-                            for (int e = 0; e < N; ++e) {
-                                const bool there = i + e >= 0 && i + e < V;
-                                if (sizeof(T) == 4) y[e] = there ? reinterpret_cast<const uint32_t*>(x)[i + e] : 0xFF800000u;
-                                else y[e / 2] |= (there ? (uint32_t)reinterpret_cast<const uint16_t*>(x)[i + e] : 0xFF80u) << (16 * (e & 1));
-                            }
-                            w[k] = make_uint4(y[0], y[1], y[2], y[3]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const int v = va + k * kThreads;
-                    if (v < vecs) {
-                        store[v] = w[k];
-                        own = max_nan(own, Elements<T>::top(w[k]));
-                    }
-                }
-            }
-            top = own;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-            if (lane == 0) sh.red[0][warp] = __float_as_uint(top);
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = max_nan(top, __uint_as_float((uint32_t)sh.red[0][w]));
-            if (blocks > 1) {
-                cluster.barrier_wait(std::move(started));       // the others' shared memory is there
-                exchange(__float_as_uint(top), 0);
-                for (int r = 0; r < blocks; ++r) top = max_nan(top, __uint_as_float((uint32_t)sh.xch[parity ^ 1][r][0]));
-            }
-            bad = !(top < INFINITY) || top == -INFINITY;
-        }
-        if (bad) {
-            if (threadIdx.x == 0 && rank == 0) {
-                answer(d, -1, 0.f);
-                report(p.d_status, CATS_ERR_INVALID_ARG);
-            }
-            if (blocks > 1 && unseen) cluster.barrier_wait(std::move(started));
-            return;
-        }
-        i64 total;
-        if (temp == 0.f) {
-            walk([&](float x, int) { return (i64)(x == top); }, [](i64) { return (i64)0; }, total);
-            if (threadIdx.x == 0 && rank == 0) answer(d, sh.index, 1.f);
-            return;
-        }
-        c = 1.4426950408889634074 / (double)temp;
-        bucket_scale = (float)fmin(2.0 * c * ((double)kBuckets - 0.5) / (double)kRange, 3e38);
-        const float least = least_of(min_p);
-        auto weighed = [&](float x, int& b) { return bucket_of(x, b); };
-        uint32_t tau = 0;               // kept: keys above tau, and at tau the ones up to index `last`
-        i64 ties = -1;                  // how many at tau; -1: all
-        int same = 0;
-        bool by_k = top_k > 0 && top_k < V;
-        if (by_k && top_k <= kFewK) {
-            int b;
-            clear();
-            if (bucket_of(own, b)) atomicAdd(&sh.cnt[b], 1u);
-            sync();
-            const Found f = find<false>([&](i64) { return (i64)top_k; }, total);
-            if (f.bucket >= 0) {        // half a bucket and what fp32 rounds below its end
-                const float x0 = (top - ((float)f.bucket + 1.f) * 2.f / bucket_scale) - fabsf(top) * 2e-7f;
-                const int n = gather(true, x0, [](float) { return true; });
-                if (n <= kFew) {
-                    if (rank == 0) finish(d, n, top_k, top_p, least, u, -1);
-                    return sync();
-                }
-            }
-        }
-        if (by_k) {
-            histogram<false>(-INFINITY, [&](float x, int& b) { return bucket_of(x, b); });
-            const Found f = find<false>([&](i64) { return (i64)top_k; }, total);
-            by_k = f.bucket >= 0;       // else fewer than top_k weigh anything
-            if (by_k && f.count_before + f.count <= kFew) {
-                const int n = gather(true, -INFINITY, [&](float x) { int b; return bucket_of(x, b) && b <= f.bucket; });
-                if (rank == 0) finish(d, n, top_k, top_p, least, u, -1);
-                return sync();
-            }
-            if (by_k) {
-                threshold<false>(f, top_k, weighed);
-                tau = sh.tau;
-                ties = top_k - sh.above;
-                same = sh.same;
-            }
-        }
-        if (top_p < 1.f) {
-            const i64 at_tau = by_k ? ties * weight(value_of(tau)) : 0;
-            i64 want = 0;
-            Found f;
-            if (by_k) {                 // few tokens
-                histogram<true>(value_of(tau), [&](float x, int& b) { return bucket_of(x, b) && key_of(x) > tau; });
-                f = find<true>([&](i64 above) { return want = share(top_p, above + at_tau); }, total);
-            } else {
-                f = by_weight(top_p, want, total);
-            }
-            if (f.bucket >= 0 && f.count_before + f.count <= kFew) {
-                const int n = gather(true, -INFINITY, [&](float x) { int b; return bucket_of(x, b) && key_of(x) > tau && b <= f.bucket; });
-                if (rank == 0) finish(d, n, INT_MAX, top_p, least, u, total + at_tau);
-                return sync();
-            }
-            if (f.bucket >= 0) {
-                threshold<true>(f, want, [&](float x, int& b) { return bucket_of(x, b) && key_of(x) > tau; });
-                tau = sh.tau;
-                const i64 w = weight(value_of(tau));
-                ties = (want - sh.above + w - 1) / w;
-                same = sh.same;
-            } else {                    // inside the tokens at the threshold of top-k
-                const i64 w = weight(value_of(tau));
-                ties = (want - total + w - 1) / w;
-            }
-        }
-        if (least > -INFINITY && key_of(least) > tau) {
-            tau = key_of(least);
-            ties = -1;
-        }
-        int last = INT_MAX;
-        if (ties >= 0 && ties < same) {
-            walk([&](float x, int) { return (i64)(key_of(x) == tau); }, [&](i64) { return ties - 1; }, total);
-            last = sh.index;
-            sync();
-        }
-        walk([&](float x, int index) {
-            const uint32_t k = key_of(x);
-            return k > tau || (k == tau && index <= last) ? weight(x) : (i64)0;
-        }, [&](i64 all) { return drawn(u, all); }, total);
-        if (threadIdx.x == 0 && rank == 0) {
-            const int i = sh.index;
-            const T v = ((const T*)p.logits + row * p.ld)[i];
-            const float x = sizeof(T) == 4 ? *reinterpret_cast<const float*>(&v) : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(&v) << 16);
-            answer(d, i, (float)(power(power_of(x)) / (double)total));
-        }
-    }
 };
+// A logit below all of bucket b: half a bucket and what fp32 rounds
+__device__ __forceinline__ float below_bucket(int b) {
+    const float top = sh.row.top;
+    return (top - ((float)b + 1.f) * 2.f / sh.row.scale) - fabsf(top) * 2e-7f;
+}
 
-template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ SampleDev p) {
-    __shared__ __align__(16) typename Row<T>::Shared sh;
-    extern __shared__ __align__(16) uint4 data[];
+// A block's elements are followed by -inf up to a whole strip.
+__device__ __forceinline__ int padded(int n) { return (n + kStrip - 1) / kStrip * kStrip; }
+// f(x, i) for all elements that are at least x0, most vectors by their largest alone
+template <typename T, typename F> __device__ __forceinline__ void each_from(float x0, F f) {
+    constexpr int N = Elements<T>::N;
+    const int n = sh.row.n / N;
+#pragma unroll 4
+    for (int v = threadIdx.x; v < n; v += kThreads) {
+        if (Elements<T>::top(row_data()[v]) >= x0) {
+#pragma unroll 1
+            for (int e = 0; e < N; ++e) {
+                const float x = Elements<T>::one(v * N + e);
+                if (x >= x0) f(x, v * N + e);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void add64(uint32_t& lo, uint32_t& hi, i64 w) {
+    const uint32_t a = (uint32_t)w, old = atomicAdd(&lo, a), b = (uint32_t)(w >> 32) + (old + a < old);
+    if (b) atomicAdd(&hi, b);
+}
+__device__ __noinline__ void clear(bool first = false) {
+    if (!first) sync_all();         // nobody reads the last histogram any more
+    for (int i = threadIdx.x; i < kBuckets; i += kThreads) sh.cnt[i] = sh.lo[i] = sh.hi[i] = 0;
+    __syncthreads();
+}
+// How many tokens each bucket has
+template <typename T> __device__ __noinline__ void count(bool first) {
+    clear(first);
+    const Bucketer bucket;
+    const int n = padded(sh.row.n);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        int b;
+        if (bucket(Elements<T>::one(i), b)) atomicAdd(&sh.cnt[b], 1u);
+    }
+    sync_all();
+}
+// Counts and weights of bucket b in all blocks
+__device__ __forceinline__ void bucket_sums(int b, bool weights, int& n, i64& w) {
+    const int blocks = n_blocks();
+    uint32_t cnt[kMaxBlocks], lo[kMaxBlocks], hi[kMaxBlocks];
+#pragma unroll
+    for (int r = 0; r < kMaxBlocks; ++r) {
+        cnt[r] = lo[r] = hi[r] = 0;
+        if (r < blocks) {
+            cnt[r] = *of_block(&sh.cnt[b], r);
+            if (weights) {
+                lo[r] = *of_block(&sh.lo[b], r);
+                hi[r] = *of_block(&sh.hi[b], r);
+            }
+        }
+    }
+    n = 0;
+    w = 0;
+#pragma unroll
+    for (int r = 0; r < kMaxBlocks; ++r) {
+        n += (int)cnt[r];
+        w += ((i64)hi[r] << 32) + lo[r];
+    }
+}
+__device__ __forceinline__ i64 share(float top_p, i64 all) {
+    const i64 want = (i64)ceil((double)top_p * (double)all);
+    return want < 1 ? 1 : want;
+}
+// The first bucket at which the running sum of the counts (or weights) over all blocks reaches `want`; want < 0: reaches share(top_p, all + more)
+__device__ __noinline__ Found find(bool weights, i64 want, float top_p, i64 more) {
+    int n0;
+    i64 w0;
+    bucket_sums(threadIdx.x, weights, n0, w0);
+    if (!weights) w0 = n0;
+    const i64 mine = warp_sum(w0);
+    const int mine_n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n0);
+    __syncthreads();
+    if (lane_id() == 0) { sh.red[0][warp_id()] = mine; sh.red_n[warp_id()] = mine_n; }
+    __syncthreads();
+    const i64 of_warp = sh.red[0][lane_id()], up = warp_upto(of_warp), total = __shfl_sync(0xffffffffu, up, 31);
+    if (want < 0) want = share(top_p, total + more);
+    const unsigned reached = __ballot_sync(0xffffffffu, up >= want);
+    const int w = reached ? __ffs(reached) - 1 : -1;
+    if (w == warp_id()) {
+        const i64 at = __shfl_sync(0xffffffffu, up - of_warp, w) + warp_upto(w0) - w0;
+        int n = (int)__reduce_add_sync(0xffffffffu, lane_id() < w ? (unsigned)sh.red_n[lane_id()] : 0u), before = n0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, before, o);
+            if (lane_id() >= o) before += t;
+        }
+        if (at < want && want <= at + w0) sh.found = {at, total, (int)threadIdx.x, n + before - n0, n0};
+    } else if (w < 0 && threadIdx.x == 0) {
+        sh.found = {0, total, -1, 0, 0};
+    }
+    __syncthreads();
+    return sh.found;
+}
+
+// After every block has its sh.n_mine: their sum, and each of them in sh.n_of
+__device__ __noinline__ int sizes() {
+    sync_all();
+    const int blocks = n_blocks();
+    if ((int)threadIdx.x < blocks) sh.n_of[threadIdx.x] = *of_block(&sh.n_mine, threadIdx.x);
+    __syncthreads();
+    int n = 0;
+    for (int k = 0; k < blocks; ++k) n += sh.n_of[k];
+    return n;
+}
+__device__ __forceinline__ void place(int i, int& r, int& at) {       // the i-th of all is the at-th of block r
+    int n = 0;
+    r = at = 0;
+    for (int k = 0; k < n_blocks(); ++k) {
+        if (i >= n) { r = k; at = i - n; }
+        n += sh.n_of[k];
+    }
+}
+// The tokens from x0 on, of all blocks, to sh.all of the first block, and how many there are to the sh.n_all of all (more than kFew: some have been left out).
+// sh.n_all is zero before.
+template <typename T> __device__ __noinline__ void gather(float x0) {
+    const int first = sh.row.first, blocks = n_blocks();
+    int* const n = of_block(&sh.n_all, 0);
+    Candidate* const all = of_block(sh.all, 0);
+    each_from<T>(x0, [&](float x, int i) {
+        const int at = atomicAdd(n, 1);
+        if (at < kFew) all[at] = {((unsigned long long)key_of(x) << 32) | (uint32_t)(0x7FFFFFFF - (first + i)), 0};
+    });
+    sync_all();
+    if (blocks > 1) {
+        if (threadIdx.x == 0 && rank_id() != 0) sh.n_all = *n;
+        __syncthreads();
+    }
+}
+// Strips: a warp has a run of neighbouring tokens, a strip at a time; lane l the elements l, l + 32, ... of it
+__device__ __forceinline__ int run_of_warp(int n) { return ((n + kWarps - 1) / kWarps + kStrip - 1) / kStrip * kStrip; }
+__device__ __forceinline__ int element_inside(int q) {
+    const int n = padded(sh.row.n);
+    return min(n, warp_id() * run_of_warp(n)) + lane_id() + 32 * noted_at(q);
+}
+struct Threshold {
+    float tau;
+    i64 above;              // sum in front of the tokens at tau
+    int same;               // how many there are
+};
+// The logit at which the running sum (of counts, or of weights) in falling order reaches `want`: among the tokens from x0 on that in(x) says lie in got's
+// bucket.  Every block finds it.
+template <typename T, bool MASS, typename F> __device__ __noinline__ Threshold threshold(Found got, i64 want, float x0, F in, int inside = -1) {
+    const Weigher weight;
+    const int blocks = n_blocks();
+    if (got.count > kList) {                // rare (equal logits, a flat row): bisection over the keys, a pass for each step
+        uint32_t hi = 0, lo = 0xFFFFFFFFu;
+        each_from<T>(x0, [&](float x, int) {
+            if (in(x)) {
+                hi = max(hi, key_of(x));
+                lo = min(lo, key_of(x));
+            }
+        });
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        __syncthreads();
+        if (lane_id() == 0) { sh.red[0][warp_id()] = hi; sh.red[1][warp_id()] = lo; }
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) {
+            hi = max(hi, (uint32_t)sh.red[0][w]);
+            lo = min(lo, (uint32_t)sh.red[1][w]);
+        }
+        if (blocks > 1) {
+            exchange(2, hi, lo);
+            for (int r = 0; r < blocks; ++r) {
+                hi = max(hi, (uint32_t)sh.xch[2][r][0]);
+                lo = min(lo, (uint32_t)sh.xch[2][r][1]);
+            }
+        }
+        int site = 3;
+        auto sum_from = [&](uint32_t least, bool weights) {
+            i64 sum = 0;
+            each_from<T>(x0, [&](float x, int) {
+                if (in(x) && key_of(x) >= least) sum += weights ? weight(x) : 1;
+            });
+            site = 7 - site;
+            return cluster_sum(site, block_sum(sum));
+        };
+        if (lo == hi) return {value_of(hi), got.before, got.count};
+        while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo + 1) / 2;
+            if (got.before + sum_from(mid, MASS) >= want) lo = mid;
+            else hi = mid - 1;
+        }
+        const i64 above = sum_from(lo + 1, MASS), n = sum_from(lo, false), n1 = sum_from(lo + 1, false);
+        return {value_of(lo), got.before + above, (int)(n - n1)};
+    }
+    sync_all();                             // nobody reads the histogram and sh.n_mine any more
+    if (threadIdx.x == 0) sh.n_mine = 0;
+    __syncthreads();
+    if (inside >= 0) {                      // this many of the thread's elements may be in the bucket
+        for (int q = 0; q < inside; ++q) {
+            const float x = Elements<T>::one(element_inside(q));
+            if (in(x)) sh.list_mine[atomicAdd(&sh.n_mine, 1)] = x;
+        }
+    } else {
+        each_from<T>(x0, [&](float x, int) {
+            if (in(x)) sh.list_mine[atomicAdd(&sh.n_mine, 1)] = x;
+        });
+    }
+    const int n = sizes();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        int r, at;
+        place(i, r, at);
+        sh.list[i] = of_block(sh.list_mine, r)[at];
+    }
+    __syncthreads();
+    // bisection over the keys of the list, by every warp for itself as long as a lane has few, else by the block
+    constexpr int kEach = kList / kThreads;
+    const bool alone = n <= 32 * kEach;
+    const int me = alone ? lane_id() : (int)threadIdx.x, step = alone ? 32 : kThreads;
+    uint32_t key[kEach], hi = 0, lo = 0xFFFFFFFFu;
+    i64 w[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        key[k] = 0;
+        w[k] = 0;
+        if (me + k * step < n) {
+            const float x = sh.list[me + k * step];
+            key[k] = key_of(x);
+            w[k] = MASS ? weight(x) : 1;
+            hi = max(hi, key[k]);
+            lo = min(lo, key[k]);
+        }
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    if (!alone) {
+        __syncthreads();
+        if (lane_id() == 0) { sh.red[0][warp_id()] = hi; sh.red[1][warp_id()] = lo; }
+        __syncthreads();
+        for (int k = 0; k < kWarps; ++k) {
+            hi = max(hi, (uint32_t)sh.red[0][k]);
+            lo = min(lo, (uint32_t)sh.red[1][k]);
+        }
+    }
+    while (lo < hi) {                       // the largest key from which on the sum reaches `want`
+        const uint32_t mid = lo + (hi - lo + 1) / 2;
+        i64 sum = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) sum += key[k] >= mid ? w[k] : 0;
+        sum = alone ? warp_sum(sum) : block_sum(sum);
+        if (got.before + sum >= want) lo = mid;
+        else hi = mid - 1;
+    }
+    i64 above = 0, same = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        above += key[k] > lo ? w[k] : 0;
+        same += key[k] == lo && me + k * step < n;
+    }
+    above = alone ? warp_sum(above) : block_sum(above);
+    same = alone ? warp_sum(same) : block_sum(same);
+    return {value_of(lo), got.before + above, (int)same};
+}
+
+// What a strip adds up: its tokens equal to tau; the weights of those from tau on; the same, but at tau only up to element `last`; or the weights above a
+// window of the weights' exponents, while all are added up and a thread notes which of its elements are inside.
+enum Sum : int { kEqual, kFrom, kKept, kAbove };
+struct Window { int high, low, shift; };
+template <typename T, int WHAT> __device__ __noinline__ i64 strips(float tau, int last, Window win, int& inside) {
+    const int n = padded(sh.row.n), run = run_of_warp(n), i0 = min(n, warp_id() * run), i1 = min(n, i0 + run);
+    const Weigher weight;
+    i64 strip = 0, all = 0;         // of lane k: the sum of strip k
+    int noted = 0;
+    for (int i = i0, k = 0; i < i1; i += kStrip, ++k) {
+        const int first = i + lane_id();
+        if (WHAT != kAbove && tau > -INFINITY) {
+            float most = -INFINITY;
+#pragma unroll 8
+            for (int e = 0; e < kStrip; e += 32) most = fmaxf(most, Elements<T>::one(first + e));
+            if (!__any_sync(0xffffffffu, most >= tau)) continue;
+        }
+        i64 sum = 0;
+        uint32_t equal = 0;
+#pragma unroll 4
+        for (int e = 0; e < kStrip; e += 32) {
+            const float x = Elements<T>::one(first + e);
+            if (WHAT == kEqual) {
+                equal += x == tau;
+            } else if (WHAT == kFrom) {
+                const i64 w = weight(x);
+                if (x >= tau) sum += w;
+            } else if (WHAT == kKept) {
+                const i64 w = weight(x);
+                if (x > tau || (x == tau && first + e <= last)) sum += w;
+            } else {
+                int at;
+                const i64 w = weight(x, at);
+                all += w;
+                if (at > win.high) sum += w;
+                if (at <= win.high && at >= win.low && w != 0) {
+                    if (noted < kInside) noted_at(noted) = (uint8_t)((i - i0 + e) / 32);
+                    ++noted;
+                }
+            }
+        }
+        sum = WHAT == kEqual ? (i64)__reduce_add_sync(0xffffffffu, equal) : warp_sum(sum);
+        if (lane_id() == k) strip = sum;
+    }
+    if (lane_id() < kStrips) {
+        sh.strip_lo[WHAT != kEqual][warp_id()][lane_id()] = (uint32_t)strip;
+        sh.strip_hi[WHAT != kEqual][warp_id()][lane_id()] = (uint32_t)(strip >> 32);
+    }
+    inside = noted;
+    return all;
+}
+// f(x, i, w, at) for the elements inside the window, at: the bin.  noted: false where a thread had no room, then they are looked for.
+template <typename T, typename F> __device__ __forceinline__ void each_inside(bool noted, int inside, Window win, F f) {
+    const Weigher weight;
+    auto one = [&](float x, int i) {
+        int at;
+        const i64 w = weight(x, at);
+        if (w != 0 && at <= win.high && at >= win.low) f(x, i, w, (win.high - at) >> win.shift);
+    };
+    if (noted) {
+        for (int q = 0; q < inside; ++q) {
+            const int i = element_inside(q);
+            one(Elements<T>::one(i), i);
+        }
+    } else {
+        for (int i = threadIdx.x; i < sh.row.n; i += kThreads) one(Elements<T>::one(i), i);
+    }
+}
+// The histogram of the window
+template <typename T> __device__ __noinline__ void bins(bool noted, int inside, Window win) {
+    each_inside<T>(noted, inside, win, [](float, int, i64 w, int b) {
+        atomicAdd(&sh.cnt[b], 1u);
+        add64(sh.lo[b], sh.hi[b], w);
+    });
+    sync_all();
+}
+// Its kept tokens, to the strips
+template <typename T> __device__ __noinline__ void add_kept(bool noted, int inside, float tau, int last, Window win) {
+    const int run = run_of_warp(padded(sh.row.n));
+    __syncthreads();
+    each_inside<T>(noted, inside, win, [=](float x, int i, i64 w, int) {
+        if (x > tau || (x == tau && i <= last)) {
+            const int of = i / run, k = (i - of * run) / kStrip;
+            add64(sh.strip_lo[1][of][k], sh.strip_hi[1][of][k], w);
+        }
+    });
+}
+__device__ __forceinline__ i64 strip_sum(int of) {      // of the warp's strip that the lane stands for
+    return lane_id() < kStrips ? ((i64)sh.strip_hi[of][warp_id()][lane_id()] << 32) + sh.strip_lo[of][warp_id()][lane_id()] : 0;
+}
+__device__ __forceinline__ i64 drawn(float u, i64 all) {
+    const double x = u < 0.f ? 0.0 : (double)u;
+    return x >= 1.0 ? all - 1 : min(all - 1, (i64)(x * (double)all));
+}
+__device__ __forceinline__ void answer(const SampleDev& p, int d, int token, float prob) {
+    p.token[d] = token;
+    if (p.prob) p.prob[d] = prob;
+}
+// The first index at which the sum over the strips' tokens passes `want` (want < 0: drawn(u, total)).  draw >= 0: it is answered as that draw's token, and nothing
+// more is to be done; else it goes to sh.index of every block.
+template <typename T> __device__ __noinline__ void locate(const SampleDev& p, int draw, int what, float tau, int last, i64 want, float u) {
+    const int n = padded(sh.row.n), i0 = min(n, warp_id() * run_of_warp(n)), blocks = n_blocks(), rank = rank_id();
+    __syncthreads();
+    const i64 strip = strip_sum(what != kEqual), up = warp_upto(strip), mine = __shfl_sync(0xffffffffu, up, 31);
+    if (lane_id() == 0) sh.red[0][warp_id()] = mine;
+    if (threadIdx.x == 0) sh.strip_at = -1;
+    __syncthreads();
+    const i64 of_warp = sh.red[0][lane_id()], warps = warp_upto(of_warp);
+    i64 at = __shfl_sync(0xffffffffu, warps - of_warp, warp_id()), total = __shfl_sync(0xffffffffu, warps, 31);
+    if (blocks > 1) {
+        exchange(1, total, 0);
+        total = 0;
+        for (int r = 0; r < blocks; ++r) {
+            if (r == rank) at += total;
+            total += sh.xch[1][r][0];
+        }
+    }
+    if (want < 0) want = drawn(u, total);
+    if (at <= want && want < at + mine) {
+        const int k = __ffs(__ballot_sync(0xffffffffu, want < at + up)) - 1;
+        const i64 sum = at + __shfl_sync(0xffffffffu, up - strip, k);
+        if (lane_id() == 0) { sh.strip_at = i0 + k * kStrip; sh.strip_before = sum; }
+    }
+    __syncthreads();
+    if (sh.strip_at >= 0) {         // a thread for each token of that strip
+        static_assert(kStrip <= kThreads, "one token per thread");
+        const Weigher weight;
+        const int i = sh.strip_at + (int)threadIdx.x;
+        i64 one = 0;
+        float x = -INFINITY;
+        if ((int)threadIdx.x < kStrip) {
+            x = Elements<T>::one(i);
+            const i64 w = what == kEqual ? 1 : weight(x);
+            if (what == kEqual ? x == tau : (x > tau || (x == tau && i <= last))) one = w;
+        }
+        const i64 to = warp_upto(one);
+        if (lane_id() == 31) sh.red[1][warp_id()] = to;
+        __syncthreads();
+        const i64 others = sh.red[1][lane_id()], before = __shfl_sync(0xffffffffu, warp_upto(others) - others, warp_id());
+        const i64 sum = sh.strip_before + before + to - one;
+        if (sum <= want && want < sum + one) {
+            if (draw >= 0) answer(p, draw, sh.row.first + i, what == kEqual ? 1.f : weight.share_of(x, total));
+            else for (int r = 0; r < blocks; ++r) *of_block(&sh.index, r) = sh.row.first + i;
+        }
+    }
+    if (draw < 0) sync_all();
+}
+
+// Top-p over the whole row: strips of what lies above the window, and the window's histogram; returns the window.  all: the weights of the row.
+template <typename T> __device__ __noinline__ Window weigh(float top_p, i64& all, bool& noted, int& inside) {
+    count<T>(true);
+    // n tokens of bucket b weigh n 2^(-b width) to within half a bucket; fp32 places a logit to 2^-23 of 1024 buckets, 2^-13 of one.  The sums are in units of 2^44.
+    constexpr float kHalf = 0.501f;
+    int count_of;
+    i64 unused;
+    bucket_sums(threadIdx.x, false, count_of, unused);
+    float a = (float)count_of * exp2f(-((float)threadIdx.x - kHalf) * kWidth), z = (float)count_of * exp2f(-((float)threadIdx.x + kHalf) * kWidth);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {          // up to and with this bucket
+        const float s = __shfl_up_sync(0xffffffffu, a, o), t = __shfl_up_sync(0xffffffffu, z, o);
+        if (lane_id() >= o) { a += s; z += t; }
+    }
+    __syncthreads();
+    if (lane_id() == 31) { sh.red[0][warp_id()] = __float_as_uint(a); sh.red[1][warp_id()] = __float_as_uint(z); }
+    if (threadIdx.x == 0) sh.window[0] = sh.window[1] = kBuckets;
+    __syncthreads();
+    float all_up = __uint_as_float((uint32_t)sh.red[0][lane_id()]), all_down = __uint_as_float((uint32_t)sh.red[1][lane_id()]);
+    const float up0 = all_up, down0 = all_down;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float s = __shfl_up_sync(0xffffffffu, all_up, o), t = __shfl_up_sync(0xffffffffu, all_down, o);
+        if (lane_id() >= o) { all_up += s; all_down += t; }
+    }
+    a += __shfl_sync(0xffffffffu, all_up - up0, warp_id());
+    z += __shfl_sync(0xffffffffu, all_down - down0, warp_id());
+    all_up = __shfl_sync(0xffffffffu, all_up, 31);
+    all_down = __shfl_sync(0xffffffffu, all_down, 31);
+    // the first bucket that may reach it, and the first that surely has
+    if (a * 1.0001f >= top_p * all_down) atomicMin(&sh.window[0], (int)threadIdx.x);
+    if (z >= top_p * all_up * 1.0001f) atomicMin(&sh.window[1], (int)threadIdx.x);
+    __syncthreads();
+    // as exponents: 256 y runs from 44 256 down to -2 256
+    const bool bounded = sh.row.scale < 3e38f;      // else the buckets are wider than that
+    Window win;
+    win.high = bounded ? (int)ceilf(256.f * (44.f - ((float)sh.window[0] - kHalf) * kWidth)) + 1 : 44 * 256 + 1;
+    win.low = bounded && sh.window[1] < kBuckets ? (int)floorf(256.f * (44.f - ((float)sh.window[1] + kHalf) * kWidth)) - 1 : -2 * 256 - 1;
+    win.shift = 0;
+    while (((win.high - win.low) >> win.shift) >= kBuckets) ++win.shift;
+    clear();
+    all = cluster_sum(0, block_sum(strips<T, kAbove>(0.f, 0, win, inside)));
+    noted = !__syncthreads_or(inside > kInside);
+    bins<T>(noted, inside, win);
+    return win;
+}
+
+// f(i, j) for all pairs of n candidates, the j of an i spread over lanes of a warp; done(i, on the first of these lanes) after sums a and b of what f
+// adds to them.  All threads take part.
+template <typename F, typename D> __device__ __forceinline__ void pairs(int n, F f, D done) {
+    int per = 1;
+    while (per < 32 && per * 2 * n <= kThreads) per *= 2;
+    for (int i0 = 0; i0 < n; i0 += kThreads / per) {
+        const int i = i0 + (int)threadIdx.x / per;
+        i64 a = 0;
+        int b = 0;
+        if (i < n) {
+#pragma unroll 4
+            for (int j = threadIdx.x % per; j < n; j += per) f(i, j, a, b);
+        }
+        for (int o = 1; o < per; o <<= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
+        }
+        if (i < n && threadIdx.x % per == 0) done(i, a, b);
+    }
+}
+// n candidates in sh.all, the first top_k of the order among them: the filters and the draw, by one block
+__device__ __noinline__ void finish(const SampleDev& p, int d, int n, int top_k, float top_p, float least, float u) {
+    const Weigher weight;
+    const bool mine = (int)threadIdx.x < n;
+    const float x = mine ? value_of((uint32_t)(sh.all[threadIdx.x].order >> 32)) : 0.f;
+    i64 w = mine ? weight(x) : 0;
+    if (mine) sh.all[threadIdx.x].w = w;
+    __syncthreads();
+    // into their order, with the weight in front of each
+    pairs(n, [&](int i, int j, i64& a, int& b) {
+        const Candidate y = sh.all[j];
+        if (y.order > sh.all[i].order) {
+            a += y.w;
+            ++b;
+        }
+    }, [&](int i, i64 a, int b) {
+        sh.mine[b] = sh.all[i];
+        sh.front[b] = a;
+    });
+    __syncthreads();
+    n = min(n, top_k);
+    const i64 all = sh.front[n - 1] + sh.mine[n - 1].w, want = top_p < 1.f ? share(top_p, all) : all + 1;
+    const bool in = (int)threadIdx.x < n && sh.front[threadIdx.x] < want && value_of((uint32_t)(sh.mine[threadIdx.x].order >> 32)) >= least;
+    n = __syncthreads_count(in);            // those in front
+    const i64 kept = sh.front[n - 1] + sh.mine[n - 1].w, r = drawn(u, kept);
+    // by index: the low words fall as the index rises
+    pairs(n, [&](int i, int j, i64& a, int&) {
+        const Candidate y = sh.mine[j];
+        if ((uint32_t)y.order > (uint32_t)sh.mine[i].order) a += y.w;
+    }, [&](int i, i64 a, int) {
+        const Candidate c = sh.mine[i];
+        if (a <= r && r < a + c.w) answer(p, d, c.index(), weight.share_of(value_of((uint32_t)(c.order >> 32)), kept));
+    });
+}
+
+// The smallest logit whose weight is at least min_p, the largest among them always
+__device__ __noinline__ float least_of(float min_p) {
+    if (!(min_p > 0.f)) return -INFINITY;
+    const float top = sh.row.top;
+    const double log_p = log2((double)min_p), c = sh.row.c;
+    if (log_p >= 0.0) return top;
+    if (c == 0.0) return -3.402823466e38f;
+    auto in = [&](float x) { return ((double)x - (double)top) * c >= log_p; };
+    float x = (float)fmax((double)top + log_p / c, -3.4028234663852886e38);
+    while (in(x) && x > -3.402823466e38f) x = value_of(key_of(x) - 1);
+    while (!in(x)) x = value_of(key_of(x) + 1);
+    return fminf(x, top);
+}
+
+template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ SampleDev p) {
+    constexpr int N = Elements<T>::N;
     pdl_launch_dependents();
+    if (threadIdx.x < 256) sh.table[threadIdx.x] = exp2((double)threadIdx.x / 256.0);
+    if (threadIdx.x == 0) sh.n_all = 0;
+    const int blocks = n_blocks(), rank = rank_id(), d = blockIdx.x / blocks, V = p.vocab;
+    cg::cluster_group::arrival_token started;
+    if (blocks > 1) started = cg::this_cluster().barrier_arrive();
     pdl_wait();
-    Row<T>(p, sh, data).run(data);
+    const int row = p.row ? p.row[d] : d;
+    const float temp = p.temperature ? p.temperature[d] : 1.f, top_p = p.top_p ? p.top_p[d] : 1.f, min_p = p.min_p ? p.min_p[d] : 0.f, u = p.u[d];
+    const int top_k = p.top_k ? p.top_k[d] : 0;
+    bool bad = row >= p.logit_rows || !(temp >= 0.f) || isnan(top_p) || isnan(min_p) || isnan(u);
+    const T* const x = (const T*)p.logits + (bad || row < 0 ? 0 : row) * p.ld;
+    float own = -INFINITY, top = -INFINITY;              // the largest of this thread's, of the row
+    if (row >= 0 && !bad) {
+        // this block's vectors: of 16 bytes on their grid; what of them lies outside the row counts as -inf
+        const int shift = (int)(((uintptr_t)x & 15) / sizeof(T)), all_vecs = (shift + V + N - 1) / N, per = (all_vecs + blocks - 1) / blocks;
+        const int v0 = min(all_vecs, rank * per), vecs = min(per, all_vecs - v0), first = v0 * N - shift;
+        const uint4* const from = reinterpret_cast<const uint4*>(x - shift) + v0;
+        constexpr int kAtOnce = 4;
+        for (int va = threadIdx.x; va < vecs; va += kThreads * kAtOnce) {
+            uint4 w[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int v = va + k * kThreads, i = first + v * N;
+                w[k] = make_uint4(0, 0, 0, 0);
+                if (v < vecs && i >= 0 && i + N <= V) w[k] = __ldcg(from + v);
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int v = va + k * kThreads, i = first + v * N;
+                if (v >= vecs) break;
+                if (i < 0 || i + N > V) {
+                    uint32_t y[4] = {0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const bool there = i + e >= 0 && i + e < V;
+                        if (sizeof(T) == 4) y[e & 3] = there ? reinterpret_cast<const uint32_t*>(x)[i + e] : 0xFF800000u;
+                        else y[e / 2] |= (there ? (uint32_t)reinterpret_cast<const uint16_t*>(x)[i + e] : 0xFF80u) << (16 * (e & 1));
+                    }
+                    w[k] = make_uint4(y[0], y[1], y[2], y[3]);
+                }
+                row_data()[v] = w[k];
+                own = max_nan(own, Elements<T>::top(w[k]));
+            }
+        }
+        const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+        for (int v = vecs + threadIdx.x; v < padded(vecs * N) / N; v += kThreads) row_data()[v] = make_uint4(none, none, none, none);
+        top = own;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (lane_id() == 0) sh.red[0][warp_id()] = __float_as_uint(top);
+        if (threadIdx.x == 0) { sh.row.n = vecs * N; sh.row.first = first; }
+        __syncthreads();
+        top = __uint_as_float((uint32_t)sh.red[0][lane_id()]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    const bool by_bound = row >= 0 && !bad && top_k > 0 && top_k < V && top_k <= kFewK && temp > 0.f;
+    float bound = -INFINITY;
+    if (by_bound) {                 // that at least `least` of the block's threads reach, and at most half as many more if a few steps find it
+        const int least = (top_k + blocks - 1) / blocks;
+        float step = fminf(temp, 1e30f), low = top - step;
+        int n = 0;
+        for (int k = 0; k < 12 && (n = __syncthreads_count(own >= low)) < least; ++k) {
+            step *= 2.f;
+            low = top - step;
+        }
+        if (n >= least) {
+            float high = low + 0.5f * step;         // too few reach that, or it is the largest
+            for (int k = 0; k < 6 && n > least + least / 2; ++k) {
+                const float mid = 0.5f * low + 0.5f * high;
+                const int m = __syncthreads_count(own >= mid);
+                if (m >= least) {
+                    low = mid;
+                    n = m;
+                } else {
+                    high = mid;
+                }
+            }
+            bound = low;
+        }
+    }
+    if (blocks > 1) cg::this_cluster().barrier_wait(std::move(started));      // the others' shared memory is there
+    if (row < 0) return;
+    if (!bad) {
+        if (blocks > 1) {
+            exchange(4, __float_as_uint(top), __float_as_uint(bound));
+            for (int r = 0; r < blocks; ++r) {
+                top = max_nan(top, __uint_as_float((uint32_t)sh.xch[4][r][0]));
+                bound = fminf(bound, __uint_as_float((uint32_t)sh.xch[4][r][1]));
+            }
+        }
+        bad = !(top < INFINITY) || top == -INFINITY;
+    }
+    if (bad) {
+        if (threadIdx.x == 0 && rank == 0) {
+            answer(p, d, -1, 0.f);
+            report(p.d_status, CATS_ERR_INVALID_ARG);
+        }
+        return sync_all();
+    }
+    const double c = temp == 0.f ? 0.0 : 1.4426950408889634074 / (double)temp;
+    if (threadIdx.x == 0) {
+        sh.row.top = top;
+        sh.row.top_d = (double)top;
+        sh.row.c = c;
+        sh.row.scale = (float)fmin(2.0 * c / (double)kWidth, 3e38);
+    }
+    __syncthreads();
+    if (temp == 0.f) {
+        int none;
+        strips<T, kEqual>(top, 0, {}, none);
+        return locate<T>(p, d, kEqual, top, 0, 0, u);
+    }
+    const float least = least_of(min_p);
+    float tau = -INFINITY;          // kept: logits above tau, and at tau the ones up to index `last`
+    i64 ties = -1;                  // how many at tau; -1: all
+    int same = 0;
+    bool by_k = top_k > 0 && top_k < V;
+    if (by_bound && bound > -INFINITY) {
+        gather<T>(bound);
+        if (sh.n_all <= kFew) {
+            if (rank == 0) finish(p, d, sh.n_all, top_k, top_p, least, u);
+            return sync_all();
+        }
+    }
+    if (by_k) {
+        count<T>(!by_bound);
+        const Found f = find(false, top_k, 0.f, 0);
+        by_k = f.bucket >= 0;       // else fewer than top_k weigh anything
+        if (by_k) {
+            const Bucketer bucket;
+            const int at = f.bucket;
+            const Threshold t = threshold<T, false>(f, top_k, below_bucket(at), [bucket, at](float y) { int b; return bucket(y, b) && b == at; });
+            tau = t.tau;
+            ties = top_k - t.above;
+            same = t.same;
+        }
+    }
+    Window win = {};
+    bool windowed = false, noted = false;       // strips of what lies above the window are there; notes of what lies inside
+    int inside = 0;
+    if (top_p < 1.f && by_k) {      // few tokens: of the logits above tau, and so many at tau
+        const Weigher weight;
+        const Bucketer bucket;
+        clear();
+        each_from<T>(tau, [&](float y, int) {
+            int b;
+            if (y > tau && bucket(y, b)) {
+                atomicAdd(&sh.cnt[b], 1u);
+                add64(sh.lo[b], sh.hi[b], weight(y));
+            }
+        });
+        sync_all();
+        const i64 w = weight(tau), at_tau = ties * w;
+        const Found f = find(true, -1, top_p, at_tau);
+        const i64 want = share(top_p, f.total + at_tau);
+        if (f.bucket >= 0) {
+            const int at = f.bucket;
+            const Threshold t = threshold<T, true>(f, want, fmaxf(tau, below_bucket(at)), [bucket, at, tau](float y) { int b; return y > tau && bucket(y, b) && b == at; });
+            tau = t.tau;
+            const i64 v = weight(tau);
+            ties = (want - t.above + v - 1) / v;
+            same = t.same;
+        } else {                    // inside the tokens at the threshold of top-k
+            ties = (want - f.total + w - 1) / w;
+        }
+    } else if (top_p < 1.f) {
+        i64 all;
+        win = weigh<T>(top_p, all, noted, inside);
+        windowed = true;
+        // in front of the window
+        i64 above = block_sum(strip_sum(1));
+        above = cluster_sum(1, above);
+        const i64 want = share(top_p, all);
+        Found f = find(true, want - above, 0.f, 0);
+        f.before += above;
+        const Weigher weight;
+        const int at = f.bucket;
+        // a logit below all of the bin: one more bin and what fp32 rounds
+        const double low = (double)(win.high - ((at + 1) << win.shift) - 2) / 256.0 - 44.0;
+        const float x0 = c == 0.0 ? -3.402823466e38f : (float)fmax((double)top + low / c - fabs((double)top) * 2e-7 - fabs(low / c) * 2e-7, -3.4028234663852886e38);
+        const Threshold t = threshold<T, true>(f, want, x0, [weight, at, win](float y) {
+            int i;
+            return weight(y, i) != 0 && i <= win.high && i >= win.low && (win.high - i) >> win.shift == at;
+        }, noted ? inside : -1);
+        tau = t.tau;
+        const i64 v = weight(tau);
+        ties = (want - t.above + v - 1) / v;
+        same = t.same;
+    }
+    if (least > tau) {
+        tau = least;
+        ties = -1;
+        windowed = false;           // the strips may hold more than that
+    }
+    int last = kMaxSampleVocab;     // an element of this block
+    if (ties >= 0 && ties < same) {
+        int none;
+        strips<T, kEqual>(tau, 0, {}, none);
+        locate<T>(p, -1, kEqual, tau, 0, ties - 1, u);
+        last = sh.index - sh.row.first;
+        sync_all();
+    }
+    if (windowed) add_kept<T>(noted, inside, tau, last, win);
+    else if (last == kMaxSampleVocab) strips<T, kFrom>(tau, last, {}, inside);
+    else strips<T, kKept>(tau, last, {}, inside);
+    locate<T>(p, d, kKept, tau, last, -1, u);
 }
 
 template <typename T> cudaError_t launch_t(const SampleDev& p, cudaStream_t st) {
-    constexpr int kMost = 200 * 1024, kUsual = 88 * 1024;      // bytes of a row per block: what fits, and with what two share an SM
+    constexpr int kMost = 196 * 1024, kUsual = 136 * 1024;     // bytes of a row per block: what fits with the rest, and what is taken where rows are many
     const long long bytes = (long long)p.vocab * sizeof(T) + 32;
-    int blocks = (int)min((long long)kMaxBlocks, (bytes + kUsual - 1) / kUsual);
-    while (blocks < kMaxBlocks && (long long)p.rows * (blocks + 1) <= 148 && bytes / blocks > 16 * 1024) ++blocks;      // SMs that no row has
-    const size_t smem = (size_t)((bytes / 16 + 2 + blocks - 1) / blocks) * 16;
+    const int blocks = (int)min((long long)kMaxBlocks, (bytes + kUsual - 1) / kUsual);
+    const size_t smem = (size_t)((bytes / 16 + 2 + blocks - 1) / blocks) * 16 + kStrip * sizeof(T) + kInside * kThreads;
     static std::atomic<uint64_t> known{0};           // devices whose attribute is set
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
