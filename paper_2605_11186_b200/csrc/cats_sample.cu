@@ -48,9 +48,15 @@ struct Found {
     int bucket;             // -1: what was asked for is not reached
     int count_before, count;
 };
+struct Threshold {
+    float tau;
+    i64 above;              // sum in front of the tokens at tau
+    int same;               // how many there are
+};
 struct Row {
     double c, top_d;        // log2 e / T; the largest logit
     float top, scale;       // the largest logit; buckets per logit, times 2
+    float floor;            // logits from here down weigh nothing (600 powers of two below the largest, that one excluded)
     int n, first;           // elements of this block (whole vectors), index of the first (negative: in front of the row)
 };
 struct Shared {
@@ -69,18 +75,20 @@ struct Shared {
     i64 xch[5][kMaxBlocks][2];
     i64 red[2][kWarps];
     int red_n[kWarps];
+    i64 sum;
     i64 front[kFew];
-    Found found;
+    Found found, result;
+    Threshold threshold;
     int n_mine, n_all, n_of[kMaxBlocks];
     int window[2];
     int index, strip_at;
     i64 strip_before;
 };
 __shared__ Shared sh;
-// Dynamic: the notes of what lies inside the window (which of a thread's elements), then this block's part of the row
+// Dynamic: the notes of what lies inside the window (which of a thread's elements; a place for those too many), then this block's part of the row
 extern __shared__ __align__(16) uint8_t dynamic[];
 __device__ __forceinline__ uint8_t& noted_at(int q) { return dynamic[q * kThreads + threadIdx.x]; }
-__device__ __forceinline__ uint4* row_data() { return reinterpret_cast<uint4*>(dynamic + kInside * kThreads); }
+__device__ __forceinline__ uint4* row_data() { return reinterpret_cast<uint4*>(dynamic + (kInside + 1) * kThreads); }
 
 // Keys in the order of the logits; -0 as 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -141,13 +149,18 @@ __device__ __forceinline__ i64 warp_upto(i64 x) {
     }
     return x;
 }
-// and over a block
+// and over a block; the second stage by one warp (by all of them, their reductions queue)
 __device__ __noinline__ i64 block_sum(i64 x) {
     x = warp_sum(x);
     __syncthreads();
     if (lane_id() == 0) sh.red[0][warp_id()] = x;
     __syncthreads();
-    return warp_sum(sh.red[0][lane_id()]);
+    if (warp_id() == 0) {
+        x = warp_sum(sh.red[0][lane_id()]);
+        if (lane_id() == 0) sh.sum = x;
+    }
+    __syncthreads();
+    return sh.sum;
 }
 // a and b of this block to every block's sh.xch[site][rank]; a site is used again only after another exchange or sync_all
 __device__ __noinline__ void exchange(int site, i64 a, i64 b) {
@@ -172,10 +185,11 @@ __device__ __noinline__ i64 cluster_sum(int site, i64 x) {      // x: of the blo
 __constant__ double kMagic = 6755399441055744.0;            // 1.5 2^52: a sum with it holds the nearest whole number in the low bits
 __constant__ double kOnes = 4503599627370496.0;             // 2^52
 __constant__ double kSeries[3] = {2.7076061740622863e-3, 3.6655655969101060e-6, 3.3083026805413710e-9};      // (ln 2 / 256)^n / n!
-__constant__ double kTop = 44.0 * 256.0, kLeast = -2.0 * 256.0;
+__constant__ double kTop = 44.0 * 256.0;
 struct Weigher {
     double top, c;
-    __device__ __forceinline__ Weigher() : top(sh.row.top_d), c(sh.row.c * 256.0) {}
+    float floor;
+    __device__ __forceinline__ Weigher() : top(sh.row.top_d), c(sh.row.c * 256.0), floor(sh.row.floor) {}
     __device__ __forceinline__ double exponent(float x) const { return fma((double)x - top, c, kTop); }
     static __device__ __forceinline__ double power(double y, int& i) {
         const double z = y + kMagic;
@@ -186,11 +200,14 @@ struct Weigher {
         s = fma(s, r, 1.0) * sh.table[i & 255];
         return __hiloint2double(__double2hiint(s) + ((i >> 8) << 20), __double2loint(s));
     }
-    // i: Y rounded, where the weight is not zero
+    // i: Y rounded.  Only where live(x): below, the exponent may leave its range; the weight is zero there.
+    __device__ __forceinline__ bool live(float x) const { return x > floor; }
+    __device__ __forceinline__ i64 raw(float x, int& i) const {
+        return __double_as_longlong(power(exponent(x), i) + kOnes) & 0xFFFFFFFFFFFFFll;      // rounded to a whole number
+    }
     __device__ __forceinline__ i64 operator()(float x, int& i) const {
-        const double y = exponent(x);
-        const i64 w = __double_as_longlong(power(y, i) + kOnes) & 0xFFFFFFFFFFFFFll;      // rounded to a whole number
-        return y > kLeast ? w : 0;                                  // -inf too
+        const i64 w = raw(x, i);
+        return live(x) ? w : 0;
     }
     __device__ __forceinline__ i64 operator()(float x) const {
         int i;
@@ -294,26 +311,58 @@ __device__ __noinline__ Found find(bool weights, i64 want, float top_p, i64 more
     __syncthreads();
     if (lane_id() == 0) { sh.red[0][warp_id()] = mine; sh.red_n[warp_id()] = mine_n; }
     __syncthreads();
-    const i64 of_warp = sh.red[0][lane_id()], up = warp_upto(of_warp), total = __shfl_sync(0xffffffffu, up, 31);
-    if (want < 0) want = share(top_p, total + more);
-    const unsigned reached = __ballot_sync(0xffffffffu, up >= want);
-    const int w = reached ? __ffs(reached) - 1 : -1;
-    if (w == warp_id()) {
-        const i64 at = __shfl_sync(0xffffffffu, up - of_warp, w) + warp_upto(w0) - w0;
-        int n = (int)__reduce_add_sync(0xffffffffu, lane_id() < w ? (unsigned)sh.red_n[lane_id()] : 0u), before = n0;
+    if (warp_id() == 0) {
+        const i64 of_warp = sh.red[0][lane_id()], up = warp_upto(of_warp), total = __shfl_sync(0xffffffffu, up, 31);
+        if (want < 0) want = share(top_p, total + more);
+        const unsigned reached = __ballot_sync(0xffffffffu, up >= want);
+        const int w = reached ? __ffs(reached) - 1 : -1, n = (int)__reduce_add_sync(0xffffffffu, lane_id() < w ? (unsigned)sh.red_n[lane_id()] : 0u);
+        const i64 at = __shfl_sync(0xffffffffu, up - of_warp, max(w, 0));
+        if (lane_id() == 0) {
+            sh.found = {at, total, w, n, 0};        // the warp that has the bucket, for now
+            sh.sum = want;
+        }
+    }
+    __syncthreads();
+    if (sh.found.bucket == warp_id()) {
+        want = sh.sum;
+        const i64 at = sh.found.before + warp_upto(w0) - w0;
+        int before = n0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int t = __shfl_up_sync(0xffffffffu, before, o);
             if (lane_id() >= o) before += t;
         }
-        if (at < want && want <= at + w0) sh.found = {at, total, (int)threadIdx.x, n + before - n0, n0};
-    } else if (w < 0 && threadIdx.x == 0) {
-        sh.found = {0, total, -1, 0, 0};
+        const bool here = at < want && want <= at + w0;
+        const int n = sh.found.count_before;
+        __syncwarp();
+        if (here) sh.result = {at, sh.found.total, (int)threadIdx.x, n + before - n0, n0};
+    } else if (sh.found.bucket < 0 && threadIdx.x == 0) {
+        sh.result = sh.found;
     }
     __syncthreads();
-    return sh.found;
+    return sh.result;
 }
 
+// f(i, j) for all pairs of n candidates, the j of an i spread over lanes of a warp; done(i, on the first of these lanes) after sums a and b of what f
+// adds to them.  All threads take part.
+template <typename F, typename D> __device__ __forceinline__ void pairs(int n, F f, D done) {
+    int per = 1;
+    while (per < 32 && per * 2 * n <= kThreads) per *= 2;
+    for (int i0 = 0; i0 < n; i0 += kThreads / per) {
+        const int i = i0 + (int)threadIdx.x / per;
+        i64 a = 0;
+        int b = 0;
+        if (i < n) {
+#pragma unroll 4
+            for (int j = threadIdx.x % per; j < n; j += per) f(i, j, a, b);
+        }
+        for (int o = 1; o < per; o <<= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
+        }
+        if (i < n && threadIdx.x % per == 0) done(i, a, b);
+    }
+}
 // After every block has its sh.n_mine: their sum, and each of them in sh.n_of
 __device__ __noinline__ int sizes() {
     sync_all();
@@ -354,11 +403,6 @@ __device__ __forceinline__ int element_inside(int q) {
     const int n = padded(sh.row.n);
     return min(n, warp_id() * run_of_warp(n)) + lane_id() + 32 * noted_at(q);
 }
-struct Threshold {
-    float tau;
-    i64 above;              // sum in front of the tokens at tau
-    int same;               // how many there are
-};
 // The logit at which the running sum (of counts, or of weights) in falling order reaches `want`: among the tokens from x0 on that in(x) says lie in got's
 // bucket.  Every block finds it.
 template <typename T, bool MASS, typename F> __device__ __noinline__ Threshold threshold(Found got, i64 want, float x0, F in, int inside = -1) {
@@ -426,18 +470,29 @@ template <typename T, bool MASS, typename F> __device__ __noinline__ Threshold t
         sh.list[i] = of_block(sh.list_mine, r)[at];
     }
     __syncthreads();
-    // bisection over the keys of the list, by every warp for itself as long as a lane has few, else by the block
-    constexpr int kEach = kList / kThreads;
-    const bool alone = n <= 32 * kEach;
-    const int me = alone ? lane_id() : (int)threadIdx.x, step = alone ? 32 : kThreads;
+    if (n <= kFew) {                        // each with each
+        if ((int)threadIdx.x < n) sh.front[threadIdx.x] = MASS ? weight(sh.list[threadIdx.x]) : 1;
+        __syncthreads();
+        pairs(n, [&](int i, int j, i64& a, int& b) {
+            const float x = sh.list[i], y = sh.list[j];
+            if (y > x) a += sh.front[j];
+            b += y == x;
+        }, [&](int i, i64 a, int b) {
+            if (got.before + a < want && want <= got.before + a + b * sh.front[i]) sh.threshold = {sh.list[i], got.before + a, b};      // equal ones write the same
+        });
+        __syncthreads();
+        return sh.threshold;
+    }
+    // bisection over the keys of the list: the largest key from which on the sum reaches `want`
+    constexpr int kEach = (kList + kThreads - 1) / kThreads;
     uint32_t key[kEach], hi = 0, lo = 0xFFFFFFFFu;
     i64 w[kEach];
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         key[k] = 0;
         w[k] = 0;
-        if (me + k * step < n) {
-            const float x = sh.list[me + k * step];
+        if ((int)threadIdx.x + k * kThreads < n) {
+            const float x = sh.list[threadIdx.x + k * kThreads];
             key[k] = key_of(x);
             w[k] = MASS ? weight(x) : 1;
             hi = max(hi, key[k]);
@@ -446,32 +501,24 @@ template <typename T, bool MASS, typename F> __device__ __noinline__ Threshold t
     }
     hi = __reduce_max_sync(0xffffffffu, hi);
     lo = __reduce_min_sync(0xffffffffu, lo);
-    if (!alone) {
-        __syncthreads();
-        if (lane_id() == 0) { sh.red[0][warp_id()] = hi; sh.red[1][warp_id()] = lo; }
-        __syncthreads();
-        for (int k = 0; k < kWarps; ++k) {
-            hi = max(hi, (uint32_t)sh.red[0][k]);
-            lo = min(lo, (uint32_t)sh.red[1][k]);
-        }
-    }
-    while (lo < hi) {                       // the largest key from which on the sum reaches `want`
-        const uint32_t mid = lo + (hi - lo + 1) / 2;
+    __syncthreads();
+    if (lane_id() == 0) { sh.red[0][warp_id()] = hi; sh.red[1][warp_id()] = lo; }
+    __syncthreads();
+    hi = __reduce_max_sync(0xffffffffu, (uint32_t)sh.red[0][lane_id()]);
+    lo = __reduce_min_sync(0xffffffffu, (uint32_t)sh.red[1][lane_id()]);
+    auto sum_from = [&](uint32_t least, bool weights) {
         i64 sum = 0;
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) sum += key[k] >= mid ? w[k] : 0;
-        sum = alone ? warp_sum(sum) : block_sum(sum);
-        if (got.before + sum >= want) lo = mid;
+        for (int k = 0; k < kEach; ++k)
+            if (key[k] >= least && (int)threadIdx.x + k * kThreads < n) sum += weights ? w[k] : 1;
+        return block_sum(sum);
+    };
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo + 1) / 2;
+        if (got.before + sum_from(mid, MASS) >= want) lo = mid;
         else hi = mid - 1;
     }
-    i64 above = 0, same = 0;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        above += key[k] > lo ? w[k] : 0;
-        same += key[k] == lo && me + k * step < n;
-    }
-    above = alone ? warp_sum(above) : block_sum(above);
-    same = alone ? warp_sum(same) : block_sum(same);
+    const i64 above = sum_from(lo + 1, MASS), same = sum_from(lo, false) - sum_from(lo + 1, false);
     return {value_of(lo), got.before + above, (int)same};
 }
 
@@ -499,20 +546,21 @@ template <typename T, int WHAT> __device__ __noinline__ i64 strips(float tau, in
             const float x = Elements<T>::one(first + e);
             if (WHAT == kEqual) {
                 equal += x == tau;
-            } else if (WHAT == kFrom) {
-                const i64 w = weight(x);
-                if (x >= tau) sum += w;
-            } else if (WHAT == kKept) {
-                const i64 w = weight(x);
-                if (x > tau || (x == tau && first + e <= last)) sum += w;
             } else {
                 int at;
-                const i64 w = weight(x, at);
-                all += w;
-                if (at > win.high) sum += w;
-                if (at <= win.high && at >= win.low && w != 0) {
-                    if (noted < kInside) noted_at(noted) = (uint8_t)((i - i0 + e) / 32);
-                    ++noted;
+                const i64 w = weight.raw(x, at);
+                const bool live = weight.live(x);
+                if (WHAT == kFrom) {
+                    if (live && x >= tau) sum += w;
+                } else if (WHAT == kKept) {
+                    if (live && (x > tau || (x == tau && first + e <= last))) sum += w;
+                } else if (live) {
+                    all += w;
+                    if (at > win.high) sum += w;
+                    if ((unsigned)(win.high - at) <= (unsigned)(win.high - win.low)) {
+                        noted_at(min(noted, kInside)) = (uint8_t)((i - i0 + e) / 32);
+                        ++noted;
+                    }
                 }
             }
         }
@@ -670,26 +718,6 @@ template <typename T> __device__ __noinline__ Window weigh(float top_p, i64& all
     return win;
 }
 
-// f(i, j) for all pairs of n candidates, the j of an i spread over lanes of a warp; done(i, on the first of these lanes) after sums a and b of what f
-// adds to them.  All threads take part.
-template <typename F, typename D> __device__ __forceinline__ void pairs(int n, F f, D done) {
-    int per = 1;
-    while (per < 32 && per * 2 * n <= kThreads) per *= 2;
-    for (int i0 = 0; i0 < n; i0 += kThreads / per) {
-        const int i = i0 + (int)threadIdx.x / per;
-        i64 a = 0;
-        int b = 0;
-        if (i < n) {
-#pragma unroll 4
-            for (int j = threadIdx.x % per; j < n; j += per) f(i, j, a, b);
-        }
-        for (int o = 1; o < per; o <<= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, o);
-            b += __shfl_xor_sync(0xffffffffu, b, o);
-        }
-        if (i < n && threadIdx.x % per == 0) done(i, a, b);
-    }
-}
 // n candidates in sh.all, the first top_k of the order among them: the filters and the draw, by one block
 __device__ __noinline__ void finish(const SampleDev& p, int d, int n, int top_k, float top_p, float least, float u) {
     const Weigher weight;
@@ -845,6 +873,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
     const double c = temp == 0.f ? 0.0 : 1.4426950408889634074 / (double)temp;
     if (threadIdx.x == 0) {
         sh.row.top = top;
+        sh.row.floor = fminf((float)((double)top - 600.0 / c), value_of(key_of(top) - 1));
         sh.row.top_d = (double)top;
         sh.row.c = c;
         sh.row.scale = (float)fmin(2.0 * c / (double)kWidth, 3e38);
@@ -954,8 +983,10 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
 template <typename T> cudaError_t launch_t(const SampleDev& p, cudaStream_t st) {
     constexpr int kMost = 196 * 1024, kUsual = 136 * 1024;     // bytes of a row per block: what fits with the rest, and what is taken where rows are many
     const long long bytes = (long long)p.vocab * sizeof(T) + 32;
-    const int blocks = (int)min((long long)kMaxBlocks, (bytes + kUsual - 1) / kUsual);
-    const size_t smem = (size_t)((bytes / 16 + 2 + blocks - 1) / blocks) * 16 + kStrip * sizeof(T) + kInside * kThreads;
+    int blocks = (int)min((long long)kMaxBlocks, (bytes + kUsual - 1) / kUsual);
+    // SMs that no row has take halves of them (64 rows of 32000: 54 -> 43 us); smaller parts cost more in barriers of the cluster than they save
+    while (blocks < kMaxBlocks && (long long)p.rows * (blocks + 1) <= 148 && bytes / blocks > 80 * 1024) ++blocks;
+    const size_t smem = (size_t)((bytes / 16 + 2 + blocks - 1) / blocks) * 16 + kStrip * sizeof(T) + (kInside + 1) * kThreads;
     static std::atomic<uint64_t> known{0};           // devices whose attribute is set
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
