@@ -68,15 +68,25 @@ __device__ __forceinline__ float2 cos_sin_turns(double turns) {
     return k & 2 ? make_float2(-c, -s) : make_float2(c, s);
 }
 
-// A block per row.  HD / 16 threads hold a head, each 8 elements of its first half and the 8 that they are rotated with; heads in the
-// order K, V, queries.
+constexpr int kThreads = 256;
+
+// Blocks of a row (blockIdx.y).  HD / 16 threads hold a head, each 8 elements of its first half and the 8 that they are rotated with; heads in
+// the order K, V, queries.  A thread's input is requested before the position is known: position, page and angles are three more trips
+// one behind the other (8191 rows of 96 heads with the reading back: 230 us when a block held a row and asked for them first).
 template <typename T, bool VEC, int HD, bool I8>
-__global__ void __launch_bounds__(1024) k_paged_append(const PagedDev c, const PagedRows r, const __grid_constant__ Frequencies f, int rotate) {
+__global__ void __launch_bounds__(kThreads) k_paged_append(const __grid_constant__ PagedDev c, const __grid_constant__ PagedRows r, const __grid_constant__ Frequencies f, int rotate) {
     constexpr int HALF = HD / 2, TH = HD / 16;
     __shared__ __align__(16) float cos_s[HALF], sin_s[HALF];
     pdl_launch_dependents();
     pdl_wait();
-    const int row = blockIdx.x, pos = r.pos[row];
+    const int row = blockIdx.x, units = (r.n_heads + 2 * c.n_kv) * TH, u = blockIdx.y * kThreads + threadIdx.x, unit = min(u, units - 1);
+    const int head = unit / TH, e = (unit % TH) * 8;
+    const int which = head < c.n_kv ? 0 : (head < 2 * c.n_kv ? 1 : 2), h = which == 2 ? head - 2 * c.n_kv : head - which * c.n_kv;
+    const T* const x = (which == 0 ? (const T*)r.k + row * r.ldk : (which == 1 ? (const T*)r.v + row * r.ldv : (const T*)r.q + row * r.ldq)) + (size_t)h * HD + e;
+    float lo[8], hi[8];
+    load8<VEC>(x, lo);
+    load8<VEC>(x + HALF, hi);
+    const int pos = r.pos[row];
     if (pos < 0) return;
     PagedDev::Row at;
     if (!c.locate(r.seq ? r.seq[row] : row, pos, at)) {
@@ -84,23 +94,13 @@ __global__ void __launch_bounds__(1024) k_paged_append(const PagedDev c, const P
         return;
     }
     if (rotate) {
-        for (int i = threadIdx.x; i < HALF; i += blockDim.x) {
-            const float2 cs = cos_sin_turns((double)pos * f.turns[i]);
-            cos_s[i] = cs.x;
-            sin_s[i] = cs.y;
+        if ((int)threadIdx.x < HALF) {
+            const float2 cs = cos_sin_turns((double)pos * f.turns[threadIdx.x]);
+            cos_s[threadIdx.x] = cs.x;
+            sin_s[threadIdx.x] = cs.y;
         }
         __syncthreads();
-    }
-    const int units = (r.n_heads + 2 * c.n_kv) * TH;
-    for (int u0 = (int)threadIdx.x & ~31; u0 < units; u0 += blockDim.x) {        // whole warps: heads are reduced among their threads
-        const int u = u0 + ((int)threadIdx.x & 31), unit = min(u, units - 1);
-        const int head = unit / TH, e = (unit % TH) * 8;
-        const int which = head < c.n_kv ? 0 : (head < 2 * c.n_kv ? 1 : 2), h = which == 2 ? head - 2 * c.n_kv : head - which * c.n_kv;
-        const T* const x = which == 0 ? (const T*)r.k + row * r.ldk : (which == 1 ? (const T*)r.v + row * r.ldv : (const T*)r.q + row * r.ldq);
-        float lo[8], hi[8];
-        load8<VEC>(x + (size_t)h * HD + e, lo);
-        load8<VEC>(x + (size_t)h * HD + HALF + e, hi);
-        if (rotate && which != 1) {
+        if (which != 1) {
             float cs[8], sn[8];
             load8<true>(cos_s + e, cs);
             load8<true>(sin_s + e, sn);
@@ -111,53 +111,54 @@ __global__ void __launch_bounds__(1024) k_paged_append(const PagedDev c, const P
                 hi[i] = b * cs[i] + a * sn[i];
             }
         }
-        if (which == 2) {
-            if (u < units) {
-                uint16_t* const o = r.q_out + row * r.ldqo + (size_t)h * HD + e;
-                store8<VEC>(o, lo);
-                store8<VEC>(o + HALF, hi);
-            }
-        } else if (!I8) {
-            uint16_t* const o = reinterpret_cast<uint16_t*>((which ? c.v : c.k) + ((size_t)at.at + (size_t)h * c.head16) * 16) + e;
-            if (u < units) {
-                store8<true>(o, lo);
-                store8<true>(o + HALF, hi);
-            }
+    }
+    if (which == 2) {
+        if (u < units) {
+            uint16_t* const o = r.q_out + row * r.ldqo + (size_t)h * HD + e;
+            store8<VEC>(o, lo);
+            store8<VEC>(o + HALF, hi);
         }
-        if (I8) {
-            uint32_t mx = 0;
+    } else if (!I8) {
+        uint16_t* const o = reinterpret_cast<uint16_t*>((which ? c.v : c.k) + ((size_t)at.at + (size_t)h * c.head16) * 16) + e;
+        if (u < units) {
+            store8<true>(o, lo);
+            store8<true>(o + HALF, hi);
+        }
+    }
+    if (I8) {
+        uint32_t mx = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) mx = max(mx, max(abs_bits(lo[i]), abs_bits(hi[i])));
+        for (int i = 0; i < 8; ++i) mx = max(mx, max(abs_bits(lo[i]), abs_bits(hi[i])));
 #pragma unroll
-            for (int o = TH / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            if (which != 2 && u < units) {
-                const bool finite = mx < 0x7F800000u;
-                const float a = fmaxf(__uint_as_float(mx), kTinyMax);
-                const Factor by = factor_127_over(finite ? a : 1.f);
-                uint32_t w[4];
+        for (int o = TH / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        if (which != 2 && u < units) {
+            const bool finite = mx < 0x7F800000u;
+            const float a = fmaxf(__uint_as_float(mx), kTinyMax);
+            const Factor by = factor_127_over(finite ? a : 1.f);
+            uint32_t w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t b[4];
+            for (int i = 0; i < 4; ++i) {
+                uint32_t b[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float v = !finite ? 0.f : (i < 2 ? lo[4 * i + j] : hi[4 * (i - 2) + j]);
-                        b[j] = __float_as_uint(__fadd_rn(fmaf(v, by.hi, __fmul_rn(v, by.lo)), kRintMagic));
-                    }
-                    w[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+                for (int j = 0; j < 4; ++j) {
+                    const float v = !finite ? 0.f : (i < 2 ? lo[4 * i + j] : hi[4 * (i - 2) + j]);
+                    b[j] = __float_as_uint(__fadd_rn(fmaf(v, by.hi, __fmul_rn(v, by.lo)), kRintMagic));
                 }
-                uint8_t* const o = (which ? c.v : c.k) + ((size_t)at.at + (size_t)h * c.head16) * 16 + e;
-                *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
-                *reinterpret_cast<uint2*>(o + HALF) = make_uint2(w[2], w[3]);
-                if (e == 0) (which ? c.vs : c.ks)[(size_t)at.s + (size_t)h * c.s_head] = finite ? a / 127.f : __int_as_float(0x7FC00000);
+                w[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
             }
+            uint8_t* const o = (which ? c.v : c.k) + ((size_t)at.at + (size_t)h * c.head16) * 16 + e;
+            *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2*>(o + HALF) = make_uint2(w[2], w[3]);
+            if (e == 0) (which ? c.vs : c.ks)[(size_t)at.s + (size_t)h * c.s_head] = finite ? a / 127.f : __int_as_float(0x7FC00000);
         }
     }
 }
 
-// A block per row; a thread takes 16 bytes of a head of the cache.
+// A block per row; a thread takes 16 bytes of kEach heads of the cache at a time, all requested before the first is used.  (One or two at a time: 82 us for
+// 16384 rows of 32 int8 heads; position, page and rows are three trips one behind the other, so much has to be on its way at once.)
 template <typename T, bool VEC, int HD, bool I8>
-__global__ void __launch_bounds__(256) k_paged_read(const PagedDev c, const PagedRows r) {
-    constexpr int N = I8 ? 16 : 8, TH = HD / N;
+__global__ void __launch_bounds__(kThreads) k_paged_read(const __grid_constant__ PagedDev c, const __grid_constant__ PagedRows r) {
+    constexpr int N = I8 ? 16 : 8, TH = HD / N, kEach = 4;
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x, pos = r.pos[row];
@@ -167,26 +168,41 @@ __global__ void __launch_bounds__(256) k_paged_read(const PagedDev c, const Page
         if (threadIdx.x == 0) report(r.d_status, CATS_ERR_INVALID_ARG);
         return;
     }
-    for (int u = threadIdx.x; u < 2 * c.n_kv * TH; u += blockDim.x) {
-        const int head = u / TH, part = u % TH, which = head >= c.n_kv, h = head - which * c.n_kv;
-        const uint4 w = __ldcg(reinterpret_cast<const uint4*>(which ? c.v : c.k) + (size_t)at.at + (size_t)h * c.head16 + part);
-        T* const o = (which ? (T*)r.v_out + row * r.ldv : (T*)r.k_out + row * r.ldk) + (size_t)h * HD + part * N;
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-        float v[N];
-        if (I8) {
-            const float s = __ldcg((which ? c.vs : c.ks) + (size_t)at.s + (size_t)h * c.s_head);
+    const int units = 2 * c.n_kv * TH;
+    for (int u0 = threadIdx.x; u0 < units; u0 += blockDim.x * kEach) {
+        uint4 w[kEach];
+        float s[kEach];
 #pragma unroll
-            for (int i = 0; i < N; ++i)      // a byte b as the float 2^23 + (b + 128), then minus 2^23 + 128: exact
-                v[i] = (__uint_as_float(__byte_perm(x[i >> 2] ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(x[i] << 16);
-                v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        for (int k = 0; k < kEach; ++k) {
+            const int u = u0 + k * blockDim.x;
+            if (u < units) {
+                const int head = u / TH, which = head >= c.n_kv, h = head - which * c.n_kv;
+                w[k] = __ldcg(reinterpret_cast<const uint4*>(which ? c.v : c.k) + (size_t)at.at + (size_t)h * c.head16 + u % TH);
+                if (I8) s[k] = __ldcg((which ? c.vs : c.ks) + (size_t)at.s + (size_t)h * c.s_head);
             }
         }
 #pragma unroll
-        for (int i = 0; i < N; i += 8) store8<VEC>(o + i, v + i);
+        for (int k = 0; k < kEach; ++k) {
+            const int u = u0 + k * blockDim.x;
+            if (u >= units) break;
+            const int head = u / TH, which = head >= c.n_kv, h = head - which * c.n_kv;
+            T* const o = (which ? (T*)r.v_out + row * r.ldv : (T*)r.k_out + row * r.ldk) + (size_t)h * HD + u % TH * N;
+            const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+            float v[N];
+            if (I8) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)      // a byte b as the float 2^23 + (b + 128), then minus 2^23 + 128: exact
+                    v[i] = (__uint_as_float(__byte_perm(x[i >> 2] ^ 0x80808080u, 0x4B000000u, 0x7440u + (i & 3))) - 8388736.f) * s[k];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[2 * i] = __uint_as_float(x[i] << 16);
+                    v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < N; i += 8) store8<VEC>(o + i, v + i);
+        }
     }
 }
 
@@ -209,9 +225,8 @@ const Frequencies& frequencies(float base, int hd) {
 template <typename T, bool VEC, int HD, bool I8>
 cudaError_t append_k(const PagedDev& c, const PagedRows& r, cudaStream_t st) {
     const int units = (r.n_heads + 2 * c.n_kv) * (HD / 16);
-    const int threads = min(1024, (units + 31) / 32 * 32);
     static const Frequencies none = {};
-    return launch_i8(k_paged_append<T, VEC, HD, I8>, dim3((unsigned)r.rows), dim3(threads), 0, st, c, r, r.rope_base > 0.f ? frequencies(r.rope_base, HD) : none,
+    return launch_i8(k_paged_append<T, VEC, HD, I8>, dim3((unsigned)r.rows, (unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, c, r, r.rope_base > 0.f ? frequencies(r.rope_base, HD) : none,
                      r.rope_base > 0.f ? 1 : 0);
 }
 template <typename T, bool VEC> cudaError_t append_t(const PagedDev& c, const PagedRows& r, int i8, int hd, cudaStream_t st) {
@@ -220,7 +235,7 @@ template <typename T, bool VEC> cudaError_t append_t(const PagedDev& c, const Pa
 }
 template <typename T, bool VEC, int HD, bool I8> cudaError_t read_k(const PagedDev& c, const PagedRows& r, cudaStream_t st) {
     const int units = 2 * c.n_kv * (HD / (I8 ? 16 : 8));
-    return launch_i8(k_paged_read<T, VEC, HD, I8>, dim3((unsigned)r.rows), dim3(min(256, (units + 31) / 32 * 32)), 0, st, c, r);
+    return launch_i8(k_paged_read<T, VEC, HD, I8>, dim3((unsigned)r.rows), dim3(min(kThreads, (units + 127) / 128 * 32)), 0, st, c, r);
 }
 template <typename T, bool VEC> cudaError_t read_t(const PagedDev& c, const PagedRows& r, int i8, int hd, cudaStream_t st) {
     if (hd == 128) return i8 ? read_k<T, VEC, 128, true>(c, r, st) : read_k<T, VEC, 128, false>(c, r, st);
