@@ -108,10 +108,7 @@ template <int HD, bool I8, int NT> struct Attn {
     struct Shared {
         uint8_t ring[kWarps][2][kStage];
         uint4 raw[NT * 8 * HD / 8];                         // the queries of the next segment, as they are
-        union {
-            uint4 q[NT][QV][32];                            // and as the second operand of K Q^T, of this segment and the next
-            float2 parts[kGroup][NT * 8];                   // behind a segment, in its half
-        } q[2];
+        uint4 q[2][NT][QV][32];                             // and as the second operand of K Q^T, of this segment and the next
         float qf[2][NT * 8];                                // factors of the scores
         float2 ml[kWarps][NT * 8];
         int o_at[kWarps];                                   // which half of its ring a warp's O is in
@@ -246,7 +243,7 @@ template <int HD, bool I8, int NT> struct Attn {
                 mine = base / f0 / f1;
             }
 #pragma unroll
-            for (int i = 0; i < QV; ++i) sh.q[to].q[nt][i][lane] = x[i];
+            for (int i = 0; i < QV; ++i) sh.q[to][nt][i][lane] = x[i];
             if (j == 0) sh.qf[to][nt * 8 + g] = mine;
         }
     }
@@ -274,7 +271,7 @@ template <int HD, bool I8, int NT> struct Attn {
                         const uint32_t a0 = f16_of_bytes(x, 0x4140), a1 = f16_of_bytes(y, 0x4140), a2 = f16_of_bytes(x, 0x4342), a3 = f16_of_bytes(y, 0x4342);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            const uint4 q = sh.q[parity].q[nt][i * 2 + (w >> 1)][lane];
+                            const uint4 q = sh.q[parity][nt][i * 2 + (w >> 1)][lane];
                             mma<I8>(s[nt][b], a0, a1, a2, a3, w & 1 ? q.z : q.x, w & 1 ? q.w : q.y);
                         }
                     }
@@ -282,7 +279,7 @@ template <int HD, bool I8, int NT> struct Attn {
             } else {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const uint4 q = sh.q[parity].q[nt][i][lane];
+                    const uint4 q = sh.q[parity][nt][i][lane];
 #pragma unroll
                     for (int b = 0; b < kBlk; ++b) {
                         mma<I8>(s[nt][b], kr[2 * b].x, kr[2 * b + 1].x, kr[2 * b].y, kr[2 * b + 1].y, q.x, q.y);
@@ -516,38 +513,56 @@ template <int HD, bool I8, int NT> struct Attn {
         __syncthreads();            // the rings are free
     }
 
-    // Parts at slots slot_of(0) .. slot_of(n - 1) added in this order: to slot `to`, or (to < 0) to the output.
-    template <typename F> __device__ __forceinline__ void add_parts(int s, int head0, int heads, int n, F slot_of, const Slots& w, int to, float2 (*parts)[NT * 8]) {
-        for (int i = threadIdx.x; i < n * heads; i += kThreads) parts[i / heads][i % heads] = __ldcg(w.ml(slot_of(i / heads)) + i % heads);
-        __syncthreads();
-        for (int i = threadIdx.x; i < heads * (HD / 4); i += kThreads) {
+    // The slot of part k of a head group whose first block is `first`.
+    static __device__ __forceinline__ int slot_of(int first, int k) { return 2 * (first + k) + (k == 0 ? 1 : 0); }
+    // Parts p0, p0 + step, ... (n of them) of a head group added in this order: to slot `to`, or (to < 0) to the output.  References, sums and values of
+    // kAtOnce parts come in one trip.
+    __device__ __forceinline__ void add_parts(const Segment& g0, int first, int p0, int step, int n, const Slots& w, int to) {
+        constexpr int kAtOnce = 6;
+        for (int i = threadIdx.x; i < g0.heads * (HD / 4); i += kThreads) {
             const int h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
             float top = -INFINITY, sum = 0.f;
-            for (int k = 0; k < n; ++k) top = fmaxf(top, parts[k][h].x);
             float4 x = make_float4(0, 0, 0, 0);
-#pragma unroll 8
-            for (int k = 0; k < n; ++k) {
-                const float f = factor(parts[k][h].x, top);
-                sum = fmaf(parts[k][h].y, f, sum);
-                add(x, __ldcg(reinterpret_cast<const float4*>(w.o(slot_of(k)) + h * HD + ch)), f);
+            for (int k0 = 0; k0 < n; k0 += kAtOnce) {
+                float2 ml[kAtOnce];
+                float4 o[kAtOnce];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const int slot = slot_of(first, p0 + min(k0 + k, n - 1) * step);
+                    ml[k] = __ldcg(w.ml(slot) + h);
+                    o[k] = __ldcg(reinterpret_cast<const float4*>(w.o(slot) + h * HD + ch));
+                }
+                float t = top;
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) t = fmaxf(t, ml[k].x);
+                const float keep = factor(top, t);
+                sum *= keep;
+                x.x *= keep; x.y *= keep; x.z *= keep; x.w *= keep;
+                top = t;
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k)
+                    if (k0 + k < n) {
+                        const float f = factor(ml[k].x, top);
+                        sum = fmaf(ml[k].y, f, sum);
+                        add(x, o[k], f);
+                    }
             }
             if (to < 0) {
-                store_out(s, head0 + h, ch, x, sum, false);
+                store_out(g0.s, g0.head0 + h, ch, x, sum, false);
             } else {
                 *reinterpret_cast<float4*>(w.o(to) + h * HD + ch) = x;
                 if (ch == 0) w.ml(to)[h] = make_float2(top, sum);
             }
         }
-        __syncthreads();
     }
     // Whether this block is the last of n to come here; it then sees what the others wrote, and the counter is zero again.
     __device__ __forceinline__ bool arrive(int* counter, int n) {
         __syncthreads();
         if (threadIdx.x == 0) {
-            __threadfence();
-            const bool last = atomicAdd(counter, 1) == n - 1;
+            int before;         // releases what the block has written (the barrier in front orders it) and acquires what the others have
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+            const bool last = before == n - 1;
             if (last) *counter = 0;
-            __threadfence();
             sh.last = last;
         }
         __syncthreads();
@@ -560,10 +575,33 @@ template <int HD, bool I8, int NT> struct Attn {
         if (asked > most) report(a.d_status, CATS_ERR_INVALID_ARG);
         return (int)min((long long)max(asked, 0), most);
     }
+    static __device__ __forceinline__ long long quotient(long long a, long long b) {      // 64-bit division is a hundred instructions
+        return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+    }
+    static __device__ __forceinline__ long long share_of(long long block, long long units, long long blocks) { return quotient(block * units, blocks); }
     static __device__ __forceinline__ int units_of(int len) { return len > 0 ? (len - 1) / kUnit + 1 : 1; }
 
     // The sequence that unit `first(total)` lies in, to sh.seq; sh.before: units per head group of those in front of it, sh.total: of all.
     template <typename F> __device__ __forceinline__ void find(int groups, F first) {
+        if (c.n_seqs <= 32) {               // a warp's lanes
+            const int n = lane < c.n_seqs ? units_of(length(lane)) : 0;
+            long long upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long t = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += t;
+            }
+            const long long total = __shfl_sync(0xffffffffu, upto, 31), want = first(total * groups);
+            if (warp == 0) {
+                if (want >= (upto - n) * groups && want < upto * groups) {
+                    sh.seq = lane;
+                    sh.before = upto - n;
+                }
+                if (lane == 0) sh.total = total * groups;
+            }
+            __syncthreads();
+            return;
+        }
         const int each = (c.n_seqs + kThreads - 1) / kThreads, s0 = min(c.n_seqs, (int)threadIdx.x * each), s1 = min(c.n_seqs, s0 + each);
         long long mine = 0;
         for (int s = s0; s < s1; ++s) mine += units_of(length(s));
@@ -603,17 +641,18 @@ template <int HD, bool I8, int NT> struct Attn {
         auto blocks_for = [&](long long units) { return (long long)min((long long)gridDim.x, units); };
         find(groups, [&](long long units) {
             const long long n = blocks_for(units);
-            return me < n ? me * units / n : -1;
+            return me < n ? share_of(me, units, n) : -1;
         });
         const long long units = sh.total, n_blocks = blocks_for(units);
         if (me >= n_blocks) return;
-        long long u = me * units / n_blocks;
-        const long long u_end = (me + 1) * units / n_blocks;
-        auto block_of = [&](long long unit) { return (int)(((unit + 1) * n_blocks - 1) / units); };
+        long long u = share_of(me, units, n_blocks);
+        const long long u_end = share_of(me + 1, units, n_blocks);
+        auto block_of = [&](long long unit) { return (int)quotient((unit + 1) * n_blocks - 1, units); };
         const Slots w = {(float*)a.ws, (int*)((float*)a.ws + 2 * kMaxBlocks * kSlotFloats)};
         // the sequence at hand, its length and the next one's, and how far the segments have come in it
         int s = sh.seq, len = length(s), len1 = s + 1 < c.n_seqs ? length(s + 1) : 0, n = units_of(len);
-        const int group0 = (int)((u - sh.before * groups) / n);
+        const long long from = u - sh.before * groups;
+        const int group0 = from >> 32 ? (int)(from / n) : (int)((uint32_t)from / (uint32_t)n);
         int kvh = group0 / chunks, chunk = group0 % chunks, unit = (int)(u - sh.before * groups - (long long)group0 * n);
         auto next_segment = [&] {                    // from unit u on
             if (unit == n) {
@@ -644,11 +683,18 @@ template <int HD, bool I8, int NT> struct Attn {
             return g;
         };
         Segment now = next_segment();
-        long long at = me * units / n_blocks;        // its first unit
+        long long at = share_of(me, units, n_blocks);        // its first unit
         used = 1;
         pending = false;
         request_q(now);
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        const int first_row = now.t0 + warp * kTile;
+        if (first_row < now.t1) {
+            request(smem_u32(sh.ring[warp]), row_of(now.s, first_row, now.t1), now.kvh);
+            pending = true;
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
         __syncthreads();
         if (warp == kWarps - 1) make_q(0);
         __syncthreads();
@@ -658,22 +704,21 @@ template <int HD, bool I8, int NT> struct Attn {
             Segment next = now;
             if (more) next = next_segment();
             const int active = segment(now, next, more, parity);
-            auto spare = sh.q[parity].parts;
             if (end - at == now.units) {
                 join(now.s, now.head0, now.heads, active, w, -1);
             } else {
                 // blocks first .. last have rows of this head group; the first of them in its second slot
                 const int first = block_of(at - now.unit), last = block_of(at - now.unit + now.units - 1), parts = last - first + 1;
-                auto slot_of = [&](int k) { return 2 * (first + k) + (k == 0 ? 1 : 0); };
-                join(now.s, now.head0, now.heads, active, w, slot_of(me - first));
-                if (parts <= kGroup) {
-                    if (arrive(w.first(first), parts)) add_parts(now.s, now.head0, now.heads, parts, slot_of, w, -1, spare);
-                } else {
-                    const int mine0 = (me - first) / kGroup * kGroup, size = min(kGroup, parts - mine0), n_groups = (parts + kGroup - 1) / kGroup;
-                    if (arrive(mine0 == 0 ? w.first(first) : w.later(first + mine0), size)) {
-                        add_parts(now.s, now.head0, now.heads, size, [&](int k) { return slot_of(mine0 + k); }, w, slot_of(mine0), spare);
-                        if (arrive(w.groups(first), n_groups)) add_parts(now.s, now.head0, now.heads, n_groups, [&](int k) { return slot_of(k * kGroup); }, w, -1, spare);
-                    }
+                join(now.s, now.head0, now.heads, active, w, slot_of(first, me - first));
+                // up to kGroup parts are added at once, more in groups of so many and then the groups
+                const bool grouped = parts > kGroup;
+                const int p0 = grouped ? (me - first) / kGroup * kGroup : 0;
+                for (int level = 0; level < 2; ++level) {
+                    const bool top = level == 1 || !grouped;
+                    const int n = !grouped ? parts : (level == 0 ? min(kGroup, parts - p0) : (parts + kGroup - 1) / kGroup);
+                    if (!arrive(level == 1 ? w.groups(first) : (p0 == 0 ? w.first(first) : w.later(first + p0)), n)) break;
+                    add_parts(now, first, level == 0 ? p0 : 0, level == 0 ? 1 : kGroup, n, w, top ? -1 : slot_of(first, p0));
+                    if (top) break;
                 }
             }
             if (!more) break;
