@@ -505,7 +505,7 @@ int cats_paged_attention(const cats_paged_kv *kv, const int32_t *d_table, int64_
  * token does not depend on how the work is split; -0 equals 0; -inf weighs nothing.
  * A row with a NaN, an infinity or nothing finite, a NaN setting, a negative temperature
  * or a row index past logit_rows: token -1, prob 0 and CATS_ERR_INVALID_ARG in *d_status.
- * vocab <= 262144 (CATS_ERR_UNSUPPORTED). */
+ * vocab <= 262144, rows <= 2^27 (CATS_ERR_UNSUPPORTED). */
 int cats_sample(const void *d_logits, int32_t type, int64_t ld, int32_t logit_rows, int32_t vocab, const int32_t *d_row, int32_t rows,
                 const float *d_temperature, const int32_t *d_top_k, const float *d_top_p, const float *d_min_p, const float *d_u,
                 int32_t *d_token, float *d_prob, int32_t *d_status, void *stream);

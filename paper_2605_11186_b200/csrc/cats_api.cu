@@ -929,7 +929,7 @@ int cats_sample(const void* d_logits, int32_t type, int64_t ld, int32_t logit_ro
     g_call_boundary = true;
     g_call_overlaps = true;
     if (bad_type(type) || logit_rows < 0 || vocab < 1 || ld < vocab || rows < 0 || (!d_row && rows > logit_rows)) return CATS_ERR_INVALID_ARG;
-    if (vocab > kMaxSampleVocab) return CATS_ERR_UNSUPPORTED;
+    if (vocab > kMaxSampleVocab || rows > kMaxSampleRows) return CATS_ERR_UNSUPPORTED;
     if (rows == 0) return CATS_OK;
     if (!d_logits || !d_u || !d_token || !d_status || misaligned(d_logits, type_size(type))) return CATS_ERR_INVALID_ARG;
     const void* words[] = {d_row, d_temperature, d_top_k, d_top_p, d_min_p, d_u, d_token, d_prob, d_status};

@@ -254,7 +254,7 @@ size_t paged_attn_workspace(int n_seqs, int n_heads, int n_kv, int hd);
 cudaError_t launch_paged_attn(const PagedDev& c, const PagedAttn& a, int i8, int hd, cudaStream_t st);
 
 // ---- sampling --------------------------------------------------------------------------------------
-constexpr int kMaxSampleVocab = 1 << 18;
+constexpr int kMaxSampleVocab = 1 << 18, kMaxSampleRows = 1 << 27;       // sums of 2^44 in 63 bits; eight blocks a row in a grid
 struct SampleDev {
     const void* logits;
     int f32;

@@ -97,7 +97,7 @@ def test_workspace_size(b):
                                          (dict(vocab=0), INVALID), (dict(rows=-1), INVALID), (dict(rows=6), INVALID), (dict(u=None), INVALID), (dict(u=A + 2), INVALID),
                                          (dict(row=A + 1), INVALID), (dict(temp=A + 1), INVALID), (dict(k=A + 1), INVALID), (dict(p=A + 1), INVALID), (dict(m=A + 1), INVALID),
                                          (dict(tok=None), INVALID), (dict(tok=A + 3), INVALID), (dict(prob=A + 1), INVALID), (dict(st=None), INVALID),
-                                         (dict(vocab=262145, ld=262145), UNSUPPORTED)])
+                                         (dict(vocab=262145, ld=262145), UNSUPPORTED), (dict(rows=2 ** 27 + 1, n=2 ** 27 + 1), UNSUPPORTED)])
 def test_sample(b, change, code):
     a = dict(x=A, t=F32, ld=100, n=5, vocab=100, row=None, rows=5, temp=A, k=A, p=A, m=A, u=A, tok=A, prob=A, st=A)
     a.update(change)
