@@ -671,9 +671,10 @@ template <typename T> __device__ __noinline__ void locate(const SampleDev& p, in
     if (draw < 0) sync_all();
 }
 
-// Top-p over the whole row: strips of what lies above the window, and the window's histogram; returns the window.  all: the weights of the row.
-template <typename T> __device__ __noinline__ Window weigh(float top_p, i64& all, bool& noted, int& inside) {
-    count<T>(true);
+// Top-p over the whole row: strips of what lies above the window, and the window's histogram; returns the window.  all: the weights of the row; first: there
+// was no histogram yet.
+template <typename T> __device__ __noinline__ Window weigh(float top_p, i64& all, bool& noted, int& inside, bool first) {
+    count<T>(first);
     // n tokens of bucket b weigh n 2^(-b width) to within half a bucket; fp32 places a logit to 2^-23 of 1024 buckets, 2^-13 of one.  The sums are in units of 2^44.
     constexpr float kHalf = 0.501f;
     int count_of;
@@ -939,7 +940,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
         }
     } else if (top_p < 1.f) {
         i64 all;
-        win = weigh<T>(top_p, all, noted, inside);
+        win = weigh<T>(top_p, all, noted, inside, top_k <= 0 || top_k >= V);     // a top-k that cuts nothing has had its histogram
         windowed = true;
         // in front of the window
         i64 above = block_sum(strip_sum(1));

@@ -230,3 +230,20 @@ def test_no_draws(cats):
     none = torch.empty(0, device="cuda")
     cats.cats_sample(logits(2, 10, torch.float32, 0), None, None, None, None, None, none, none.int(), None, cats.new_status())
     assert cats.last_launch_count() == 0
+
+
+@pytest.mark.parametrize("weighing", [300, 900])
+@pytest.mark.parametrize("vocab", [100003, 262144])
+def test_top_p_after_a_top_k_that_cuts_nothing(cats, vocab, weighing):
+    """Fewer tokens weigh anything than top-k asks for, over several blocks: the counts of top-k are read to their end before those of top-p begin."""
+    n = 24
+    x = torch.full((n, vocab), -INF, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(weighing)
+    at = torch.rand(n, vocab, generator=g, device="cuda").argsort(1)[:, :weighing]
+    x.scatter_(1, at, torch.randn(n, weighing, generator=g, device="cuda"))
+    u = uniform(n, 9)
+    first = draw(cats, x, u, k=[1000] * n, p=[0.8] * n)
+    check(cats, x, u, k=[1000] * n, p=[0.8] * n)
+    for _ in range(20):
+        assert draw(cats, x, u, k=[1000] * n, p=[0.8] * n) == first
+    assert draw(cats, x, u, p=[0.8] * n) == first
