@@ -46,7 +46,7 @@ struct Candidate {
 struct Found {
     i64 before, total;      // counts or weights in front of the bucket, and all
     int bucket;             // -1: what was asked for is not reached
-    int count_before, count;
+    int count;              // of the bucket's tokens
 };
 struct Threshold {
     float tau;
@@ -74,7 +74,6 @@ struct Shared {
     uint32_t strip_lo[2][kWarps][kStrips], strip_hi[2][kWarps][kStrips];  // of counts and of weights
     i64 xch[5][kMaxBlocks][2];
     i64 red[2][kWarps];
-    int red_n[kWarps];
     i64 sum;
     i64 front[kFew];
     Found found, result;
@@ -307,18 +306,17 @@ __device__ __noinline__ Found find(bool weights, i64 want, float top_p, i64 more
     bucket_sums(threadIdx.x, weights, n0, w0);
     if (!weights) w0 = n0;
     const i64 mine = warp_sum(w0);
-    const int mine_n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n0);
     __syncthreads();
-    if (lane_id() == 0) { sh.red[0][warp_id()] = mine; sh.red_n[warp_id()] = mine_n; }
+    if (lane_id() == 0) sh.red[0][warp_id()] = mine;
     __syncthreads();
     if (warp_id() == 0) {
         const i64 of_warp = sh.red[0][lane_id()], up = warp_upto(of_warp), total = __shfl_sync(0xffffffffu, up, 31);
         if (want < 0) want = share(top_p, total + more);
         const unsigned reached = __ballot_sync(0xffffffffu, up >= want);
-        const int w = reached ? __ffs(reached) - 1 : -1, n = (int)__reduce_add_sync(0xffffffffu, lane_id() < w ? (unsigned)sh.red_n[lane_id()] : 0u);
+        const int w = reached ? __ffs(reached) - 1 : -1;
         const i64 at = __shfl_sync(0xffffffffu, up - of_warp, max(w, 0));
         if (lane_id() == 0) {
-            sh.found = {at, total, w, n, 0};        // the warp that has the bucket, for now
+            sh.found = {at, total, w, 0};        // the warp that has the bucket, for now
             sh.sum = want;
         }
     }
@@ -326,16 +324,7 @@ __device__ __noinline__ Found find(bool weights, i64 want, float top_p, i64 more
     if (sh.found.bucket == warp_id()) {
         want = sh.sum;
         const i64 at = sh.found.before + warp_upto(w0) - w0;
-        int before = n0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, before, o);
-            if (lane_id() >= o) before += t;
-        }
-        const bool here = at < want && want <= at + w0;
-        const int n = sh.found.count_before;
-        __syncwarp();
-        if (here) sh.result = {at, sh.found.total, (int)threadIdx.x, n + before - n0, n0};
+        if (at < want && want <= at + w0) sh.result = {at, sh.found.total, (int)threadIdx.x, n0};
     } else if (sh.found.bucket < 0 && threadIdx.x == 0) {
         sh.result = sh.found;
     }
