@@ -113,9 +113,10 @@ template <typename T, bool VEC> struct Raw16 {
 // A block takes R rows and (blockIdx.y) 128 of the pieces of their heads: HD / 32 threads hold a head, each 16 elements of its first half and the 16 that they are
 // rotated with; heads in the order K, V, queries.  The inputs of all R rows are requested first: positions, pages and angles are three
 // more trips one behind the other, during which nothing else would be on its way (8191 rows of 96 heads and reading them back: 230 us with a row
-// per block that asked for its inputs last, 135 with 256 threads of one row that asked first).
+// per block that asked for its inputs last, 135 with 256 threads of one row that asked first; then 114, and 106 with registers for 7
+// blocks on an SM: 6 of them 108, 8 107, 9 115.  One row a block: 8191 rows of fp32 144 us with 7, 140 with 8, 137 with 9; 500 rows of bf16 9.4, 8.4, 9.3.)
 template <typename T, bool VEC, int HD, bool I8, int R>
-__global__ void __launch_bounds__(kAppendThreads) k_paged_append(const __grid_constant__ PagedDev c, const __grid_constant__ PagedRows r, const __grid_constant__ Frequencies f, int rotate, int wide) {
+__global__ void __launch_bounds__(kAppendThreads, R == 2 ? 7 : 8) k_paged_append(const __grid_constant__ PagedDev c, const __grid_constant__ PagedRows r, const __grid_constant__ Frequencies f, int rotate, int wide) {
     constexpr int HALF = HD / 2, TH = HD / 32;
     static_assert(R * HALF <= kAppendThreads, "one thread per angle");
     __shared__ __align__(16) float cos_s[R][HALF], sin_s[R][HALF];
