@@ -84,6 +84,11 @@ void cats_debug_l2_warm(int which, int period, int phase);
  * numbering; else up to `bytes` bytes are copied to the HOST buffer. */
 int cats_debug_timeline(int kernel, void *host, size_t bytes);
 
+/* The logit from which on cats_sample keeps tokens of a row whose largest logit
+ * is `top` for min_p: the same search as the kernel's, on the host.
+ * temperature > 0 (inf included). */
+float cats_debug_sample_least(float top, float temperature, float min_p);
+
 #ifdef __cplusplus
 }
 #endif

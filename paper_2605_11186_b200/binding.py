@@ -217,6 +217,15 @@ def l2_warm(which: int, period: int, phase: int = 0) -> None:
     lib.cats_debug_l2_warm(C.c_int(which), C.c_int(period), C.c_int(phase))
 
 
+lib.cats_debug_sample_least.restype = C.c_float
+lib.cats_debug_sample_least.argtypes = [C.c_float] * 3
+
+
+def sample_least(top: float, temperature: float, min_p: float) -> float:
+    """cats_debug_sample_least: the logit from which on cats_sample keeps tokens for min_p."""
+    return lib.cats_debug_sample_least(top, temperature, min_p)
+
+
 TIMELINE_SLOTS = {0: 512, 1: 128, 2: 256}     # launch slots per kernel (projection, tcgen05 attention, register norm)
 
 

@@ -269,5 +269,6 @@ struct SampleDev {
     int32_t* d_status;
 };
 cudaError_t launch_sample(const SampleDev& p, cudaStream_t st);
+float sample_least(float top, float temperature, float min_p);      // what the kernel cuts at for min-p, on the host
 
 }  // namespace cats

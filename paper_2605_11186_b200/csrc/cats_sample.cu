@@ -20,6 +20,8 @@
 // Measured: one row of 32000 fp32 logits 12 us (latency), 64 with mixed filters 41 us, 256 rows of 128001 in bf16 174 us; of these unfiltered 86 us, top-k of few
 // 66, top-p alone 255: bound by the passes' instructions and the cluster's barriers, not by reading (10 us).
 #include <cooperative_groups.h>
+#include <math.h>
+#include <string.h>
 
 #include <atomic>
 #include <utility>
@@ -91,12 +93,22 @@ extern __shared__ __align__(16) uint8_t dynamic[];
 __device__ __forceinline__ uint8_t& noted_at(int q) { return dynamic[q * kThreads + threadIdx.x]; }
 __device__ __forceinline__ uint4* row_data() { return reinterpret_cast<uint4*>(dynamic + (kInside + 1) * kThreads); }
 
-// Keys in the order of the logits; -0 as 0.
-__device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x + 0.f);
+// Keys in the order of the logits; -0 as 0.  (Of the keys between, only that of -0 is no number's: it stands for 0, too.)
+__host__ __device__ __forceinline__ uint32_t bits_of(float x) {
+    uint32_t b;
+    memcpy(&b, &x, sizeof b);
+    return b;
+}
+__host__ __device__ __forceinline__ uint32_t key_of(float x) {
+    const uint32_t b = bits_of(x + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+__host__ __device__ __forceinline__ float value_of(uint32_t key) {
+    const uint32_t b = key & 0x80000000u ? key ^ 0x80000000u : ~key;
+    float x;
+    memcpy(&x, &b, sizeof x);
+    return x;
+}
 __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
     return a;
@@ -745,18 +757,28 @@ __device__ __noinline__ void finish(const SampleDev& p, int d, int n, int top_k,
     });
 }
 
-// The smallest logit whose weight is at least min_p, the largest among them always
-__device__ __noinline__ float least_of(float min_p) {
+// log2 e / T, 0 at temperature 0
+__host__ __device__ __forceinline__ double per_logit(float temp) { return temp == 0.f ? 0.0 : 1.4426950408889634074 / (double)temp; }
+// The smallest logit whose weight is at least min_p, the largest among them always: bisection over the keys.  It lies within a few keys of what fp64 says,
+// unless the sum cancels (a threshold next to 0 has more neighbours than fp64 tells apart) or is no fp32 number; then the search is over all.
+__host__ __device__ __noinline__ float least_of(float top, double c, float min_p) {
     if (!(min_p > 0.f)) return -INFINITY;
-    const float top = sh.row.top;
-    const double log_p = log2((double)min_p), c = sh.row.c;
+    constexpr float kLowest = -3.402823466e38f;
+    constexpr uint32_t kNear = 8;
+    const double log_p = log2((double)min_p);
     if (log_p >= 0.0) return top;
-    if (c == 0.0) return -3.402823466e38f;
-    auto in = [&](float x) { return ((double)x - (double)top) * c >= log_p; };
-    float x = (float)fmax((double)top + log_p / c, -3.4028234663852886e38);
-    while (in(x) && x > -3.402823466e38f) x = value_of(key_of(x) - 1);
-    while (!in(x)) x = value_of(key_of(x) + 1);
-    return fminf(x, top);
+    if (c == 0.0) return kLowest;
+    auto in = [&](uint32_t key) { return ((double)value_of(key) - (double)top) * c >= log_p; };      // of the largest: 0 >= log_p
+    const uint32_t first = key_of(kLowest), last = key_of(top), guess = key_of((float)fmax((double)top + log_p / c, (double)kLowest));
+    uint32_t lo = guess - first > kNear ? guess - kNear : first, hi = last - guess > kNear ? guess + kNear : last;
+    if (in(lo)) lo = first;
+    if (!in(hi)) hi = last;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (in(mid)) hi = mid;
+        else lo = mid + 1;
+    }
+    return value_of(hi);
 }
 
 template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ SampleDev p) {
@@ -862,7 +884,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
         }
         return sync_all();
     }
-    const double c = temp == 0.f ? 0.0 : 1.4426950408889634074 / (double)temp;
+    const double c = per_logit(temp);
     if (threadIdx.x == 0) {
         sh.row.top = top;
         sh.row.floor = fminf((float)((double)top - 600.0 / c), value_of(key_of(top) - 1));
@@ -876,7 +898,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
         strips<T, kEqual>(top, 0, {}, none);
         return locate<T>(p, d, kEqual, top, 0, 0, u);
     }
-    const float least = least_of(min_p);
+    const float least = least_of(top, c, min_p);
     float tau = -INFINITY;          // kept: logits above tau, and at tau the ones up to index `last`
     i64 ties = -1;                  // how many at tau; -1: all
     int same = 0;
@@ -1008,6 +1030,7 @@ template <typename T> cudaError_t launch_t(const SampleDev& p, cudaStream_t st) 
 
 }  // namespace
 
+float sample_least(float top, float temperature, float min_p) { return least_of(top, per_logit(temperature), min_p); }
 cudaError_t launch_sample(const SampleDev& p, cudaStream_t st) { return p.f32 ? launch_t<float>(p, st) : launch_t<uint16_t>(p, st); }
 
 }  // namespace cats
