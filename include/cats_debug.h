@@ -89,6 +89,11 @@ int cats_debug_timeline(int kernel, void *host, size_t bytes);
  * temperature > 0 (inf included). */
 float cats_debug_sample_least(float top, float temperature, float min_p);
 
+/* Whether cats_paged_attention copies a cache row at 16-byte unit `at` as one that
+ * lies `behind` units behind the row at unit at0 (1) or on its own (0): the same
+ * comparison as the kernel's, on the host. */
+int cats_debug_paged_lies_behind(uint32_t at0, uint32_t at, uint32_t behind);
+
 #ifdef __cplusplus
 }
 #endif

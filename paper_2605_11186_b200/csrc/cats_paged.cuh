@@ -18,6 +18,10 @@ inline Divisor divisor(uint32_t d) {
     return {(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), 31 + l};
 }
 
+// Whether a row that starts at unit `at` lies `behind` units behind one at `at0`.  The last unit of a cache of 2^36 bytes is 2^32 - 1, and at0 + behind may pass it:
+// the sum is 0 then, where another row may lie.
+__host__ __device__ __forceinline__ bool lies_behind(uint32_t at0, uint32_t at, uint32_t behind) { return at >= at0 && at - at0 == behind; }
+
 struct PagedDev {
     uint8_t *k, *v;
     float *ks, *vs;                         // int8 caches

@@ -164,7 +164,7 @@ template <int HD, bool I8, int NT> struct Attn {
             copy<4>(stage + kScales + 128 + lane * 4, c.vs + (size_t)kvh * c.s_head + row.s, row.at != kNoRow);
         }
         const uint32_t at0 = __shfl_sync(0xffffffffu, row.at, 0);
-        if (__all_sync(0xffffffffu, (kTile < 32 && lane >= kTile) || (row.at != kNoRow && row.at == at0 + lane * RP))) {      // rows that follow each other
+        if (__all_sync(0xffffffffu, (kTile < 32 && lane >= kTile) || (row.at != kNoRow && lies_behind(at0, row.at, lane * RP)))) {      // rows that follow each other
 #pragma unroll
             for (int n = 0; n < kCopies; ++n) {
                 const int r = n * kPerCopy + lane / RP;
