@@ -521,8 +521,12 @@ template <int HD, bool I8, int NT> struct Attn {
     // kAtOnce parts come in one trip.
     __device__ __forceinline__ void add_parts(const Segment& g0, int first, int p0, int step, int n, const Slots& w, int to) {
         constexpr int kAtOnce = 6;
-        for (int i = threadIdx.x; i < g0.heads * (HD / 4); i += kThreads) {
-            const int h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
+        // A sum goes to the slot of its first part: a head's threads, which are of one warp, have all read that part's reference before one of them
+        // writes the sum's.  So all lanes go through the loop together, those without a channel with another's.
+        const int n_all = g0.heads * (HD / 4);
+        for (int i0 = warp * 32; i0 < n_all; i0 += kThreads) {
+            const bool mine = i0 + lane < n_all;
+            const int i = mine ? i0 + lane : n_all - 1, h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
             float top = -INFINITY, sum = 0.f;
             float4 x = make_float4(0, 0, 0, 0);
             for (int k0 = 0; k0 < n; k0 += kAtOnce) {
@@ -549,6 +553,8 @@ template <int HD, bool I8, int NT> struct Attn {
                         add(x, o[k], f);
                     }
             }
+            __syncwarp();
+            if (!mine) continue;
             if (to < 0) {
                 store_out(g0.s, g0.head0 + h, ch, x, sum, false);
             } else {
