@@ -570,7 +570,8 @@ lib.cats_sample.argtypes = [_vp, _i32, _i64, _i32, _i32, _vp, _i32, _vp, _vp, _v
 class PagedKV:
     """The pages of one layer's cache (cats_paged_kv): k, v bf16 or int8 [n_pages][page_size][n_kv_heads][head_dim] in any order of
     memory in which a head's elements lie together, and for int8 k_scale, v_scale fp32 [n_pages][page_size][n_kv_heads].  Keeps the
-    tensors; their addresses and strides are taken here.  ValueError for tensors that do not fit each other."""
+    tensors; their addresses and strides are taken here, and calls refuse a cache one of whose tensors has been moved since.  ValueError for
+    tensors that do not fit each other."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         where = "PagedKV"
@@ -617,20 +618,20 @@ def new_paged_kv(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, d
 def _paged(where, kv):
     if not isinstance(kv, PagedKV):
         raise ValueError("%s: cache must be a PagedKV" % where)
-    return kv
+    return kv.k, kv.v, kv.k_scale, kv.v_scale
 
 
 def cats_paged_append(kv, table, seq, pos, q, k, v, rope_base, q_out, status):
     """Rows k, v (fp32 or bf16 [rows][n_kv_heads * head_dim], or [rows][n_kv_heads][head_dim]) become rows pos[i] of the sequences seq[i]
     (None: of sequence i); q and q_out (bf16) may be None.  table: int32 [n_seqs][pages].  rope_base 0: no rotation."""
-    rc = (_ext or _marshal()).paged_append(_paged("cats_paged_append", kv).k, kv.desc, table, seq, pos, q, k, v, rope_base, q_out, status)
+    rc = (_ext or _marshal()).paged_append(_paged("cats_paged_append", kv), kv.desc, table, seq, pos, q, k, v, rope_base, q_out, status)
     if rc:
         raise CatsError(rc, "cats_paged_append")
 
 
 def cats_paged_read(kv, table, seq, pos, k_out, v_out, status):
     """Rows pos[i] of the sequences seq[i] (None: of sequence i) to k_out, v_out, fp32 or bf16 [rows][n_kv_heads * head_dim]."""
-    rc = (_ext or _marshal()).paged_read(_paged("cats_paged_read", kv).k, kv.desc, table, seq, pos, k_out, v_out, status)
+    rc = (_ext or _marshal()).paged_read(_paged("cats_paged_read", kv), kv.desc, table, seq, pos, k_out, v_out, status)
     if rc:
         raise CatsError(rc, "cats_paged_read")
 
@@ -647,7 +648,7 @@ def new_workspace_paged(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: in
 
 def cats_paged_attention(kv, table, lens, q, scale, out, ws, status):
     """q, out: bf16 [n_seqs][n_heads * head_dim] or [n_seqs][n_heads][head_dim]; lens: int32 [n_seqs]; ws: new_workspace_paged."""
-    rc = (_ext or _marshal()).paged_attention(_paged("cats_paged_attention", kv).k, kv.desc, table, lens, q, scale, out, ws, status)
+    rc = (_ext or _marshal()).paged_attention(_paged("cats_paged_attention", kv), kv.desc, table, lens, q, scale, out, ws, status)
     if rc:
         raise CatsError(rc, "cats_paged_attention")
 

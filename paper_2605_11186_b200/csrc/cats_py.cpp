@@ -207,19 +207,28 @@ Matrix heads(Call& c, PyObject* o, const char* name, int64_t rows, int64_t cols,
     return m;
 }
 
-// The cache (its K tensor and its cats_paged_kv as bytes) and the table of its pages.
+// The cache (its tensors, None where it has none, and its cats_paged_kv as bytes) and the table of its pages.
 struct Paged {
     cats_paged_kv kv;
     const int32_t* table;
     int64_t ld, width, n_seqs;
 };
-Paged paged(Call& c, PyObject* k, PyObject* desc, PyObject* table) {
-    const at::Tensor& t = tensor(k, c.what, "cache");
-    c.place(t, "cache");
+Paged paged(Call& c, PyObject* tensors, PyObject* desc, PyObject* table) {
     Paged p;
-    if (!PyBytes_Check(desc) || PyBytes_GET_SIZE(desc) != (Py_ssize_t)sizeof p.kv) refuse(c.what, "cache", "must be a PagedKV");
+    if (!PyTuple_Check(tensors) || PyTuple_GET_SIZE(tensors) != 4 || !PyBytes_Check(desc) || PyBytes_GET_SIZE(desc) != (Py_ssize_t)sizeof p.kv)
+        refuse(c.what, "cache", "must be a PagedKV");
     std::memcpy(&p.kv, PyBytes_AS_STRING(desc), sizeof p.kv);
-    if (p.kv.k != t.data_ptr()) refuse(c.what, "cache", "has been moved");
+    const void* const at[] = {p.kv.k, p.kv.v, p.kv.k_scale, p.kv.v_scale};
+    for (int i = 0; i < 4; ++i) {
+        PyObject* const o = PyTuple_GET_ITEM(tensors, i);
+        const void* now = nullptr;
+        if (i < 2 || o != Py_None) {
+            const at::Tensor& t = tensor(o, c.what, "cache");
+            c.place(t, "cache");
+            now = t.data_ptr();
+        }
+        if (now != at[i]) refuse(c.what, "cache", "has been moved");      // its layout is that of the tensors it was made from
+    }
     const at::Tensor& b = tensor(table, c.what, "table");
     c.place(b, "table");
     if (b.dim() != 2 || b.scalar_type() != at::kInt) refuse(c.what, "table", "must be an int32 matrix");
@@ -241,7 +250,7 @@ double number(PyObject* o) {
     return x;
 }
 
-// (k pages, desc, table, seq, pos, q, k, v, rope_base, q_out, status)
+// (tensors, desc, table, seq, pos, q, k, v, rope_base, q_out, status)
 PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded("cats_paged_append", n, 11, [&] {
         Call c{"cats_paged_append"};
@@ -267,7 +276,7 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// (k pages, desc, table, seq, pos, k_out, v_out, status)
+// (tensors, desc, table, seq, pos, k_out, v_out, status)
 PyObject* py_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded("cats_paged_read", n, 8, [&] {
         Call c{"cats_paged_read"};
@@ -285,7 +294,7 @@ PyObject* py_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// (k pages, desc, table, lens, q, scale, out, ws, status)
+// (tensors, desc, table, lens, q, scale, out, ws, status)
 PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded("cats_paged_attention", n, 9, [&] {
         Call c{"cats_paged_attention"};
