@@ -592,6 +592,8 @@ class PagedKV:
         st = pair(("k", "v"), k, v, 4, (torch.bfloat16, torch.int8))
         if max(k.shape) > 2 ** 31 - 1:
             raise ValueError("%s: k is too large" % where)
+        if min(k.shape) < 1:
+            raise ValueError("%s: k is empty" % where)
         if k.shape[3] > 1 and st[3] != 1:
             raise ValueError("%s: the elements of a head must be contiguous" % where)
         i8, ss = k.dtype == torch.int8, [0, 0, 0]

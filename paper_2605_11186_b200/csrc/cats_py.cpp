@@ -218,6 +218,7 @@ Paged paged(Call& c, PyObject* tensors, PyObject* desc, PyObject* table) {
     if (!PyTuple_Check(tensors) || PyTuple_GET_SIZE(tensors) != 4 || !PyBytes_Check(desc) || PyBytes_GET_SIZE(desc) != (Py_ssize_t)sizeof p.kv)
         refuse(c.what, "cache", "must be a PagedKV");
     std::memcpy(&p.kv, PyBytes_AS_STRING(desc), sizeof p.kv);
+    if (p.kv.n_kv_heads < 1 || p.kv.head_dim < 1) refuse(c.what, "cache", "has no heads");      // shapes are divided by them
     const void* const at[] = {p.kv.k, p.kv.v, p.kv.k_scale, p.kv.v_scale};
     for (int i = 0; i < 4; ++i) {
         PyObject* const o = PyTuple_GET_ITEM(tensors, i);
