@@ -305,7 +305,7 @@ template <int HD, bool I8, int NT> struct Attn {
                     ks = lds_float(stage + kScales + row * 4);
                     const float sv = lds_float(stage + kScales + 128 + row * 4);
                     ref[b][h] = lg2(fmaxf(fabsf(sv), 6.2e-33f));
-                    vs[b][h] = sv * 32768.f;
+                    vs[b][h] = sv;
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -358,7 +358,7 @@ template <int HD, bool I8, int NT> struct Attn {
                     l[nt][0] += p0;
                     l[nt][1] += p1;
                     if (I8) {
-                        p[nt][b][h] = transpose8x8(pack_f16x2(p0 * vs[b][h], p1 * vs[b][h]));
+                        p[nt][b][h] = transpose8x8(pack_f16x2(p0 * vs[b][h] * 32768.f, p1 * vs[b][h] * 32768.f));      // p scale_v is at most 1, scale_v 2^15 may pass fp32
                     } else {
                         const uint32_t hi = pack_bf16x2(p0, p1);
                         lo[nt][b][h] = transpose8x8(pack_bf16x2(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xFFFF0000u)));
