@@ -10,8 +10,8 @@
 //
 // One pass with a running maximum and sum per head and warp.  Probabilities enter the second product as two bf16 parts (16
 // bits) over a bf16 cache.  An int8 cache's bytes are whole numbers in fp16, exact; the row's scale is part of the weight
-// w = p scale_v, which is rounded to fp16: the running maximum is that of score + log2 scale_v, so that w is at most 1, times 2^15, and
-// what is 2^-28 of the largest is still a normal number (a long flat tail behind one large row keeps its bits).
+// w = p scale_v, which is rounded to fp16 with a running exponent of its own (fit): what is 2^-23 of the largest is still a normal number, and
+// a long flat tail behind one large row keeps its bits.
 //
 // Work: the rows of every (sequence, head group) are cut into units of 4 tiles; all units in one line are dealt out evenly to the
 // blocks, three per SM (12 warps with 8 KB of rows in flight each; HBM needs about 45 KB per SM).  A block of four warps takes
@@ -34,18 +34,21 @@ constexpr int kMaxHeads = 16;       // query heads per block
 constexpr int kMaxLen = INT32_MAX - 1023;       // a tile's rows behind the last one are still numbers
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 static_assert(kGroup * kGroup >= kMaxBlocks, "two steps have to do");
+constexpr float kLowest = -110.f;   // int8: of the weights' exponent `up`; 2^(15 - up) is a number
+constexpr float kRoom = 6.f;        // and how far below 2^15 the largest weight is when `up` is set
 
 // Workspace: two part slots per block (a head group that began before its first unit, one that goes on behind its last), then counters.  A
 // block is the first of at most one head group that goes on in the next, and a later one of at most one: a counter each.
-constexpr size_t kSlotFloats = (size_t)kMaxHeads * (128 + 2);
+constexpr size_t kSlotFloats = (size_t)kMaxHeads * (128 + 4);
+typedef float4 Part;            // of a head: reference of its probabilities, exponent of its weights (int8), sum of its probabilities
 struct Slots {
-    float* part;
+    float* values;
     int* counters;              // zero between calls
     __device__ __forceinline__ int* first(int block) const { return counters + block; }                       // parts that begin with a first block's
     __device__ __forceinline__ int* later(int block) const { return counters + kMaxBlocks + block; }          // with a later one's
     __device__ __forceinline__ int* groups(int block) const { return counters + 2 * kMaxBlocks + block; }     // sums of kGroup parts, by first block
-    __device__ __forceinline__ float* o(int slot) const { return part + (size_t)slot * kSlotFloats; }
-    __device__ __forceinline__ float2* ml(int slot) const { return reinterpret_cast<float2*>(part + (size_t)slot * kSlotFloats + kMaxHeads * 128); }
+    __device__ __forceinline__ float* o(int slot) const { return values + (size_t)slot * kSlotFloats; }
+    __device__ __forceinline__ Part* part_of(int slot) const { return reinterpret_cast<Part*>(values + (size_t)slot * kSlotFloats + kMaxHeads * 128); }
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -112,7 +115,7 @@ template <int HD, bool I8, int NT> struct Attn {
         uint4 raw[NT * 8 * HD / 8];                         // the queries of the next segment, as they are
         uint4 q[2][NT][QV][32];                             // and as the second operand of K Q^T, of this segment and the next
         float qf[2][NT * 8];                                // factors of the scores
-        float2 ml[kWarps][NT * 8];
+        Part part[kWarps][NT * 8];
         int o_at[kWarps];                                   // which half of its ring a warp's O is in
         long long total, before;        // units of all sequences, and of those in front of `seq`
         int seq, last;
@@ -125,6 +128,7 @@ template <int HD, bool I8, int NT> struct Attn {
     const int lane, warp, g, j;
     float acc[NT][MT][4];
     float m[NT][2], l[NT][2], qf[NT][2];       // heads 2j and 2j + 1 of each 8: reference, sum, factor of the scores
+    float up[NT][2], times[NT][2];             // int8: the weights' exponent and 2^(15 - up)
 
     __device__ __forceinline__ Attn(const PagedDev& c_, const PagedAttn& a_, Shared& s_)
         : c(c_), a(a_), sh(s_), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), g((threadIdx.x & 31) >> 2), j(threadIdx.x & 3) {}
@@ -250,8 +254,76 @@ template <int HD, bool I8, int NT> struct Attn {
         }
     }
 
-    // One tile: scores, weights, O^T.  left: rows of the sequence from the tile's first on.
-    __device__ __forceinline__ void step(uint32_t stage, int left, int parity) {
+    static __device__ __forceinline__ float over_rows(float x) {       // the largest of the lanes that have rows of the same heads
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+        return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+    }
+    __device__ __forceinline__ void rescale(const float (&keep)[NT][2]) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[nt][t][e] *= keep[nt][e & 1];
+    }
+    // int8.  A probability is relative to 2^m, m a whole number a little above the largest score so far; a weight p scale_v has a factor of its own, 2^(15 - up).
+    // (One reference, the maximum of score + log2 scale_v, for both: probabilities of rows with a small scale, or next to a row with a
+    // large one, leave the range of fp32, and the sum loses them.)  O^T is in units of 2^(m + up - 15).
+    // Most tiles change neither: their scores are below m, and scale_v 2^(15 - up) is a number of fp16, so the weights are.  For that, what is the largest
+    // weight when `up` is set is put 2^6 below 2^15, where the smallest that fp16 tells from 0 is 2^-34 of it.
+    __device__ __forceinline__ void fit(const float (&s)[NT][kBlk][4], const float (&sv)[kBlk][2], bool first) {
+        float x[NT][2], size = 0.f;
+        bool over = false;
+#pragma unroll
+        for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) size = fmaxf(size, fabsf(sv[b][h]));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                x[nt][e] = s[nt][0][e];
+#pragma unroll
+                for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) x[nt][e] = fmaxf(x[nt][e], s[nt][b][h * 2 + e]);
+                over |= x[nt][e] > m[nt][e] || size * times[nt][e] > 65504.f;
+            }
+        if (!__any_sync(0xffffffffu, over)) return;
+        // the largest score and the largest score + log2 scale_v, both relative to one lane's, so that large scores leave the logarithms their bits
+        float lg[kBlk][2], keep[NT][2];
+        bool changed = false;
+#pragma unroll
+        for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) lg[b][h] = lg2(fabsf(sv[b][h]));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float r = __shfl_sync(0xffffffffu, x[nt][e], j);
+                r = fabsf(r) < INFINITY ? r : 0.f;
+                float z = (s[nt][0][e] - r) + lg[0][0];
+#pragma unroll
+                for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) z = fmaxf(z, (s[nt][b][h * 2 + e] - r) + lg[b][h]);
+                const float top = over_rows(x[nt][e]), most = over_rows(z), to = top > m[nt][e] ? ceilf(top) + 2.f : m[nt][e];
+                const float by = m[nt][e] == to ? 0.f : m[nt][e] - to, from = up[nt][e] + by, need = most + (r - to);
+                const float with = fmaxf(need > from + 0.99f ? ceilf(need) + kRoom : from, kLowest);
+                keep[nt][e] = ex2(from - with);
+                changed |= with != from;
+                l[nt][e] *= ex2(by);
+                up[nt][e] = with;
+                times[nt][e] = ex2(15.f - with);
+                m[nt][e] = to;
+            }
+        if (!first && __any_sync(0xffffffffu, changed)) rescale(keep);
+    }
+
+    // One tile: scores, weights, O^T.  left: rows of the sequence from the tile's first on; first: nothing has been added to O^T yet.
+    __device__ __forceinline__ void step(uint32_t stage, int left, int parity, bool first) {
         float s[NT][kBlk][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -290,8 +362,8 @@ template <int HD, bool I8, int NT> struct Attn {
                 }
             }
         }
-        // scores in log2, and what the running reference is the maximum of: for int8 with the row's log2 scale_v (no less than the scale of a row of zeros)
-        float vs[kBlk][2], ref[kBlk][2];
+        // scores in log2
+        float vs[kBlk][2];
 #pragma unroll
         for (int b = 0; b < kBlk; ++b)
 #pragma unroll
@@ -300,71 +372,75 @@ template <int HD, bool I8, int NT> struct Attn {
                 const float none = row < left ? 0.f : -INFINITY;
                 float ks = 1.f;
                 vs[b][h] = 1.f;
-                ref[b][h] = 0.f;
                 if (I8) {
                     ks = lds_float(stage + kScales + row * 4);
-                    const float sv = lds_float(stage + kScales + 128 + row * 4);
-                    ref[b][h] = lg2(fmaxf(fabsf(sv), 6.2e-33f));
-                    vs[b][h] = sv;
+                    vs[b][h] = lds_float(stage + kScales + 128 + row * 4);
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) s[nt][b][h * 2 + e] = s[nt][b][h * 2 + e] * qf[nt][e] * ks + none;
             }
-        bool moved = false;
-        float keep[NT][2];
+        // weights, turned into the second operand of V^T P^T: heads along the lanes' groups, rows along a thread
+        uint32_t p[NT][kBlk][2], lo[NT][kBlk][2];
+        if constexpr (I8) {
+            fit(s, vs, first);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float x = s[nt][0][e] + ref[0][0];
+            for (int nt = 0; nt < NT; ++nt) {
+                const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1], f0 = times[nt][0], f1 = times[nt][1];
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) x = fmaxf(x, s[nt][b][h * 2 + e] + ref[b][h]);
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                x = fmaxf(x, m[nt][e]);
-                keep[nt][e] = 1.f;
-                if (x != m[nt][e]) {
-                    keep[nt][e] = ex2(m[nt][e] - x);
-                    m[nt][e] = x;
-                    moved = true;
+                    for (int h = 0; h < 2; ++h) {
+                        const float p0 = ex2(s[nt][b][h * 2] - m0), p1 = ex2(s[nt][b][h * 2 + 1] - m1);
+                        l[nt][0] += p0;
+                        l[nt][1] += p1;
+                        p[nt][b][h] = transpose8x8(pack_f16x2(p0 * vs[b][h] * f0, p1 * vs[b][h] * f1));
+                    }
+            }
+        } else {
+            bool moved = false;
+            float keep[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = s[nt][0][e];
+#pragma unroll
+                    for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) x = fmaxf(x, s[nt][b][h * 2 + e]);
+                    x = fmaxf(over_rows(x), m[nt][e]);
+                    keep[nt][e] = 1.f;
+                    if (x != m[nt][e]) {
+                        keep[nt][e] = ex2(m[nt][e] - x);
+                        m[nt][e] = x;
+                        moved = true;
+                    }
+                }
+            if (__any_sync(0xffffffffu, moved)) {
+                rescale(keep);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    l[nt][0] *= keep[nt][0];
+                    l[nt][1] *= keep[nt][1];
                 }
             }
-        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
+                const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
+                for (int b = 0; b < kBlk; ++b)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[nt][t][e] *= keep[nt][e & 1];
-                l[nt][0] *= keep[nt][0];
-                l[nt][1] *= keep[nt][1];
-            }
-        }
-        // weights, turned into the second operand of V^T P^T: heads along the lanes' groups, rows along a thread
-        uint32_t p[NT][kBlk][2], lo[NT][kBlk][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
-#pragma unroll
-            for (int b = 0; b < kBlk; ++b)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float p0 = ex2(s[nt][b][h * 2] - m0), p1 = ex2(s[nt][b][h * 2 + 1] - m1);
-                    l[nt][0] += p0;
-                    l[nt][1] += p1;
-                    if (I8) {
-                        p[nt][b][h] = transpose8x8(pack_f16x2(p0 * vs[b][h] * 32768.f, p1 * vs[b][h] * 32768.f));      // p scale_v is at most 1, scale_v 2^15 may pass fp32
-                    } else {
+                    for (int h = 0; h < 2; ++h) {
+                        const float p0 = ex2(s[nt][b][h * 2] - m0), p1 = ex2(s[nt][b][h * 2 + 1] - m1);
+                        l[nt][0] += p0;
+                        l[nt][1] += p1;
                         const uint32_t hi = pack_bf16x2(p0, p1);
                         lo[nt][b][h] = transpose8x8(pack_bf16x2(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xFFFF0000u)));
                         p[nt][b][h] = transpose8x8(hi);
                     }
-                }
+            }
         }
 #pragma unroll
         for (int b = 0; b < kBlk; ++b) {
@@ -432,6 +508,8 @@ template <int HD, bool I8, int NT> struct Attn {
             for (int e = 0; e < 2; ++e) {
                 m[nt][e] = -INFINITY;
                 l[nt][e] = 0.f;
+                up[nt][e] = I8 ? kLowest : 0.f;
+                times[nt][e] = ex2(15.f - kLowest);
                 qf[nt][e] = sh.qf[parity][nt * 8 + 2 * j + e];
             }
 #pragma unroll
@@ -450,7 +528,7 @@ template <int HD, bool I8, int NT> struct Attn {
                 if (i + 2 < tiles) next = row_of(g0.s, first + (i + 2) * kUnit, g0.t1);
                 else if (i + 2 == tiles && next_has) next = row_of(g1.s, first1, g1.t1);
             }
-            step(ring + used * kStage, g0.t1 - (first + i * kUnit), parity);
+            step(ring + used * kStage, g0.t1 - (first + i * kUnit), parity, i == 0);
         }
         const int active = min(kWarps, (g0.t1 - g0.t0 + kTile - 1) / kTile);
         if (warp < active) {
@@ -464,8 +542,8 @@ template <int HD, bool I8, int NT> struct Attn {
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], d);
                 if (g == 0) {
-                    sh.ml[warp][nt * 8 + 2 * j] = make_float2(m[nt][0], l[nt][0]);
-                    sh.ml[warp][nt * 8 + 2 * j + 1] = make_float2(m[nt][1], l[nt][1]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) sh.part[warp][nt * 8 + 2 * j + e] = make_float4(m[nt][e], up[nt][e], l[nt][e], 0.f);
                 }
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
@@ -482,34 +560,61 @@ template <int HD, bool I8, int NT> struct Attn {
         return active;
     }
 
-    __device__ __forceinline__ static float factor(float mi, float top) { return ex2(mi - (top == -INFINITY ? 0.f : top)); }
-    __device__ __forceinline__ void store_out(int s, int head, int ch, const float4& x, float sum, bool empty) {
-        const float f = empty ? 0.f : (I8 ? 1.f / 32768.f : 1.f) / sum;
+    // Parts joined so far: where their references lie and what they add up to.  Values of a part are in units of 2^(m + up).
+    struct Sum {
+        float m = -INFINITY, up = -INFINITY, l = 0.f;
+        float4 x = make_float4(0, 0, 0, 0);
+        // To the references of these parts too
+        template <int N> __device__ __forceinline__ void raise(const Part (&p)[N], int n) {
+            float to = m;
+#pragma unroll
+            for (int k = 0; k < N; ++k) if (k < n) to = fmaxf(to, p[k].x);
+            const float zero = to == -INFINITY ? 0.f : to, by = ex2(m - zero);
+            l *= by;
+            if (I8) {
+                const float from = up + (m - zero);
+                float with = from;
+#pragma unroll
+                for (int k = 0; k < N; ++k) if (k < n) with = fmaxf(with, p[k].y + (p[k].x - zero));
+                up = with;
+                scale(ex2(from - (with == -INFINITY ? 0.f : with)));
+            } else {
+                scale(by);
+            }
+            m = to;
+        }
+        __device__ __forceinline__ void scale(float f) { x.x *= f; x.y *= f; x.z *= f; x.w *= f; }
+        __device__ __forceinline__ void add(const Part& p, const float4& o) {
+            const float by = p.x - (m == -INFINITY ? 0.f : m), f = ex2(by), fx = I8 ? ex2(p.y + by - (up == -INFINITY ? 0.f : up)) : f;
+            l = fmaf(p.z, f, l);
+            x.x = fmaf(o.x, fx, x.x); x.y = fmaf(o.y, fx, x.y); x.z = fmaf(o.z, fx, x.z); x.w = fmaf(o.w, fx, x.w);
+        }
+    };
+    __device__ __forceinline__ void store_out(int s, int head, int ch, Sum& r, bool empty) {
+        r.scale(1.f / r.l);
+        if (I8) r.scale(ex2(r.up - 15.f));          // apart: the product may lie below fp32
         uint32_t* const o = reinterpret_cast<uint32_t*>(a.out + s * a.ldo + (size_t)head * HD + ch);
-        o[0] = empty ? 0u : pack_bf16x2(x.x * f, x.y * f);
-        o[1] = empty ? 0u : pack_bf16x2(x.z * f, x.w * f);
-    }
-    static __device__ __forceinline__ void add(float4& x, const float4& y, float f) {
-        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+        o[0] = empty ? 0u : pack_bf16x2(r.x.x, r.x.y);
+        o[1] = empty ? 0u : pack_bf16x2(r.x.z, r.x.w);
     }
 
     // The block's warps joined: to `slot`, or (slot < 0) to the output.
     __device__ __forceinline__ void join(int s, int head0, int heads, int active, const Slots& w, int slot) {
         for (int i = threadIdx.x; i < heads * (HD / 4); i += kThreads) {
             const int h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
-            float top = -INFINITY, sum = 0.f;
-            for (int k = 0; k < active; ++k) top = fmaxf(top, sh.ml[k][h].x);
-            float4 x = make_float4(0, 0, 0, 0);
-            for (int k = 0; k < active; ++k) {
-                const float f = factor(sh.ml[k][h].x, top);
-                sum = fmaf(sh.ml[k][h].y, f, sum);
-                add(x, *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(sh.ring[k][sh.o_at[k]]) + h * kPad + ch), f);
-            }
+            Part p[kWarps];
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) p[k] = sh.part[k][h];      // of the active ones
+            Sum r;
+            r.raise(p, active);
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k)
+                if (k < active) r.add(p[k], *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(sh.ring[k][sh.o_at[k]]) + h * kPad + ch));
             if (slot < 0) {
-                store_out(s, head0 + h, ch, x, sum, active == 0);
+                store_out(s, head0 + h, ch, r, active == 0);
             } else {
-                *reinterpret_cast<float4*>(w.o(slot) + h * HD + ch) = x;
-                if (ch == 0) w.ml(slot)[h] = make_float2(top, sum);
+                *reinterpret_cast<float4*>(w.o(slot) + h * HD + ch) = r.x;
+                if (ch == 0) w.part_of(slot)[h] = make_float4(r.m, r.up, r.l, 0.f);
             }
         }
         __syncthreads();            // the rings are free
@@ -527,39 +632,28 @@ template <int HD, bool I8, int NT> struct Attn {
         for (int i0 = warp * 32; i0 < n_all; i0 += kThreads) {
             const bool mine = i0 + lane < n_all;
             const int i = mine ? i0 + lane : n_all - 1, h = i / (HD / 4), ch = (i % (HD / 4)) * 4;
-            float top = -INFINITY, sum = 0.f;
-            float4 x = make_float4(0, 0, 0, 0);
+            Sum r;
             for (int k0 = 0; k0 < n; k0 += kAtOnce) {
-                float2 ml[kAtOnce];
+                Part p[kAtOnce];
                 float4 o[kAtOnce];
 #pragma unroll
                 for (int k = 0; k < kAtOnce; ++k) {
                     const int slot = slot_of(first, p0 + min(k0 + k, n - 1) * step);
-                    ml[k] = __ldcg(w.ml(slot) + h);
+                    p[k] = __ldcg(w.part_of(slot) + h);
                     o[k] = __ldcg(reinterpret_cast<const float4*>(w.o(slot) + h * HD + ch));
                 }
-                float t = top;
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) t = fmaxf(t, ml[k].x);
-                const float keep = factor(top, t);
-                sum *= keep;
-                x.x *= keep; x.y *= keep; x.z *= keep; x.w *= keep;
-                top = t;
+                r.raise(p, kAtOnce);    // those behind the last are the last again
 #pragma unroll
                 for (int k = 0; k < kAtOnce; ++k)
-                    if (k0 + k < n) {
-                        const float f = factor(ml[k].x, top);
-                        sum = fmaf(ml[k].y, f, sum);
-                        add(x, o[k], f);
-                    }
+                    if (k0 + k < n) r.add(p[k], o[k]);
             }
             __syncwarp();
             if (!mine) continue;
             if (to < 0) {
-                store_out(g0.s, g0.head0 + h, ch, x, sum, false);
+                store_out(g0.s, g0.head0 + h, ch, r, false);
             } else {
-                *reinterpret_cast<float4*>(w.o(to) + h * HD + ch) = x;
-                if (ch == 0) w.ml(to)[h] = make_float2(top, sum);
+                *reinterpret_cast<float4*>(w.o(to) + h * HD + ch) = r.x;
+                if (ch == 0) w.part_of(to)[h] = make_float4(r.m, r.up, r.l, 0.f);
             }
         }
     }
