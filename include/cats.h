@@ -479,7 +479,9 @@ int cats_paged_read(const cats_paged_kv *kv, const int32_t *d_table, int64_t ld_
  * n_heads is a multiple of n_kv_heads.  d_len[s] <= 0: the row of out is zeros.  Lengths
  * past table_width * page_size, or 2^31 - 1024, are cut there and reported.  Scores and softmax are fp32, the
  * probabilities enter the second product with 16 significant bits over a bf16 cache and with 11
- * over an int8 cache.  Rows behind a sequence's length are not read.
+ * over an int8 cache.  Rows behind a sequence's length are not read.  An infinite v makes its
+ * infinity of the output's channel (both: NaN), unless its row is 2^126 or more behind the
+ * largest: there a probability is 0, and 0 times an infinity NaN.
  * Workspace: cats_paged_workspace_bytes (0 for arguments that are refused), 1024-byte
  * aligned, one per stream, ZEROED once by the caller; a call leaves it fit for the next of
  * any size that it is large enough for. */

@@ -56,6 +56,12 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two bf16 with infinities as the largest number of their sign (NaN as some number)
+__device__ __forceinline__ uint32_t finite(uint32_t a) {
+    uint32_t r;
+    asm("min.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(0x7F7F7F7Fu));
+    return r;
+}
 __device__ __forceinline__ float lg2(float x) {
     float y;
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -476,9 +482,9 @@ template <int HD, bool I8, int NT> struct Attn {
                         const uint32_t t0 = word_of(vr[0], w), t1 = word_of(vr[1], w), t2 = word_of(vr[2], w), t3 = word_of(vr[3], w);
                         const uint32_t a0 = __byte_perm(t0, t1, 0x5410), a1 = __byte_perm(t0, t1, 0x7632), a2 = __byte_perm(t2, t3, 0x5410), a3 = __byte_perm(t2, t3, 0x7632);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
+                        for (int nt = 0; nt < NT; ++nt) {          // a second part may be 0 or negative, and infinities have had their weight from the first
                             mma<I8>(acc[nt][i * 4 + w], a0, a1, a2, a3, p[nt][b][0], p[nt][b][1]);
-                            mma<I8>(acc[nt][i * 4 + w], a0, a1, a2, a3, lo[nt][b][0], lo[nt][b][1]);
+                            mma<I8>(acc[nt][i * 4 + w], finite(a0), finite(a1), finite(a2), finite(a3), lo[nt][b][0], lo[nt][b][1]);
                         }
                     }
                 }
