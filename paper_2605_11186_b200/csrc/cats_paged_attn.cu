@@ -10,8 +10,9 @@
 //
 // One pass with a running maximum and sum per head and warp.  Probabilities enter the second product as two bf16 parts (16
 // bits) over a bf16 cache.  An int8 cache's bytes are whole numbers in fp16, exact; the row's scale is part of the weight
-// w = p scale_v, which is rounded to fp16 with a running exponent of its own (fit): what is 2^-23 of the largest is still a normal number, and
-// a long flat tail behind one large row keeps its bits.
+// w = p scale_v, which enters as two fp16 parts (22 bits) with a running exponent of its own (fit).  Groups of up to four heads have room for both parts
+// in the columns of one product: their queries stand there twice (48 sequences of up to 1500 rows, 40 heads over 40: 102 us; with a second
+// product, as larger groups take it, 108; with one part of 11 bits 100, and outputs 4e-4 to 1e-3 from those of fp32 weights instead of 3e-5 to 2e-4).
 //
 // Work: the rows of every (sequence, head group) are cut into units of 4 tiles; all units in one line are dealt out evenly to the
 // blocks, three per SM (12 warps with 8 KB of rows in flight each; HBM needs about 45 KB per SM).  A block of four warps takes
@@ -85,6 +86,16 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+__device__ __forceinline__ float f16_low(uint32_t a) {
+    float x;
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, l; }" : "=f"(x) : "r"(a));
+    return x;
+}
+__device__ __forceinline__ float f16_high(uint32_t a) {
+    float x;
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, h; }" : "=f"(x) : "r"(a));
+    return x;
+}
 // Bytes 0 and 1 (which = 0x4140) or 2 and 3 (0x4342) of w, each 128 more than the number it stands for, as fp16: 0x6400 + b is 1024 + b
 __device__ __forceinline__ uint32_t f16_of_bytes(uint32_t w, uint32_t which) {
     uint32_t r, x = __byte_perm(w, 0x64646464u, which);
@@ -101,7 +112,9 @@ struct Segment {
     __device__ __forceinline__ int tiles(int first, int step) const { return first < t1 ? (t1 - first + step - 1) / step : 0; }
 };
 
-template <int HD, bool I8, int NT> struct Attn {
+// BOTH (int8, groups of up to four): columns 4 to 7 of both products are those of 0 to 3 once more, and the second parts of their weights stand there.
+template <int HD, bool I8, int NT, bool BOTH> struct Attn {
+    static_assert(!BOTH || (I8 && NT == 1), "two parts of each weight, in the columns of one product");
     static constexpr int kTile = I8 || HD == 64 ? 32 : 16;      // rows per warp and step
     static constexpr int kUnit = kTile * kWarps;
     static constexpr int kBlk = kTile / 16;
@@ -228,7 +241,7 @@ template <int HD, bool I8, int NT> struct Attn {
         for (int nt = 0; nt < NT; ++nt) {
             uint4 x[QV];
 #pragma unroll
-            for (int i = 0; i < QV; ++i) x[i] = sh.raw[(nt * 8 + g) * (HD / 8) + (I8 ? (i >> 1) * 8 + j * 2 + (i & 1) : i * 4 + j)];
+            for (int i = 0; i < QV; ++i) x[i] = sh.raw[(nt * 8 + (BOTH ? g & 3 : g)) * (HD / 8) + (I8 ? (i >> 1) * 8 + j * 2 + (i & 1) : i * 4 + j)];
             float mine = base;
             if (I8) {
                 uint32_t mx = 0;
@@ -391,6 +404,7 @@ template <int HD, bool I8, int NT> struct Attn {
         uint32_t p[NT][kBlk][2], lo[NT][kBlk][2];
         if constexpr (I8) {
             fit(s, vs, first);
+            const float second = j < 2 ? 0.f : -1.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1], f0 = times[nt][0], f1 = times[nt][1];
@@ -401,7 +415,14 @@ template <int HD, bool I8, int NT> struct Attn {
                         const float p0 = ex2(s[nt][b][h * 2] - m0), p1 = ex2(s[nt][b][h * 2 + 1] - m1);
                         l[nt][0] += p0;
                         l[nt][1] += p1;
-                        p[nt][b][h] = transpose8x8(pack_f16x2(p0 * vs[b][h] * f0, p1 * vs[b][h] * f1));
+                        const float w0 = p0 * vs[b][h] * f0, w1 = p1 * vs[b][h] * f1;
+                        const uint32_t hi = pack_f16x2(w0, w1);
+                        if (BOTH) {
+                            p[nt][b][h] = transpose8x8(pack_f16x2(fmaf(f16_low(hi), second, w0), fmaf(f16_high(hi), second, w1)));
+                        } else {
+                            p[nt][b][h] = transpose8x8(hi);
+                            lo[nt][b][h] = transpose8x8(pack_f16x2(w0 - f16_low(hi), w1 - f16_high(hi)));
+                        }
                     }
             }
         } else {
@@ -468,7 +489,10 @@ template <int HD, bool I8, int NT> struct Attn {
                         const uint32_t z0 = half ? y[0] : x[0], z1 = half ? y[1] : x[1];
                         const uint32_t a0 = f16_of_bytes(z0, 0x4140), a1 = f16_of_bytes(z0, 0x4342), a2 = f16_of_bytes(z1, 0x4140), a3 = f16_of_bytes(z1, 0x4342);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma<I8>(acc[nt][w * 2 + half], a0, a1, a2, a3, p[nt][b][0], p[nt][b][1]);
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma<I8>(acc[nt][w * 2 + half], a0, a1, a2, a3, p[nt][b][0], p[nt][b][1]);
+                            if (!BOTH) mma<I8>(acc[nt][w * 2 + half], a0, a1, a2, a3, lo[nt][b][0], lo[nt][b][1]);
+                        }
                     }
                 }
             } else {
@@ -615,7 +639,15 @@ template <int HD, bool I8, int NT> struct Attn {
             r.raise(p, active);
 #pragma unroll
             for (int k = 0; k < kWarps; ++k)
-                if (k < active) r.add(p[k], *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(sh.ring[k][sh.o_at[k]]) + h * kPad + ch));
+                if (k < active) {
+                    const float* const o = reinterpret_cast<const float*>(sh.ring[k][sh.o_at[k]]) + h * kPad + ch;
+                    float4 x = *reinterpret_cast<const float4*>(o);
+                    if (BOTH) {
+                        const float4 y = *reinterpret_cast<const float4*>(o + 4 * kPad);
+                        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                    }
+                    r.add(p[k], x);
+                }
             if (slot < 0) {
                 store_out(s, head0 + h, ch, r, active == 0);
             } else {
@@ -836,16 +868,16 @@ template <int HD, bool I8, int NT> struct Attn {
     }
 };
 
-template <int HD, bool I8, int NT> __global__ void __launch_bounds__(kThreads, NT == 1 ? kBlocksPerSm : 2) k_paged_attn(const __grid_constant__ PagedDev c, const __grid_constant__ PagedAttn a) {
+template <int HD, bool I8, int NT, bool BOTH> __global__ void __launch_bounds__(kThreads, NT == 1 ? kBlocksPerSm : 2) k_paged_attn(const __grid_constant__ PagedDev c, const __grid_constant__ PagedAttn a) {
     extern __shared__ __align__(16) uint8_t smem[];
-    typename Attn<HD, I8, NT>::Shared& sh = *reinterpret_cast<typename Attn<HD, I8, NT>::Shared*>(smem);
+    typename Attn<HD, I8, NT, BOTH>::Shared& sh = *reinterpret_cast<typename Attn<HD, I8, NT, BOTH>::Shared*>(smem);
     pdl_launch_dependents();
     pdl_wait();
-    Attn<HD, I8, NT>(c, a, sh).run();
+    Attn<HD, I8, NT, BOTH>(c, a, sh).run();
 }
 
-template <int HD, bool I8, int NT> cudaError_t launch_k(const PagedDev& c, const PagedAttn& a, cudaStream_t st) {
-    typedef Attn<HD, I8, NT> A;
+template <int HD, bool I8, int NT, bool BOTH> cudaError_t launch_k(const PagedDev& c, const PagedAttn& a, cudaStream_t st) {
+    typedef Attn<HD, I8, NT, BOTH> A;
     const long long per_kv = a.n_heads / c.n_kv, groups = c.n_kv * ((per_kv + NT * 8 - 1) / (NT * 8));
     const long long most = (long long)c.width * c.page_size, units = (most - 1) / A::kUnit + 1;
     const long long fit = NT == 1 ? kMaxBlocks : 148 * 2, blocks = units >= fit ? fit : min(fit, units * groups * c.n_seqs);
@@ -857,26 +889,26 @@ template <int HD, bool I8, int NT> cudaError_t launch_k(const PagedDev& c, const
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!(known.load(std::memory_order_acquire) >> dev & 1)) {
-        e = cudaFuncSetAttribute(k_paged_attn<HD, I8, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = cudaFuncSetAttribute(k_paged_attn<HD, I8, NT, BOTH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         known.fetch_or((uint64_t)1 << dev, std::memory_order_release);
     }
-    return launch_i8(k_paged_attn<HD, I8, NT>, dim3((unsigned)blocks), dim3(kThreads), smem, st, c, a);
+    return launch_i8(k_paged_attn<HD, I8, NT, BOTH>, dim3((unsigned)blocks), dim3(kThreads), smem, st, c, a);
 }
 
 }  // namespace
 
 size_t paged_attn_workspace(int, int, int, int) { return 2 * kMaxBlocks * kSlotFloats * 4 + 3 * kMaxBlocks * sizeof(int); }
 
-cudaError_t launch_paged_attn(const PagedDev& c, const PagedAttn& a, int i8, int hd, cudaStream_t st) {
+template <int HD> cudaError_t launch_hd(const PagedDev& c, const PagedAttn& a, int i8, cudaStream_t st) {
     // eight heads at a time while the group has no more: the accumulators of sixteen leave registers for half the rows in flight
-    const bool one = a.n_heads / c.n_kv <= 8;
-    if (hd == 128) {
-        if (i8) return one ? launch_k<128, true, 1>(c, a, st) : launch_k<128, true, 2>(c, a, st);
-        return one ? launch_k<128, false, 1>(c, a, st) : launch_k<128, false, 2>(c, a, st);
-    }
-    if (i8) return one ? launch_k<64, true, 1>(c, a, st) : launch_k<64, true, 2>(c, a, st);
-    return one ? launch_k<64, false, 1>(c, a, st) : launch_k<64, false, 2>(c, a, st);
+    const int group = a.n_heads / c.n_kv;
+    if (i8) return group <= 4 ? launch_k<HD, true, 1, true>(c, a, st) : (group <= 8 ? launch_k<HD, true, 1, false>(c, a, st) : launch_k<HD, true, 2, false>(c, a, st));
+    return group <= 8 ? launch_k<HD, false, 1, false>(c, a, st) : launch_k<HD, false, 2, false>(c, a, st);
+}
+
+cudaError_t launch_paged_attn(const PagedDev& c, const PagedAttn& a, int i8, int hd, cudaStream_t st) {
+    return hd == 128 ? launch_hd<128>(c, a, i8, st) : launch_hd<64>(c, a, i8, st);
 }
 
 }  // namespace cats
