@@ -89,6 +89,10 @@ int cats_debug_timeline(int kernel, void *host, size_t bytes);
  * temperature > 0 (inf included). */
 float cats_debug_sample_least(float top, float temperature, float min_p);
 
+/* x * all rounded down, or (up) up to a whole number, 0 <= x < 1, 0 <= all < 2^62:
+ * what cats_sample makes of top_p and of the random number, on the host. */
+int64_t cats_debug_sample_part(float x, int64_t all, int up);
+
 /* Whether cats_paged_attention copies a cache row at 16-byte unit `at` as one that
  * lies `behind` units behind the row at unit at0 (1) or on its own (0): the same
  * comparison as the kernel's, on the host. */

@@ -277,6 +277,7 @@ int cats_debug_wait_limit_ns(unsigned long long ns) {
     return CATS_OK;
 }
 float cats_debug_sample_least(float top, float temperature, float min_p) { return sample_least(top, temperature, min_p); }
+int64_t cats_debug_sample_part(float x, int64_t all, int up) { return sample_part(x, all, up != 0); }
 int cats_debug_paged_lies_behind(uint32_t at0, uint32_t at, uint32_t behind) { return lies_behind(at0, at, behind); }
 int cats_debug_workspace_layout(const cats_model_cfg* cfg, int32_t T, size_t* out) {
     if (check_cfg(cfg) != CATS_OK || T < 1 || T > CATS_MAX_TREE || !out) return CATS_ERR_INVALID_ARG;

@@ -270,5 +270,6 @@ struct SampleDev {
 };
 cudaError_t launch_sample(const SampleDev& p, cudaStream_t st);
 float sample_least(float top, float temperature, float min_p);      // what the kernel cuts at for min-p, on the host
+long long sample_part(float x, long long all, bool up);             // and its products of a sum with top-p and the random number
 
 }  // namespace cats

@@ -309,9 +309,16 @@ __device__ __forceinline__ void bucket_sums(int b, bool weights, int& n, i64& w)
         w += ((i64)hi[r] << 32) + lo[r];
     }
 }
-__device__ __forceinline__ i64 share(float top_p, i64 all) {
-    const i64 want = (i64)ceil((double)top_p * (double)all);
-    return want < 1 ? 1 : want;
+// x all for 0 <= x < 1, rounded down, or up; all digits of it (fp64 holds 53 bits of a sum of up to 62)
+__host__ __device__ __forceinline__ i64 part_of(float x, i64 all, bool up) {
+    const uint32_t b = bits_of(x), e = b >> 23, m = ((b & 0x7FFFFFu) | (e ? 0x800000u : 0u)) << 8;       // x = m 2^-(k + 32), k >= 0
+    const int k = 126 - (int)(e ? e : 1u), s = k < 63 ? k : 63;
+    const unsigned long long low = (unsigned long long)m * (uint32_t)all, high = (unsigned long long)m * (uint32_t)(all >> 32) + (low >> 32);
+    const unsigned long long q = high >> s;
+    return (i64)(q + (up && ((high - (q << s)) | (uint32_t)low)));
+}
+__device__ __forceinline__ i64 share(float top_p, i64 all) {    // top_p < 1
+    return top_p > 0.f ? max(part_of(top_p, all, true), (i64)1) : 1;
 }
 // The first bucket at which the running sum of the counts (or weights) over all blocks reaches `want`; want < 0: reaches share(top_p, all + more)
 __device__ __noinline__ Found find(bool weights, i64 want, float top_p, i64 more) {
@@ -617,8 +624,7 @@ __device__ __forceinline__ i64 strip_sum(int of) {      // of the warp's strip t
     return lane_id() < kStrips ? ((i64)sh.strip_hi[of][warp_id()][lane_id()] << 32) + sh.strip_lo[of][warp_id()][lane_id()] : 0;
 }
 __device__ __forceinline__ i64 drawn(float u, i64 all) {
-    const double x = u < 0.f ? 0.0 : (double)u;
-    return x >= 1.0 ? all - 1 : min(all - 1, (i64)(x * (double)all));
+    return u > 0.f ? (u < 1.f ? part_of(u, all, false) : all - 1) : 0;
 }
 __device__ __forceinline__ void answer(const SampleDev& p, int d, int token, float prob) {
     p.token[d] = token;
@@ -1030,6 +1036,7 @@ template <typename T> cudaError_t launch_t(const SampleDev& p, cudaStream_t st) 
 
 }  // namespace
 
+long long sample_part(float x, long long all, bool up) { return part_of(x, all, up); }
 float sample_least(float top, float temperature, float min_p) { return least_of(top, per_logit(temperature), min_p); }
 cudaError_t launch_sample(const SampleDev& p, cudaStream_t st) { return p.f32 ? launch_t<float>(p, st) : launch_t<uint16_t>(p, st); }
 
