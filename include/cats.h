@@ -479,7 +479,8 @@ int cats_paged_read(const cats_paged_kv *kv, const int32_t *d_table, int64_t ld_
  * n_heads is a multiple of n_kv_heads.  d_len[s] <= 0: the row of out is zeros.  Lengths
  * past table_width * page_size, or 2^31 - 1024, are cut there and reported.  Scores and softmax are fp32, the
  * probabilities enter the second product with 16 significant bits over a bf16 cache and, times
- * the rows' scales, with 22 over an int8 cache.  Rows behind a sequence's length are not read.  An infinite v makes its
+ * the rows' scales, with 22 over an int8 cache (11 at 2^-28 of the head's largest; the last bit is
+ * 2^-39 of it).  Rows behind a sequence's length are not read.  An infinite v makes its
  * infinity of the output's channel (both: NaN), unless its row is 2^126 or more behind the
  * largest: there a probability is 0, and 0 times an infinity NaN.
  * Workspace: cats_paged_workspace_bytes (0 for arguments that are refused), 1024-byte

@@ -10,7 +10,7 @@
 //
 // One pass with a running maximum and sum per head and warp.  Probabilities enter the second product as two bf16 parts (16
 // bits) over a bf16 cache.  An int8 cache's bytes are whole numbers in fp16, exact; the row's scale is part of the weight
-// w = p scale_v, which enters as two fp16 parts (22 bits) with a running exponent of its own (fit).  Groups of up to four heads have room for both parts
+// w = p scale_v, which enters as two fp16 parts (22 bits, and 11 at 2^-28 of the largest) with a running exponent of its own (fit).  Groups of up to four heads have room for both parts
 // in the columns of one product: their queries stand there twice (48 sequences of up to 1500 rows, 40 heads over 40: 102 us; with a second
 // product, as larger groups take it, 108; with one part of 11 bits 100, and outputs 4e-4 to 1e-3 from those of fp32 weights instead of 3e-5 to 2e-4).
 //
@@ -36,7 +36,6 @@ constexpr int kMaxLen = INT32_MAX - 1023;       // a tile's rows behind the last
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 static_assert(kGroup * kGroup >= kMaxBlocks, "two steps have to do");
 constexpr float kLowest = -110.f;   // int8: of the weights' exponent `up`; 2^(15 - up) is a number
-constexpr float kRoom = 6.f;        // and how far below 2^15 the largest weight is when `up` is set
 
 // Workspace: two part slots per block (a head group that began before its first unit, one that goes on behind its last), then counters.  A
 // block is the first of at most one head group that goes on in the next, and a later one of at most one: a counter each.
@@ -289,8 +288,8 @@ template <int HD, bool I8, int NT, bool BOTH> struct Attn {
     // int8.  A probability is relative to 2^m, m a whole number a little above the largest score so far; a weight p scale_v has a factor of its own, 2^(15 - up).
     // (One reference, the maximum of score + log2 scale_v, for both: probabilities of rows with a small scale, or next to a row with a
     // large one, leave the range of fp32, and the sum loses them.)  O^T is in units of 2^(m + up - 15).
-    // Most tiles change neither: their scores are below m, and scale_v 2^(15 - up) is a number of fp16, so the weights are.  For that, what is the largest
-    // weight when `up` is set is put 2^6 below 2^15, where the smallest that fp16 tells from 0 is 2^-34 of it.
+    // The largest weight when `up` is set becomes 2^14 to 2^15: what is 2^-28 of it is still a normal number of fp16.  Most tiles change neither m nor
+    // `up`: their scores are below m, and the largest score's probability times the largest scale is a number of fp16, so the weights are.
     __device__ __forceinline__ void fit(const float (&s)[NT][kBlk][4], const float (&sv)[kBlk][2], bool first) {
         float x[NT][2], size = 0.f;
         bool over = false;
@@ -307,7 +306,7 @@ template <int HD, bool I8, int NT, bool BOTH> struct Attn {
                 for (int b = 0; b < kBlk; ++b)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) x[nt][e] = fmaxf(x[nt][e], s[nt][b][h * 2 + e]);
-                over |= x[nt][e] > m[nt][e] || size * times[nt][e] > 65504.f;
+                over |= x[nt][e] > m[nt][e] || size * times[nt][e] * ex2(x[nt][e] - m[nt][e]) > 65504.f;
             }
         if (!__any_sync(0xffffffffu, over)) return;
         // the largest score and the largest score + log2 scale_v, both relative to one lane's, so that large scores leave the logarithms their bits
@@ -330,7 +329,7 @@ template <int HD, bool I8, int NT, bool BOTH> struct Attn {
                     for (int h = 0; h < 2; ++h) z = fmaxf(z, (s[nt][b][h * 2 + e] - r) + lg[b][h]);
                 const float top = over_rows(x[nt][e]), most = over_rows(z), to = top > m[nt][e] ? ceilf(top) + 2.f : m[nt][e];
                 const float by = m[nt][e] == to ? 0.f : m[nt][e] - to, from = up[nt][e] + by, need = most + (r - to);
-                const float with = fmaxf(need > from + 0.99f ? ceilf(need) + kRoom : from, kLowest);
+                const float with = fmaxf(need > from + 0.99f ? ceilf(need) : from, kLowest);
                 keep[nt][e] = ex2(from - with);
                 changed |= with != from;
                 l[nt][e] *= ex2(by);

@@ -106,3 +106,30 @@ def test_scores_and_sizes_along_a_sequence(cats, sizes, scores, heads, kv, dim):
     p.cache.vs[at] = (10.0 ** tens).float().clamp(1e-32, 1e32)[:, None].expand(-1, kv)
     p.run(1.0)
     p.check()
+
+
+@pytest.mark.parametrize("heads", [1, 4, 5, 16])
+@pytest.mark.parametrize("behind", [4, 12, 20, 24, 27, 28])
+@pytest.mark.parametrize("by", ["score", "scale"])
+def test_a_channel_that_the_largest_row_leaves_to_others(cats, by, behind, heads):
+    """Channels in which the row with the largest weight is 0 show a row 2^-behind of it, to half a step of fp16 and the output's rounding."""
+    p = Problem(cats, [300], heads, 1, 64, 16, "i8")
+    p.cache.k.zero_()
+    p.cache.v.zero_()
+    p.q.zero_()
+    p.q[:, :, 0] = 1.0
+    _written(p.cache.ks, 1.0)
+    _written(p.cache.vs, ZEROS)
+    a, b = (p.table[0, 3].long(), 2), (p.table[0, 17].long(), 9)
+    for at, score in ((a, 100), (b, 100 - (behind if by == "score" else 0))):
+        p.cache.k[at] = score
+        p.cache.vs[at] = 1.0
+    p.cache.vs[b] = 1.0 if by == "score" else 2.0 ** -behind
+    p.cache.v[a][..., ::2] = 90
+    p.cache.v[b][..., 1::2] = 77
+    p.run(0.6931471805599453)                       # scores are powers of two; all other rows are 2^-100 behind
+    share = 1 / (1 + 2.0 ** -behind) if by == "score" else 0.5
+    want = torch.zeros(heads, 64, dtype=torch.float64, device="cuda")
+    want[:, ::2], want[:, 1::2] = 90 * share, 77 * share * 2.0 ** -behind
+    assert ((p.out[0].double() / want - 1).abs() <= 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -16).all(), (p.out[0, 0, :2].tolist(), want[0, :2].tolist())
+    assert int(p.st.item()) == 0
