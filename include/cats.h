@@ -498,7 +498,7 @@ int cats_paged_attention(const cats_paged_kv *kv, const int32_t *d_table, int64_
  *     w = exp((logit - largest) / temperature).
  * Kept are, one after the other: the first top_k of the order (0 or less: all); of
  * those the shortest run from the front whose w add up to top_p of theirs, at least
- * one token (top_p >= 1: all); of those the ones with w >= min_p, and the largest.  The token is the
+ * one token (top_p >= 1: all); of those the ones with w >= min_p, and the first of the order.  The token is the
  * first in INDEX order at which the sum of the kept w exceeds u times their whole sum
  * (u < 0 counts as 0, u >= 1 takes the last kept token); d_prob its share of that sum.
  * temperature 0: the first token of the order, d_prob 1.  temperature inf: equal weights.

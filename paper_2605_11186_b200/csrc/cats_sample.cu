@@ -765,15 +765,17 @@ __device__ __noinline__ void finish(const SampleDev& p, int d, int n, int top_k,
 
 // log2 e / T, 0 at temperature 0
 __host__ __device__ __forceinline__ double per_logit(float temp) { return temp == 0.f ? 0.0 : 1.4426950408889634074 / (double)temp; }
-// The smallest logit whose weight is at least min_p, the largest among them always: bisection over the keys.  It lies within a few keys of what fp64 says,
+// The smallest logit whose weight is at least min_p, the largest among them always: bisection over the keys.  Weights are whole units of 2^-44, so that the
+// first to reach min_p is what rounds to the next whole unit: half a unit less.  The logit lies within a few keys of what fp64 says,
 // unless the sum cancels (a threshold next to 0 has more neighbours than fp64 tells apart) or is no fp32 number; then the search is over all.
 __host__ __device__ __noinline__ float least_of(float top, double c, float min_p) {
     if (!(min_p > 0.f)) return -INFINITY;
     constexpr float kLowest = -3.402823466e38f;
     constexpr uint32_t kNear = 8;
-    const double log_p = log2((double)min_p);
-    if (log_p >= 0.0) return top;
+    if (min_p > 1.f) return top;
     if (c == 0.0) return kLowest;
+    constexpr double kUnits = 17592186044416.0;                 // 2^44
+    const double log_p = log2((ceil((double)min_p * kUnits) - 0.5) / kUnits);
     auto in = [&](uint32_t key) { return ((double)value_of(key) - (double)top) * c >= log_p; };      // of the largest: 0 >= log_p
     const uint32_t first = key_of(kLowest), last = key_of(top), guess = key_of((float)fmax((double)top + log_p / c, (double)kLowest));
     uint32_t lo = guess - first > kNear ? guess - kNear : first, hi = last - guess > kNear ? guess + kNear : last;
@@ -798,7 +800,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
     pdl_wait();
     const int row = p.row ? p.row[d] : d;
     const float temp = p.temperature ? p.temperature[d] : 1.f, top_p = p.top_p ? p.top_p[d] : 1.f, min_p = p.min_p ? p.min_p[d] : 0.f, u = p.u[d];
-    const int top_k = p.top_k ? p.top_k[d] : 0;
+    const int top_k = min_p > 1.f ? 1 : (p.top_k ? p.top_k[d] : 0);      // no weight reaches that: the first of the order alone
     bool bad = row >= p.logit_rows || !(temp >= 0.f) || isnan(top_p) || isnan(min_p) || isnan(u);
     const T* const x = (const T*)p.logits + (bad || row < 0 ? 0 : row) * p.ld;
     float own = -INFINITY, top = -INFINITY;              // the largest of this thread's, of the row

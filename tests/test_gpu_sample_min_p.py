@@ -58,3 +58,27 @@ def test_the_cut_is_where_the_host_finds_it(cats, vocab):
             for k in (None, [30] * 3):
                 token, _ = draw(cats, x, [1.0, 0.0, 7.0], t=[t] * 3, k=k, m=[m] * 3)
                 assert first <= token[0] <= last and token == [token[0], 0, token[0]], (t, m, top)
+
+
+@pytest.mark.parametrize("vocab", [40, 50000])
+def test_equal_weights_reach_a_min_p_of_one(cats, vocab):
+    """At temperature inf, or one so large that all weights round to 1, min-p 1 keeps every token."""
+    x = logits(6, vocab, torch.float32, 3)
+    x[:, ::3] = -INF
+    for k in (None, [20] * 6, [vocab] * 6):
+        check(cats, x, uniform(6, 4), t=[INF, 1e30, 3e38, INF, 1e20, 1e25], k=k, m=[1.0] * 6)
+        check(cats, x, uniform(6, 5), t=[INF, 1e30, 3e38, INF, 1e20, 1e25], k=k, p=[0.7] * 6, m=[1.0] * 6)
+
+
+@pytest.mark.parametrize("vocab", [40, 50000, 200000])
+def test_a_min_p_that_no_weight_reaches(cats, vocab):
+    """The first of the order is left, also where others equal it."""
+    x = logits(5, vocab, torch.bfloat16, 4)
+    x[2] = 1.0
+    x[3, ::7] = 30.0
+    first = [int((r == r.max()).nonzero()[0]) for r in x]
+    for t in (1.0, 0.0, INF, 1e-30):
+        for m in (1 + 2.0 ** -23, 2.0, INF):
+            for k in (None, [9] * 5):
+                token, prob = draw(cats, x, [0.99, 1.0, 0.5, 1.0, 0.0], t=[t] * 5, k=k, p=[1.0, 0.9, 0.9, 1.0, 0.1], m=[m] * 5)
+                assert token == first and prob == [1.0] * 5, (t, m)

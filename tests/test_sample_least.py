@@ -1,6 +1,9 @@
-"""The logit that min-p cuts at, against the definition in 60 digits: exp((x - top) / T) >= min_p.  On the CPU; the kernel runs the same code."""
+"""The logit that min-p cuts at, against the definition in 60 digits: exp((x - top) / T), rounded to whole units of 2^-44, >= min_p.  On the CPU; the kernel runs the
+same code."""
+import math
 import random
 from decimal import Decimal, getcontext
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -21,12 +24,13 @@ def _check(least, top, t, m):
     top, t, m = float(F32(top)), float(F32(t)), float(F32(m))
     x = least(top, t, m)
     assert x <= top and x == float(F32(x)), (top, t, m, x)
-    if m >= 1:
+    if m > 1:
         assert x == top
         return
-    at = Decimal(top) + Decimal(t) * Decimal(m).ln()
-    # fp64: log2 min_p and log2 e / T are rounded once or twice each, the difference and the product once
-    off = 6 * Decimal(2) ** -53 * abs(Decimal(t) * Decimal(m).ln())
+    reach = (Decimal(math.ceil(Fraction(m) * 2 ** 44)) - Decimal(0.5)) / 2 ** 44
+    at = Decimal(top) + Decimal(t) * reach.ln()
+    # fp64: the logarithm and log2 e / T are rounded once or twice each, the difference and the product once
+    off = 6 * Decimal(2) ** -53 * abs(Decimal(t) * reach.ln())
     if at - off <= Decimal(LOWEST):
         assert x == LOWEST or Decimal(x) - at <= off
         return
@@ -82,4 +86,5 @@ def test_any_row(least):
 def test_no_min_p(least):
     for m in (0.0, -0.0, -1.0):
         assert least(3.0, 1.0, m) == -float("inf")
-    assert least(3.0, float("inf"), 0.3) == LOWEST and least(3.0, float("inf"), 1.0) == 3.0
+    inf = float("inf")
+    assert least(3.0, inf, 0.3) == LOWEST and least(3.0, inf, 1.0) == LOWEST and least(3.0, inf, 1.5) == 3.0
