@@ -800,7 +800,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
     pdl_wait();
     const int row = p.row ? p.row[d] : d;
     const float temp = p.temperature ? p.temperature[d] : 1.f, top_p = p.top_p ? p.top_p[d] : 1.f, min_p = p.min_p ? p.min_p[d] : 0.f, u = p.u[d];
-    const int top_k = min_p > 1.f ? 1 : (p.top_k ? p.top_k[d] : 0);      // no weight reaches that: the first of the order alone
+    int top_k = p.top_k ? p.top_k[d] : 0;
     bool bad = row >= p.logit_rows || !(temp >= 0.f) || isnan(top_p) || isnan(min_p) || isnan(u);
     const T* const x = (const T*)p.logits + (bad || row < 0 ? 0 : row) * p.ld;
     float own = -INFINITY, top = -INFINITY;              // the largest of this thread's, of the row
@@ -848,6 +848,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_sample(const
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
     }
+    if (min_p > 1.f) top_k = 1;             // no weight reaches that: the first of the order alone
     const bool by_bound = row >= 0 && !bad && top_k > 0 && top_k < V && top_k <= kFewK && temp > 0.f;
     float bound = -INFINITY;
     if (by_bound) {                 // that at least `least` of the block's threads reach, and at most half as many more if a few steps find it
