@@ -4,8 +4,8 @@
 //   a = max(max|y|, 2^-100),   q = rint(127 y / a),   scale = a / 127,
 // a head that holds an infinity or a NaN as zeros with a NaN scale.  Queries are rotated and rounded to bf16 in the same pass.
 // Read: the same rows back, q scale.  Both move every byte once: bound by HBM for a prompt, by latency for a token.
-// Measured: 8191 rows of 32 int8 heads of 128 with 32 query heads appended in 70 us (338 MB; the barriers in front of the angles and instructions), 16384
-// such rows read as bf16 in 70 us (5.8 TB/s, two thirds of it writes), one row or 64 in 2.5 us.
+// Measured: 8191 rows of 32 int8 heads of 128 with 32 query heads appended in 70 us (338 MB at 4.8 TB/s: threads wait at the two barriers in front of the
+// angles, and instructions take 55 % of the issue slots), 16384 such rows read as bf16 in 70 us (5.8 TB/s, two thirds of it writes), one row or 64 in 2.5 us.
 #include <math.h>
 #include <string.h>
 

@@ -19,8 +19,11 @@
 // its units sequence by sequence, the warps tile by tile, and joins its warps through shared memory.  What one block has of a
 // head group that others have rows of goes to the workspace; the last to arrive (a counter) adds the parts in order of their rows,
 // so the result does not depend on who that is.  More than kGroup parts are added in two steps.  No block ever waits for another.
-// Measured: 64 sequences of up to 8191 rows, 32 heads over 8 in bf16 165 us (6.5 TB/s); one of 131071 in int8 54 us (5.2 TB/s; loads alone 52); 48 of up to 1500,
-// 40 heads over 40 in int8 98 us (loads alone 75: here every byte is converted for one head); one of 513 8.2 us, a chain of latencies.
+// Measured: 64 sequences of up to 8191 rows, 32 heads over 8 in bf16 165 us (6.5 TB/s, the copy rate); one of 131071 in int8 54 us (5.1 TB/s; loads alone 50, 49
+// without the scales); 48 of up to 1500, 40 heads over 40 in int8 102 us: loads alone 74 (of it 10 because 1920 head groups each start and end, at four
+// times the length they run at the copy rate; 3 because pages of 24 rows break tiles, 2 for the scales), the rest a tile's chain of dependent
+// instructions in three warps a scheduler, which leaves 46 % of the issue slots empty; one of 513 8.5 us, a chain of latencies; one of 131071 with 16 heads over 1 in
+// bf16 34 us (2.0 TB/s): two blocks an SM, the same chain for two halves of the heads.
 #include <atomic>
 
 #include "cats_paged.cuh"

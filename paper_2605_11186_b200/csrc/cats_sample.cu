@@ -17,8 +17,9 @@
 //   - the draw looks for the strip in which the sum passes u times the whole, and goes through that strip alone.
 // The fp64 exponential is 12 instructions at half rate and as many for its integers.  The functions that pass over a row are not
 // inlined and work on variables at fixed places of shared memory: together in one body they were fetched as slowly as they ran.
-// Measured: one row of 32000 fp32 logits 12 us (latency), 64 with mixed filters 41 us, 256 rows of 128001 in bf16 174 us; of these unfiltered 86 us, top-k of few
-// 66, top-p alone 255: bound by the passes' instructions and the cluster's barriers, not by reading (10 us).
+// Measured: one row of 32000 fp32 logits 12 us (latency: two blocks' barriers), 64 with mixed filters 41 us, 256 rows of 128001 in bf16 with mixed filters 174 us. All
+// rows alike, 256 x 128001: greedy 46 us, min-p alone 63, top-k of 50 65, unfiltered 86, top-k of 1000 223, top-p of 0.9 255 to 274: bound by the passes'
+// instructions and the cluster's barriers, a block an SM with nothing beside it, not by reading (10 us).
 #include <cooperative_groups.h>
 #include <math.h>
 #include <string.h>
@@ -1007,7 +1008,10 @@ template <typename T> cudaError_t launch_t(const SampleDev& p, cudaStream_t st) 
     constexpr int kMost = 196 * 1024, kUsual = 136 * 1024;     // bytes of a row per block: what fits with the rest, and what is taken where rows are many
     const long long bytes = (long long)p.vocab * sizeof(T) + 32;
     int blocks = (int)min((long long)kMaxBlocks, (bytes + kUsual - 1) / kUsual);
-    // SMs that no row has take halves of them (64 rows of 32000: 54 -> 43 us when it was added); smaller parts cost more in barriers of the cluster than they save
+    // kUsual: 256 rows of 128001 in bf16 with top-p 274 us, with 104 KB 343, with 68 KB 411 (three and four blocks a row); 160 KB is the same there and for 32000,
+    // 50257, 100003 and 200000 tokens, and better where it saves a block (151936 in bf16 380 -> 314).
+    // SMs that no row has take halves of them (64 rows of 32000: 54 -> 43 us when it was added; smaller parts cost more in barriers of the cluster than they save: 16
+    // rows of 128001 14 us in parts of 80 KB, 23 in parts of 40)
     while (blocks < kMaxBlocks && (long long)p.rows * (blocks + 1) <= 148 && bytes / blocks > 80 * 1024) ++blocks;
     const size_t smem = (size_t)((bytes / 16 + 2 + blocks - 1) / blocks) * 16 + kStrip * sizeof(T) + (kInside + 1) * kThreads;
     static std::atomic<uint64_t> known{0};           // devices whose attribute is set
