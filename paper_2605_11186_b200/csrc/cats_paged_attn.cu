@@ -312,7 +312,7 @@ template <int HD, bool I8, int NT, bool BOTH> struct Attn {
                 over |= x[nt][e] > m[nt][e] || size * times[nt][e] * ex2(x[nt][e] - m[nt][e]) > 65504.f;
             }
         if (!__any_sync(0xffffffffu, over)) return;
-        // the largest score and the largest score + log2 scale_v, both relative to one lane's, so that large scores leave the logarithms their bits
+        // the largest score and the largest score + log2 scale_v, the second relative to the first, so that large scores leave the logarithms their bits
         float lg[kBlk][2], keep[NT][2];
         bool changed = false;
 #pragma unroll
@@ -323,15 +323,19 @@ template <int HD, bool I8, int NT, bool BOTH> struct Attn {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float r = __shfl_sync(0xffffffffu, x[nt][e], j);
-                r = fabsf(r) < INFINITY ? r : 0.f;
-                float z = (s[nt][0][e] - r) + lg[0][0];
+                float top = x[nt][e], most = (s[nt][0][e] - top) + lg[0][0];
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) z = fmaxf(z, (s[nt][b][h * 2 + e] - r) + lg[b][h]);
-                const float top = over_rows(x[nt][e]), most = over_rows(z), to = top > m[nt][e] ? ceilf(top) + 2.f : m[nt][e];
-                const float by = m[nt][e] == to ? 0.f : m[nt][e] - to, from = up[nt][e] + by, need = most + (r - to);
+                    for (int h = 0; h < 2; ++h) most = fmaxf(most, (s[nt][b][h * 2 + e] - top) + lg[b][h]);
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    const float x1 = __shfl_xor_sync(0xffffffffu, top, d), z1 = __shfl_xor_sync(0xffffffffu, most, d), larger = fmaxf(top, x1);
+                    most = fmaxf(most + (top - larger), z1 + (x1 - larger));
+                    top = larger;
+                }
+                const float to = top > m[nt][e] ? ceilf(top) + 2.f : m[nt][e];
+                const float by = m[nt][e] == to ? 0.f : m[nt][e] - to, from = up[nt][e] + by, need = most + (top - to);
                 const float with = fmaxf(need > from + 0.99f ? ceilf(need) : from, kLowest);
                 keep[nt][e] = ex2(from - with);
                 changed |= with != from;

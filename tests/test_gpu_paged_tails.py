@@ -133,3 +133,30 @@ def test_a_channel_that_the_largest_row_leaves_to_others(cats, by, behind, heads
     want[:, ::2], want[:, 1::2] = 90 * share, 77 * share * 2.0 ** -behind
     assert ((p.out[0].double() / want - 1).abs() <= 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -16).all(), (p.out[0, 0, :2].tolist(), want[0, :2].tolist())
     assert int(p.st.item()) == 0
+
+
+@pytest.mark.parametrize("heads,dim", [(1, 128), (4, 64), (8, 128), (16, 64)])
+@pytest.mark.parametrize("step", [100.0, 3e4, 1e6, 1e20])
+def test_scores_far_apart(cats, step, heads, dim):
+    """Scores that lie `step` apart, in any order: the largest row alone is left, whatever the scales of V are.  (The others weigh n e^-step of it at most, and
+    their values are up to 127e4, which shows in channels where the largest row is 0.)"""
+    lens = [257 + i for i in range(60)]
+    p = Problem(cats, lens, heads, 1, dim, 16, "i8", seed=heads)
+    g = _rand(8)
+    p.cache.k.zero_()
+    p.cache.k[..., 0] = 1
+    p.q.zero_()
+    p.q[:, :, 0] = 1.0
+    _written(p.cache.vs, 10.0 ** (torch.rand(p.cache.vs.shape, generator=g, device="cuda") * 8 - 4))
+    want = []
+    for i, n in enumerate(lens):
+        at = torch.arange(n, device="cuda")
+        at = ref.places(p.table, 16, torch.full_like(at, i), at)
+        rank = torch.randperm(n, generator=g, device="cuda")
+        p.cache.ks[at] = (rank - n // 2).float()[:, None]
+        last = rank.argmax()
+        want.append(p.cache.rows("v", at[0][last], at[1][last]).float()[0])
+    p.run(step)
+    want = torch.stack(want).double()[:, None].expand(-1, heads, -1)
+    ref.check_bf16(p.out, want, 2.0 ** -20 * want.abs() + 320 * 2.718281828459045 ** -min(step, 700.0) * 127e4)
+    assert int(p.st.item()) == 0
